@@ -31,9 +31,10 @@
  *   - A plan is not re-entrant: at most one mgi_plan_run per plan may be in
  *     flight on the device at a time unless the runs are ordered by the stream.
  *   - Tensor shapes are (n, h, w, c): batch, height, width, channels.  Graph
- *     inputs are NHWC arrays in fp32 or fp16.  Graph outputs are NHWC arrays
- *     of fp32 values (an output of global_avgpool / fc / softmax is (n, c));
- *     argmax outputs are int32 arrays of shape (n, h, w).
+ *     inputs are NHWC arrays in fp32 or fp16 (or of int32 channel indices).
+ *     Graph outputs are NHWC arrays of fp32 values (an output of
+ *     global_avgpool / fc / softmax is (n, c)); argmax outputs are int32 arrays
+ *     of shape (n, h, w), topk outputs of shape (n, h, w, k).
  *   - Tensor ids are assigned in call order, starting at 0, one per
  *     graph-building call that returns an id.
  */
@@ -230,6 +231,51 @@ mgi_status mgi_graph_add_resize_bilinear(mgi_graph *g, int in, int oh, int ow, i
 /* Per-pixel index of the largest channel (ties: lowest index), int32. */
 mgi_status mgi_graph_add_argmax(mgi_graph *g, int in, int *out);
 
+/* Fully connected layer with 4-bit weights: as mgi_graph_add_fc with
+ *     w[o][i] = scales[o][i / group] * (code[o][i] - zeros[o][i / group]).
+ * codes: cout rows of (cin + 1) / 2 bytes, code 2j in the low and 2j + 1 in the
+ * high half of byte j (with an odd cin the last high half is ignored); scales
+ * and zeros: cout x ceil(cin / group) values, the last group may be shorter;
+ * zeros: 0..15, NULL = 8 throughout; bias: cout floats, NULL = zeros.
+ * group: a positive multiple of 32 (MGI_ERR_UNSUPPORTED otherwise), scales
+ * finite.  Products of codes and activations are summed exactly as the 16-bit
+ * layer sums them; scales are kept in the plan's 16-bit storage type, each
+ * output channel's around a power of two of its own, so that none underflows
+ * beside the channel's largest.  fp32 output (n, 1, 1, cout), like fc. */
+mgi_status mgi_graph_add_fc_int4(mgi_graph *g, int in, int cout, int group,
+                                 const unsigned char *codes, const float *scales,
+                                 const unsigned char *zeros, const float *bias, int *out);
+
+/* ---------------------------------------------------------------------------
+ * questions about the channels of each pixel, mostly logits (of fc, fc_int4 or
+ * a graph input; any other tensor is widened to fp32 first).  With fusion on,
+ * those about the same tensor are answered in one pass by one kernel.  A plan
+ * that asks them about a graph input, or for the channels in one, reads those
+ * inputs in place: its outputs must not overlap its inputs
+ * (MGI_ERR_INVALID_ARG from the run).
+ * ------------------------------------------------------------------------- */
+/* A graph input of channel indices: an (n, h, w, c) int32 array supplied to
+ * run, for mgi_graph_add_log_prob only (MGI_ERR_UNSUPPORTED elsewhere). */
+mgi_status mgi_graph_add_index_input(mgi_graph *g, int n, int h, int w, int c, int *out);
+
+/* The k channels with the largest values of each pixel, largest first, equal
+ * values by ascending channel: int32 (n, h, w, k), 1 <= k <= 64, k at most the
+ * channels (MGI_ERR_SHAPE).  NaN ranks with -inf.  At most 2^19 channels. */
+mgi_status mgi_graph_add_topk(mgi_graph *g, int in, int k, int *out);
+
+/* The logarithm of the softmax of each pixel's channels, for the channels that
+ * `index` names: an index input or the output of topk or argmax, with in's n,
+ * h and w (MGI_ERR_SHAPE) and any channel count, in any order, repeats
+ * allowed.  Output: fp32, index's shape.  A channel of -inf has -inf, also
+ * where all have; an index outside in's channels gives NaN, and so does every
+ * index of a pixel with a NaN or +inf among its channels. */
+mgi_status mgi_graph_add_log_prob(mgi_graph *g, int in, int index, int *out);
+
+/* Entropy, in nats, of the softmax of each pixel's channels: fp32 (n, h, w, 1).
+ * Channels of -inf take no part; 0 where all are, NaN where one is NaN or
+ * +inf. */
+mgi_status mgi_graph_add_entropy(mgi_graph *g, int in, int *out);
+
 /* Mark a tensor as a graph output (in call order: output index 0, 1, ...).
  * Graph inputs cannot be outputs. */
 mgi_status mgi_graph_mark_output(mgi_graph *g, int id);
@@ -247,7 +293,7 @@ mgi_status mgi_plan_destroy(mgi_plan *p); /* NULL is accepted */
 
 /* Bytes of device workspace (the arena holding every intermediate tensor,
  * then a small state region: the arrival counters of fused FC + softmax
- * nodes) and of packed weights that the caller must allocate for
+ * nodes and of nodes that split their sums over workgroups) and of packed weights that the caller must allocate for
  * mgi_plan_bind.  Both buffers must be 256-byte aligned. */
 mgi_status mgi_plan_workspace_bytes(const mgi_plan *p, size_t *bytes);
 mgi_status mgi_plan_weight_bytes(const mgi_plan *p, size_t *bytes);
@@ -260,7 +306,7 @@ mgi_status mgi_plan_memory_report(const mgi_plan *p, size_t *naive, size_t *plan
 
 /* Graph inputs and outputs of the plan, in declaration / marking order. */
 mgi_status mgi_plan_num_io(const mgi_plan *p, int *n_inputs, int *n_outputs);
-/* Shape and element type (FP32 / FP16 for inputs, FP32 / INT32 for outputs)
+/* Shape and element type (FP32 / FP16 / INT32 for inputs, FP32 / INT32 for outputs)
  * of input or output `index` (is_output selects which); bytes = total size. */
 mgi_status mgi_plan_io_info(const mgi_plan *p, int is_output, int index, int *n, int *h, int *w,
                             int *c, int *dtype, size_t *bytes);
@@ -325,7 +371,7 @@ mgi_status mgi_plan_node_count(const mgi_plan *p, int *count);
 mgi_status mgi_plan_node_info(const mgi_plan *p, int i, const char **kind, int *tensor_id, int *n,
                               int *h, int *w, int *c, int *n_fused);
 
-/* Copy node i's output, as an NHWC fp32 array (int32 for argmax), to
+/* Copy node i's output, as an NHWC fp32 array (int32 for argmax and topk), to
  * dev_dst on `stream`.  Requires materialize_all (MGI_ERR_STATE otherwise)
  * and a completed or stream-ordered run. */
 mgi_status mgi_plan_read_node(mgi_plan *p, int i, void *dev_dst, void *stream);

@@ -199,6 +199,57 @@ def argmax(x):
     return y
 
 
+def fc_int4(x, q, scales, zeros, group, b):
+    """Fully connected layer with 4-bit codes, two to a byte (even input channel
+    in the low half): weight = scale of the group * (code - zero point), 8 where
+    no zero points are given.  x: (n, 1, 1, cin) -> (n, 1, 1, cout)."""
+    x = _f64(x)
+    n, cin = x.shape[0], x.shape[3]
+    scales = _f64(scales).reshape(len(q), -1)
+    zeros = np.full(scales.shape, 8.0) if zeros is None else _f64(zeros).reshape(scales.shape)
+    w = np.zeros((len(q), cin))
+    for i in range(cin):
+        code = (np.asarray(q)[:, i // 2] >> (4 * (i % 2))) % 16
+        w[:, i] = scales[:, i // group] * (code - zeros[:, i // group])
+    y = x.reshape(n, cin) @ w.T
+    return (y if b is None else y + _f64(b)).reshape(n, 1, 1, len(q))
+
+
+def topk(x, k):
+    """Channels of the k largest values, largest first, equal ones by channel;
+    NaN with -inf."""
+    x = np.where(np.isnan(x), -np.inf, _f64(x))
+    return np.argsort(-x, axis=-1, kind="stable")[..., :k].astype(np.int32)
+
+
+def _log_softmax(x):
+    """Log softmax over channels: -inf where the channel is -inf, NaN for every
+    channel of a pixel with a NaN or +inf."""
+    x = _f64(x)
+    bad = np.isnan(x).any(-1, keepdims=True) | np.isposinf(x).any(-1, keepdims=True)
+    m = np.max(np.where(np.isfinite(x), x, -np.inf), axis=-1, keepdims=True)
+    empty = np.isneginf(m) & ~bad
+    with np.errstate(invalid="ignore", divide="ignore"):
+        d = np.where(np.isneginf(x) | empty, -np.inf, x - m)
+        y = d - np.log(np.where(empty, 1.0, np.exp(d).sum(-1, keepdims=True)))
+    return np.where(bad, np.nan, y)
+
+
+def log_prob(x, index):
+    """Log softmax at the given channels (last axis of ``index``), NaN for
+    channels that do not exist."""
+    y = _log_softmax(x)
+    ok = (index >= 0) & (index < y.shape[-1])
+    return np.where(ok, np.take_along_axis(y, np.where(ok, index, 0).astype(np.int64), -1), np.nan)
+
+
+def entropy(x):
+    """Entropy of the softmax over channels, in nats; 0 where all are -inf."""
+    y = _log_softmax(x)
+    with np.errstate(invalid="ignore"):
+        return -np.where(np.isneginf(y), 0.0, np.exp(y) * y).sum(-1, keepdims=True)
+
+
 # ----------------------------------------------------------------------------
 # graphs
 # ----------------------------------------------------------------------------
@@ -234,9 +285,17 @@ def tensor_shapes(graph):
         elif k == "resize_bilinear":
             n, h, w, c = shapes[op["in"]]
             shapes.append((n, op["oh"], op["ow"], c))
-        elif k == "argmax":
+        elif k in ("argmax", "entropy"):
             n, h, w, c = shapes[op["in"]]
             shapes.append((n, h, w, 1))
+        elif k == "fc_int4":
+            shapes.append((shapes[op["in"]][0], 1, 1, op["cout"]))
+        elif k == "index_input":
+            shapes.append(tuple(op["shape"]))
+        elif k == "topk":
+            shapes.append(shapes[op["in"]][:3] + (op["k"],))
+        elif k == "log_prob":
+            shapes.append(shapes[op["index"]])
         else:
             raise ValueError(f"unknown op {k}")
     return shapes
@@ -244,8 +303,10 @@ def tensor_shapes(graph):
 
 def op_inputs(op):
     k = op["op"]
-    if k == "input":
+    if k in ("input", "index_input"):
         return []
+    if k == "log_prob":
+        return [op["in"], op["index"]]
     if k == "add":
         return [op["a"], op["b"]]
     if k == "concat":
@@ -288,6 +349,16 @@ def eval_op(op, operands):
         return resize_bilinear(operands[0], op["oh"], op["ow"], op["align_corners"])
     if k == "argmax":
         return argmax(operands[0])
+    if k == "fc_int4":
+        return fc_int4(operands[0], op["q"], op["scales"], op["zeros"], op["group"], op["b"])
+    if k == "index_input":
+        return np.asarray(op["data"], np.int32)
+    if k == "topk":
+        return topk(operands[0], op["k"])
+    if k == "log_prob":
+        return log_prob(operands[0], operands[1])
+    if k == "entropy":
+        return entropy(operands[0])
     raise ValueError(f"unknown op {k}")
 
 

@@ -50,6 +50,7 @@ I = ctypes.c_int
 IP = ctypes.POINTER(ctypes.c_int)
 SP = ctypes.POINTER(ctypes.c_size_t)
 FP = ctypes.POINTER(ctypes.c_float)
+UP = ctypes.POINTER(ctypes.c_ubyte)
 
 _SIGS = {
     "mgi_status_str": ([I], ctypes.c_char_p),
@@ -68,6 +69,11 @@ _SIGS = {
     "mgi_graph_add_concat": ([P, IP, I, IP], I),
     "mgi_graph_add_resize_bilinear": ([P, I, I, I, I, IP], I),
     "mgi_graph_add_argmax": ([P, I, IP], I),
+    "mgi_graph_add_fc_int4": ([P, I, I, I, UP, FP, UP, FP, IP], I),
+    "mgi_graph_add_index_input": ([P, I, I, I, I, IP], I),
+    "mgi_graph_add_topk": ([P, I, I, IP], I),
+    "mgi_graph_add_log_prob": ([P, I, I, IP], I),
+    "mgi_graph_add_entropy": ([P, I, IP], I),
     "mgi_graph_mark_output": ([P, I], I),
     "mgi_options_default": ([ctypes.POINTER(Options)], None),
     "mgi_graph_finalize": ([P, ctypes.POINTER(Options), ctypes.POINTER(P)], I),
@@ -217,6 +223,33 @@ def mgi_graph_add_resize_bilinear(g, x, oh, ow, align_corners=1):
 
 def mgi_graph_add_argmax(g, x):
     return _out(lib().mgi_graph_add_argmax, g, x)
+
+
+def _u8(a):
+    import numpy as np
+    return None if a is None else np.ascontiguousarray(a, dtype=np.uint8)
+
+
+def mgi_graph_add_fc_int4(g, x, cout, group, codes, scales, zeros=None, b=None):
+    codes, scales, zeros, b = _u8(codes), _f32(scales), _u8(zeros), _f32(b)
+    ptr = [a.ctypes.data_as(UP) if a is not None else None for a in (codes, zeros)]
+    return _out(lib().mgi_graph_add_fc_int4, g, x, cout, group, ptr[0], _fptr(scales), ptr[1], _fptr(b))
+
+
+def mgi_graph_add_index_input(g, n, h, w, c):
+    return _out(lib().mgi_graph_add_index_input, g, n, h, w, c)
+
+
+def mgi_graph_add_topk(g, x, k):
+    return _out(lib().mgi_graph_add_topk, g, x, k)
+
+
+def mgi_graph_add_log_prob(g, x, index):
+    return _out(lib().mgi_graph_add_log_prob, g, x, index)
+
+
+def mgi_graph_add_entropy(g, x):
+    return _out(lib().mgi_graph_add_entropy, g, x)
 
 
 def mgi_graph_mark_output(g, t):

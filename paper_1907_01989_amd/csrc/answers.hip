@@ -1,0 +1,389 @@
+// Questions about the channels of each pixel: the k largest, the logarithm of
+// the softmax at given channels, the softmax's entropy.
+//
+// With m the row's maximum, s = sum exp(x - m) and t = sum exp(x - m) (x - m):
+//     log softmax(x)_i = (x_i - m) - log s,    entropy = log s - t / s.
+// Both terms of the entropy are non-negative, so neither loses digits to the
+// other.  Sums are fp32.
+//
+// One workgroup owns a row, or a segment of one, and holds it in registers, so
+// the row is read once whatever is asked: a call is bound by the row's bytes.
+// Where rows are few or long they are split into segments; each leaves its
+// (m, s, t) and its own k best, and the workgroup that arrives last joins them.
+#include "device.h"
+
+namespace mgi {
+namespace kern {
+
+namespace {
+
+constexpr int kCap = 1024;            // candidates a workgroup ranks
+constexpr float kLog2e = 1.44269504088896341f;
+
+// unsigned integers in the order of the values (-0 as +0)
+__device__ __forceinline__ uint32_t order_of(float v) {
+    const uint32_t u = __float_as_uint(v + 0.0f);
+    return u ^ ((uint32_t)((int)u >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float value_of(uint32_t o) {
+    return __uint_as_float(o & 0x80000000u ? o ^ 0x80000000u : ~o);
+}
+// ... and of values, then of descending columns: larger keys come first, and
+// no two columns share one; 0 is below every key
+__device__ __forceinline__ unsigned long long key_of(float v, int col) {
+    return (unsigned long long)order_of(v) << 32 | (uint32_t)~col;
+}
+
+__device__ __forceinline__ float wave_max(float v) {
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) v = fmaxf(v, __shfl_xor(v, off, 64));
+    return v;
+}
+__device__ __forceinline__ float wave_sum(float v) {
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) v += __shfl_xor(v, off, 64);
+    return v;
+}
+
+// The r-th largest of a wave's 64 values, bit by bit.
+__device__ __forceinline__ float wave_rth(float v, int r) {
+    const uint32_t o = order_of(v);
+    uint32_t ans = 0;
+    for (int b = 31; b >= 0; --b) {
+        const uint32_t c = ans | 1u << b;
+        if (__popcll(__ballot(o >= c)) >= r) ans = c;
+    }
+    return value_of(ans);
+}
+
+__device__ __forceinline__ int lanes_below(unsigned long long mask) {
+    return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
+}
+
+template <int W>
+struct Shared {
+    unsigned long long cand[kCap];
+    float top_val[kMaxTopK];
+    float m[W], th[W], s[W], t[W];
+    int cnt[W];
+    int n, last;
+};
+
+// A workgroup's values: element e of vector i of a thread is column at(i) + e
+// of the row; vectors that would pass the segment's end are moved back to end
+// there, and repeat columns that other threads (or none) own, which do not
+// count.  Slots that hold no column hold -inf.
+template <typename T, int NT, int PER>
+struct Held {
+    static constexpr int VEC = 16 / (int)sizeof(T), I = PER / VEC;
+    float v[PER];
+    int lo, hi;
+    __device__ __forceinline__ int own(int i) const { return lo + (i * NT + (int)threadIdx.x) * VEC; }
+    __device__ __forceinline__ int at(int i) const {
+        const int j = own(i);
+        return hi - lo >= VEC ? min(j, hi - VEC) : j;
+    }
+    __device__ __forceinline__ bool valid(int i, int e) const {
+        const int c = at(i) + e;
+        return c >= own(i) && c < hi;
+    }
+    __device__ __forceinline__ void load(const T *x, int lo_, int hi_) {
+        typedef T tv __attribute__((ext_vector_type(VEC)));
+        typedef tv tvu __attribute__((aligned(sizeof(T))));   // (rows start anywhere)
+        lo = lo_;
+        hi = hi_;
+        if (hi - lo < VEC) {
+#pragma unroll
+            for (int q = 0; q < PER; ++q) v[q] = (float)x[min(own(q / VEC) + q % VEC, hi - 1)];
+        } else {
+            tv b[I];
+#pragma unroll
+            for (int i = 0; i < I; ++i) b[i] = *(const tvu *)(x + at(i));
+#pragma unroll
+            for (int q = 0; q < PER; ++q) v[q] = (float)b[q / VEC][q % VEC];
+        }
+#pragma unroll
+        for (int i = 0; i < I; ++i)
+            if (lo + (i + 1) * NT * VEC > hi) {
+#pragma unroll
+                for (int e = 0; e < VEC; ++e)
+                    if (!valid(i, e)) v[i * VEC + e] = -INFINITY;
+            }
+    }
+};
+
+// Adds the values of at least `th` to the candidates.
+template <int W, typename H>
+__device__ __forceinline__ void push(Shared<W> &sh, const H &h, float th) {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int i = 0; i < H::I; ++i)
+#pragma unroll
+        for (int e = 0; e < H::VEC; ++e) {
+            const float v = h.v[i * H::VEC + e];
+            const unsigned long long mask = __ballot(v >= th);
+            if (mask == 0) continue;
+            int base = 0;
+            if (lane == 0) base = atomicAdd(&sh.n, __popcll(mask));
+            base = __builtin_amdgcn_readfirstlane(base);
+            const int slot = base + lanes_below(mask);
+            if (v >= th && slot < kCap) sh.cand[slot] = key_of(v, h.at(i) + e);
+        }
+}
+
+// Called by the whole workgroup where `push` found fewer than k candidates (all
+// others are -inf) or more than there is room for: the exact k-th largest
+// value, what is above it, and of its equals the first columns.  Leaves
+// exactly k candidates.  (Rows that are mostly masked, or mostly equal.)
+template <int W, typename H>
+__device__ __forceinline__ void push_exact(Shared<W> &sh, const H &h, int k) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    float kth = -INFINITY;
+    if (sh.n > kCap) {
+        uint32_t ans = 0;
+        for (int b = 31; b >= 0; --b) {
+            const uint32_t c = ans | 1u << b;
+            int n = 0;
+#pragma unroll
+            for (int q = 0; q < H::I * H::VEC; ++q) n += __popcll(__ballot(order_of(fmaxf(h.v[q], -INFINITY)) >= c));
+            __syncthreads();
+            if (lane == 0) sh.cnt[wave] = n;
+            __syncthreads();
+            n = 0;
+            for (int w = 0; w < W; ++w) n += sh.cnt[w];
+            if (n >= k) ans = c;
+        }
+        kth = value_of(ans);
+        __syncthreads();
+        if (threadIdx.x == 0) sh.n = 0;
+        __syncthreads();
+        push(sh, h, value_of(ans + 1));   // (the next value up: fewer than k are there)
+        __syncthreads();
+    }
+    int have = sh.n;
+#pragma unroll
+    for (int i = 0; i < H::I; ++i)
+        if (have < k) {
+            bool eq[H::VEC];
+            int mine = 0, before = 0, total = 0;
+#pragma unroll
+            for (int e = 0; e < H::VEC; ++e) {
+                eq[e] = fmaxf(h.v[i * H::VEC + e], -INFINITY) == kth && h.valid(i, e);
+                const unsigned long long mask = __ballot(eq[e]);
+                before += lanes_below(mask);
+                total += __popcll(mask);
+            }
+            __syncthreads();
+            if (lane == 0) sh.cnt[wave] = total;
+            __syncthreads();
+            total = 0;
+            for (int w = 0; w < W; ++w) {
+                if (w < wave) before += sh.cnt[w];
+                total += sh.cnt[w];
+            }
+#pragma unroll
+            for (int e = 0; e < H::VEC; ++e) {
+                const int slot = have + before + mine;
+                if (eq[e] && slot < k) sh.cand[slot] = key_of(kth, h.at(i) + e);
+                mine += eq[e];
+            }
+            have += total;
+        }
+    __syncthreads();
+    if (threadIdx.x == 0) sh.n = k;
+    __syncthreads();
+}
+
+template <typename T, int NT, int PER>
+__global__ __launch_bounds__(NT) void answers_kernel(AnswersParams p, int segs, int seglen) {
+    constexpr int W = NT / 64;
+    __shared__ Shared<W> sh;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int row = blockIdx.x / segs, seg = blockIdx.x - row * segs;
+    const T *x = (const T *)p.x + (size_t)row * p.cols;
+    Held<T, NT, PER> h;
+    h.load(x, seg * seglen, min(p.cols, (seg + 1) * seglen));
+    const int k = min(p.k, h.hi - h.lo);
+    const bool stats = p.n_lists > 0 || p.entropy;
+
+    // The k-th largest value is at least the smallest of the waves' r-th
+    // largest lane maxima, r = ceil(k / waves): few values pass it.  (Waves
+    // past the end of a short row hold nothing and do not count.)
+    const int held = min(W, (h.hi - h.lo + 64 * h.VEC - 1) / (64 * h.VEC));
+    float mx = -INFINITY;
+#pragma unroll
+    for (int q = 0; q < PER; ++q) mx = fmaxf(mx, h.v[q]);
+    {
+        const float wm = wave_max(mx);
+        const int r = (k + held - 1) / held;
+        const float th = r > 1 ? wave_rth(mx, r) : wm;
+        if (lane == 0) {
+            sh.m[wave] = wm;
+            sh.th[wave] = wave < held ? th : INFINITY;
+        }
+        if (tid == 0) sh.n = 0;
+    }
+    __syncthreads();
+    float m = -FLT_MAX, th = INFINITY;    // (rows of -inf only: s = 0)
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+        m = fmaxf(m, sh.m[w]);
+        th = fminf(th, sh.th[w]);
+    }
+    if (k > 0) push(sh, h, fmaxf(th, -FLT_MAX));
+    float s = 0.0f, t = 0.0f;
+    if (stats) {
+#pragma unroll
+        for (int q = 0; q < PER; ++q) {
+            const float d = h.v[q] - m, e = __builtin_amdgcn_exp2f(d * kLog2e);
+            s += e;
+            t = fmaf(e, fmaxf(d, -1e30f), t);     // (0 times -inf)
+        }
+        s = wave_sum(s);
+        t = wave_sum(t);
+        if (lane == 0) {
+            sh.s[wave] = s;
+            sh.t[wave] = t;
+        }
+    }
+    __syncthreads();
+    if (stats) {
+        s = t = 0.0f;
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+            s += sh.s[w];
+            t += sh.t[w];
+        }
+    }
+    if (k > 0) {
+        if (sh.n < k || sh.n > kCap) push_exact(sh, h, k);
+        const int n = sh.n;
+        for (int j = tid; j < n; j += NT) {
+            const unsigned long long key = sh.cand[j];
+            int r = 0;
+            for (int q = 0; q < n; ++q) r += sh.cand[q] > key;
+            if (r >= k) continue;
+            if (segs > 1) {
+                p.part_keys[((size_t)row * segs + seg) * p.k + r] = key;
+            } else {
+                p.top[(size_t)row * p.k + r] = (int)~(uint32_t)key;
+                sh.top_val[r] = value_of((uint32_t)(key >> 32));
+            }
+        }
+        if (segs > 1)
+            for (int r = k + tid; r < p.k; r += NT) p.part_keys[((size_t)row * segs + seg) * p.k + r] = 0;
+    }
+    if (segs > 1) {
+        float *st = p.part_stats + (size_t)row * segs * 4;
+        if (tid == 0) *(f4 *)(st + 4 * seg) = f4{m, s, t, 0.0f};
+        // every wave's stores are in the L2 before the workgroup arrives; one
+        // release writes it back for all of them
+        __builtin_amdgcn_s_waitcnt(0x0F70);
+        __syncthreads();
+        if (tid == 0) {
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "agent");
+            sh.last = atomicAdd(p.cnt + row, 1) == segs - 1;
+        }
+        __syncthreads();
+        if (!sh.last) return;
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
+        if (tid == 0) atomicExch(p.cnt + row, 0);
+        if (p.k > 0) {
+            const int n = segs * p.k;
+            for (int j = tid; j < n; j += NT) sh.cand[j] = p.part_keys[(size_t)row * n + j];
+        }
+        if (stats) {
+            float ms = -FLT_MAX, s0 = 0.0f, t0 = 0.0f;
+            for (int g = lane; g < segs; g += 64) ms = fmaxf(ms, st[4 * g]);
+            ms = wave_max(ms);
+            for (int g = lane; g < segs; g += 64) {
+                const f4 q = *(const f4 *)(st + 4 * g);
+                const float d = fmaxf(q[0] - ms, -1e30f), w = __builtin_amdgcn_exp2f(d * kLog2e);
+                s0 = fmaf(w, q[1], s0);
+                t0 = fmaf(w, fmaf(q[1], d, q[2]), t0);
+            }
+            m = ms;
+            s = wave_sum(s0);
+            t = wave_sum(t0);
+        }
+        __syncthreads();
+        if (p.k > 0) {
+            const int n = segs * p.k;
+            for (int j = tid; j < n; j += NT) {
+                const unsigned long long key = sh.cand[j];
+                int r = 0;
+                for (int q = 0; q < n; ++q) r += sh.cand[q] > key;
+                if (r >= p.k || key == 0) continue;
+                p.top[(size_t)row * p.k + r] = (int)~(uint32_t)key;
+                sh.top_val[r] = value_of((uint32_t)(key >> 32));
+            }
+        }
+    }
+    if (!stats) return;
+    __syncthreads();
+    const float logs = logf(s);
+    for (int l = 0; l < p.n_lists; ++l) {
+        const int *list = p.list[l];
+        const int nl = p.list_n[l];
+        for (int q = tid; q < nl; q += NT) {
+            float v = NAN;
+            if (!list) {
+                v = sh.top_val[q];
+            } else {
+                const int c = list[(size_t)row * nl + q];
+                if (c >= 0 && c < p.cols) v = (float)x[c];
+            }
+            p.list_out[l][(size_t)row * nl + q] = s == 0.0f && v == v ? -INFINITY : (v - m) - logs;
+        }
+    }
+    if (p.entropy && tid == 0) p.entropy[row] = s == 0.0f ? 0.0f : logs - t / s;
+}
+
+template <typename T>
+hipError_t launch_t(const AnswersParams &p, const AnswersGeom &g, hipStream_t st) {
+    const dim3 grid((unsigned)p.rows * (unsigned)g.segs);
+#define MGI_ANSWERS(NT_, PER_)                                                                   \
+    if (g.nt == NT_ && g.per == PER_) {                                                           \
+        launch(answers_kernel<T, NT_, PER_>, grid, dim3(NT_), 0, st, p, g.segs, g.seglen);       \
+        return hipGetLastError();                                                                 \
+    }
+    MGI_ANSWERS(64, 8) MGI_ANSWERS(256, 8) MGI_ANSWERS(256, 16) MGI_ANSWERS(256, 32)
+    MGI_ANSWERS(512, 32) MGI_ANSWERS(512, 64)
+#undef MGI_ANSWERS
+    return hipErrorInvalidValue;
+}
+
+}  // namespace
+
+// Segments: as many as a workgroup's registers make necessary, more where rows
+// alone would leave compute units idle, none shorter than 2048 columns, and no
+// more than the last workgroup can rank.
+AnswersGeom answers_geom(int rows, int cols, int k) {
+    AnswersGeom g{};
+    const int most = k > 0 ? kCap / k : 64;
+    int segs = (cols + 32767) / 32768;
+    segs = std::max(segs, std::min({256 / std::max(rows, 1), (cols + 2047) / 2048, most}));
+    g.seglen = ((cols + segs - 1) / segs + 7) / 8 * 8;
+    g.segs = (cols + g.seglen - 1) / g.seglen;
+    const int sizes[6][2] = {{64, 8}, {256, 8}, {256, 16}, {256, 32}, {512, 32}, {512, 64}};
+    for (auto &s : sizes) {
+        g.nt = s[0];
+        g.per = s[1];
+        if (g.nt * g.per >= g.seglen) break;
+    }
+    return g;
+}
+
+hipError_t launch_answers(const AnswersParams &p, const AnswersGeom &g, hipStream_t st) {
+    if (p.rows <= 0) return hipSuccess;
+    if (g.segs < 1 || (long)g.nt * g.per < g.seglen || (long)g.segs * g.seglen < p.cols || (g.segs - 1) * g.seglen >= p.cols ||
+        (long)g.segs * p.k > kCap || p.k > kMaxTopK || (g.segs > 1 && (!p.cnt || !p.part_stats)) ||
+        (size_t)p.rows * g.segs > 0x7fffffffu)
+        return hipErrorInvalidValue;
+    for (int l = 0; l < p.n_lists; ++l)
+        if (!p.list[l] && p.list_n[l] != p.k) return hipErrorInvalidValue;
+    return p.fp16_in ? launch_t<_Float16>(p, g, st) : launch_t<float>(p, g, st);
+}
+
+}  // namespace kern
+}  // namespace mgi

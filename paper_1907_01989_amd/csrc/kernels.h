@@ -4,6 +4,8 @@
 #include <hip/hip_ext.h>
 #include <hip/hip_runtime.h>
 
+#include <cstdint>
+
 #include "../../include/mgi.h"
 
 namespace mgi {
@@ -106,6 +108,62 @@ hipError_t launch_gemm_pool(const GemmParams &p, int bm, int bn, hipStream_t st)
 // ceil(M / (16 * fm)) counters, zero on entry and left at zero).
 hipError_t launch_fc(const GemmParams &p, int fm, int kb, hipStream_t st);
 size_t gemm_xs_lds_bytes(int ksp, int wm, int bn);
+
+// Fully connected layer with 4-bit weights (fcint4.hip), fp32 (M x cout) output.
+// K runs in blocks of 128 (four MFMA steps of 32); `gs` steps share a scale.
+struct FcInt4Params {
+    const h8 *x;             // as GemmParams: element (slice, row) at x[slice * xs + row * xp]
+    int xs, xp;
+    const h8 *zero;          // one zeroed element (read for slices past ksl)
+    const uint32_t *w;       // codes [nb16][kb][64 lanes][4 steps], eight to a word
+    const uint16_t *scales;  // [nb16][kb][16 channels][4 / gs], storage type
+    const uint8_t *zp;       // zero points, laid out as the scales; null: 8
+    const float *mul;        // [nb16 * 16] power of two taken out of each channel's scales
+    const float *bias;       // [nb16 * 16]
+    float *y;
+    float *part;             // sums of the splits [tile][split][fm * fn][64 lanes][4] (splits > 1)
+    int *cnt;                // ... and their arrival counters [tile], zero before and after
+    int M, ksl, kb, nb16, cout, act, bf16;
+    int mtiles, ntiles;      // set by the launcher
+};
+// rows per workgroup 16 * fm, output channels 16 * fn, waves that share K,
+// workgroups that share K, MFMA steps per scale
+struct FcInt4Geom {
+    int fm, fn, waves, splits, gs;
+    size_t tiles(int M, int nb16) const {
+        return (size_t)((M + 16 * fm - 1) / (16 * fm)) * (size_t)((nb16 + fn - 1) / fn);
+    }
+    size_t part_bytes(int M, int nb16) const { return splits > 1 ? tiles(M, nb16) * splits * fm * fn * 1024 : 0; }
+};
+FcInt4Geom fcint4_geom(int M, int nb16, int kb, int group);
+hipError_t launch_fcint4(const FcInt4Params &p, const FcInt4Geom &g, hipStream_t st);
+
+// Questions about rows of values (answers.hip): the k largest, the logarithm
+// of the softmax at given columns, the softmax's entropy, in one pass.
+constexpr int kMaxTopK = 64, kMaxAnswerCols = 1 << 19, kAnswerLists = 4;
+struct AnswersParams {
+    const void *x;           // rows x cols, fp32 or fp16
+    int rows, cols, fp16_in;
+    int k;                   // 0: no top columns asked
+    int *top;                // rows x k
+    float *entropy;          // rows, or null
+    int n_lists;             // lists of columns whose log probabilities are asked
+    const int *list[kAnswerLists];   // rows x list_n, null: the top columns of this call
+    float *list_out[kAnswerLists];
+    int list_n[kAnswerLists];
+    // rows split into segments: what each found, and arrival counters per row
+    // (zero before and after)
+    unsigned long long *part_keys;   // [row][segment][k]
+    float *part_stats;               // [row][segment][4]: max, sum, weighted sum
+    int *cnt;
+};
+// threads per workgroup, values per thread, segments per row and their length
+struct AnswersGeom {
+    int nt, per, segs, seglen;
+    size_t part_bytes(int rows, int k) const { return segs > 1 ? (size_t)rows * segs * (8 * k + 16) : 0; }
+};
+AnswersGeom answers_geom(int rows, int cols, int k);
+hipError_t launch_answers(const AnswersParams &p, const AnswersGeom &g, hipStream_t st);
 
 // Depthwise 3x3 (stride 1 or 2, dilation 1) fused into the pointwise GEMM
 // that consumes it: x is the depthwise input (sliced, N*H*W pixels per

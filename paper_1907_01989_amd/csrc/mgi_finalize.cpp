@@ -20,6 +20,7 @@
 // sliced layout is skipped).
 #include <algorithm>
 #include <climits>
+#include <cmath>
 #include <cstring>
 #include <new>
 
@@ -780,6 +781,73 @@ void fuse_softmax_into_fc(mgi_plan &p) {
     p.nodes.swap(kept);
 }
 
+// Questions about the same rows are answered by the first one's node, one pass
+// over the rows for all of them: up to one topk, one entropy and kAnswerLists
+// lists of channels.  A list joins when its indices are ready before that node
+// or come from its own topk.  (Only lists wait for other questions' results, so
+// the earlier place is right for every reader.)
+void fuse_answers(mgi_plan &p) {
+    std::vector<int> producer(p.bufs.size(), -1);
+    for (size_t i = 0; i < p.nodes.size(); ++i) producer[p.nodes[i].out] = (int)i;
+    std::vector<char> drop(p.nodes.size(), 0);
+    for (size_t i = 0; i < p.nodes.size(); ++i) {
+        Node &a = p.nodes[i];
+        if (a.kind != NodeKind::Answers || drop[i]) continue;
+        for (size_t j = i + 1; j < p.nodes.size(); ++j) {
+            const Node &b = p.nodes[j];
+            if (b.kind != NodeKind::Answers || drop[j] || b.in[0] != a.in[0]) continue;
+            if (b.out_top >= 0) {
+                if (a.out_top >= 0) continue;
+                a.out_top = b.out_top;
+                a.k = b.k;
+            } else if (b.out_entropy >= 0) {
+                if (a.out_entropy >= 0) continue;
+                a.out_entropy = b.out_entropy;
+            } else {
+                const int ib = b.list_in[0];
+                if (a.n_lists == kern::kAnswerLists || (ib != a.out_top && producer[ib] >= (int)i)) continue;
+                if (ib != a.out_top) a.in.push_back(ib);
+                a.list_in[a.n_lists] = ib;
+                a.list_out[a.n_lists++] = b.out;
+            }
+            a.kname = "answers";
+            a.n_fused += b.n_fused;
+            drop[j] = 1;
+            producer[b.out] = (int)i;
+        }
+    }
+    std::vector<Node> kept;
+    for (size_t i = 0; i < p.nodes.size(); ++i)
+        if (!drop[i]) kept.push_back(std::move(p.nodes[i]));
+    p.nodes.swap(kept);
+}
+
+// Geometry of the FcInt4 and Answers kernels, the scratch tensors and counters
+// of those that split their sums over workgroups, and whether questions are
+// about graph inputs.
+void plan_splits(mgi_plan &p) {
+    for (Node &nd : p.nodes) {
+        size_t part = 0;
+        if (nd.kind == NodeKind::FcInt4) {
+            const int M = (int)p.bufs[nd.in[0]].shape.pixels();
+            part = nd.fq_geo.part_bytes(M, nd.nb16);
+            nd.cnt_bytes = part ? nd.fq_geo.tiles(M, nd.nb16) * sizeof(int) : 0;
+        } else if (nd.kind == NodeKind::Answers) {
+            const Shape s = p.bufs[nd.in[0]].shape;
+            nd.an_geo = kern::answers_geom((int)s.pixels(), s.c, nd.k);
+            part = nd.an_geo.part_bytes((int)s.pixels(), nd.k);
+            nd.cnt_bytes = part ? s.pixels() * sizeof(int) : 0;
+            for (int b : nd.in) p.reads_inputs_late = p.reads_inputs_late || p.bufs[b].loc == Loc::Input;
+        }
+        if (part == 0) continue;
+        Buf b;
+        b.layout = Layout::F32;
+        b.bytes = part;
+        nd.scratch = (int)p.bufs.size();
+        p.bufs.push_back(b);
+    }
+}
+
 // Pipelined pointwise kernel (K >= 64, at least 64 output channels): a
 // 128 x 128 tile when there are at least 512 channels, else 128 x 64, as long
 // as that still gives 384 workgroups (1.5 per CU); otherwise 64 x 64, which
@@ -996,7 +1064,7 @@ std::vector<Group> group_operators(const mgi_graph &g, const mgi_options &o, con
                 Group &G = groups[gi];
                 OpKind hk = g.ops[G.head].kind;
                 bool ok_kind = hk == OpKind::Conv2d || hk == OpKind::Depthwise ||
-                               hk == OpKind::FC || hk == OpKind::Add;
+                               hk == OpKind::FC || hk == OpKind::FcInt4 || hk == OpKind::Add;
                 int &slot = (G.residual_tensor >= 0) ? G.act2 : G.act1;
                 if (ok_kind && !G.resize_argmax && slot == MGI_ACT_NONE) {
                     slot = op.act;
@@ -1061,11 +1129,12 @@ struct Lowering {
     std::vector<int> c8_buf;     // graph tensor -> C8 (or other) buffer holding it
     std::vector<int> flat_buf;   // graph tensor -> F32 / I32 buffer
     std::vector<int> in_buf;     // graph input tensor -> NHWC_IN buffer
+    std::vector<int> rows_buf;   // graph tensor -> fp32 copy of its sliced form, for Answers nodes
     std::vector<int> out_index;  // graph tensor -> graph output index
 
     Lowering(const mgi_graph &g_, mgi_plan &p_)
         : g(g_), p(p_), c8_buf(g_.ops.size(), -1), flat_buf(g_.ops.size(), -1), in_buf(g_.ops.size(), -1),
-          out_index(g_.ops.size(), -1) {
+          rows_buf(g_.ops.size(), -1), out_index(g_.ops.size(), -1) {
         for (size_t k = 0; k < g.outputs.size(); ++k) out_index[g.outputs[k]] = (int)k;
     }
     void add_inputs();
@@ -1075,6 +1144,8 @@ struct Lowering {
         return (int)p.nodes.size() - 1;
     }
     int need_c8(int t);
+    int export_f32(int c8, const Shape &s);
+    mgi_status lower_answers(const Group &G, const GOp &op, const Shape &out_shape, Node &nd);
     mgi_status lower_conv(const Group &G, const GOp &op, const Shape &out_shape, Node &nd);
     mgi_status lower_other(const Group &G, const GOp &op, const Shape &out_shape, Node &nd);
     mgi_status lower(const Group &G);
@@ -1122,7 +1193,7 @@ int Lowering::new_buf(Layout L, const Shape &s, int tensor) {
 // a C8 view of graph tensor t, converting a graph input on first use
 int Lowering::need_c8(int t) {
     if (c8_buf[t] >= 0) return c8_buf[t];
-    if (g.ops[t].kind == OpKind::Input) {
+    if (g.ops[t].kind == OpKind::Input && g.ops[t].in_dtype != MGI_DTYPE_INT32) {
         Node nd;
         nd.kind = NodeKind::Ingest;
         nd.kname = "ingest";
@@ -1137,6 +1208,57 @@ int Lowering::need_c8(int t) {
         return ob;
     }
     return -1;
+}
+
+// an fp32 NHWC copy of a sliced buffer
+int Lowering::export_f32(int c8, const Shape &s) {
+    Node ex;
+    ex.kind = NodeKind::Export;
+    ex.kname = "export";
+    ex.out_tensor = -1;
+    ex.n_fused = 0;
+    ex.in = {c8};
+    ex.out = new_buf(Layout::F32, s, -1);
+    const int b = ex.out;
+    add_node(std::move(ex));
+    return b;
+}
+
+// One question about the channels of each pixel.  Its rows are an fp32 buffer
+// (logits), a graph input read in place, or a copy of a sliced tensor that all
+// questions about it share.
+mgi_status Lowering::lower_answers(const Group &G, const GOp &op, const Shape &out_shape, Node &nd) {
+    const int t = op.in[0];
+    const Shape x = g.ops[t].out;
+    int xb = flat_buf[t];
+    if (xb < 0) xb = in_buf[t];
+    if (xb < 0) {
+        if (rows_buf[t] < 0 && c8_buf[t] >= 0) rows_buf[t] = export_f32(c8_buf[t], x);
+        xb = rows_buf[t];
+    }
+    if (xb < 0 || p.bufs[xb].layout == Layout::I32)
+        return fail(MGI_ERR_UNSUPPORTED, "operand of topk, log_prob or entropy has no values");
+    nd.kind = NodeKind::Answers;
+    nd.in = {xb};
+    nd.out = new_buf(op.kind == OpKind::TopK ? Layout::I32 : Layout::F32, out_shape, G.last);
+    flat_buf[G.last] = nd.out;
+    if (op.kind == OpKind::TopK) {
+        nd.kname = "topk";
+        nd.k = op.k;
+        nd.out_top = nd.out;
+    } else if (op.kind == OpKind::Entropy) {
+        nd.kname = "entropy";
+        nd.out_entropy = nd.out;
+    } else {
+        const int u = op.in[1], ib = in_buf[u] >= 0 ? in_buf[u] : flat_buf[u];
+        if (ib < 0) return fail(MGI_ERR_UNSUPPORTED, "index of log_prob unavailable");
+        nd.kname = "log_prob";
+        nd.in.push_back(ib);
+        nd.n_lists = 1;
+        nd.list_in[0] = ib;
+        nd.list_out[0] = nd.out;
+    }
+    return MGI_OK;
 }
 
 // A convolution group: the stem kernel when it reads a graph input through a
@@ -1195,7 +1317,7 @@ mgi_status Lowering::lower_conv(const Group &G, const GOp &op, const Shape &out_
 // One node for an operator group (Sec. 3.2: the element-wise operators a
 // group absorbed run in the head operator's epilogue), plus an export node
 // when the group's output is a graph output kept in sliced form.
-// Groups headed by a fully-connected layer, softmax, concatenation, resize,
+// Groups headed by a fully-connected layer (16- or 4-bit weights), softmax, concatenation, resize,
 // argmax or padding.
 mgi_status Lowering::lower_other(const Group &G, const GOp &op, const Shape &out_shape, Node &nd) {
     switch (op.kind) {
@@ -1215,6 +1337,21 @@ mgi_status Lowering::lower_other(const Group &G, const GOp &op, const Shape &out
             nd.tile = pick_tile(out_shape.pixels(), op.cout);
             nd.out = new_buf(Layout::F32, out_shape, G.last);
             flat_buf[G.last] = nd.out;
+            return MGI_OK;
+        }
+        case OpKind::FcInt4: {
+            int xb = need_c8(op.in[0]);
+            if (xb < 0) return fail(MGI_ERR_UNSUPPORTED, "fc_int4 input must come from a sliced tensor");
+            const Shape x = g.ops[op.in[0]].out;
+            nd.kind = NodeKind::FcInt4;
+            nd.kname = "fc_int4";
+            nd.in = {xb};
+            nd.ksl = slices(x.c);
+            nd.ksp = (nd.ksl + 15) / 16;   // blocks of 128 input channels
+            nd.nb16 = (op.cout + 15) / 16;
+            nd.out = new_buf(Layout::F32, out_shape, G.last);
+            flat_buf[G.last] = nd.out;
+            nd.fq_geo = kern::fcint4_geom(x.n, nd.nb16, nd.ksp, op.group);
             return MGI_OK;
         }
         case OpKind::Softmax: {
@@ -1354,7 +1491,15 @@ mgi_status Lowering::lower(const Group &G) {
             c8_buf[G.last] = nd.out;
             break;
         }
+        case OpKind::TopK:
+        case OpKind::LogProb:
+        case OpKind::Entropy: {
+            const mgi_status st = lower_answers(G, op, out_shape, nd);
+            if (st != MGI_OK) return st;
+            break;
+        }
         case OpKind::FC:
+        case OpKind::FcInt4:
         case OpKind::Softmax:
         case OpKind::Concat:
         case OpKind::ResizeBilinear:
@@ -1421,6 +1566,9 @@ void compute_lifetimes(mgi_plan &p) {
     for (size_t i = 0; i < p.nodes.size(); ++i) {
         const Node &nd = p.nodes[i];
         p.bufs[nd.out].producer = (int)i;
+        for (int b : {nd.out_top, nd.out_entropy})
+            if (b >= 0) p.bufs[b].producer = (int)i;
+        for (int l = 0; l < nd.n_lists; ++l) p.bufs[nd.list_out[l]].producer = (int)i;
         for (int b : nd.in) p.bufs[b].last_use = (int)i;
         if (nd.residual >= 0) p.bufs[nd.residual].last_use = (int)i;
         if (nd.scratch >= 0) p.bufs[nd.scratch].producer = p.bufs[nd.scratch].last_use = (int)i;
@@ -1495,9 +1643,78 @@ void plan_memory(mgi_plan &p, const mgi_options &o) {
         nd.cnt_off = p.state_off + state;
         state = align256(state + ((p.bufs[nd.out].shape.pixels() + 15) / 16) * sizeof(int));
     }
+    // ... and the counters of sums that are split over workgroups
+    for (Node &nd : p.nodes) {
+        if (nd.cnt_bytes == 0) continue;
+        nd.cnt_off = p.state_off + state;
+        state = align256(state + nd.cnt_bytes);
+    }
     p.state_bytes = state;
     p.workspace_bytes = std::max<size_t>(p.state_off + state, 256);
 
+}
+
+// Codes, scales, zero points, exponents and biases of a 4-bit layer.  A wave's
+// codes of 16 output channels x 128 input channels are one KiB, 16 bytes to a
+// lane in the order of the MFMA A operand: word s of lane l holds channel
+// l % 16's inputs 32 s + 8 (l / 16) .. + 7, input 2i at bits 4i and input
+// 2i + 1 at bits 16 + 4i, so that a shift and a mask give a pair of 16-bit
+// values.  Inputs past the last take their group's zero point: weight 0.
+// Scales are divided by a power of two per output channel that brings the
+// channel's largest near 1 and are then rounded to the storage type (half a
+// unit in the last place, 2^-11 in fp16 and 2^-9 in bf16): in fp16 a scale below
+// 6e-5 would lose bits, and one below 6e-8 vanish, without it.
+template <typename Reserve, typename Bits>
+void pack_fc_int4(const GOp &op, int cin, Node &nd, std::vector<uint8_t> &blob, Reserve reserve, Bits to_bits) {
+    const int cout = op.cout, kb = nd.ksp, gs = nd.fq_geo.gs, per = 4 / gs, groups = (cin + op.group - 1) / op.group;
+    const size_t row_bytes = ((size_t)cin + 1) / 2, nscales = (size_t)nd.nb16 * kb * 16 * per;
+    nd.w_bytes = (size_t)nd.nb16 * kb * 1024;
+    nd.w_off = reserve(nd.w_bytes);
+    nd.s_off = reserve(nscales * 2);
+    nd.z_off = op.zeros.empty() ? 0 : reserve(nscales);
+    nd.e_off = reserve((size_t)nd.nb16 * 16 * 4);
+    nd.b_bytes = (size_t)nd.nb16 * 16 * 4;
+    nd.b_off = reserve(nd.b_bytes);
+    uint32_t *wp = reinterpret_cast<uint32_t *>(blob.data() + nd.w_off);
+    uint16_t *sp = reinterpret_cast<uint16_t *>(blob.data() + nd.s_off);
+    uint8_t *zp = nd.z_off ? blob.data() + nd.z_off : nullptr;
+    float *ep = reinterpret_cast<float *>(blob.data() + nd.e_off);
+    float *bp = reinterpret_cast<float *>(blob.data() + nd.b_off);
+    std::vector<uint8_t> code((size_t)kb * 128);
+    for (int co = 0; co < nd.nb16 * 16; ++co) {
+        const int nb = co / 16, row = co % 16;
+        if (co >= cout) {   // channels past the last: weight 0 (never stored, but in range)
+            std::fill(code.begin(), code.end(), 8);
+        } else {
+            const uint8_t *src = op.codes.data() + (size_t)co * row_bytes;
+            const float *sc = op.w.data() + (size_t)co * groups;
+            for (int i = 0; i < cin; ++i) code[i] = (src[i >> 1] >> (i & 1 ? 4 : 0)) & 15;
+            const uint8_t last = op.zeros.empty() ? 8 : op.zeros[(size_t)co * groups + groups - 1];
+            std::fill(code.begin() + cin, code.end(), last);
+            float top = 0.0f;
+            for (int gi = 0; gi < groups; ++gi) top = std::max(top, std::fabs(sc[gi]));
+            // (exponents as far as both powers of two stay normal numbers)
+            int e = 0;
+            if (top > 0.0f) e = std::min(std::max(std::ilogb(top), -126), 126);
+            ep[co] = std::ldexp(1.0f, e);
+            bp[co] = op.b[co];
+            for (int b = 0; b < kb; ++b)
+                for (int q = 0; q < per; ++q) {
+                    const int gi = std::min((b * 128 + q * gs * 32) / op.group, groups - 1);
+                    const size_t at = (((size_t)nb * kb + b) * 16 + row) * per + q;
+                    sp[at] = to_bits(std::ldexp(sc[gi], -e));
+                    if (zp) zp[at] = op.zeros[(size_t)co * groups + gi];
+                }
+        }
+        for (int b = 0; b < kb; ++b)
+            for (int s = 0; s < 4; ++s)
+                for (int q = 0; q < 4; ++q) {
+                    const uint8_t *c = code.data() + (size_t)b * 128 + s * 32 + q * 8;
+                    uint32_t v = 0;
+                    for (int i = 0; i < 4; ++i) v |= (uint32_t)c[2 * i] << (4 * i) | (uint32_t)c[2 * i + 1] << (16 + 4 * i);
+                    wp[(((size_t)nb * kb + b) * 64 + q * 16 + row) * 4 + s] = v;
+                }
+    }
 }
 
 // The packed weight blob, uploaded by mgi_plan_bind.
@@ -1519,6 +1736,7 @@ void pack_weights(const mgi_graph &g, mgi_plan &p, const mgi_options &o) {
     p.zero_off = reserve(256);  // zeroed block read by kernels for out-of-range taps
     for (Node &nd : p.nodes) {
         const GOp &op = g.ops[nd.op >= 0 ? nd.op : 0];
+        if (nd.kind == NodeKind::FcInt4) pack_fc_int4(op, g.ops[op.in[0]].out.c, nd, blob, reserve, to_bits);
         if (nd.kind == NodeKind::DwPw) {
             // depthwise taps of the absorbed op, laid out as for a depthwise node
             const GOp &dop = g.ops[nd.dw_op];
@@ -1739,6 +1957,7 @@ void absorb_ingests(mgi_plan &p, const mgi_options &o) {
                 case NodeKind::Gemm:
                 case NodeKind::PwDw:
                 case NodeKind::GemmPool:
+                case NodeKind::FcInt4:
                 case NodeKind::Gap: all = all && same; break;
                 default: all = false;
             }
@@ -1769,6 +1988,8 @@ mgi_status build_plan_impl(const mgi_graph &g, const mgi_options &o, mgi_plan &p
     if (o.fuse && o.fuse_pool) fuse_pool_into_pw(p, o.fuse_pool == 2);
     if (o.fuse && o.fuse_softmax) fuse_softmax_into_fc(p);
     if (o.fuse && o.fuse_dwpw) fuse_dw_into_pw(p);
+    if (o.fuse && !o.materialize_all) fuse_answers(p);
+    plan_splits(p);
     if (o.fuse && !o.materialize_all) {
         alias_concats(p, o);
         absorb_exports(p);

@@ -3,6 +3,8 @@
 // Each add call checks its operands the way the paper's delegate checks that
 // an operator is supported before taking it over (Sec. 3.1); there is no CPU
 // fallback, an unsupported operator is reported as MGI_ERR_UNSUPPORTED.
+#include <climits>
+#include <cmath>
 #include <cstdio>
 #include <cstring>
 #include <new>
@@ -67,6 +69,32 @@ mgi_status check_tensor(const mgi_graph *g, int id, const char *who) {
     return MGI_OK;
 }
 
+bool is_index(const GOp &op) {
+    return op.kind == OpKind::TopK || op.kind == OpKind::Argmax ||
+           (op.kind == OpKind::Input && op.in_dtype == MGI_DTYPE_INT32);
+}
+
+// an operand that holds values: not the indices of topk or of an index input
+mgi_status check_values(const mgi_graph *g, int id, const char *who) {
+    const mgi_status s = check_tensor(g, id, who);
+    if (s) return s;
+    if (is_index(g->ops[id]) && g->ops[id].kind != OpKind::Argmax)   // (argmax: finalize says so)
+        return fail(MGI_ERR_UNSUPPORTED, std::string(who) + ": tensor " + std::to_string(id) + " holds indices");
+    return MGI_OK;
+}
+
+// the operand of topk, log_prob and entropy
+mgi_status check_rows(const mgi_graph *g, int id, const char *who) {
+    const mgi_status s = check_values(g, id, who);
+    if (s) return s;
+    if (g->ops[id].kind == OpKind::Argmax)
+        return fail(MGI_ERR_UNSUPPORTED, std::string(who) + ": tensor " + std::to_string(id) + " holds indices");
+    const Shape x = g->ops[id].out;
+    if (x.c > kern::kMaxAnswerCols || x.pixels() > (size_t)INT_MAX / 8)
+        return fail(MGI_ERR_UNSUPPORTED, std::string(who) + ": at most 2^19 channels and 2^28 - 1 pixels");
+    return MGI_OK;
+}
+
 mgi_status push(mgi_graph *g, GOp &&op, int *out) {
     try {
         g->ops.push_back(std::move(op));
@@ -118,7 +146,7 @@ extern "C" mgi_status mgi_graph_add_input(mgi_graph *g, int n, int h, int w, int
 extern "C" mgi_status mgi_graph_add_conv2d(mgi_graph *g, int in, const mgi_conv_desc *d,
                                            const float *w, const float *bias, int *out) {
     MGI_ABI_TRY
-    mgi_status s = check_tensor(g, in, "mgi_graph_add_conv2d");
+    mgi_status s = check_values(g, in, "mgi_graph_add_conv2d");
     if (s) return s;
     if (!out || !w) return fail(MGI_ERR_INVALID_ARG, "mgi_graph_add_conv2d: null pointer");
     const Shape x = g->ops[in].out;
@@ -145,7 +173,7 @@ extern "C" mgi_status mgi_graph_add_conv2d(mgi_graph *g, int in, const mgi_conv_
 extern "C" mgi_status mgi_graph_add_depthwise(mgi_graph *g, int in, const mgi_conv_desc *d,
                                               const float *w, const float *bias, int *out) {
     MGI_ABI_TRY
-    mgi_status s = check_tensor(g, in, "mgi_graph_add_depthwise");
+    mgi_status s = check_values(g, in, "mgi_graph_add_depthwise");
     if (s) return s;
     if (!out || !w) return fail(MGI_ERR_INVALID_ARG, "mgi_graph_add_depthwise: null pointer");
     const Shape x = g->ops[in].out;
@@ -176,7 +204,7 @@ static bool same_shape(const Shape &a, const Shape &b) {
 extern "C" mgi_status mgi_graph_add_add(mgi_graph *g, int a, int b, int act, int *out) {
     MGI_ABI_TRY
     mgi_status s;
-    if ((s = check_tensor(g, a, "mgi_graph_add_add")) || (s = check_tensor(g, b, "mgi_graph_add_add")))
+    if ((s = check_values(g, a, "mgi_graph_add_add")) || (s = check_values(g, b, "mgi_graph_add_add")))
         return s;
     if (!out) return fail(MGI_ERR_INVALID_ARG, "mgi_graph_add_add: null pointer");
     if (!valid_act(act)) return fail(MGI_ERR_INVALID_ARG, "mgi_graph_add_add: bad activation");
@@ -193,7 +221,7 @@ extern "C" mgi_status mgi_graph_add_add(mgi_graph *g, int a, int b, int act, int
 
 extern "C" mgi_status mgi_graph_add_activation(mgi_graph *g, int in, int act, int *out) {
     MGI_ABI_TRY
-    mgi_status s = check_tensor(g, in, "mgi_graph_add_activation");
+    mgi_status s = check_values(g, in, "mgi_graph_add_activation");
     if (s) return s;
     if (!out) return fail(MGI_ERR_INVALID_ARG, "mgi_graph_add_activation: null pointer");
     if (!valid_act(act)) return fail(MGI_ERR_INVALID_ARG, "mgi_graph_add_activation: bad activation");
@@ -209,7 +237,7 @@ extern "C" mgi_status mgi_graph_add_activation(mgi_graph *g, int in, int act, in
 extern "C" mgi_status mgi_graph_add_pad(mgi_graph *g, int in, int pad_t, int pad_b, int pad_l,
                                         int pad_r, int *out) {
     MGI_ABI_TRY
-    mgi_status s = check_tensor(g, in, "mgi_graph_add_pad");
+    mgi_status s = check_values(g, in, "mgi_graph_add_pad");
     if (s) return s;
     if (!out) return fail(MGI_ERR_INVALID_ARG, "mgi_graph_add_pad: null pointer");
     if (pad_t < 0 || pad_b < 0 || pad_l < 0 || pad_r < 0)
@@ -230,7 +258,7 @@ extern "C" mgi_status mgi_graph_add_pad(mgi_graph *g, int in, int pad_t, int pad
 
 extern "C" mgi_status mgi_graph_add_global_avgpool(mgi_graph *g, int in, int *out) {
     MGI_ABI_TRY
-    mgi_status s = check_tensor(g, in, "mgi_graph_add_global_avgpool");
+    mgi_status s = check_values(g, in, "mgi_graph_add_global_avgpool");
     if (s) return s;
     if (!out) return fail(MGI_ERR_INVALID_ARG, "mgi_graph_add_global_avgpool: null pointer");
     GOp op;
@@ -245,7 +273,7 @@ extern "C" mgi_status mgi_graph_add_global_avgpool(mgi_graph *g, int in, int *ou
 extern "C" mgi_status mgi_graph_add_fc(mgi_graph *g, int in, int cout, const float *w,
                                        const float *bias, int *out) {
     MGI_ABI_TRY
-    mgi_status s = check_tensor(g, in, "mgi_graph_add_fc");
+    mgi_status s = check_values(g, in, "mgi_graph_add_fc");
     if (s) return s;
     if (!out || !w) return fail(MGI_ERR_INVALID_ARG, "mgi_graph_add_fc: null pointer");
     if (cout <= 0) return fail(MGI_ERR_INVALID_ARG, "mgi_graph_add_fc: cout must be positive");
@@ -269,7 +297,7 @@ extern "C" mgi_status mgi_graph_add_fc(mgi_graph *g, int in, int cout, const flo
 
 extern "C" mgi_status mgi_graph_add_softmax(mgi_graph *g, int in, int *out) {
     MGI_ABI_TRY
-    mgi_status s = check_tensor(g, in, "mgi_graph_add_softmax");
+    mgi_status s = check_values(g, in, "mgi_graph_add_softmax");
     if (s) return s;
     if (!out) return fail(MGI_ERR_INVALID_ARG, "mgi_graph_add_softmax: null pointer");
     GOp op;
@@ -288,7 +316,7 @@ extern "C" mgi_status mgi_graph_add_concat(mgi_graph *g, const int *ins, int cou
                     "mgi_graph_add_concat: 1 to 8 inputs");
     Shape o{};
     for (int i = 0; i < count; ++i) {
-        mgi_status s = check_tensor(g, ins[i], "mgi_graph_add_concat");
+        mgi_status s = check_values(g, ins[i], "mgi_graph_add_concat");
         if (s) return s;
         const Shape x = g->ops[ins[i]].out;
         if (i == 0) o = x, o.c = 0;
@@ -307,7 +335,7 @@ extern "C" mgi_status mgi_graph_add_concat(mgi_graph *g, const int *ins, int cou
 extern "C" mgi_status mgi_graph_add_resize_bilinear(mgi_graph *g, int in, int oh, int ow,
                                                     int align_corners, int *out) {
     MGI_ABI_TRY
-    mgi_status s = check_tensor(g, in, "mgi_graph_add_resize_bilinear");
+    mgi_status s = check_values(g, in, "mgi_graph_add_resize_bilinear");
     if (s) return s;
     if (!out) return fail(MGI_ERR_INVALID_ARG, "mgi_graph_add_resize_bilinear: null pointer");
     if (oh <= 0 || ow <= 0)
@@ -326,7 +354,7 @@ extern "C" mgi_status mgi_graph_add_resize_bilinear(mgi_graph *g, int in, int oh
 
 extern "C" mgi_status mgi_graph_add_argmax(mgi_graph *g, int in, int *out) {
     MGI_ABI_TRY
-    mgi_status s = check_tensor(g, in, "mgi_graph_add_argmax");
+    mgi_status s = check_values(g, in, "mgi_graph_add_argmax");
     if (s) return s;
     if (!out) return fail(MGI_ERR_INVALID_ARG, "mgi_graph_add_argmax: null pointer");
     GOp op;
@@ -336,6 +364,110 @@ extern "C" mgi_status mgi_graph_add_argmax(mgi_graph *g, int in, int *out) {
     op.out = {x.n, x.h, x.w, 1};
     return push(g, std::move(op), out);
     MGI_ABI_CATCH("mgi_graph_add_argmax")
+}
+
+extern "C" mgi_status mgi_graph_add_fc_int4(mgi_graph *g, int in, int cout, int group,
+                                            const unsigned char *codes, const float *scales,
+                                            const unsigned char *zeros, const float *bias, int *out) {
+    MGI_ABI_TRY
+    const char *who = "mgi_graph_add_fc_int4";
+    mgi_status s = check_values(g, in, who);
+    if (s) return s;
+    if (!out || !codes || !scales) return fail(MGI_ERR_INVALID_ARG, std::string(who) + ": null pointer");
+    if (cout <= 0) return fail(MGI_ERR_INVALID_ARG, std::string(who) + ": cout must be positive");
+    if (group <= 0) return fail(MGI_ERR_INVALID_ARG, std::string(who) + ": group must be positive");
+    if (group % 32 != 0) return fail(MGI_ERR_UNSUPPORTED, std::string(who) + ": group must be a multiple of 32");
+    const Shape x = g->ops[in].out;
+    if (x.h != 1 || x.w != 1)
+        return fail(MGI_ERR_UNSUPPORTED, std::string(who) + ": input must be 1x1 spatially");
+    const size_t groups = ((size_t)x.c + group - 1) / group, n = (size_t)cout * groups;
+    for (size_t i = 0; i < n; ++i)
+        if (!std::isfinite(scales[i])) return fail(MGI_ERR_INVALID_ARG, std::string(who) + ": scales must be finite");
+    for (size_t i = 0; zeros && i < n; ++i)
+        if (zeros[i] > 15) return fail(MGI_ERR_INVALID_ARG, std::string(who) + ": zero points are 0..15");
+    GOp op;
+    op.kind = OpKind::FcInt4;
+    op.in = {in};
+    op.cout = cout;
+    op.group = group;
+    op.out = {x.n, 1, 1, cout};
+    try {
+        op.codes.assign(codes, codes + (size_t)cout * ((x.c + 1) / 2));
+        op.w.assign(scales, scales + n);
+        if (zeros) op.zeros.assign(zeros, zeros + n);
+        if (bias) op.b.assign(bias, bias + cout); else op.b.assign(cout, 0.0f);
+    } catch (const std::bad_alloc &) {
+        return fail(MGI_ERR_OOM_HOST, std::string(who) + ": out of host memory");
+    }
+    return push(g, std::move(op), out);
+    MGI_ABI_CATCH("mgi_graph_add_fc_int4")
+}
+
+extern "C" mgi_status mgi_graph_add_index_input(mgi_graph *g, int n, int h, int w, int c, int *out) {
+    MGI_ABI_TRY
+    if (!g || !out) return fail(MGI_ERR_INVALID_ARG, "mgi_graph_add_index_input: null pointer");
+    if (n <= 0 || h <= 0 || w <= 0 || c <= 0)
+        return fail(MGI_ERR_INVALID_ARG, "mgi_graph_add_index_input: sizes must be positive");
+    GOp op;
+    op.kind = OpKind::Input;
+    op.out = {n, h, w, c};
+    op.in_dtype = MGI_DTYPE_INT32;
+    mgi_status s = push(g, std::move(op), out);
+    if (s == MGI_OK) g->inputs.push_back(*out);
+    return s;
+    MGI_ABI_CATCH("mgi_graph_add_index_input")
+}
+
+extern "C" mgi_status mgi_graph_add_topk(mgi_graph *g, int in, int k, int *out) {
+    MGI_ABI_TRY
+    mgi_status s = check_rows(g, in, "mgi_graph_add_topk");
+    if (s) return s;
+    if (!out) return fail(MGI_ERR_INVALID_ARG, "mgi_graph_add_topk: null pointer");
+    if (k <= 0) return fail(MGI_ERR_INVALID_ARG, "mgi_graph_add_topk: k must be positive");
+    const Shape x = g->ops[in].out;
+    if (k > x.c) return fail(MGI_ERR_SHAPE, "mgi_graph_add_topk: k exceeds the channels");
+    if (k > kern::kMaxTopK)
+        return fail(MGI_ERR_UNSUPPORTED, "mgi_graph_add_topk: k is at most " + std::to_string(kern::kMaxTopK));
+    GOp op;
+    op.kind = OpKind::TopK;
+    op.in = {in};
+    op.k = k;
+    op.out = {x.n, x.h, x.w, k};
+    return push(g, std::move(op), out);
+    MGI_ABI_CATCH("mgi_graph_add_topk")
+}
+
+extern "C" mgi_status mgi_graph_add_log_prob(mgi_graph *g, int in, int index, int *out) {
+    MGI_ABI_TRY
+    mgi_status s = check_rows(g, in, "mgi_graph_add_log_prob");
+    if (s || (s = check_tensor(g, index, "mgi_graph_add_log_prob"))) return s;
+    if (!out) return fail(MGI_ERR_INVALID_ARG, "mgi_graph_add_log_prob: null pointer");
+    const GOp &ix = g->ops[index];
+    if (!is_index(ix))
+        return fail(MGI_ERR_INVALID_ARG, "mgi_graph_add_log_prob: index is an index input or the output of topk or argmax");
+    const Shape x = g->ops[in].out;
+    if (ix.out.n != x.n || ix.out.h != x.h || ix.out.w != x.w)
+        return fail(MGI_ERR_SHAPE, "mgi_graph_add_log_prob: index differs in n, h or w");
+    GOp op;
+    op.kind = OpKind::LogProb;
+    op.in = {in, index};
+    op.out = ix.out;
+    return push(g, std::move(op), out);
+    MGI_ABI_CATCH("mgi_graph_add_log_prob")
+}
+
+extern "C" mgi_status mgi_graph_add_entropy(mgi_graph *g, int in, int *out) {
+    MGI_ABI_TRY
+    mgi_status s = check_rows(g, in, "mgi_graph_add_entropy");
+    if (s) return s;
+    if (!out) return fail(MGI_ERR_INVALID_ARG, "mgi_graph_add_entropy: null pointer");
+    GOp op;
+    op.kind = OpKind::Entropy;
+    op.in = {in};
+    op.out = g->ops[in].out;
+    op.out.c = 1;
+    return push(g, std::move(op), out);
+    MGI_ABI_CATCH("mgi_graph_add_entropy")
 }
 
 extern "C" mgi_status mgi_graph_mark_output(mgi_graph *g, int id) {

@@ -41,7 +41,7 @@ namespace mgi {
 
 enum class OpKind {
     Input, Conv2d, Depthwise, Add, Activation, GlobalAvgPool, FC, Softmax, Concat,
-    ResizeBilinear, Argmax, Pad
+    ResizeBilinear, Argmax, Pad, FcInt4, TopK, LogProb, Entropy
 };
 
 struct Shape {
@@ -59,7 +59,10 @@ struct GOp {
     int act = MGI_ACT_NONE;     // Conv2d / Depthwise / Add / Activation
     int in_dtype = MGI_DTYPE_FP32;  // Input
     int oh = 0, ow = 0, align_corners = 1;  // ResizeBilinear
-    int cout = 0;               // FC
+    int cout = 0;               // FC, FcInt4
+    int group = 0;              // FcInt4: input channels per scale (the scales are in w)
+    std::vector<uint8_t> codes, zeros;  // FcInt4: packed codes as given, zero points (empty: 8)
+    int k = 0;                  // TopK
     int pads[4] = {0, 0, 0, 0}; // Pad: top, bottom, left, right
     std::vector<float> w, b;    // weights as given (OHWI / CHW / COUT x CIN), bias
 };
@@ -100,7 +103,7 @@ struct Buf {
 
 enum class NodeKind {
     Ingest, Stem, Gemm, Depthwise, Add, Act, Gap, FC, Softmax, Concat, Resize, Argmax,
-    ResizeArgmax, Export, Pad, DwPw, PwDw, StemDw, GemmPool, FcSoftmax, Irb
+    ResizeArgmax, Export, Pad, DwPw, PwDw, StemDw, GemmPool, FcSoftmax, Irb, FcInt4, Answers
 };
 
 // Tile shape of the MFMA GEMM (pointwise, implicit-GEMM convolution, FC).
@@ -172,7 +175,19 @@ struct Node {
                             // (stemdw_configs, irb_configs)
     kern::PwDwGeom pwdw_geo{};   // PwDw, Irb (mode 1): geometry of the fused pair's kernel
     size_t cnt_off = 0;     // FcSoftmax: its row-tile arrival counters in the workspace's
-                            // state region
+                            // state region; FcInt4, Answers: counters of split sums
+    size_t cnt_bytes = 0;   // FcInt4, Answers: bytes of those counters (0: not split)
+    // FcInt4: geometry of its kernel, K steps of 32 per packed scale, packed
+    // scales, zero points (0: none) and exponents of the output channels
+    kern::FcInt4Geom fq_geo{};
+    size_t s_off = 0, z_off = 0, e_off = 0;
+    // Answers: in[0] holds the rows; buffers of the top channels and the
+    // entropy (-1: not asked), and of each list of channels whose log
+    // probabilities are asked, with the buffer they go to; `scratch`: what the
+    // segments of a row found
+    kern::AnswersGeom an_geo{};
+    int k = 0, out_top = -1, out_entropy = -1;
+    int n_lists = 0, list_in[kern::kAnswerLists] = {}, list_out[kern::kAnswerLists] = {};
     // Irb (a PwDw node that also runs the pointwise projection reading its
     // output): the projection's graph op, packed weights, GEMM geometry and
     // epilogue (residual in `residual`), the depthwise output kept as a
@@ -230,6 +245,7 @@ struct mgi_plan {
     size_t mem_naive = 0, mem_planned = 0;
     int n_objects = 0;
     mgi_options opt{};
+    bool reads_inputs_late = false;  // Answers nodes read graph inputs: outputs must not overlap them
     void *dev_ws = nullptr;
     void *dev_w = nullptr;
     bool bound = false;

@@ -437,6 +437,57 @@ hipError_t launch_dwpw_node(const mgi_plan &p, const Node &nd, const Bases &B, v
     return launch_dwpw(q, t, st);
 }
 
+hipError_t launch_fcint4_node(const mgi_plan &p, const Node &nd, const Bases &B, void *y, hipStream_t st) {
+    const char *wbase = static_cast<const char *>(p.dev_w);
+    FcInt4Params q{};
+    const Operand x = operand(p, nd.in[0], B);
+    q.x = x.x; q.xs = x.s; q.xp = x.p;
+    q.zero = (const h8 *)(wbase + p.zero_off);
+    q.w = (const uint32_t *)(wbase + nd.w_off);
+    q.scales = (const uint16_t *)(wbase + nd.s_off);
+    q.zp = nd.z_off ? (const uint8_t *)(wbase + nd.z_off) : nullptr;
+    q.mul = (const float *)(wbase + nd.e_off);
+    q.bias = (const float *)(wbase + nd.b_off);
+    q.y = (float *)y;
+    if (nd.cnt_bytes) {
+        q.part = (float *)buf_ptr(p, nd.scratch, B);
+        q.cnt = (int *)(B.ws + nd.cnt_off);
+    }
+    q.M = (int)p.bufs[nd.in[0]].shape.pixels();
+    q.ksl = nd.ksl; q.kb = nd.ksp; q.nb16 = nd.nb16;
+    q.cout = p.bufs[nd.out].shape.c;
+    q.act = nd.act1;
+    q.bf16 = p.opt.dtype == MGI_DTYPE_BF16;
+    return launch_fcint4(q, nd.fq_geo, st);
+}
+
+hipError_t launch_answers_node(const mgi_plan &p, const Node &nd, const Bases &B, hipStream_t st) {
+    const Buf &x = p.bufs[nd.in[0]];
+    AnswersParams q{};
+    q.x = buf_ptr(p, nd.in[0], B);
+    q.rows = (int)x.shape.pixels();
+    q.cols = x.shape.c;
+    q.fp16_in = x.layout == Layout::NHWC_IN && x.in_dtype == MGI_DTYPE_FP16;
+    if (nd.out_top >= 0) {
+        q.k = nd.k;
+        q.top = (int *)buf_ptr(p, nd.out_top, B);
+    }
+    if (nd.out_entropy >= 0) q.entropy = (float *)buf_ptr(p, nd.out_entropy, B);
+    q.n_lists = nd.n_lists;
+    for (int l = 0; l < nd.n_lists; ++l) {
+        q.list[l] = nd.list_in[l] == nd.out_top ? nullptr : (const int *)buf_ptr(p, nd.list_in[l], B);
+        q.list_out[l] = (float *)buf_ptr(p, nd.list_out[l], B);
+        q.list_n[l] = p.bufs[nd.list_out[l]].shape.c;
+    }
+    if (nd.cnt_bytes) {
+        char *part = (char *)buf_ptr(p, nd.scratch, B);
+        q.part_stats = (float *)part;
+        q.part_keys = (unsigned long long *)(part + (size_t)q.rows * nd.an_geo.segs * 16);
+        q.cnt = (int *)(B.ws + nd.cnt_off);
+    }
+    return launch_answers(q, nd.an_geo, st);
+}
+
 // A node that launches nothing in this run: a timed run's events are still
 // recorded.
 hipError_t mark_events(hipStream_t st) {
@@ -563,6 +614,10 @@ hipError_t launch_node(const mgi_plan &p, const Node &nd, const Bases &B, hipStr
                               (const h8 *)(wbase + p.zero_off), ib.shape.n,
                               ib.shape.h * ib.shape.w, slices(ib.shape.c), bf, st);
         }
+        case NodeKind::FcInt4:
+            return launch_fcint4_node(p, nd, B, y, st);
+        case NodeKind::Answers:
+            return launch_answers_node(p, nd, B, st);
         case NodeKind::Softmax:
             return launch_softmax((const float *)buf_ptr(p, nd.in[0], B), (float *)y,
                                   (int)os.pixels(), os.c, st);
@@ -689,6 +744,9 @@ mgi_status run_plan(mgi_plan *p, const void *const *dev_inputs, void *const *dev
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (!ws) ws = static_cast<char *>(p->dev_ws);
     Bases B{ws, dev_inputs, dev_outputs, io_disjoint(*p, dev_inputs, dev_outputs)};
+    if (p->reads_inputs_late && !B.direct)
+        return fail(MGI_ERR_INVALID_ARG, std::string(who) + ": an output overlaps an input, and this plan reads "
+                                                            "inputs while it writes outputs");
     B.in_place = inputs_in_place(*p, B);
     LaunchEvents &ev = launch_events();
     for (size_t i = 0; i < p->nodes.size(); ++i) {

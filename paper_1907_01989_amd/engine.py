@@ -35,6 +35,36 @@ def _torch_types():
     return _TORCH_TYPES
 
 
+def _channels(ops, t):
+    """Channels of tensor ``t`` of an operator list."""
+    op = ops[t]
+    if "shape" in op:
+        return op["shape"][3]
+    if op["op"] == "concat":
+        return sum(_channels(ops, u) for u in op["ins"])
+    if op["op"] in ("argmax", "entropy"):
+        return 1
+    if op["op"] == "topk":
+        return op["k"]
+    return op["cout"] if "cout" in op else _channels(ops, op.get("index", op.get("in", op.get("a"))))
+
+
+def _add_fc_int4(g, ops, op):
+    """The library receives raw pointers: arrays of other sizes are refused here."""
+    cin, cout, group = _channels(ops, op["in"]), op["cout"], op["group"]
+    groups = -(-cin // group) if group > 0 else 0
+    for name, size in (("q", cout * ((cin + 1) // 2)), ("scales", cout * groups), ("zeros", cout * groups), ("b", cout)):
+        a = op.get(name)
+        if a is None and name in ("zeros", "b"):
+            continue
+        if np.size(a) != size:
+            raise ValueError(f"fc_int4: {name} must hold {size} values ({cout} classes, {cin} channels, "
+                             f"groups of {group}), got {np.size(a)}")
+        if name in ("q", "zeros") and np.asarray(a).dtype != np.uint8:
+            raise ValueError(f"fc_int4: {name} must be uint8, got {np.asarray(a).dtype}")
+    return B.mgi_graph_add_fc_int4(g, op["in"], cout, group, op["q"], op["scales"], op.get("zeros"), op.get("b"))
+
+
 def build_graph(desc):
     """Create an mgi graph from ``desc`` (dict with "ops" and "outputs").
     Returns the graph handle; tensor ids equal op indices."""
@@ -72,6 +102,17 @@ def build_graph(desc):
                                                     op["align_corners"])
             elif k == "argmax":
                 t = B.mgi_graph_add_argmax(g, op["in"])
+            elif k == "fc_int4":
+                t = _add_fc_int4(g, desc["ops"], op)
+            elif k == "index_input":
+                n, h, w, c = op["shape"]
+                t = B.mgi_graph_add_index_input(g, n, h, w, c)
+            elif k == "topk":
+                t = B.mgi_graph_add_topk(g, op["in"], op["k"])
+            elif k == "log_prob":
+                t = B.mgi_graph_add_log_prob(g, op["in"], op["index"])
+            elif k == "entropy":
+                t = B.mgi_graph_add_entropy(g, op["in"])
             else:
                 raise ValueError(f"unknown op {k}")
             if t != i:
@@ -138,10 +179,10 @@ class Plan:
     def alloc_outputs(self):
         import torch
         outs = []
-        for shape, dt, _ in self.outputs_info:
+        for t, (shape, dt, _) in zip(self.desc["outputs"], self.outputs_info):
             n, h, w, c = shape
             tdt = torch.int32 if dt == B.DTYPE_INT32 else torch.float32
-            if dt == B.DTYPE_INT32:
+            if dt == B.DTYPE_INT32 and self.desc["ops"][t]["op"] == "argmax":
                 outs.append(torch.empty((n, h, w), dtype=tdt, device=self.device))
             elif h == 1 and w == 1:
                 outs.append(torch.empty((n, c), dtype=tdt, device=self.device))
@@ -162,7 +203,7 @@ class Plan:
             raise ValueError(f"plan takes {self.n_inputs} inputs and {self.n_outputs} outputs, "
                              f"got {len(inputs)} and {len(outputs)}")
         dev = torch.device(self.device)
-        in_types = {B.DTYPE_FP16: torch.float16, B.DTYPE_FP32: torch.float32}
+        in_types = {B.DTYPE_FP16: torch.float16, B.DTYPE_FP32: torch.float32, B.DTYPE_INT32: torch.int32}
         out_types = {B.DTYPE_INT32: torch.int32, B.DTYPE_FP32: torch.float32}
         for role, ts, info, types in (("input", inputs, self.inputs_info, in_types),
                                       ("output", outputs, self.outputs_info, out_types)):
@@ -244,6 +285,8 @@ class Plan:
             if op["op"] == "input":
                 dt = torch.float16 if op.get("dtype", B.DTYPE_FP32) == B.DTYPE_FP16 else torch.float32
                 xs.append(torch.from_numpy(np.ascontiguousarray(op["data"])).to(self.device, dt))
+            elif op["op"] == "index_input":
+                xs.append(torch.from_numpy(np.ascontiguousarray(op["data"], dtype=np.int32)).to(self.device))
         return xs
 
     # --------------------------------------------------------- introspection
@@ -254,8 +297,8 @@ class Plan:
         import torch
         info = B.mgi_plan_node_info(self.handle, i)
         n, h, w, c = info["shape"]
-        if info["kind"] in ("argmax", "resize_argmax"):
-            dst = torch.empty((n, h, w, 1), dtype=torch.int32, device=self.device)
+        if info["kind"] in ("argmax", "resize_argmax", "topk"):
+            dst = torch.empty((n, h, w, c), dtype=torch.int32, device=self.device)
         else:
             dst = torch.empty((n, h, w, c), dtype=torch.float32, device=self.device)
         B.mgi_plan_read_node(self.handle, i, dst.data_ptr(), _stream_handle(stream))

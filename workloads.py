@@ -159,6 +159,43 @@ class NetBuilder:
         return self._push({"op": "fc", "name": name or f"fc{idx}", "in": x, "cout": cout,
                            "w": wt, "b": b}, (1, 1, cout))
 
+    def fc_int4(self, x, cout, group=32, zeros=False, name=None):
+        """A fully connected layer with 4-bit weights: He-normal weights rounded
+        to codes of about 2.5 steps to a standard deviation, with scales that
+        differ by group (bf16 values, exact in fp16 too) and, with ``zeros``,
+        zero points."""
+        _, _, cin = self._hwc[x]
+        idx = len(self.ops)
+        rng = rng_for(self.seed, idx)
+        groups = -(-cin // group)
+        z = rng.integers(4, 12, size=(cout, groups)).astype(np.uint8) if zeros else None
+        code = rng.standard_normal((cout, cin)) * 2.5 + (8 if z is None else np.repeat(z, group, axis=1)[:, :cin])
+        code = np.clip(np.rint(code), 0, 15).astype(np.uint8)
+        code = np.pad(code, ((0, 0), (0, cin % 2)))
+        scales = bf16_round(np.exp(rng.standard_normal((cout, groups)) * 0.2) * 0.4 * np.sqrt(2.0 / cin))
+        b = bias_normal(rng, cout)
+        return self._push({"op": "fc_int4", "name": name or f"fc_int4_{idx}", "in": x, "cout": cout, "group": group,
+                           "q": code[:, 0::2] | code[:, 1::2] << 4, "scales": scales, "zeros": z, "b": b},
+                          (1, 1, cout))
+
+    def index_input(self, index, name=None):
+        """A graph input of channel indices, an (n, h, w, c) int32 array."""
+        index = np.asarray(index, np.int32)
+        return self._push({"op": "index_input", "name": name or f"index{len(self.ops)}", "shape": index.shape,
+                           "data": index}, index.shape[1:])
+
+    def topk(self, x, k, name=None):
+        h, w, _ = self._hwc[x]
+        return self._push({"op": "topk", "name": name or f"topk{len(self.ops)}", "in": x, "k": k}, (h, w, k))
+
+    def log_prob(self, x, index, name=None):
+        return self._push({"op": "log_prob", "name": name or f"log_prob{len(self.ops)}", "in": x, "index": index},
+                          self._hwc[index])
+
+    def entropy(self, x, name=None):
+        h, w, _ = self._hwc[x]
+        return self._push({"op": "entropy", "name": name or f"entropy{len(self.ops)}", "in": x}, (h, w, 1))
+
     def softmax(self, x, name=None):
         return self._push({"op": "softmax", "name": name or f"softmax{len(self.ops)}", "in": x},
                           self._hwc[x])
