@@ -45,15 +45,14 @@ __device__ __forceinline__ float wave_sum(float v) {
     return v;
 }
 
-// The r-th largest of a wave's 64 values, bit by bit.
-__device__ __forceinline__ float wave_rth(float v, int r) {
-    const uint32_t o = order_of(v);
+// The r-th largest of a wave's 64 integers, bit by bit.
+__device__ __forceinline__ uint32_t wave_rth(uint32_t o, int r) {
     uint32_t ans = 0;
     for (int b = 31; b >= 0; --b) {
         const uint32_t c = ans | 1u << b;
         if (__popcll(__ballot(o >= c)) >= r) ans = c;
     }
-    return value_of(ans);
+    return ans;
 }
 
 __device__ __forceinline__ int lanes_below(unsigned long long mask) {
@@ -65,6 +64,7 @@ struct Shared {
     unsigned long long cand[kCap];
     float top_val[kMaxTopK];
     float m[W], th[W], s[W], t[W];
+    uint32_t key_th[W];
     int cnt[W];
     int n, last;
 };
@@ -131,71 +131,96 @@ __device__ __forceinline__ void push(Shared<W> &sh, const H &h, float th) {
         }
 }
 
+// Hands every candidate of the first k to `found`, with its rank: the number of
+// larger ones.  2^g neighbouring lanes share a candidate's comparisons.
+template <int NT, typename F>
+__device__ __forceinline__ void rank(const unsigned long long *cand, int n, int k, F found) {
+    int g = 0;
+    while (g < 6 && (n << (g + 1)) <= NT) ++g;
+    const int part = threadIdx.x & ((1 << g) - 1);
+    for (int j = threadIdx.x >> g; j < n; j += NT >> g) {
+        const unsigned long long key = cand[j];
+        int r = 0;
+#pragma unroll 8
+        for (int q = part; q < n; q += 1 << g) r += cand[q] > key;
+        for (int b = 0; b < g; ++b) r += __shfl_xor(r, 1 << b, 64);
+        if (part == 0 && r < k) found(r, key);
+    }
+}
+
 // Called by the whole workgroup where `push` found fewer than k candidates (all
-// others are -inf) or more than there is room for: the exact k-th largest
-// value, what is above it, and of its equals the first columns.  Leaves
-// exactly k candidates.  (Rows that are mostly masked, or mostly equal.)
-template <int W, typename H>
-__device__ __forceinline__ void push_exact(Shared<W> &sh, const H &h, int k) {
+// others are -inf) or more than there is room for (more than that many equal
+// values, most often): the exact k-th largest value, what is above it, and of
+// its equals the first columns.  Leaves exactly k candidates.  Reads the row
+// again: a call that keeps the values in registers takes them from the usual
+// case's second workgroup of a compute unit.
+template <typename T, int NT>
+__device__ __noinline__ void push_exact(Shared<NT / 64> &sh, const T *x, int lo, int hi, int k) {
+    constexpr int W = NT / 64;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    float kth = -INFINITY;
-    if (sh.n > kCap) {
-        uint32_t ans = 0;
-        for (int b = 31; b >= 0; --b) {
-            const uint32_t c = ans | 1u << b;
-            int n = 0;
-#pragma unroll
-            for (int q = 0; q < H::I * H::VEC; ++q) n += __popcll(__ballot(order_of(fmaxf(h.v[q], -INFINITY)) >= c));
-            __syncthreads();
-            if (lane == 0) sh.cnt[wave] = n;
-            __syncthreads();
-            n = 0;
-            for (int w = 0; w < W; ++w) n += sh.cnt[w];
-            if (n >= k) ans = c;
+    auto value = [&](int c) { return fmaxf((float)x[min(c, hi - 1)], -INFINITY); };   // NaN: -inf
+    // the sum over the workgroup of a wave's count, before: of the waves before this one
+    auto total = [&](int n, int &before) {
+        __syncthreads();
+        if (lane == 0) sh.cnt[wave] = n;
+        __syncthreads();
+        n = before = 0;
+        for (int w = 0; w < W; ++w) {
+            if (w < wave) before += sh.cnt[w];
+            n += sh.cnt[w];
         }
-        kth = value_of(ans);
+        return n;
+    };
+    const int found = sh.n;
+    int have = found, before;
+    uint32_t kth = order_of(-INFINITY);
+    if (found > kCap) {
+        // two bits at a time: the largest key that at least k reach
+        kth = 0;
+        for (int b = 30; b >= 0; b -= 2) {
+            int n[3] = {0, 0, 0};
+            for (int c0 = lo; c0 < hi; c0 += 4 * NT) {
+                uint32_t o[4];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const int c = c0 + u * NT + (int)threadIdx.x;
+                    const float v = value(c);
+                    o[u] = c < hi ? order_of(v) : 0;
+                }
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+#pragma unroll
+                    for (uint32_t q = 0; q < 3; ++q) n[q] += __popcll(__ballot(o[u] >= (kth | (q + 1) << b)));
+            }
+            uint32_t digit = 0;
+#pragma unroll
+            for (uint32_t q = 0; q < 3; ++q)
+                if (total(n[q], before) >= k) digit = q + 1;
+            kth |= digit << b;
+        }
         __syncthreads();
         if (threadIdx.x == 0) sh.n = 0;
         __syncthreads();
-        push(sh, h, value_of(ans + 1));   // (the next value up: fewer than k are there)
+        for (int c = lo + (int)threadIdx.x; c < hi; c += NT)
+            if (order_of(value(c)) > kth) sh.cand[atomicAdd(&sh.n, 1)] = key_of(value(c), c);   // fewer than k
         __syncthreads();
+        have = sh.n;
     }
-    int have = sh.n;
-#pragma unroll
-    for (int i = 0; i < H::I; ++i)
-        if (have < k) {
-            bool eq[H::VEC];
-            int mine = 0, before = 0, total = 0;
-#pragma unroll
-            for (int e = 0; e < H::VEC; ++e) {
-                eq[e] = fmaxf(h.v[i * H::VEC + e], -INFINITY) == kth && h.valid(i, e);
-                const unsigned long long mask = __ballot(eq[e]);
-                before += lanes_below(mask);
-                total += __popcll(mask);
-            }
-            __syncthreads();
-            if (lane == 0) sh.cnt[wave] = total;
-            __syncthreads();
-            total = 0;
-            for (int w = 0; w < W; ++w) {
-                if (w < wave) before += sh.cnt[w];
-                total += sh.cnt[w];
-            }
-#pragma unroll
-            for (int e = 0; e < H::VEC; ++e) {
-                const int slot = have + before + mine;
-                if (eq[e] && slot < k) sh.cand[slot] = key_of(kth, h.at(i) + e);
-                mine += eq[e];
-            }
-            have += total;
-        }
+    for (int c0 = lo; have < k && c0 < hi; c0 += NT) {
+        const int c = c0 + (int)threadIdx.x;
+        const bool eq = c < hi && order_of(value(c)) == kth;
+        const unsigned long long mask = __ballot(eq);
+        const int n = total(__popcll(mask), before), slot = have + before + lanes_below(mask);
+        if (eq && slot < k) sh.cand[slot] = key_of(value_of(kth), c);
+        have += n;
+    }
     __syncthreads();
     if (threadIdx.x == 0) sh.n = k;
     __syncthreads();
 }
 
 template <typename T, int NT, int PER>
-__global__ __launch_bounds__(NT) void answers_kernel(AnswersParams p, int segs, int seglen) {
+__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(PER == 64 ? 4 : 1))) void answers_kernel(AnswersParams p, int segs, int seglen) {
     constexpr int W = NT / 64;
     __shared__ Shared<W> sh;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -216,7 +241,7 @@ __global__ __launch_bounds__(NT) void answers_kernel(AnswersParams p, int segs, 
     {
         const float wm = wave_max(mx);
         const int r = (k + held - 1) / held;
-        const float th = r > 1 ? wave_rth(mx, r) : wm;
+        const float th = r > 1 ? value_of(wave_rth(order_of(mx), r)) : wm;
         if (lane == 0) {
             sh.m[wave] = wm;
             sh.th[wave] = wave < held ? th : INFINITY;
@@ -256,20 +281,15 @@ __global__ __launch_bounds__(NT) void answers_kernel(AnswersParams p, int segs, 
         }
     }
     if (k > 0) {
-        if (sh.n < k || sh.n > kCap) push_exact(sh, h, k);
-        const int n = sh.n;
-        for (int j = tid; j < n; j += NT) {
-            const unsigned long long key = sh.cand[j];
-            int r = 0;
-            for (int q = 0; q < n; ++q) r += sh.cand[q] > key;
-            if (r >= k) continue;
+        if (sh.n < k || sh.n > kCap) push_exact<T, NT>(sh, x, h.lo, h.hi, k);
+        rank<NT>(sh.cand, sh.n, k, [&](int r, unsigned long long key) {
             if (segs > 1) {
                 p.part_keys[((size_t)row * segs + seg) * p.k + r] = key;
             } else {
                 p.top[(size_t)row * p.k + r] = (int)~(uint32_t)key;
                 sh.top_val[r] = value_of((uint32_t)(key >> 32));
             }
-        }
+        });
         if (segs > 1)
             for (int r = k + tid; r < p.k; r += NT) p.part_keys[((size_t)row * segs + seg) * p.k + r] = 0;
     }
@@ -288,9 +308,24 @@ __global__ __launch_bounds__(NT) void answers_kernel(AnswersParams p, int segs, 
         if (!sh.last) return;
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
         if (tid == 0) atomicExch(p.cnt + row, 0);
+        constexpr int C = kCap / NT;
+        const int n = segs * p.k;
+        unsigned long long key[C];
         if (p.k > 0) {
-            const int n = segs * p.k;
-            for (int j = tid; j < n; j += NT) sh.cand[j] = p.part_keys[(size_t)row * n + j];
+            // as above: a bound from the lanes' largest, of the waves that
+            // hold keys; then what reaches it
+            uint32_t top = 0;
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                const int j = c * NT + tid;
+                key[c] = j < n ? p.part_keys[(size_t)row * n + j] : 0;
+            }
+#pragma unroll
+            for (int c = 0; c < C; ++c) top = max(top, (uint32_t)(key[c] >> 32));
+            const int have = min(W, (n + 63) / 64);
+            const uint32_t bound = wave_rth(top, (p.k + have - 1) / have);
+            if (lane == 0) sh.key_th[wave] = wave < have ? bound : 0xFFFFFFFFu;
+            if (tid == 0) sh.n = 0;
         }
         if (stats) {
             float ms = -FLT_MAX, s0 = 0.0f, t0 = 0.0f;
@@ -308,15 +343,25 @@ __global__ __launch_bounds__(NT) void answers_kernel(AnswersParams p, int segs, 
         }
         __syncthreads();
         if (p.k > 0) {
-            const int n = segs * p.k;
-            for (int j = tid; j < n; j += NT) {
-                const unsigned long long key = sh.cand[j];
-                int r = 0;
-                for (int q = 0; q < n; ++q) r += sh.cand[q] > key;
-                if (r >= p.k || key == 0) continue;
-                p.top[(size_t)row * p.k + r] = (int)~(uint32_t)key;
-                sh.top_val[r] = value_of((uint32_t)(key >> 32));
+            uint32_t bound = 0xFFFFFFFFu;
+#pragma unroll
+            for (int w = 0; w < W; ++w) bound = min(bound, sh.key_th[w]);
+            bound = max(bound, 1u);                // (not the filling of short segments)
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                const bool in = (uint32_t)(key[c] >> 32) >= bound;
+                const unsigned long long mask = __ballot(in);
+                if (mask == 0) continue;
+                int base = 0;
+                if (lane == 0) base = atomicAdd(&sh.n, __popcll(mask));
+                base = __builtin_amdgcn_readfirstlane(base);
+                if (in) sh.cand[base + lanes_below(mask)] = key[c];
             }
+            __syncthreads();
+            rank<NT>(sh.cand, sh.n, p.k, [&](int r, unsigned long long k1) {
+                p.top[(size_t)row * p.k + r] = (int)~(uint32_t)k1;
+                sh.top_val[r] = value_of((uint32_t)(k1 >> 32));
+            });
         }
     }
     if (!stats) return;
