@@ -34,23 +34,52 @@ __device__ __forceinline__ unsigned long long key_of(float v, int col) {
     return (unsigned long long)order_of(v) << 32 | (uint32_t)~col;
 }
 
+// Reductions over a wave by cross-lane moves of the vector unit (lanes 1, 2, 4
+// and 8 below, then the last lane of the row and of the half below): lane 63
+// has all.  A shuffle through the LDS costs some 100 cycles a step, this 12.
+constexpr int kRowShr = 0x110, kRowBcast15 = 0x142, kRowBcast31 = 0x143;
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int below(int v, int none) {
+    return __builtin_amdgcn_update_dpp(none, v, CTRL, ROWS, 0xf, false);
+}
+template <typename T, typename F>
+__device__ __forceinline__ T wave_scan(T v, T none, F join) {   // inclusive
+    const int z = __builtin_bit_cast(int, none);
+    auto in = [](T a) { return __builtin_bit_cast(int, a); };
+    auto out = [](int a) { return __builtin_bit_cast(T, a); };
+    v = join(v, out(below<kRowShr + 1, 0xf>(in(v), z)));
+    v = join(v, out(below<kRowShr + 2, 0xf>(in(v), z)));
+    v = join(v, out(below<kRowShr + 4, 0xf>(in(v), z)));
+    v = join(v, out(below<kRowShr + 8, 0xf>(in(v), z)));
+    v = join(v, out(below<kRowBcast15, 0xa>(in(v), z)));
+    return join(v, out(below<kRowBcast31, 0xc>(in(v), z)));
+}
+template <typename T, typename F>
+__device__ __forceinline__ T wave_all(T v, T none, F join) {
+    return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, wave_scan(v, none, join)), 63));
+}
 __device__ __forceinline__ float wave_max(float v) {
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) v = fmaxf(v, __shfl_xor(v, off, 64));
-    return v;
+    return wave_all(v, -INFINITY, [](float a, float b) { return fmaxf(a, b); });
 }
 __device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) v += __shfl_xor(v, off, 64);
-    return v;
+    return wave_all(v, 0.0f, [](float a, float b) { return a + b; });
 }
 
-// The r-th largest of a wave's 64 integers, bit by bit.
-__device__ __forceinline__ uint32_t wave_rth(uint32_t o, int r) {
-    uint32_t ans = 0;
-    for (int b = 31; b >= 0; --b) {
-        const uint32_t c = ans | 1u << b;
-        if (__popcll(__ballot(o >= c)) >= r) ans = c;
+// A bound that at least r of a wave's 64 integers, all from lo to hi, reach: the
+// r-th largest, or less where exactly r reach it already.  Two bits a step,
+// from the first that differ.
+__device__ __forceinline__ uint32_t wave_bound(uint32_t o, uint32_t lo, uint32_t hi, int r) {
+    if (lo == hi) return hi;
+    int b = (31 - __builtin_clz(lo ^ hi)) & ~1;
+    uint32_t ans = hi >> b >> 2 << b << 2;
+#pragma unroll 1
+    for (; b >= 0; b -= 2) {
+        int n[3];
+#pragma unroll
+        for (uint32_t q = 0; q < 3; ++q) n[q] = __popcll(__ballot(o >= (ans | (q + 1) << b)));
+        const int got = n[2] >= r ? n[2] : n[1] >= r ? n[1] : n[0];
+        ans |= (n[2] >= r ? 3u : n[1] >= r ? 2u : n[0] >= r ? 1u : 0u) << b;
+        if (got == r) break;
     }
     return ans;
 }
@@ -59,12 +88,23 @@ __device__ __forceinline__ int lanes_below(unsigned long long mask) {
     return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
 }
 
+// Room for a lane's n candidates behind the other lanes': the first slot, or -1
+// for a wave without any.
+__device__ __forceinline__ int take_slots(int *count, int n) {
+    const int upto = wave_scan(n, 0, [](int a, int b) { return a + b; });
+    const int all = __builtin_amdgcn_readlane(upto, 63);
+    if (all == 0) return -1;
+    int base = 0;
+    if ((threadIdx.x & 63) == 0) base = atomicAdd(count, all);
+    return __builtin_amdgcn_readfirstlane(base) + upto - n;
+}
+
 template <int W>
 struct Shared {
-    unsigned long long cand[kCap];
+    alignas(16) unsigned long long cand[kCap + 8];
     float top_val[kMaxTopK];
-    float m[W], th[W], s[W], t[W];
-    uint32_t key_th[W];
+    float m[W], s[W], t[W];
+    uint32_t bound[W];
     int cnt[W];
     int n, last;
 };
@@ -112,39 +152,45 @@ struct Held {
     }
 };
 
-// Adds the values of at least `th` to the candidates.
-template <int W, typename H>
-__device__ __forceinline__ void push(Shared<W> &sh, const H &h, float th) {
-    const int lane = threadIdx.x & 63;
+// Adds the values of at least `th` to the candidates.  A lane marks its own and
+// then takes them one after the other, reading them again from memory (the
+// cache): few lanes have more than two or three, but among a wave's lanes
+// nearly every register has one.
+template <int W, typename T, typename H>
+__device__ __forceinline__ void push(Shared<W> &sh, const H &h, const T *x, float th) {
+    constexpr int PER = H::I * H::VEC;
+    uint32_t mark[(PER + 31) / 32] = {};
 #pragma unroll
-    for (int i = 0; i < H::I; ++i)
+    for (int q = 0; q < PER; ++q) mark[q / 32] |= h.v[q] >= th ? 1u << q % 32 : 0u;
+    int n = 0;
 #pragma unroll
-        for (int e = 0; e < H::VEC; ++e) {
-            const float v = h.v[i * H::VEC + e];
-            const unsigned long long mask = __ballot(v >= th);
-            if (mask == 0) continue;
-            int base = 0;
-            if (lane == 0) base = atomicAdd(&sh.n, __popcll(mask));
-            base = __builtin_amdgcn_readfirstlane(base);
-            const int slot = base + lanes_below(mask);
-            if (v >= th && slot < kCap) sh.cand[slot] = key_of(v, h.at(i) + e);
+    for (uint32_t m : mark) n += __popc(m);
+    int slot = take_slots(&sh.n, n);
+    if (slot < 0) return;
+#pragma unroll
+    for (int w = 0; w < (PER + 31) / 32; ++w)
+#pragma unroll 1
+        for (uint32_t m = mark[w]; m; m &= m - 1) {
+            const int q = w * 32 + __ffs(m) - 1, c = h.at(q / H::VEC) + q % H::VEC;
+            if (slot < kCap) sh.cand[slot] = key_of((float)x[c], c);
+            ++slot;
         }
 }
 
 // Hands every candidate of the first k to `found`, with its rank: the number of
-// larger ones.  2^g neighbouring lanes share a candidate's comparisons.
+// larger ones.  Behind the last there are seven zeros, below every key.
 template <int NT, typename F>
 __device__ __forceinline__ void rank(const unsigned long long *cand, int n, int k, F found) {
-    int g = 0;
-    while (g < 6 && (n << (g + 1)) <= NT) ++g;
-    const int part = threadIdx.x & ((1 << g) - 1);
-    for (int j = threadIdx.x >> g; j < n; j += NT >> g) {
+    n = __builtin_amdgcn_readfirstlane(n);
+    for (int j = threadIdx.x; j < n; j += NT) {
         const unsigned long long key = cand[j];
         int r = 0;
-#pragma unroll 8
-        for (int q = part; q < n; q += 1 << g) r += cand[q] > key;
-        for (int b = 0; b < g; ++b) r += __shfl_xor(r, 1 << b, 64);
-        if (part == 0 && r < k) found(r, key);
+#pragma unroll 1
+        for (int q = 0; q < n; q += 8) {
+#pragma unroll
+            for (int u = 0; u < 8; ++u) r += cand[q + u] > key;
+        }
+        if (r < k) found(r, key);
     }
 }
 
@@ -215,6 +261,7 @@ __device__ __noinline__ void push_exact(Shared<NT / 64> &sh, const T *x, int lo,
         have += n;
     }
     __syncthreads();
+    if (threadIdx.x < 8) sh.cand[k + threadIdx.x] = 0;
     if (threadIdx.x == 0) sh.n = k;
     __syncthreads();
 }
@@ -226,6 +273,15 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(PER == 64 ? 
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int row = blockIdx.x / segs, seg = blockIdx.x - row * segs;
     const T *x = (const T *)p.x + (size_t)row * p.cols;
+    // channels of the lists, their values next, both long before they are used
+    int listed[kAnswerLists];
+    float value[kAnswerLists];
+#pragma unroll
+    for (int l = 0; l < kAnswerLists; ++l) {
+        listed[l] = -1;
+        if (tid < p.list_given[l]) listed[l] = p.list[l][(size_t)row * p.list_given[l] + tid];
+    }
+    for (int j = tid; j < kCap + 8; j += NT) sh.cand[j] = 0;
     Held<T, NT, PER> h;
     h.load(x, seg * seglen, min(p.cols, (seg + 1) * seglen));
     const int k = min(p.k, h.hi - h.lo);
@@ -239,23 +295,27 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(PER == 64 ? 
 #pragma unroll
     for (int q = 0; q < PER; ++q) mx = fmaxf(mx, h.v[q]);
     {
-        const float wm = wave_max(mx);
+        const float wm = wave_max(mx), wl = -wave_max(-mx);
         const int r = (k + held - 1) / held;
-        const float th = r > 1 ? value_of(wave_rth(order_of(mx), r)) : wm;
+        const uint32_t bound = r > 1 ? wave_bound(order_of(mx), order_of(wl), order_of(wm), r) : order_of(wm);
         if (lane == 0) {
             sh.m[wave] = wm;
-            sh.th[wave] = wave < held ? th : INFINITY;
+            sh.bound[wave] = wave < held ? bound : 0xFFFFFFFFu;
         }
         if (tid == 0) sh.n = 0;
     }
     __syncthreads();
-    float m = -FLT_MAX, th = INFINITY;    // (rows of -inf only: s = 0)
+#pragma unroll
+    for (int l = 0; l < kAnswerLists; ++l)
+        value[l] = listed[l] >= 0 && listed[l] < p.cols ? (float)x[listed[l]] : NAN;
+    float m = -FLT_MAX;                   // (rows of -inf only: s = 0)
+    uint32_t bound = 0xFFFFFFFFu;
 #pragma unroll
     for (int w = 0; w < W; ++w) {
         m = fmaxf(m, sh.m[w]);
-        th = fminf(th, sh.th[w]);
+        bound = min(bound, sh.bound[w]);
     }
-    if (k > 0) push(sh, h, fmaxf(th, -FLT_MAX));
+    if (k > 0) push(sh, h, x, value_of(max(bound, order_of(-FLT_MAX))));   // (-inf: push_exact)
     float s = 0.0f, t = 0.0f;
     if (stats) {
 #pragma unroll
@@ -284,33 +344,28 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(PER == 64 ? 
         if (sh.n < k || sh.n > kCap) push_exact<T, NT>(sh, x, h.lo, h.hi, k);
         rank<NT>(sh.cand, sh.n, k, [&](int r, unsigned long long key) {
             if (segs > 1) {
-                p.part_keys[((size_t)row * segs + seg) * p.k + r] = key;
+                put(p.part_keys + ((size_t)row * segs + seg) * p.k + r, key);
             } else {
                 p.top[(size_t)row * p.k + r] = (int)~(uint32_t)key;
                 sh.top_val[r] = value_of((uint32_t)(key >> 32));
             }
         });
         if (segs > 1)
-            for (int r = k + tid; r < p.k; r += NT) p.part_keys[((size_t)row * segs + seg) * p.k + r] = 0;
+            for (int r = k + tid; r < p.k; r += NT) put(p.part_keys + ((size_t)row * segs + seg) * p.k + r, 0ull);
     }
     if (segs > 1) {
         float *st = p.part_stats + (size_t)row * segs * 4;
-        if (tid == 0) *(f4 *)(st + 4 * seg) = f4{m, s, t, 0.0f};
-        // every wave's stores are in the L2 before the workgroup arrives; one
-        // release writes it back for all of them
-        __builtin_amdgcn_s_waitcnt(0x0F70);
-        __syncthreads();
         if (tid == 0) {
-            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "agent");
-            sh.last = atomicAdd(p.cnt + row, 1) == segs - 1;
+            put((unsigned long long *)(st + 4 * seg), (unsigned long long)__float_as_uint(s) << 32 | __float_as_uint(m));
+            put((unsigned long long *)(st + 4 * seg) + 1, (unsigned long long)__float_as_uint(t));
         }
-        __syncthreads();
-        if (!sh.last) return;
-        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
-        if (tid == 0) atomicExch(p.cnt + row, 0);
+        if (!arrive_last(p.cnt + row, segs, &sh.last)) return;
         constexpr int C = kCap / NT;
         const int n = segs * p.k;
         unsigned long long key[C];
+        // (a segment to a lane: there are at most 64)
+        f4 found = *(const f4 *)(st + 4 * min(lane, segs - 1));
+        if (lane >= segs) found = f4{-FLT_MAX, 0.0f, 0.0f, 0.0f};
         if (p.k > 0) {
             // as above: a bound from the lanes' largest, of the waves that
             // hold keys; then what reaches it
@@ -318,45 +373,43 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(PER == 64 ? 
 #pragma unroll
             for (int c = 0; c < C; ++c) {
                 const int j = c * NT + tid;
-                key[c] = j < n ? p.part_keys[(size_t)row * n + j] : 0;
+                key[c] = p.part_keys[(size_t)row * n + min(j, n - 1)];
+            }
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                const int j = c * NT + tid;
+                if (j >= n) key[c] = 0;
+                sh.cand[j] = 0;
             }
 #pragma unroll
             for (int c = 0; c < C; ++c) top = max(top, (uint32_t)(key[c] >> 32));
             const int have = min(W, (n + 63) / 64);
-            const uint32_t bound = wave_rth(top, (p.k + have - 1) / have);
-            if (lane == 0) sh.key_th[wave] = wave < have ? bound : 0xFFFFFFFFu;
+            const uint32_t hi = wave_all(top, 0u, [](uint32_t a, uint32_t b) { return max(a, b); });
+            const uint32_t lo = wave_all(top, 0xFFFFFFFFu, [](uint32_t a, uint32_t b) { return min(a, b); });
+            const int r = (p.k + have - 1) / have;
+            const uint32_t bound = r > 1 ? wave_bound(top, lo, hi, r) : hi;
+            if (lane == 0) sh.bound[wave] = wave < have ? bound : 0xFFFFFFFFu;
             if (tid == 0) sh.n = 0;
         }
         if (stats) {
-            float ms = -FLT_MAX, s0 = 0.0f, t0 = 0.0f;
-            for (int g = lane; g < segs; g += 64) ms = fmaxf(ms, st[4 * g]);
-            ms = wave_max(ms);
-            for (int g = lane; g < segs; g += 64) {
-                const f4 q = *(const f4 *)(st + 4 * g);
-                const float d = fmaxf(q[0] - ms, -1e30f), w = __builtin_amdgcn_exp2f(d * kLog2e);
-                s0 = fmaf(w, q[1], s0);
-                t0 = fmaf(w, fmaf(q[1], d, q[2]), t0);
-            }
-            m = ms;
-            s = wave_sum(s0);
-            t = wave_sum(t0);
+            m = wave_max(found[0]);
+            const float d = fmaxf(found[0] - m, -1e30f), w = __builtin_amdgcn_exp2f(d * kLog2e);
+            s = wave_sum(w * found[1]);
+            t = wave_sum(w * fmaf(found[1], d, found[2]));
         }
         __syncthreads();
         if (p.k > 0) {
-            uint32_t bound = 0xFFFFFFFFu;
+            bound = 0xFFFFFFFFu;
 #pragma unroll
-            for (int w = 0; w < W; ++w) bound = min(bound, sh.key_th[w]);
+            for (int w = 0; w < W; ++w) bound = min(bound, sh.bound[w]);
             bound = max(bound, 1u);                // (not the filling of short segments)
+            int mine = 0;
 #pragma unroll
-            for (int c = 0; c < C; ++c) {
-                const bool in = (uint32_t)(key[c] >> 32) >= bound;
-                const unsigned long long mask = __ballot(in);
-                if (mask == 0) continue;
-                int base = 0;
-                if (lane == 0) base = atomicAdd(&sh.n, __popcll(mask));
-                base = __builtin_amdgcn_readfirstlane(base);
-                if (in) sh.cand[base + lanes_below(mask)] = key[c];
-            }
+            for (int c = 0; c < C; ++c) mine += (uint32_t)(key[c] >> 32) >= bound;
+            int slot = take_slots(&sh.n, mine);
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+                if ((uint32_t)(key[c] >> 32) >= bound) sh.cand[slot++] = key[c];
             __syncthreads();
             rank<NT>(sh.cand, sh.n, p.k, [&](int r, unsigned long long k1) {
                 p.top[(size_t)row * p.k + r] = (int)~(uint32_t)k1;
@@ -367,16 +420,16 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(PER == 64 ? 
     if (!stats) return;
     __syncthreads();
     const float logs = logf(s);
-    for (int l = 0; l < p.n_lists; ++l) {
+#pragma unroll
+    for (int l = 0; l < kAnswerLists; ++l) {
+        if (l >= p.n_lists) break;
         const int *list = p.list[l];
         const int nl = p.list_n[l];
         for (int q = tid; q < nl; q += NT) {
-            float v = NAN;
-            if (!list) {
-                v = sh.top_val[q];
-            } else {
+            float v = list ? value[l] : sh.top_val[q];
+            if (list && q != tid) {
                 const int c = list[(size_t)row * nl + q];
-                if (c >= 0 && c < p.cols) v = (float)x[c];
+                v = c >= 0 && c < p.cols ? (float)x[c] : NAN;
             }
             p.list_out[l][(size_t)row * nl + q] = s == 0.0f && v == v ? -INFINITY : (v - m) - logs;
         }
@@ -405,7 +458,7 @@ hipError_t launch_t(const AnswersParams &p, const AnswersGeom &g, hipStream_t st
 // more than the last workgroup can rank.
 AnswersGeom answers_geom(int rows, int cols, int k) {
     AnswersGeom g{};
-    const int most = k > 0 ? kCap / k : 64;
+    const int most = k > 0 ? std::min(kCap / k, 64) : 64;
     int segs = (cols + 32767) / 32768;
     segs = std::max(segs, std::min({256 / std::max(rows, 1), (cols + 2047) / 2048, most}));
     g.seglen = ((cols + segs - 1) / segs + 7) / 8 * 8;
@@ -422,12 +475,15 @@ AnswersGeom answers_geom(int rows, int cols, int k) {
 hipError_t launch_answers(const AnswersParams &p, const AnswersGeom &g, hipStream_t st) {
     if (p.rows <= 0) return hipSuccess;
     if (g.segs < 1 || (long)g.nt * g.per < g.seglen || (long)g.segs * g.seglen < p.cols || (g.segs - 1) * g.seglen >= p.cols ||
-        (long)g.segs * p.k > kCap || p.k > kMaxTopK || (g.segs > 1 && (!p.cnt || !p.part_stats)) ||
+        g.segs > 64 || (long)g.segs * p.k > kCap || p.k > kMaxTopK || (g.segs > 1 && (!p.cnt || !p.part_stats)) ||
         (size_t)p.rows * g.segs > 0x7fffffffu)
         return hipErrorInvalidValue;
-    for (int l = 0; l < p.n_lists; ++l)
-        if (!p.list[l] && p.list_n[l] != p.k) return hipErrorInvalidValue;
-    return p.fp16_in ? launch_t<_Float16>(p, g, st) : launch_t<float>(p, g, st);
+    AnswersParams q = p;
+    for (int l = 0; l < kAnswerLists; ++l) {
+        q.list_given[l] = l < p.n_lists && p.list[l] ? p.list_n[l] : 0;
+        if (l < p.n_lists && !p.list[l] && p.list_n[l] != p.k) return hipErrorInvalidValue;
+    }
+    return p.fp16_in ? launch_t<_Float16>(q, g, st) : launch_t<float>(q, g, st);
 }
 
 }  // namespace kern

@@ -217,6 +217,29 @@ struct BF16 {
     __device__ static uint16_t bits(float f) { return __builtin_bit_cast(uint16_t, (__bf16)f); }
 };
 
+// Work of one result split over several workgroups.  Each leaves its part with
+// `put`, stores at device scope, which go through the L2 (every XCD has its
+// own) to memory that all share; then all call arrive_last, and the one that
+// gets true reads the parts.  A store is complete when vmcnt no longer counts
+// it, so waiting for that before the arrival is all that is needed: a release
+// fence would write back the whole L2, 1 to 2 us where other lines are dirty.
+// The last workgroup's acquire drops what its own caches hold of earlier parts.
+// `count` is zero before and after; `last`: a word of LDS.
+template <typename T>
+__device__ __forceinline__ void put(T *p, T v) {
+    __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ bool arrive_last(int *count, int parts, int *last) {
+    __builtin_amdgcn_s_waitcnt(0x0F70);   // (vmcnt 0, the other counters at their maxima)
+    __syncthreads();
+    if (threadIdx.x == 0) *last = atomicAdd(count, 1) == parts - 1;
+    __syncthreads();
+    if (!*last) return false;
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
+    if (threadIdx.x == 0) atomicExch(count, 0);
+    return true;
+}
+
 // 16 bytes per lane from global memory straight into LDS: lane l writes
 // lds + 16*l, so the LDS side is one contiguous KiB per wave.  Issued as
 // inline asm so that the compiler does not track it: it would otherwise

@@ -163,20 +163,17 @@ __global__ __launch_bounds__(512) void fcint4_kernel(FcInt4Params p, int splits)
     for (int f = wave; f < F; f += waves) {
         f4 v = red[f * 64 + lane];
         for (int w = 1; w < waves; ++w) v += red[(w * F + f) * 64 + lane];
-        if (splits > 1) mine[f * 64 + lane] = v;
-        else red[f * 64 + lane] = v;
+        if (splits > 1) {
+            typedef unsigned long long u64;
+            u64 *to = (u64 *)(mine + f * 64 + lane);
+            put(to, (u64)__float_as_uint(v[1]) << 32 | __float_as_uint(v[0]));
+            put(to + 1, (u64)__float_as_uint(v[3]) << 32 | __float_as_uint(v[2]));
+        } else {
+            red[f * 64 + lane] = v;
+        }
     }
     if (splits > 1) {
-        __builtin_amdgcn_s_waitcnt(0x0F70);   // (vmcnt 0: this wave's stores are in the L2)
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "agent");
-            last = atomicAdd(p.cnt + nt * p.mtiles + mt, 1) == splits - 1;
-        }
-        __syncthreads();
-        if (!last) return;
-        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
-        if (threadIdx.x == 0) atomicExch(p.cnt + nt * p.mtiles + mt, 0);
+        if (!arrive_last(p.cnt + nt * p.mtiles + mt, splits, &last)) return;
         const f4 *first = mine - (size_t)split * F * 64;
         for (int f = wave; f < F; f += waves) {
             f4 v = first[f * 64 + lane];

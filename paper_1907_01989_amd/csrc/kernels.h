@@ -151,6 +151,7 @@ struct AnswersParams {
     const int *list[kAnswerLists];   // rows x list_n, null: the top columns of this call
     float *list_out[kAnswerLists];
     int list_n[kAnswerLists];
+    int list_given[kAnswerLists];    // list_n where there is a list, else 0 (set by the launcher)
     // rows split into segments: what each found, and arrival counters per row
     // (zero before and after)
     unsigned long long *part_keys;   // [row][segment][k]
