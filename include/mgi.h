@@ -293,7 +293,7 @@ mgi_status mgi_plan_destroy(mgi_plan *p); /* NULL is accepted */
 
 /* Bytes of device workspace (the arena holding every intermediate tensor,
  * then a small state region: the arrival counters of fused FC + softmax
- * nodes and of nodes that split their sums over workgroups) and of packed weights that the caller must allocate for
+ * nodes and of questions about long rows) and of packed weights that the caller must allocate for
  * mgi_plan_bind.  Both buffers must be 256-byte aligned. */
 mgi_status mgi_plan_workspace_bytes(const mgi_plan *p, size_t *bytes);
 mgi_status mgi_plan_weight_bytes(const mgi_plan *p, size_t *bytes);

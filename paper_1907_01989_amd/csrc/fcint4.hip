@@ -4,11 +4,12 @@
 // The differences code - z are whole numbers of at most 15, exact in either
 // 16-bit type, so the inner sums run on the matrix cores with no rounding but
 // that of the fp32 accumulator, and the scale multiplies the group's sum, not
-// the weights.  A wave owns 16 FN output channels for up to 16 FM rows and a
-// range of K; it streams codes and activations from global memory straight to
-// registers in the operands' own order.
+// the weights.  Weights come as blocks of 16 output channels x 128 inputs (see
+// pack_fc_int4), a KiB of codes in the MFMA operand's own order.
 //
-// At few rows the codes' bytes bound it, at many rows the products.
+// At few rows the bytes of the weights bound it, at many the vector work of
+// taking codes apart (bf16: 19 instructions for eight codes, fp16: 11) beside
+// the products.
 #include "device.h"
 
 namespace mgi {
@@ -27,9 +28,10 @@ struct Codes;
 template <>
 struct Codes<F16> {
     h2 off;
-    __device__ __forceinline__ explicit Codes(uint32_t z) {
-        const uint32_t b = 0xE400u | z;                    // -(1024 + z)
-        off = __builtin_bit_cast(h2, b | b << 16);
+    // byte q of the word z holds the zero point
+    __device__ __forceinline__ Codes(uint32_t z, int q) {
+        const uint32_t b = __builtin_amdgcn_perm(z, z, 0x0c000c00u + 0x00010001u * q) | 0xE400E400u;   // -(1024 + z)
+        off = __builtin_bit_cast(h2, b);
     }
     __device__ __forceinline__ h8 frag(uint32_t w) const {
         u4x r;
@@ -42,199 +44,375 @@ struct Codes<F16> {
     }
 };
 
-// bf16: through fp32, whose upper halves are the (exact) bf16 values
+// bf16: code - z of four codes at once as signed bytes (128 + code - z carries
+// into no neighbour), then through fp32, whose upper halves are the (exact)
+// bf16 values
+__device__ __forceinline__ float byte_f32(uint32_t v, int i) { return (float)(int8_t)(v >> (8 * i)); }
 template <>
 struct Codes<BF16> {
-    float z;
-    __device__ __forceinline__ explicit Codes(uint32_t z_) : z((float)z_) {}
+    uint32_t off;
+    __device__ __forceinline__ Codes(uint32_t z, int q) : off(0x80808080u - __builtin_amdgcn_perm(z, z, 0x01010101u * q)) {}
     __device__ __forceinline__ h8 frag(uint32_t w) const {
-        const uint32_t even = w & 0x0F0F0F0Fu, odd = w >> 4 & 0x0F0F0F0Fu;   // pairs 0, 2 and 1, 3
+        // pairs 0, 2 and 1, 3
+        const uint32_t even = ((w & 0x0F0F0F0Fu) + off) ^ 0x80808080u, odd = ((w >> 4 & 0x0F0F0F0Fu) + off) ^ 0x80808080u;
         u4x r;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const uint32_t q = (i & 1 ? odd : even) >> (i & 2 ? 8 : 0);
-            const float lo = (float)(q & 0xFFu) - z, hi = (float)(q >> 16 & 0xFFu) - z;
+            const float lo = byte_f32(i & 1 ? odd : even, i >> 1), hi = byte_f32(i & 1 ? odd : even, 2 + (i >> 1));
             r[i] = __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
         }
         return __builtin_bit_cast(h8, r);
     }
 };
 
+// scale i of a row of them
 template <typename E>
-__device__ __forceinline__ float scale_of(uint16_t b) {
-    return E::bf ? __uint_as_float((uint32_t)b << 16) : (float)__builtin_bit_cast(_Float16, b);
+__device__ __forceinline__ float scale_of(const uint32_t *s, int i) {
+    const uint32_t v = s[i >> 1];
+    if (E::bf) return __uint_as_float(i & 1 ? v & 0xFFFF0000u : v << 16);
+    return (float)__builtin_bit_cast(_Float16, (uint16_t)(i & 1 ? v >> 16 : v));
 }
 
+// Bytes of a block of 16 output channels x 128 inputs: a wave's codes, then the
+// scales and zero points [16 channels][4 / gs].
+constexpr int block_bytes(int gs, bool zp) { return 1024 + (zp ? 48 : 32) * (4 / gs); }
+
 // One block of 128 inputs in flight: codes, scales, zero points, activations.
-template <int FM, int FN, int GS, bool ZP>
+template <int GS>
 struct Stage {
     static constexpr int SG = 4 / GS;      // scales per channel and block
-    u4v w[FN];
-    uint32_t s[FN][2 * SG], z[FN];
-    h8 x[4][FM];
+    u4v w;
+    uint32_t s[2 * SG], z;
+    h8 x[4];
 };
 
-template <typename E, int FM, int FN, int GS, bool ZP>
-__global__ __launch_bounds__(512) void fcint4_kernel(FcInt4Params p, int splits) {
-    constexpr int F = FM * FN, PF = 2;
-    typedef Stage<FM, FN, GS, ZP> St;
+// A 16 x 16 tile of sums to the logits: the scales' power of two, bias, activation.
+__device__ __forceinline__ void store_tile(const FcInt4Params &p, const f4 &v, int nb, int m0, int lane) {
+    const int m = m0 + (lane & 15), n = nb * 16 + 4 * (lane >> 4);
+    if (nb >= p.nb16 || m >= p.M) return;
+    const f4 mul = *(const f4 *)(p.mul + n), bias = *(const f4 *)(p.bias + n);
+    f4 o;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {          // (comparisons keep a NaN, a clamp would not)
+        const float u = fmaf(v[c], mul[c], bias[c]);
+        o[c] = p.act != MGI_ACT_NONE && u < 0.0f ? 0.0f : p.act == MGI_ACT_RELU6 && u > 6.0f ? 6.0f : u;
+    }
+    float *y = p.y + (size_t)m * p.cout + n;
+    if (p.cout % 4 == 0 && ((uintptr_t)p.y & 15) == 0) {
+        if (n < p.cout) *(f4 *)y = o;
+    } else {
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+            if (n + c < p.cout) y[c] = o[c];
+    }
+}
+
+// Up to 16 rows, few output channels: a workgroup takes 16 channels, its waves
+// share K.  Each streams codes and activations from memory to registers, one
+// block ahead; the waves' sums are added in a fixed order.
+template <typename E, int GS, bool ZP>
+__global__ __launch_bounds__(512) void fcint4_kernel(FcInt4Params p) {
+    constexpr int PF = 2;
+    typedef Stage<GS> St;
     constexpr int SG = St::SG;
-    extern __shared__ f4 red[];            // [waves][F][64]
-    __shared__ int last;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+    __shared__ f4 red[8][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
     // row tiles of the same weights are neighbours, which xcd_tile puts on one XCD
     const int t = xcd_tile(blockIdx.x, gridDim.x);
-    const int mt = t % p.mtiles, r = t / p.mtiles, split = r % splits, nt = r / splits;
-    const int m0 = mt * 16 * FM, nb0 = nt * FN;
-    const int parts = waves * splits, part = split * waves + wave;
-    const int b0 = (int)((long)p.kb * part / parts), b1 = (int)((long)p.kb * (part + 1) / parts);
-    const h8 *xl[FM];
-#pragma unroll
-    for (int j = 0; j < FM; ++j) xl[j] = p.x + (size_t)min(m0 + j * 16 + (lane & 15), p.M - 1) * p.xp;
-    f4 acc[FN][FM];
-#pragma unroll
-    for (int i = 0; i < FN; ++i)
-#pragma unroll
-        for (int j = 0; j < FM; ++j) acc[i][j] = f4{0.f, 0.f, 0.f, 0.f};
+    const int nb = t / p.mtiles, m0 = (t - nb * p.mtiles) * 16;
+    const int b0 = (int)((long)p.kb * wave / waves), b1 = (int)((long)p.kb * (wave + 1) / waves);
+    // Addresses are uniform bases plus 32-bit lane offsets that stay the same
+    // from block to block, so that a load needs no vector arithmetic.
+    const int kg = lane >> 4;
+    const h8 *xbase = p.x + (size_t)m0 * p.xp;
+    const uint32_t xrow = 16u * (uint32_t)(min(lane & 15, p.M - 1 - m0) * p.xp);
+    f4 acc = f4{0.f, 0.f, 0.f, 0.f};
 
     auto load = [&](int b, St &st) {
+        const char *w = (const char *)p.w + ((size_t)nb * p.kb + b) * block_bytes(GS, ZP);
+        st.w = *(const u4v *)(w + 16u * (uint32_t)lane);
+        __builtin_memcpy(st.s, w + 1024u + (uint32_t)(8 * SG * kg), 8 * SG);
+        if (ZP) {
+            const char *z = w + (1024u + 32 * SG) + (uint32_t)(SG * (lane & 15));
+            st.z = SG == 4 ? *(const uint32_t *)z : SG == 2 ? *(const uint16_t *)z : *(const uint8_t *)z;
+        }
+        // slices past the last are read as the last (and cleared before use)
+        const bool edge = b * 16 + 16 > p.ksl;
+        uint32_t off[4];
 #pragma unroll
-        for (int i = 0; i < FN; ++i) {
-            const size_t at = (size_t)min(nb0 + i, p.nb16 - 1) * p.kb + b;
-            st.w[i] = ((const u4v *)p.w)[at * 64 + lane];
-            __builtin_memcpy(st.s[i], p.scales + (at * 16 + 4 * (lane >> 4)) * SG, 8 * SG);
-            if (ZP) {
-                const uint8_t *z = p.zp + (at * 16 + (lane & 15)) * SG;
-                st.z[i] = SG == 4 ? *(const uint32_t *)z : SG == 2 ? *(const uint16_t *)z : *z;
+        for (int s = 0; s < 4; ++s) off[s] = 16u * (uint32_t)(kg * p.xs);
+        if (edge) {
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                const int k0 = min(b * 16 + s * 4, max(p.ksl - 4, 0));
+                off[s] = 16u * (uint32_t)((min(b * 16 + s * 4 + kg, p.ksl - 1) - k0) * p.xs);
             }
         }
-        const bool edge = b * 16 + 16 > p.ksl;
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
-            const int ks = b * 16 + s * 4 + (lane >> 4);
-#pragma unroll
-            for (int j = 0; j < FM; ++j)
-                st.x[s][j] = *(edge && ks >= p.ksl ? p.zero : xl[j] + (size_t)ks * p.xs);
+            const int k0 = min(b * 16 + s * 4, max(p.ksl - 4, 0));
+            st.x[s] = *(const h8 *)((const char *)(xbase + (size_t)k0 * p.xs) + (off[s] + xrow));
         }
     };
-    auto compute = [&](const St &st) {
+    auto compute = [&](int b, St &st) {
+        if (b * 16 + 16 > p.ksl) {
 #pragma unroll
-        for (int q = 0; q < SG; ++q)
+            for (int s = 0; s < 4; ++s)
+                if (b * 16 + s * 4 + kg >= p.ksl) st.x[s] = zero_h8();
+        }
 #pragma unroll
-            for (int i = 0; i < FN; ++i) {
-                const Codes<E> code(ZP ? st.z[i] >> (8 * q) & 15 : 8);
-                f4 g[FM];
+        for (int q = 0; q < SG; ++q) {
+            const Codes<E> code(ZP ? st.z : 0x08080808u, q);
+            f4 g = f4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int j = 0; j < FM; ++j) g[j] = f4{0.f, 0.f, 0.f, 0.f};
+            for (int s = q * GS; s < (q + 1) * GS; ++s) g = E::mma(code.frag(st.w[s]), st.x[s], g);
 #pragma unroll
-                for (int s = 0; s < GS; ++s) {
-                    const h8 w = code.frag(st.w[i][q * GS + s]);
-#pragma unroll
-                    for (int j = 0; j < FM; ++j) g[j] = E::mma(w, st.x[q * GS + s][j], g[j]);
-                }
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    const float sc = scale_of<E>((uint16_t)(st.s[i][(c * SG + q) >> 1] >> (16 * ((c * SG + q) & 1))));
-#pragma unroll
-                    for (int j = 0; j < FM; ++j) acc[i][j][c] = fmaf(sc, g[j][c], acc[i][j][c]);
-                }
-            }
+            for (int c = 0; c < 4; ++c) acc[c] = fmaf(scale_of<E>(st.s, c * SG + q), g[c], acc[c]);
+        }
     };
     if (b0 < b1) {
         St st[PF];
 #pragma unroll
         for (int u = 0; u < PF; ++u) load(min(b0 + u, b1 - 1), st[u]);
-        for (int b = b0; b < b1; b += PF) {
+        // (a load under a condition would make every wait behind it one for all
+        // loads: the last blocks have their own copy of the loop's body)
+        int b = b0;
+        for (; b + 2 * PF <= b1; b += PF) {
 #pragma unroll
             for (int u = 0; u < PF; ++u) {
-                if (b + u < b1) compute(st[u]);
-                if (b + u + PF < b1) load(b + u + PF, st[u]);
+                compute(b + u, st[u]);
+                load(b + u + PF, st[u]);
             }
         }
+#pragma unroll
+        for (int u = 0; u < PF; ++u) {
+            if (b + u < b1) compute(b + u, st[u]);
+            if (u + 1 < PF) load(min(b + u + PF, b1 - 1), st[u]);
+        }
+#pragma unroll
+        for (int u = 0; u + 1 < PF; ++u)
+            if (b + PF + u < b1) compute(b + PF + u, st[u]);
     }
-#pragma unroll
-    for (int i = 0; i < FN; ++i)
-#pragma unroll
-        for (int j = 0; j < FM; ++j) red[(wave * F + i * FM + j) * 64 + lane] = acc[i][j];
+    red[wave][lane] = acc;
     __syncthreads();
-    // the waves' sums, in a fixed order; of several workgroups that share K
-    // each leaves its sum, and the last to arrive adds them, again in order
-    f4 *mine = splits > 1 ? (f4 *)p.part + ((size_t)(nt * p.mtiles + mt) * splits + split) * F * 64 : nullptr;
-    for (int f = wave; f < F; f += waves) {
-        f4 v = red[f * 64 + lane];
-        for (int w = 1; w < waves; ++w) v += red[(w * F + f) * 64 + lane];
-        if (splits > 1) {
-            typedef unsigned long long u64;
-            u64 *to = (u64 *)(mine + f * 64 + lane);
-            put(to, (u64)__float_as_uint(v[1]) << 32 | __float_as_uint(v[0]));
-            put(to + 1, (u64)__float_as_uint(v[3]) << 32 | __float_as_uint(v[2]));
-        } else {
-            red[f * 64 + lane] = v;
-        }
-    }
-    if (splits > 1) {
-        if (!arrive_last(p.cnt + nt * p.mtiles + mt, splits, &last)) return;
-        const f4 *first = mine - (size_t)split * F * 64;
-        for (int f = wave; f < F; f += waves) {
-            f4 v = first[f * 64 + lane];
-            for (int q = 1; q < splits; ++q) v += first[((size_t)q * F + f) * 64 + lane];
-            red[f * 64 + lane] = v;
-        }
-    }
-    const bool vec = p.cout % 4 == 0 && ((uintptr_t)p.y & 15) == 0;
-    for (int f = wave; f < F; f += waves) {
-        const f4 v = red[f * 64 + lane];       // (written by this wave)
-        const int nb = nb0 + f / FM, m = m0 + (f % FM) * 16 + (lane & 15), n = nb * 16 + 4 * (lane >> 4);
-        if (nb >= p.nb16 || m >= p.M) continue;
-        const f4 mul = *(const f4 *)(p.mul + n), bias = *(const f4 *)(p.bias + n);
-        f4 o;
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {          // (comparisons keep a NaN, a clamp would not)
-            const float u = fmaf(v[c], mul[c], bias[c]);
-            o[c] = p.act != MGI_ACT_NONE && u < 0.0f ? 0.0f : p.act == MGI_ACT_RELU6 && u > 6.0f ? 6.0f : u;
-        }
-        float *y = p.y + (size_t)m * p.cout + n;
-        if (vec) {
-            if (n < p.cout) *(f4 *)y = o;
-        } else {
-#pragma unroll
-            for (int c = 0; c < 4; ++c)
-                if (n + c < p.cout) y[c] = o[c];
-        }
-    }
+    if (wave > 0) return;
+    for (int w = 1; w < waves; ++w) acc += red[w][lane];
+    store_tile(p, acc, nb, m0, lane);
 }
 
-template <typename E, int FM, int FN, int GS>
-hipError_t launch_z(const FcInt4Params &p, const FcInt4Geom &g, hipStream_t st) {
-    const size_t lds = (size_t)g.waves * FM * FN * 1024;
-    const dim3 grid((unsigned)(g.tiles(p.M, p.nb16) * g.splits)), block(64 * g.waves);
-    if (p.zp) launch(fcint4_kernel<E, FM, FN, GS, true>, grid, block, lds, st, p, g.splits);
-    else launch(fcint4_kernel<E, FM, FN, GS, false>, grid, block, lds, st, p, g.splits);
+// More rows or more output channels: a group of NW waves takes 16 channels each
+// for the same 16 FM rows, and a wave of its own fetches for it, block after
+// block, the rows' activations and the waves' codes into a ring of three stages
+// in LDS.  The waves that compute then read activations once per row tile and
+// spend no instructions on loads (256 x 4096 x 4096, bf16: 20.7 us where every
+// wave fetched its share, 17.1 with the fetching wave; 16 x 8192 x 8192 13.4 and
+// 10.3).  kgroups such groups share K.
+template <int FM, int NW>
+struct TileLds {
+    static constexpr int X = FM * 4096, W = 1280, STAGE = X + NW * W, STAGES = 3;
+};
+
+template <typename E, int FM, int NW, int GS, bool ZP, bool NHWC>
+__global__ __launch_bounds__(768) void fcint4_tile_kernel(FcInt4Params p, int kgroups) {
+    typedef TileLds<FM, NW> L;
+    constexpr int SG = 4 / GS, BLOCK = block_bytes(GS, ZP);
+    extern __shared__ f4 red[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int t = xcd_tile(blockIdx.x, gridDim.x);
+    const int nt = t / p.mtiles, m0 = (t - nt * p.mtiles) * 16 * FM;
+    const int steps = (p.kb + kgroups - 1) / kgroups;
+
+    if (wave >= NW * kgroups) {                       // fetch for group kq
+        const int kq = wave - NW * kgroups;
+        const int b0 = (int)((long)p.kb * kq / kgroups), b1 = (int)((long)p.kb * (kq + 1) / kgroups);
+        char *ring = (char *)red + (size_t)kq * L::STAGES * L::STAGE;
+        // Activations of a block: 16 FM rows x 16 slices of 16 bytes.  NHWC: a
+        // load is four rows of 256 bytes, slices swapped by the row so that the
+        // reads meet no bank twice; sliced: slice after slice.  Addresses are
+        // uniform bases plus lane offsets that do not change.
+        constexpr int XL = FM * 4;
+        uint32_t xofs[XL];
+        int xslice[XL];
+        const int rows = min(16 * FM, p.M - m0);
+#pragma unroll
+        for (int q = 0; q < XL; ++q) {
+            const int slot = q * 64 + lane;
+            const int row = NHWC ? slot >> 4 : slot % (16 * FM);
+            xslice[q] = NHWC ? (slot & 15) ^ (row & 15) : slot / (16 * FM);
+            xofs[q] = 16u * (uint32_t)(min(row, rows - 1) * p.xp + xslice[q] * p.xs);
+        }
+        const h8 *xbase = p.x + (size_t)m0 * p.xp;
+        const char *wbase[NW];
+#pragma unroll
+        for (int i = 0; i < NW; ++i)
+            wbase[i] = (const char *)p.w + (size_t)__builtin_amdgcn_readfirstlane(min(nt * NW + i, p.nb16 - 1)) * p.kb * BLOCK;
+        auto issue = [&](int i, char *st) {           // (past the range: its last block again)
+            const int b = __builtin_amdgcn_readfirstlane(min(min(b0 + i, b1 - 1), p.kb - 1));
+            const h8 *x = xbase + (size_t)(b * 16) * p.xs;
+            if (b * 16 + 16 <= p.ksl) {
+#pragma unroll
+                for (int q = 0; q < XL; ++q) load_lds16(x, xofs[q], (const h8 *)(st + q * 1024));
+            } else {                                  // slices past the last: zeros
+#pragma unroll
+                for (int q = 0; q < XL; ++q)
+                    load_lds16(b * 16 + xslice[q] < p.ksl ? (const h8 *)((const char *)x + xofs[q]) : p.zero,
+                               (const h8 *)(st + q * 1024));
+            }
+#pragma unroll
+            for (int n = 0; n < NW; ++n)
+                load_lds16((const h8 *)(wbase[n] + (size_t)b * BLOCK), 16u * (uint32_t)lane, (const h8 *)(st + L::X + n * L::W));
+            if (lane < (BLOCK - 1024) / 16) {
+#pragma unroll
+                for (int n = 0; n < NW; ++n)
+                    load_lds16((const h8 *)(wbase[n] + (size_t)b * BLOCK), 1024u + 16u * (uint32_t)lane,
+                               (const h8 *)(st + L::X + n * L::W + 1024));
+            }
+        };
+        char *const end = ring + L::STAGES * L::STAGE;
+        char *fill = ring + (L::STAGES - 1) * L::STAGE;
+#pragma unroll
+        for (int i = 0; i < L::STAGES - 1; ++i) issue(i, ring + i * L::STAGE);
+        for (int i = 0; i < steps; ++i) {
+            // a stage is whole once only the loads of later ones are in flight;
+            // behind the barrier all waves are done with the one before it
+            wait_vm_lds<(L::STAGES - 2) * (XL + 2 * NW)>();
+            __builtin_amdgcn_s_barrier();
+            issue(i + L::STAGES - 1, fill);
+            fill = fill + L::STAGE == end ? ring : fill + L::STAGE;
+        }
+        wait_vm_lds<0>();
+        __builtin_amdgcn_s_barrier();
+        if (kgroups > 1) __syncthreads();
+        return;
+    }
+
+    const int ng = wave % NW, kq = wave / NW, kg = lane >> 4, nb = nt * NW + ng;
+    const int blocks = (int)((long)p.kb * (kq + 1) / kgroups) - (int)((long)p.kb * kq / kgroups);
+    int xoff[4];
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+        xoff[s] = NHWC ? (lane & 15) * 256 + ((s * 4 + kg) ^ (lane & 15)) * 16 : ((s * 4 + kg) * 16 * FM + (lane & 15)) * 16;
+    f4 acc[FM];
+#pragma unroll
+    for (int j = 0; j < FM; ++j) acc[j] = f4{0.f, 0.f, 0.f, 0.f};
+    auto compute = [&](const char *st) {
+        const char *w = st + L::X + ng * L::W;
+        const u4v codes = *(const u4v *)(w + lane * 16);
+        uint32_t sc[2 * SG], z = 0x08080808u;
+        __builtin_memcpy(sc, w + 1024 + kg * 8 * SG, 8 * SG);
+        if (ZP) {
+            const char *zp = w + 1024 + 32 * SG + (lane & 15) * SG;
+            z = SG == 4 ? *(const uint32_t *)zp : SG == 2 ? *(const uint16_t *)zp : *(const uint8_t *)zp;
+        }
+        h8 x[4][FM];
+#pragma unroll
+        for (int s = 0; s < 4; ++s)
+#pragma unroll
+            for (int j = 0; j < FM; ++j) x[s][j] = *(const h8 *)(st + xoff[s] + j * (NHWC ? 4096 : 256));
+#pragma unroll
+        for (int q = 0; q < SG; ++q) {
+            const Codes<E> code(z, q);
+            f4 g[FM];
+#pragma unroll
+            for (int j = 0; j < FM; ++j) g[j] = f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int s = q * GS; s < (q + 1) * GS; ++s) {
+                const h8 a = code.frag(codes[s]);
+#pragma unroll
+                for (int j = 0; j < FM; ++j) g[j] = E::mma(a, x[s][j], g[j]);
+            }
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const float f = scale_of<E>(sc, c * SG + q);
+#pragma unroll
+                for (int j = 0; j < FM; ++j) acc[j][c] = fmaf(f, g[j][c], acc[j][c]);
+            }
+        }
+    };
+    const char *const ring = (const char *)red + (size_t)kq * L::STAGES * L::STAGE, *const end = ring + L::STAGES * L::STAGE;
+    const char *cur = ring;
+    for (int i = 0; i < steps; ++i) {
+        wait_vm_lds<0>();               // (this wave's reads of the stage before)
+        __builtin_amdgcn_s_barrier();
+        if (i < blocks) compute(cur);
+        cur = cur + L::STAGE == end ? ring : cur + L::STAGE;
+    }
+    wait_vm_lds<0>();
+    __builtin_amdgcn_s_barrier();
+    if (kgroups > 1) {                  // the groups' sums, in a fixed order
+#pragma unroll
+        for (int j = 0; j < FM; ++j) red[(wave * FM + j) * 64 + lane] = acc[j];
+        __syncthreads();
+        if (kq > 0) return;
+#pragma unroll
+        for (int j = 0; j < FM; ++j)
+            for (int q = 1; q < kgroups; ++q) acc[j] += red[((q * NW + ng) * FM + j) * 64 + lane];
+    }
+#pragma unroll
+    for (int j = 0; j < FM; ++j) store_tile(p, acc[j], nb, m0 + j * 16, lane);
+}
+
+template <typename E, int GS>
+hipError_t launch_stream(const FcInt4Params &p, const FcInt4Geom &g, hipStream_t st) {
+    const dim3 grid((unsigned)p.mtiles * p.nb16), block(64 * g.waves);
+    if (p.zp) launch(fcint4_kernel<E, GS, true>, grid, block, 0, st, p);
+    else launch(fcint4_kernel<E, GS, false>, grid, block, 0, st, p);
     return hipGetLastError();
 }
 
-template <typename E>
+template <typename E, int FM, int NW, int GS>
+hipError_t launch_tile(const FcInt4Params &p, const FcInt4Geom &g, hipStream_t st) {
+    typedef TileLds<FM, NW> L;
+    static_assert(L::STAGES * L::STAGE >= NW * FM * 1024, "the groups' sums fit into the ring");
+    const size_t lds = (size_t)g.kgroups * L::STAGES * L::STAGE;
+    const dim3 grid((unsigned)p.mtiles * ((p.nb16 + NW - 1) / NW)), block(64 * (NW + 1) * g.kgroups);
+    if (lds > 160 * 1024 || block.x > 768) return hipErrorInvalidValue;
+    if (p.xp == 1 && p.zp) launch(fcint4_tile_kernel<E, FM, NW, GS, true, false>, grid, block, lds, st, p, g.kgroups);
+    else if (p.xp == 1) launch(fcint4_tile_kernel<E, FM, NW, GS, false, false>, grid, block, lds, st, p, g.kgroups);
+    else if (p.zp) launch(fcint4_tile_kernel<E, FM, NW, GS, true, true>, grid, block, lds, st, p, g.kgroups);
+    else launch(fcint4_tile_kernel<E, FM, NW, GS, false, true>, grid, block, lds, st, p, g.kgroups);
+    return hipGetLastError();
+}
+
+template <typename E, int GS>
 hipError_t launch_e(const FcInt4Params &p, const FcInt4Geom &g, hipStream_t st) {
-#define MGI_FCINT4(FM_, FN_)                                                     \
-    if (g.fm == FM_ && g.fn == FN_) {                                             \
-        if (g.gs == 1) return launch_z<E, FM_, FN_, 1>(p, g, st);                 \
-        if (g.gs == 2) return launch_z<E, FM_, FN_, 2>(p, g, st);                 \
-        if (g.gs == 4) return launch_z<E, FM_, FN_, 4>(p, g, st);                 \
-    }
-    MGI_FCINT4(1, 1) MGI_FCINT4(1, 2) MGI_FCINT4(2, 2)
-#undef MGI_FCINT4
+    if (g.kgroups == 0) return launch_stream<E, GS>(p, g, st);
+    if (g.fm == 1 && g.waves == 2) return launch_tile<E, 1, 2, GS>(p, g, st);
+    if (g.fm == 1 && g.waves == 4) return launch_tile<E, 1, 4, GS>(p, g, st);
+    if (g.fm == 2 && g.waves == 2) return launch_tile<E, 2, 2, GS>(p, g, st);
+    if (g.fm == 4 && g.waves == 4) return launch_tile<E, 4, 4, GS>(p, g, st);
     return hipErrorInvalidValue;
 }
 
 }  // namespace
 
+// Up to 16 rows: the streaming kernel while each compute unit gets at most one
+// block of 16 channels (1 x 4096 x 4096 4.8 us, the tile kernel 6.0; 5 x 6816 x
+// 1424 6.8 and 10.0), with up to eight waves of at least two blocks of K each;
+// else tiles of 32 channels with four groups along K (7 x 2001 x 5003 5.1 us,
+// streaming 5.8; 16 x 8192 x 8192 10.3 and 13.4), or, for more than 16384
+// channels, of 64 with two (1 x 4096 x 32000 bf16 18.0 us, 19.8).
+// More: tiles of 64 rows x 64 channels where they give every compute unit one
+// and K is long enough to be worth the fetching wave's start (256 x 4096 x 4096
+// bf16 17.1 us, 32 x 32 tiles 20.4), else of 32 x 32 (45 x 283 x 12291 5.6 us,
+// large ones 6.5; 64 x 1024 x 1000 4.7).
 FcInt4Geom fcint4_geom(int M, int nb16, int kb, int group) {
     FcInt4Geom g{};
     g.gs = group % 128 == 0 ? 4 : group % 64 == 0 ? 2 : 1;
-    g.fm = M <= 16 ? 1 : 2;
-    g.fn = g.fm == 1 && nb16 < 512 ? 1 : 2;
-    g.waves = std::max(1, std::min(4, kb));
-    g.splits = 1;
+    g.fm = 1;
+    if (M <= 16 && nb16 <= 256) {
+        g.waves = std::max(1, std::min(8, kb / 2));
+        return g;
+    }
+    if (M <= 16) {
+        g.waves = nb16 > 1024 ? 4 : 2;
+        g.kgroups = std::max(1, std::min(nb16 > 1024 ? 2 : 4, kb / 2));
+    } else {
+        const bool large = (size_t)((M + 63) / 64) * ((nb16 + 3) / 4) >= 256 && kb >= 8;
+        g.fm = large ? 4 : 2;
+        g.waves = large ? 4 : 2;
+        g.kgroups = kb >= 8 ? 2 : 1;
+    }
     return g;
 }
 
@@ -242,11 +420,13 @@ hipError_t launch_fcint4(const FcInt4Params &p0, const FcInt4Geom &g, hipStream_
     FcInt4Params p = p0;
     if (p.M <= 0) return hipSuccess;
     p.mtiles = (p.M + 16 * g.fm - 1) / (16 * g.fm);
-    p.ntiles = (p.nb16 + g.fn - 1) / g.fn;
-    if (g.waves < 1 || g.waves > 8 || g.splits < 1 || (g.splits > 1 && (!p.part || !p.cnt)) ||
-        (size_t)p.mtiles * p.ntiles * g.splits > 0x7fffffffu || p.kb * 16 < p.ksl)
+    if (g.waves < 1 || g.waves > 8 || g.kgroups < 0 || (size_t)p.mtiles * p.nb16 > 0x7fffffffu || p.kb * 16 < p.ksl ||
+        (p.kb - 1) * 16 >= p.ksl)
         return hipErrorInvalidValue;
-    return p.bf16 ? launch_e<BF16>(p, g, st) : launch_e<F16>(p, g, st);
+    if (g.gs == 1) return p.bf16 ? launch_e<BF16, 1>(p, g, st) : launch_e<F16, 1>(p, g, st);
+    if (g.gs == 2) return p.bf16 ? launch_e<BF16, 2>(p, g, st) : launch_e<F16, 2>(p, g, st);
+    if (g.gs == 4) return p.bf16 ? launch_e<BF16, 4>(p, g, st) : launch_e<F16, 4>(p, g, st);
+    return hipErrorInvalidValue;
 }
 
 }  // namespace kern

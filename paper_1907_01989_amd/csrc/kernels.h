@@ -115,25 +115,22 @@ struct FcInt4Params {
     const h8 *x;             // as GemmParams: element (slice, row) at x[slice * xs + row * xp]
     int xs, xp;
     const h8 *zero;          // one zeroed element (read for slices past ksl)
-    const uint32_t *w;       // codes [nb16][kb][64 lanes][4 steps], eight to a word
-    const uint16_t *scales;  // [nb16][kb][16 channels][4 / gs], storage type
-    const uint8_t *zp;       // zero points, laid out as the scales; null: 8
+    // blocks [nb16][kb]: codes [64 lanes][4 steps], eight to a word, then scales
+    // [16 channels][4 / gs] in the storage type and, with zero points (else 8),
+    // those [16 channels][4 / gs], bytes
+    const uint32_t *w;
+    int zp;
     const float *mul;        // [nb16 * 16] power of two taken out of each channel's scales
     const float *bias;       // [nb16 * 16]
     float *y;
-    float *part;             // sums of the splits [tile][split][fm * fn][64 lanes][4] (splits > 1)
-    int *cnt;                // ... and their arrival counters [tile], zero before and after
     int M, ksl, kb, nb16, cout, act, bf16;
-    int mtiles, ntiles;      // set by the launcher
+    int mtiles;              // set by the launcher
 };
-// rows per workgroup 16 * fm, output channels 16 * fn, waves that share K,
-// workgroups that share K, MFMA steps per scale
+// The streaming kernel (kgroups 0): `waves` waves share K.  The tile kernel:
+// `waves` waves of 16 channels to a group, kgroups groups share K, 16 * fm rows.
+// gs: MFMA steps per scale.
 struct FcInt4Geom {
-    int fm, fn, waves, splits, gs;
-    size_t tiles(int M, int nb16) const {
-        return (size_t)((M + 16 * fm - 1) / (16 * fm)) * (size_t)((nb16 + fn - 1) / fn);
-    }
-    size_t part_bytes(int M, int nb16) const { return splits > 1 ? tiles(M, nb16) * splits * fm * fn * 1024 : 0; }
+    int fm, waves, kgroups, gs;
 };
 FcInt4Geom fcint4_geom(int M, int nb16, int kb, int group);
 hipError_t launch_fcint4(const FcInt4Params &p, const FcInt4Geom &g, hipStream_t st);

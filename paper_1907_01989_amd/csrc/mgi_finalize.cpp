@@ -822,17 +822,12 @@ void fuse_answers(mgi_plan &p) {
     p.nodes.swap(kept);
 }
 
-// Geometry of the FcInt4 and Answers kernels, the scratch tensors and counters
-// of those that split their sums over workgroups, and whether questions are
-// about graph inputs.
+// Geometry of the Answers kernels, the scratch tensors and counters of those
+// that split rows over workgroups, and whether questions are about graph inputs.
 void plan_splits(mgi_plan &p) {
     for (Node &nd : p.nodes) {
         size_t part = 0;
-        if (nd.kind == NodeKind::FcInt4) {
-            const int M = (int)p.bufs[nd.in[0]].shape.pixels();
-            part = nd.fq_geo.part_bytes(M, nd.nb16);
-            nd.cnt_bytes = part ? nd.fq_geo.tiles(M, nd.nb16) * sizeof(int) : 0;
-        } else if (nd.kind == NodeKind::Answers) {
+        if (nd.kind == NodeKind::Answers) {
             const Shape s = p.bufs[nd.in[0]].shape;
             nd.an_geo = kern::answers_geom((int)s.pixels(), s.c, nd.k);
             part = nd.an_geo.part_bytes((int)s.pixels(), nd.k);
@@ -1643,7 +1638,7 @@ void plan_memory(mgi_plan &p, const mgi_options &o) {
         nd.cnt_off = p.state_off + state;
         state = align256(state + ((p.bufs[nd.out].shape.pixels() + 15) / 16) * sizeof(int));
     }
-    // ... and the counters of sums that are split over workgroups
+    // ... and of Answers nodes whose rows are split over workgroups, one per row
     for (Node &nd : p.nodes) {
         if (nd.cnt_bytes == 0) continue;
         nd.cnt_off = p.state_off + state;
@@ -1654,12 +1649,13 @@ void plan_memory(mgi_plan &p, const mgi_options &o) {
 
 }
 
-// Codes, scales, zero points, exponents and biases of a 4-bit layer.  A wave's
-// codes of 16 output channels x 128 input channels are one KiB, 16 bytes to a
-// lane in the order of the MFMA A operand: word s of lane l holds channel
-// l % 16's inputs 32 s + 8 (l / 16) .. + 7, input 2i at bits 4i and input
-// 2i + 1 at bits 16 + 4i, so that a shift and a mask give a pair of 16-bit
-// values.  Inputs past the last take their group's zero point: weight 0.
+// Codes, scales, zero points, exponents and biases of a 4-bit layer, in blocks
+// of 16 output channels x 128 input channels, a row of blocks in one stretch of
+// memory.  A block's codes are one KiB, 16 bytes to a lane in the order of the
+// MFMA A operand: word s of lane l holds channel l % 16's inputs 32 s + 8
+// (l / 16) .. + 7, input 2i at bits 4i and input 2i + 1 at bits 16 + 4i, so that
+// a shift and a mask give a pair of 16-bit values.  Its scales, then its zero
+// points, follow: [16 channels][scales per block].  Inputs past the last take their group's zero point: weight 0.
 // Scales are divided by a power of two per output channel that brings the
 // channel's largest near 1 and are then rounded to the storage type (half a
 // unit in the last place, 2^-11 in fp16 and 2^-9 in bf16): in fp16 a scale below
@@ -1667,17 +1663,14 @@ void plan_memory(mgi_plan &p, const mgi_options &o) {
 template <typename Reserve, typename Bits>
 void pack_fc_int4(const GOp &op, int cin, Node &nd, std::vector<uint8_t> &blob, Reserve reserve, Bits to_bits) {
     const int cout = op.cout, kb = nd.ksp, gs = nd.fq_geo.gs, per = 4 / gs, groups = (cin + op.group - 1) / op.group;
-    const size_t row_bytes = ((size_t)cin + 1) / 2, nscales = (size_t)nd.nb16 * kb * 16 * per;
-    nd.w_bytes = (size_t)nd.nb16 * kb * 1024;
+    nd.zeros = !op.zeros.empty();
+    const size_t row_bytes = ((size_t)cin + 1) / 2, block = 1024 + (nd.zeros ? 48 : 32) * (size_t)per;
+    nd.w_bytes = (size_t)nd.nb16 * kb * block;
     nd.w_off = reserve(nd.w_bytes);
-    nd.s_off = reserve(nscales * 2);
-    nd.z_off = op.zeros.empty() ? 0 : reserve(nscales);
     nd.e_off = reserve((size_t)nd.nb16 * 16 * 4);
     nd.b_bytes = (size_t)nd.nb16 * 16 * 4;
     nd.b_off = reserve(nd.b_bytes);
-    uint32_t *wp = reinterpret_cast<uint32_t *>(blob.data() + nd.w_off);
-    uint16_t *sp = reinterpret_cast<uint16_t *>(blob.data() + nd.s_off);
-    uint8_t *zp = nd.z_off ? blob.data() + nd.z_off : nullptr;
+    uint8_t *wp = blob.data() + nd.w_off;
     float *ep = reinterpret_cast<float *>(blob.data() + nd.e_off);
     float *bp = reinterpret_cast<float *>(blob.data() + nd.b_off);
     std::vector<uint8_t> code((size_t)kb * 128);
@@ -1701,9 +1694,10 @@ void pack_fc_int4(const GOp &op, int cin, Node &nd, std::vector<uint8_t> &blob, 
             for (int b = 0; b < kb; ++b)
                 for (int q = 0; q < per; ++q) {
                     const int gi = std::min((b * 128 + q * gs * 32) / op.group, groups - 1);
-                    const size_t at = (((size_t)nb * kb + b) * 16 + row) * per + q;
-                    sp[at] = to_bits(std::ldexp(sc[gi], -e));
-                    if (zp) zp[at] = op.zeros[(size_t)co * groups + gi];
+                    uint8_t *at = wp + ((size_t)nb * kb + b) * block + 1024;
+                    const uint16_t bits = to_bits(std::ldexp(sc[gi], -e));
+                    std::memcpy(at + 2 * (row * per + q), &bits, 2);
+                    if (nd.zeros) at[32 * per + row * per + q] = op.zeros[(size_t)co * groups + gi];
                 }
         }
         for (int b = 0; b < kb; ++b)
@@ -1712,7 +1706,7 @@ void pack_fc_int4(const GOp &op, int cin, Node &nd, std::vector<uint8_t> &blob, 
                     const uint8_t *c = code.data() + (size_t)b * 128 + s * 32 + q * 8;
                     uint32_t v = 0;
                     for (int i = 0; i < 4; ++i) v |= (uint32_t)c[2 * i] << (4 * i) | (uint32_t)c[2 * i + 1] << (16 + 4 * i);
-                    wp[(((size_t)nb * kb + b) * 64 + q * 16 + row) * 4 + s] = v;
+                    std::memcpy(wp + ((size_t)nb * kb + b) * block + ((q * 16 + row) * 4 + s) * 4, &v, 4);
                 }
     }
 }

@@ -175,12 +175,13 @@ struct Node {
                             // (stemdw_configs, irb_configs)
     kern::PwDwGeom pwdw_geo{};   // PwDw, Irb (mode 1): geometry of the fused pair's kernel
     size_t cnt_off = 0;     // FcSoftmax: its row-tile arrival counters in the workspace's
-                            // state region; FcInt4, Answers: counters of split sums
-    size_t cnt_bytes = 0;   // FcInt4, Answers: bytes of those counters (0: not split)
-    // FcInt4: geometry of its kernel, K steps of 32 per packed scale, packed
-    // scales, zero points (0: none) and exponents of the output channels
+                            // state region; Answers: counters of split rows
+    size_t cnt_bytes = 0;   // Answers: bytes of those counters (0: not split)
+    // FcInt4: geometry of its kernel, whether it has zero points, and where the
+    // power of two of each output channel's scales is
     kern::FcInt4Geom fq_geo{};
-    size_t s_off = 0, z_off = 0, e_off = 0;
+    bool zeros = false;
+    size_t e_off = 0;
     // Answers: in[0] holds the rows; buffers of the top channels and the
     // entropy (-1: not asked), and of each list of channels whose log
     // probabilities are asked, with the buffer they go to; `scratch`: what the

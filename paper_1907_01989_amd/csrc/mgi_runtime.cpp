@@ -444,15 +444,10 @@ hipError_t launch_fcint4_node(const mgi_plan &p, const Node &nd, const Bases &B,
     q.x = x.x; q.xs = x.s; q.xp = x.p;
     q.zero = (const h8 *)(wbase + p.zero_off);
     q.w = (const uint32_t *)(wbase + nd.w_off);
-    q.scales = (const uint16_t *)(wbase + nd.s_off);
-    q.zp = nd.z_off ? (const uint8_t *)(wbase + nd.z_off) : nullptr;
+    q.zp = nd.zeros;
     q.mul = (const float *)(wbase + nd.e_off);
     q.bias = (const float *)(wbase + nd.b_off);
     q.y = (float *)y;
-    if (nd.cnt_bytes) {
-        q.part = (float *)buf_ptr(p, nd.scratch, B);
-        q.cnt = (int *)(B.ws + nd.cnt_off);
-    }
     q.M = (int)p.bufs[nd.in[0]].shape.pixels();
     q.ksl = nd.ksl; q.kb = nd.ksp; q.nb16 = nd.nb16;
     q.cout = p.bufs[nd.out].shape.c;
