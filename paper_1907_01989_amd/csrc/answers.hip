@@ -65,23 +65,27 @@ __device__ __forceinline__ float wave_sum(float v) {
     return wave_all(v, 0.0f, [](float a, float b) { return a + b; });
 }
 
-// A bound that at least r of a wave's 64 integers, all from lo to hi, reach: the
-// r-th largest, or less where exactly r reach it already.  Two bits a step,
-// from the first that differ.
-__device__ __forceinline__ uint32_t wave_bound(uint32_t o, uint32_t lo, uint32_t hi, int r) {
-    if (lo == hi) return hi;
-    int b = (31 - __builtin_clz(lo ^ hi)) & ~1;
-    uint32_t ans = hi >> b >> 2 << b << 2;
+// The r-th largest different value of a wave, which at least r lanes reach, or
+// `none`: r rounds of the maximum, those that hold it dropping out.  All lanes
+// get the maximum: rotations within rows of 16, then rows and halves swapped.
+template <typename T, typename F>
+__device__ __forceinline__ T wave_rth(T v, T none, int r, F join) {
+    T top = none;
 #pragma unroll 1
-    for (; b >= 0; b -= 2) {
-        int n[3];
-#pragma unroll
-        for (uint32_t q = 0; q < 3; ++q) n[q] = __popcll(__ballot(o >= (ans | (q + 1) << b)));
-        const int got = n[2] >= r ? n[2] : n[1] >= r ? n[1] : n[0];
-        ans |= (n[2] >= r ? 3u : n[1] >= r ? 2u : n[0] >= r ? 1u : 0u) << b;
-        if (got == r) break;
+    for (int i = 0; i < r; ++i) {
+        int u = __builtin_bit_cast(int, v);
+        auto max2 = [&](int a, int b) { return __builtin_bit_cast(int, join(__builtin_bit_cast(T, a), __builtin_bit_cast(T, b))); };
+        u = max2(u, below<0x128, 0xf>(u, 0));   // (row_ror)
+        u = max2(u, below<0x124, 0xf>(u, 0));
+        u = max2(u, below<0x122, 0xf>(u, 0));
+        u = max2(u, below<0x121, 0xf>(u, 0));
+        auto rows = __builtin_amdgcn_permlane16_swap((unsigned)u, (unsigned)u, false, false);
+        u = max2((int)rows[0], (int)rows[1]);
+        auto halves = __builtin_amdgcn_permlane32_swap((unsigned)u, (unsigned)u, false, false);
+        top = __builtin_bit_cast(T, max2((int)halves[0], (int)halves[1]));
+        if (v == top) v = none;
     }
-    return ans;
+    return top;
 }
 
 __device__ __forceinline__ int lanes_below(unsigned long long mask) {
@@ -101,10 +105,11 @@ __device__ __forceinline__ int take_slots(int *count, int n) {
 
 template <int W>
 struct Shared {
-    alignas(16) unsigned long long cand[kCap + 8];
-    float top_val[kMaxTopK];
-    float m[W], s[W], t[W];
-    uint32_t bound[W];
+    alignas(16) unsigned long long cand[kCap + kMaxTopK + 8];   // zeros behind the candidates
+    unsigned long long best[kMaxTopK];
+    int rank[kCap + kMaxTopK];
+    float m[W], bound[W], s[W], t[W];
+    uint32_t key_bound[W];
     int cnt[W];
     int n, last;
 };
@@ -177,21 +182,39 @@ __device__ __forceinline__ void push(Shared<W> &sh, const H &h, const T *x, floa
         }
 }
 
-// Hands every candidate of the first k to `found`, with its rank: the number of
-// larger ones.  Behind the last there are seven zeros, below every key.
-template <int NT, typename F>
-__device__ __forceinline__ void rank(const unsigned long long *cand, int n, int k, F found) {
+// The first k of n candidates, in order, to sh.best: a candidate's place is the
+// number of larger ones, and every wave counts among its share of them.
+template <int W>
+__device__ __forceinline__ void rank(Shared<W> &sh, int n, int k) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     n = __builtin_amdgcn_readfirstlane(n);
-    for (int j = threadIdx.x; j < n; j += NT) {
-        const unsigned long long key = cand[j];
+    const int share = ((n + W - 1) / W + 7) / 8 * 8, q0 = wave * share, q1 = min(q0 + share, n);
+    for (int j = lane; j < n && q0 < n; j += 64) {
+        const unsigned long long key = sh.cand[j];
         int r = 0;
 #pragma unroll 1
-        for (int q = 0; q < n; q += 8) {
+        for (int q = q0; q < q1; q += 8) {
 #pragma unroll
-            for (int u = 0; u < 8; ++u) r += cand[q + u] > key;
+            for (int u = 0; u < 8; ++u) r += sh.cand[q + u] > key;   // (no key is above itself; zeros are above none)
         }
-        if (r < k) found(r, key);
+        if (W > 1) atomicAdd(&sh.rank[j], r);
+        else if (r < k) sh.best[r] = key;
     }
+    __syncthreads();
+    if (W > 1) {
+        for (int j = threadIdx.x; j < n; j += 64 * W)
+            if (sh.rank[j] < k) sh.best[sh.rank[j]] = sh.cand[j];
+        __syncthreads();
+    }
+}
+
+// Empty candidates and places (all threads of the workgroup; none may read the
+// old ones any more).
+template <int W>
+__device__ __forceinline__ void clear(Shared<W> &sh) {
+    for (int j = threadIdx.x; j < kCap + kMaxTopK + 8; j += 64 * W) sh.cand[j] = 0;
+    for (int j = threadIdx.x; j < kCap + kMaxTopK; j += 64 * W) sh.rank[j] = 0;
+    if (threadIdx.x == 0) sh.n = 0;
 }
 
 // Called by the whole workgroup where `push` found fewer than k candidates (all
@@ -266,8 +289,8 @@ __device__ __noinline__ void push_exact(Shared<NT / 64> &sh, const T *x, int lo,
     __syncthreads();
 }
 
-template <typename T, int NT, int PER>
-__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(PER == 64 ? 4 : 1))) void answers_kernel(AnswersParams p, int segs, int seglen) {
+template <typename T, int NT, int PER, bool MORE>
+__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(PER == 64 ? 4 : 1))) void answers_kernel(AnswersParams p, int segs, int rounds, int seglen) {
     constexpr int W = NT / 64;
     __shared__ Shared<W> sh;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -281,79 +304,93 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(PER == 64 ? 
         listed[l] = -1;
         if (tid < p.list_given[l]) listed[l] = p.list[l][(size_t)row * p.list_given[l] + tid];
     }
-    for (int j = tid; j < kCap + 8; j += NT) sh.cand[j] = 0;
-    Held<T, NT, PER> h;
-    h.load(x, seg * seglen, min(p.cols, (seg + 1) * seglen));
-    const int k = min(p.k, h.hi - h.lo);
+    clear(sh);
     const bool stats = p.n_lists > 0 || p.entropy;
-
-    // The k-th largest value is at least the smallest of the waves' r-th
-    // largest lane maxima, r = ceil(k / waves): few values pass it.  (Waves
-    // past the end of a short row hold nothing and do not count.)
-    const int held = min(W, (h.hi - h.lo + 64 * h.VEC - 1) / (64 * h.VEC));
-    float mx = -INFINITY;
+    int lo = seg * rounds * seglen, hi = min(p.cols, lo + seglen);
+    Held<T, NT, PER> h;
+    h.load(x, lo, hi);
+    float m = -FLT_MAX, s = 0.0f, t = 0.0f;    // (rows of -inf only: s = 0)
+    int k = 0;                                 // keys in sh.best
+    for (int round = 0;;) {
+        // The k-th largest value is at least the smallest of the waves' r-th
+        // largest lane maxima, r = ceil(k / waves): few values pass it.  (Waves
+        // past the end of a short row hold nothing and do not count.)  Of a
+        // later stretch of the row only what reaches the k-th so far does.
+        const int len = hi - lo, kc = min(p.k, len), held = min(W, (len + 64 * h.VEC - 1) / (64 * h.VEC));
+        float mx = -INFINITY;
 #pragma unroll
-    for (int q = 0; q < PER; ++q) mx = fmaxf(mx, h.v[q]);
-    {
-        const float wm = wave_max(mx), wl = -wave_max(-mx);
-        const int r = (k + held - 1) / held;
-        const uint32_t bound = r > 1 ? wave_bound(order_of(mx), order_of(wl), order_of(wm), r) : order_of(wm);
+        for (int q = 0; q < PER; ++q) mx = fmaxf(mx, h.v[q]);
+        const float wm = wave_max(mx);
+        float bound = wave_rth(mx, -INFINITY, (kc + held - 1) / held, [](float a, float b) { return fmaxf(a, b); });
         if (lane == 0) {
             sh.m[wave] = wm;
-            sh.bound[wave] = wave < held ? bound : 0xFFFFFFFFu;
+            sh.bound[wave] = wave < held ? bound : INFINITY;
         }
-        if (tid == 0) sh.n = 0;
-    }
-    __syncthreads();
+        __syncthreads();
+        if (round == 0) {
 #pragma unroll
-    for (int l = 0; l < kAnswerLists; ++l)
-        value[l] = listed[l] >= 0 && listed[l] < p.cols ? (float)x[listed[l]] : NAN;
-    float m = -FLT_MAX;                   // (rows of -inf only: s = 0)
-    uint32_t bound = 0xFFFFFFFFu;
-#pragma unroll
-    for (int w = 0; w < W; ++w) {
-        m = fmaxf(m, sh.m[w]);
-        bound = min(bound, sh.bound[w]);
-    }
-    if (k > 0) push(sh, h, x, value_of(max(bound, order_of(-FLT_MAX))));   // (-inf: push_exact)
-    float s = 0.0f, t = 0.0f;
-    if (stats) {
-#pragma unroll
-        for (int q = 0; q < PER; ++q) {
-            const float d = h.v[q] - m, e = __builtin_amdgcn_exp2f(d * kLog2e);
-            s += e;
-            t = fmaf(e, fmaxf(d, -1e30f), t);     // (0 times -inf)
+            for (int l = 0; l < kAnswerLists; ++l)
+                value[l] = listed[l] >= 0 && listed[l] < p.cols ? (float)x[listed[l]] : NAN;
         }
-        s = wave_sum(s);
-        t = wave_sum(t);
-        if (lane == 0) {
-            sh.s[wave] = s;
-            sh.t[wave] = t;
-        }
-    }
-    __syncthreads();
-    if (stats) {
-        s = t = 0.0f;
+        const float before = m;
+        bound = INFINITY;
 #pragma unroll
         for (int w = 0; w < W; ++w) {
-            s += sh.s[w];
-            t += sh.t[w];
+            m = fmaxf(m, sh.m[w]);
+            bound = fminf(bound, sh.bound[w]);
         }
-    }
-    if (k > 0) {
-        if (sh.n < k || sh.n > kCap) push_exact<T, NT>(sh, x, h.lo, h.hi, k);
-        rank<NT>(sh.cand, sh.n, k, [&](int r, unsigned long long key) {
-            if (segs > 1) {
-                put(p.part_keys + ((size_t)row * segs + seg) * p.k + r, key);
-            } else {
-                p.top[(size_t)row * p.k + r] = (int)~(uint32_t)key;
-                sh.top_val[r] = value_of((uint32_t)(key >> 32));
+        if (MORE && round > 0 && p.k > 0) bound = fmaxf(bound, value_of((uint32_t)(sh.best[p.k - 1] >> 32)));
+        if (kc > 0) push(sh, h, x, fmaxf(bound, -FLT_MAX));   // (-inf: push_exact)
+        if (stats) {
+            float s0 = 0.0f, t0 = 0.0f;
+#pragma unroll
+            for (int q = 0; q < PER; ++q) {
+                const float d = h.v[q] - m, e = __builtin_amdgcn_exp2f(d * kLog2e);
+                s0 += e;
+                t0 = fmaf(e, fmaxf(d, -1e30f), t0);     // (0 times -inf)
             }
-        });
-        if (segs > 1)
-            for (int r = k + tid; r < p.k; r += NT) put(p.part_keys + ((size_t)row * segs + seg) * p.k + r, 0ull);
+            s0 = wave_sum(s0);
+            t0 = wave_sum(t0);
+            if (lane == 0) {
+                sh.s[wave] = s0;
+                sh.t[wave] = t0;
+            }
+        }
+        __syncthreads();
+        if (stats) {
+            if (MORE) {
+                const float d = fmaxf(before - m, -1e30f), w0 = __builtin_amdgcn_exp2f(d * kLog2e);
+                t = w0 * fmaf(s, d, t);
+                s *= w0;
+            }
+#pragma unroll
+            for (int w = 0; w < W; ++w) {
+                s += sh.s[w];
+                t += sh.t[w];
+            }
+        }
+        if (kc > 0) {
+            int n = sh.n;
+            if (n > kCap || (k == 0 && n < kc)) {
+                push_exact<T, NT>(sh, x, lo, hi, kc);
+                n = kc;
+            }
+            if (MORE && k > 0) {                       // and the best so far
+                if (tid < k) sh.cand[n + tid] = sh.best[tid];
+                n += k;
+                __syncthreads();
+            }
+            k = min(p.k, k + len);
+            rank(sh, n, k);
+        }
+        if (!MORE || ++round == rounds || hi == p.cols) break;
+        lo = hi;
+        hi = min(p.cols, hi + seglen);
+        h.load(x, lo, hi);
+        clear(sh);
     }
     if (segs > 1) {
+        for (int r = tid; r < p.k; r += NT) put(p.part_keys + ((size_t)row * segs + seg) * p.k + r, r < k ? sh.best[r] : 0ull);
         float *st = p.part_stats + (size_t)row * segs * 4;
         if (tid == 0) {
             put((unsigned long long *)(st + 4 * seg), (unsigned long long)__float_as_uint(s) << 32 | __float_as_uint(m));
@@ -371,25 +408,16 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(PER == 64 ? 
             // hold keys; then what reaches it
             uint32_t top = 0;
 #pragma unroll
-            for (int c = 0; c < C; ++c) {
-                const int j = c * NT + tid;
-                key[c] = p.part_keys[(size_t)row * n + min(j, n - 1)];
-            }
+            for (int c = 0; c < C; ++c) key[c] = p.part_keys[(size_t)row * n + min(c * NT + tid, n - 1)];
+            clear(sh);
 #pragma unroll
             for (int c = 0; c < C; ++c) {
-                const int j = c * NT + tid;
-                if (j >= n) key[c] = 0;
-                sh.cand[j] = 0;
+                if (c * NT + tid >= n) key[c] = 0;
+                top = max(top, (uint32_t)(key[c] >> 32));
             }
-#pragma unroll
-            for (int c = 0; c < C; ++c) top = max(top, (uint32_t)(key[c] >> 32));
             const int have = min(W, (n + 63) / 64);
-            const uint32_t hi = wave_all(top, 0u, [](uint32_t a, uint32_t b) { return max(a, b); });
-            const uint32_t lo = wave_all(top, 0xFFFFFFFFu, [](uint32_t a, uint32_t b) { return min(a, b); });
-            const int r = (p.k + have - 1) / have;
-            const uint32_t bound = r > 1 ? wave_bound(top, lo, hi, r) : hi;
-            if (lane == 0) sh.bound[wave] = wave < have ? bound : 0xFFFFFFFFu;
-            if (tid == 0) sh.n = 0;
+            const uint32_t bound = wave_rth(top, 0u, (p.k + have - 1) / have, [](uint32_t a, uint32_t b) { return max(a, b); });
+            if (lane == 0) sh.key_bound[wave] = wave < have ? bound : 0xFFFFFFFFu;
         }
         if (stats) {
             m = wave_max(found[0]);
@@ -399,9 +427,9 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(PER == 64 ? 
         }
         __syncthreads();
         if (p.k > 0) {
-            bound = 0xFFFFFFFFu;
+            uint32_t bound = 0xFFFFFFFFu;
 #pragma unroll
-            for (int w = 0; w < W; ++w) bound = min(bound, sh.bound[w]);
+            for (int w = 0; w < W; ++w) bound = min(bound, sh.key_bound[w]);
             bound = max(bound, 1u);                // (not the filling of short segments)
             int mine = 0;
 #pragma unroll
@@ -411,14 +439,11 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(PER == 64 ? 
             for (int c = 0; c < C; ++c)
                 if ((uint32_t)(key[c] >> 32) >= bound) sh.cand[slot++] = key[c];
             __syncthreads();
-            rank<NT>(sh.cand, sh.n, p.k, [&](int r, unsigned long long k1) {
-                p.top[(size_t)row * p.k + r] = (int)~(uint32_t)k1;
-                sh.top_val[r] = value_of((uint32_t)(k1 >> 32));
-            });
+            rank(sh, sh.n, p.k);
         }
     }
+    for (int r = tid; r < p.k; r += NT) p.top[(size_t)row * p.k + r] = (int)~(uint32_t)sh.best[r];
     if (!stats) return;
-    __syncthreads();
     const float logs = logf(s);
 #pragma unroll
     for (int l = 0; l < kAnswerLists; ++l) {
@@ -426,8 +451,10 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(PER == 64 ? 
         const int *list = p.list[l];
         const int nl = p.list_n[l];
         for (int q = tid; q < nl; q += NT) {
-            float v = list ? value[l] : sh.top_val[q];
-            if (list && q != tid) {
+            float v = value[l];
+            if (!list) {
+                v = value_of((uint32_t)(sh.best[q] >> 32));
+            } else if (q != tid) {
                 const int c = list[(size_t)row * nl + q];
                 v = c >= 0 && c < p.cols ? (float)x[c] : NAN;
             }
@@ -440,29 +467,31 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(PER == 64 ? 
 template <typename T>
 hipError_t launch_t(const AnswersParams &p, const AnswersGeom &g, hipStream_t st) {
     const dim3 grid((unsigned)p.rows * (unsigned)g.segs);
-#define MGI_ANSWERS(NT_, PER_)                                                                   \
-    if (g.nt == NT_ && g.per == PER_) {                                                           \
-        launch(answers_kernel<T, NT_, PER_>, grid, dim3(NT_), 0, st, p, g.segs, g.seglen);       \
-        return hipGetLastError();                                                                 \
+#define MGI_ANSWERS(NT_, PER_, MORE_)                                                                   \
+    if (g.nt == NT_ && g.per == PER_ && (g.rounds > 1) == MORE_) {                                       \
+        launch(answers_kernel<T, NT_, PER_, MORE_>, grid, dim3(NT_), 0, st, p, g.segs, g.rounds, g.seglen); \
+        return hipGetLastError();                                                                       \
     }
-    MGI_ANSWERS(64, 8) MGI_ANSWERS(256, 8) MGI_ANSWERS(256, 16) MGI_ANSWERS(256, 32)
-    MGI_ANSWERS(512, 32) MGI_ANSWERS(512, 64)
+    MGI_ANSWERS(64, 8, false) MGI_ANSWERS(256, 8, false) MGI_ANSWERS(256, 16, false) MGI_ANSWERS(256, 32, false)
+    MGI_ANSWERS(512, 32, false) MGI_ANSWERS(512, 64, false) MGI_ANSWERS(512, 64, true)
 #undef MGI_ANSWERS
     return hipErrorInvalidValue;
 }
 
 }  // namespace
 
-// Segments: as many as a workgroup's registers make necessary, more where rows
-// alone would leave compute units idle, none shorter than 2048 columns, and no
-// more than the last workgroup can rank.
+// Segments: more than one where rows alone would leave compute units idle, none
+// shorter than 2048 columns, and no more than the last workgroup can rank.  A
+// workgroup takes its segment in as many rounds as its registers make
+// necessary (668 x 68012, k = 20: three segments with a join 128 us).
 AnswersGeom answers_geom(int rows, int cols, int k) {
     AnswersGeom g{};
     const int most = k > 0 ? std::min(kCap / k, 64) : 64;
-    int segs = (cols + 32767) / 32768;
-    segs = std::max(segs, std::min({256 / std::max(rows, 1), (cols + 2047) / 2048, most}));
-    g.seglen = ((cols + segs - 1) / segs + 7) / 8 * 8;
-    g.segs = (cols + g.seglen - 1) / g.seglen;
+    g.segs = std::max(1, std::min({256 / std::max(rows, 1), (cols + 2047) / 2048, most}));
+    const int len = (cols + g.segs - 1) / g.segs;
+    g.rounds = (len + 32767) / 32768;
+    g.seglen = ((len + g.rounds - 1) / g.rounds + 7) / 8 * 8;
+    g.segs = (cols + g.rounds * g.seglen - 1) / (g.rounds * g.seglen);
     const int sizes[6][2] = {{64, 8}, {256, 8}, {256, 16}, {256, 32}, {512, 32}, {512, 64}};
     for (auto &s : sizes) {
         g.nt = s[0];
@@ -474,7 +503,9 @@ AnswersGeom answers_geom(int rows, int cols, int k) {
 
 hipError_t launch_answers(const AnswersParams &p, const AnswersGeom &g, hipStream_t st) {
     if (p.rows <= 0) return hipSuccess;
-    if (g.segs < 1 || (long)g.nt * g.per < g.seglen || (long)g.segs * g.seglen < p.cols || (g.segs - 1) * g.seglen >= p.cols ||
+    const long len = (long)g.rounds * g.seglen;
+    if (g.segs < 1 || g.rounds < 1 || (long)g.nt * g.per < g.seglen || g.segs * len < p.cols || (g.segs - 1) * len >= p.cols ||
+        (g.rounds > 1 && g.seglen < kMaxTopK) ||
         g.segs > 64 || (long)g.segs * p.k > kCap || p.k > kMaxTopK || (g.segs > 1 && (!p.cnt || !p.part_stats)) ||
         (size_t)p.rows * g.segs > 0x7fffffffu)
         return hipErrorInvalidValue;

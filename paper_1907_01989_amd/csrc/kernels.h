@@ -155,9 +155,10 @@ struct AnswersParams {
     float *part_stats;               // [row][segment][4]: max, sum, weighted sum
     int *cnt;
 };
-// threads per workgroup, values per thread, segments per row and their length
+// threads per workgroup, values per thread, segments per row (workgroups), and
+// the stretches of seglen columns that each takes one after the other
 struct AnswersGeom {
-    int nt, per, segs, seglen;
+    int nt, per, segs, rounds, seglen;
     size_t part_bytes(int rows, int k) const { return segs > 1 ? (size_t)rows * segs * (8 * k + 16) : 0; }
 };
 AnswersGeom answers_geom(int rows, int cols, int k);
