@@ -10,6 +10,8 @@
 // At few rows the bytes of the weights bound it, at many the vector work of
 // taking codes apart (bf16: 19 instructions for eight codes, fp16: 11) beside
 // the products.
+#include <type_traits>
+
 #include "device.h"
 
 namespace mgi {
@@ -77,10 +79,52 @@ __device__ __forceinline__ float scale_of(const uint32_t *s, int i) {
 // scales and zero points [16 channels][4 / gs].
 constexpr int block_bytes(int gs, bool zp) { return 1024 + (zp ? 48 : 32) * (4 / gs); }
 
-// One block of 128 inputs in flight: codes, scales, zero points, activations.
-template <int GS>
+// Channels k .. k + 7 of a row of a graph input that is read as it is: fp32, or
+// fp16 in rows that are not whole slices or for a bf16 plan.  cin >= 8: near the
+// end of a row the load is of its last eight, shifted when they are used.
+template <typename T>
+struct Raw {
+    typedef T v8 __attribute__((ext_vector_type(8)));
+    typedef v8 v8u __attribute__((aligned(sizeof(T))));   // (rows start anywhere)
+    v8 v;
+    __device__ __forceinline__ void load(const T *row, int k, int cin) { v = *(const v8u *)(row + min(k, cin - 8)); }
+    // in the plan's type; edge: some row's eight may be past its end (zeros)
+    template <typename E>
+    __device__ __forceinline__ h8 stored(int k, int cin, bool edge) const {
+        v8 u = v;
+        if (edge) {
+            const int past = k + 8 - cin;
+            const v8 zero = (v8)(T)0.0f;
+            if (past > 0) {
+                if (past & 1) u = __builtin_shufflevector(u, zero, 1, 2, 3, 4, 5, 6, 7, 8);
+                if (past & 2) u = __builtin_shufflevector(u, zero, 2, 3, 4, 5, 6, 7, 8, 9);
+                if (past & 4) u = __builtin_shufflevector(u, zero, 4, 5, 6, 7, 8, 9, 10, 11);
+                if (past >= 8) u = zero;
+            }
+        }
+        if constexpr (sizeof(T) == 2 && !E::bf) {
+            return u;
+        } else {
+            float f[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) f[i] = (float)u[i];
+            return E::pack(f);
+        }
+    }
+};
+
+// One block of 128 inputs in flight: codes, scales, zero points, activations
+// (T: of a graph input read as it is, or void).
+template <int GS, typename T>
 struct Stage {
     static constexpr int SG = 4 / GS;      // scales per channel and block
+    u4v w;
+    uint32_t s[2 * SG], z;
+    Raw<T> x[4];
+};
+template <int GS>
+struct Stage<GS, void> {
+    static constexpr int SG = 4 / GS;
     u4v w;
     uint32_t s[2 * SG], z;
     h8 x[4];
@@ -110,10 +154,11 @@ __device__ __forceinline__ void store_tile(const FcInt4Params &p, const f4 &v, i
 // Up to 16 rows, few output channels: a workgroup takes 16 channels, its waves
 // share K.  Each streams codes and activations from memory to registers, one
 // block ahead; the waves' sums are added in a fixed order.
-template <typename E, int GS, bool ZP>
+template <typename E, int GS, bool ZP, typename T>
 __global__ __launch_bounds__(512) void fcint4_kernel(FcInt4Params p) {
     constexpr int PF = 2;
-    typedef Stage<GS> St;
+    constexpr bool RAW = !std::is_void<T>::value;
+    typedef Stage<GS, T> St;
     constexpr int SG = St::SG;
     __shared__ f4 red[8][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
@@ -136,6 +181,12 @@ __global__ __launch_bounds__(512) void fcint4_kernel(FcInt4Params p) {
             const char *z = w + (1024u + 32 * SG) + (uint32_t)(SG * (lane & 15));
             st.z = SG == 4 ? *(const uint32_t *)z : SG == 2 ? *(const uint16_t *)z : *(const uint8_t *)z;
         }
+        if constexpr (RAW) {
+            const T *row = (const T *)p.xin + (size_t)(m0 + min(lane & 15, p.M - 1 - m0)) * p.cin;
+#pragma unroll
+            for (int s = 0; s < 4; ++s) st.x[s].load(row, b * 128 + s * 32 + kg * 8, p.cin);
+            return;
+        } else {
         // slices past the last are read as the last (and cleared before use)
         const bool edge = b * 16 + 16 > p.ksl;
         uint32_t off[4];
@@ -153,19 +204,26 @@ __global__ __launch_bounds__(512) void fcint4_kernel(FcInt4Params p) {
             const int k0 = min(b * 16 + s * 4, max(p.ksl - 4, 0));
             st.x[s] = *(const h8 *)((const char *)(xbase + (size_t)k0 * p.xs) + (off[s] + xrow));
         }
+        }
     };
     auto compute = [&](int b, St &st) {
-        if (b * 16 + 16 > p.ksl) {
+        h8 x[4];
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            if constexpr (RAW) x[s] = st.x[s].template stored<E>(b * 128 + s * 32 + kg * 8, p.cin, b * 128 + 128 > p.cin);
+            else x[s] = st.x[s];
+        }
+        if (!RAW && b * 16 + 16 > p.ksl) {
 #pragma unroll
             for (int s = 0; s < 4; ++s)
-                if (b * 16 + s * 4 + kg >= p.ksl) st.x[s] = zero_h8();
+                if (b * 16 + s * 4 + kg >= p.ksl) x[s] = zero_h8();
         }
 #pragma unroll
         for (int q = 0; q < SG; ++q) {
             const Codes<E> code(ZP ? st.z : 0x08080808u, q);
             f4 g = f4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int s = q * GS; s < (q + 1) * GS; ++s) g = E::mma(code.frag(st.w[s]), st.x[s], g);
+            for (int s = q * GS; s < (q + 1) * GS; ++s) g = E::mma(code.frag(st.w[s]), x[s], g);
 #pragma unroll
             for (int c = 0; c < 4; ++c) acc[c] = fmaf(scale_of<E>(st.s, c * SG + q), g[c], acc[c]);
         }
@@ -212,9 +270,71 @@ struct TileLds {
     static constexpr int X = FM * 4096, W = 1280, STAGE = X + NW * W, STAGES = 3;
 };
 
-template <typename E, int FM, int NW, int GS, bool ZP, bool NHWC>
-__global__ __launch_bounds__(768) void fcint4_tile_kernel(FcInt4Params p, int kgroups) {
+// A barrier that no access of LDS is moved across (and no wait: each wave has
+// waited for what the others are to see).
+__device__ __forceinline__ void ring_barrier() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+__device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
+// The wave that fetches a raw graph input for a group of one row tile: through
+// registers, a block ahead of the ring, since the values are converted on the
+// way; laid out as kNhwc.
+template <typename E, typename T, int NW>
+__device__ __forceinline__ void fetch_raw(const FcInt4Params &p, int kgroups, int kq, int m0, int steps, char *ring) {
+    typedef TileLds<1, NW> L;
+    constexpr int XL = 4, AHEAD = L::STAGES - 1;
+    const int lane = threadIdx.x & 63, rows = min(16, p.M - m0);
+    const int b0 = (int)((long)p.kb * kq / kgroups), b1 = (int)((long)p.kb * (kq + 1) / kgroups);
+    const T *row[XL];
+    int slice[XL];
+#pragma unroll
+    for (int q = 0; q < XL; ++q) {
+        const int r = q * 4 + (lane >> 4);
+        slice[q] = (lane & 15) ^ (r & 15);
+        row[q] = (const T *)p.xin + (size_t)(m0 + min(r, rows - 1)) * p.cin;
+    }
+    Raw<T> x[XL];
+    auto block = [&](int i) { return min(b0 + i, b1 - 1); };   // (past the range: its last again)
+    auto load = [&](int i) {
+#pragma unroll
+        for (int q = 0; q < XL; ++q)                           // (what rows past the last hold is not stored)
+            if (q * 4 < rows) x[q].load(row[q], block(i) * 128 + slice[q] * 8, p.cin);
+    };
+    auto write = [&](int i, char *st) {
+        const int b = block(i);
+#pragma unroll
+        for (int q = 0; q < XL; ++q)
+            if (q * 4 < rows)
+                *(h8 *)(st + (q * 64 + lane) * 16) = x[q].template stored<E>(b * 128 + slice[q] * 8, p.cin, b * 128 + 128 > p.cin);
+    };
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+        load(i);
+        write(i, ring + i * L::STAGE);
+    }
+    load(AHEAD);
+    char *const end = ring + L::STAGES * L::STAGE;
+    char *fill = ring + AHEAD * L::STAGE;
+    for (int i = 0; i < steps; ++i) {
+        wait_lds();                                            // (the writes are done)
+        ring_barrier();
+        write(i + AHEAD, fill);
+        load(i + AHEAD + 1);
+        fill = fill + L::STAGE == end ? ring : fill + L::STAGE;
+    }
+    wait_lds();
+    ring_barrier();
+}
+
+// (MODE: how the activations are stored, see FcInt4Params)
+constexpr int kSliced = 0, kNhwc = 1, kRaw = 2;
+template <typename E, int FM, int NW, int GS, bool ZP, int MODE>
+__global__ __launch_bounds__(MODE == kRaw ? 1024 : 768) void fcint4_tile_kernel(FcInt4Params p, int kgroups) {
     typedef TileLds<FM, NW> L;
+    constexpr bool NHWC = MODE != kSliced;
     constexpr int SG = 4 / GS, BLOCK = block_bytes(GS, ZP);
     extern __shared__ f4 red[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -222,6 +342,15 @@ __global__ __launch_bounds__(768) void fcint4_tile_kernel(FcInt4Params p, int kg
     const int nt = t / p.mtiles, m0 = (t - nt * p.mtiles) * 16 * FM;
     const int steps = (p.kb + kgroups - 1) / kgroups;
 
+    if constexpr (MODE == kRaw)
+    if (wave >= (NW + 1) * kgroups) {
+        const int kq = wave - (NW + 1) * kgroups;
+        char *ring = (char *)red + (size_t)kq * L::STAGES * L::STAGE;
+        if (p.fp16_in) fetch_raw<E, _Float16, NW>(p, kgroups, kq, m0, steps, ring);
+        else fetch_raw<E, float, NW>(p, kgroups, kq, m0, steps, ring);
+        if (kgroups > 1) __syncthreads();
+        return;
+    }
     if (wave >= NW * kgroups) {                       // fetch for group kq
         const int kq = wave - NW * kgroups;
         const int b0 = (int)((long)p.kb * kq / kgroups), b1 = (int)((long)p.kb * (kq + 1) / kgroups);
@@ -230,9 +359,9 @@ __global__ __launch_bounds__(768) void fcint4_tile_kernel(FcInt4Params p, int kg
         // load is four rows of 256 bytes, slices swapped by the row so that the
         // reads meet no bank twice; sliced: slice after slice.  Addresses are
         // uniform bases plus lane offsets that do not change.
-        constexpr int XL = FM * 4;
-        uint32_t xofs[XL];
-        int xslice[XL];
+        constexpr int XL = MODE == kRaw ? 0 : FM * 4;
+        uint32_t xofs[XL ? XL : 1];
+        int xslice[XL ? XL : 1];
         const int rows = min(16 * FM, p.M - m0);
 #pragma unroll
         for (int q = 0; q < XL; ++q) {
@@ -276,12 +405,12 @@ __global__ __launch_bounds__(768) void fcint4_tile_kernel(FcInt4Params p, int kg
             // a stage is whole once only the loads of later ones are in flight;
             // behind the barrier all waves are done with the one before it
             wait_vm_lds<(L::STAGES - 2) * (XL + 2 * NW)>();
-            __builtin_amdgcn_s_barrier();
+            ring_barrier();
             issue(i + L::STAGES - 1, fill);
             fill = fill + L::STAGE == end ? ring : fill + L::STAGE;
         }
         wait_vm_lds<0>();
-        __builtin_amdgcn_s_barrier();
+        ring_barrier();
         if (kgroups > 1) __syncthreads();
         return;
     }
@@ -332,13 +461,13 @@ __global__ __launch_bounds__(768) void fcint4_tile_kernel(FcInt4Params p, int kg
     const char *const ring = (const char *)red + (size_t)kq * L::STAGES * L::STAGE, *const end = ring + L::STAGES * L::STAGE;
     const char *cur = ring;
     for (int i = 0; i < steps; ++i) {
-        wait_vm_lds<0>();               // (this wave's reads of the stage before)
-        __builtin_amdgcn_s_barrier();
+        wait_lds();                     // (this wave's reads of the stage before)
+        ring_barrier();
         if (i < blocks) compute(cur);
         cur = cur + L::STAGE == end ? ring : cur + L::STAGE;
     }
-    wait_vm_lds<0>();
-    __builtin_amdgcn_s_barrier();
+    wait_lds();
+    ring_barrier();
     if (kgroups > 1) {                  // the groups' sums, in a fixed order
 #pragma unroll
         for (int j = 0; j < FM; ++j) red[(wave * FM + j) * 64 + lane] = acc[j];
@@ -352,35 +481,45 @@ __global__ __launch_bounds__(768) void fcint4_tile_kernel(FcInt4Params p, int kg
     for (int j = 0; j < FM; ++j) store_tile(p, acc[j], nb, m0 + j * 16, lane);
 }
 
-template <typename E, int GS>
+template <typename E, int GS, typename T>
 hipError_t launch_stream(const FcInt4Params &p, const FcInt4Geom &g, hipStream_t st) {
     const dim3 grid((unsigned)p.mtiles * p.nb16), block(64 * g.waves);
-    if (p.zp) launch(fcint4_kernel<E, GS, true>, grid, block, 0, st, p);
-    else launch(fcint4_kernel<E, GS, false>, grid, block, 0, st, p);
+    if (p.zp) launch(fcint4_kernel<E, GS, true, T>, grid, block, 0, st, p);
+    else launch(fcint4_kernel<E, GS, false, T>, grid, block, 0, st, p);
     return hipGetLastError();
 }
 
-template <typename E, int FM, int NW, int GS>
+template <typename E, int FM, int NW, int GS, int MODE>
 hipError_t launch_tile(const FcInt4Params &p, const FcInt4Geom &g, hipStream_t st) {
     typedef TileLds<FM, NW> L;
     static_assert(L::STAGES * L::STAGE >= NW * FM * 1024, "the groups' sums fit into the ring");
     const size_t lds = (size_t)g.kgroups * L::STAGES * L::STAGE;
-    const dim3 grid((unsigned)p.mtiles * ((p.nb16 + NW - 1) / NW)), block(64 * (NW + 1) * g.kgroups);
-    if (lds > 160 * 1024 || block.x > 768) return hipErrorInvalidValue;
-    if (p.xp == 1 && p.zp) launch(fcint4_tile_kernel<E, FM, NW, GS, true, false>, grid, block, lds, st, p, g.kgroups);
-    else if (p.xp == 1) launch(fcint4_tile_kernel<E, FM, NW, GS, false, false>, grid, block, lds, st, p, g.kgroups);
-    else if (p.zp) launch(fcint4_tile_kernel<E, FM, NW, GS, true, true>, grid, block, lds, st, p, g.kgroups);
-    else launch(fcint4_tile_kernel<E, FM, NW, GS, false, true>, grid, block, lds, st, p, g.kgroups);
+    const dim3 grid((unsigned)p.mtiles * ((p.nb16 + NW - 1) / NW)), block(64 * (NW + (MODE == kRaw ? 2 : 1)) * g.kgroups);
+    if (lds > 160 * 1024 || block.x > (MODE == kRaw ? 1024 : 768)) return hipErrorInvalidValue;
+    if (p.zp) launch(fcint4_tile_kernel<E, FM, NW, GS, true, MODE>, grid, block, lds, st, p, g.kgroups);
+    else launch(fcint4_tile_kernel<E, FM, NW, GS, false, MODE>, grid, block, lds, st, p, g.kgroups);
     return hipGetLastError();
+}
+
+template <typename E, int FM, int NW, int GS>
+hipError_t launch_mode(const FcInt4Params &p, const FcInt4Geom &g, hipStream_t st) {
+    if constexpr (FM == 1)
+        if (p.xin) return launch_tile<E, FM, NW, GS, kRaw>(p, g, st);
+    if (p.xin) return hipErrorInvalidValue;
+    if (p.xp == 1) return launch_tile<E, FM, NW, GS, kSliced>(p, g, st);
+    if constexpr (!E::bf) return launch_tile<E, FM, NW, GS, kNhwc>(p, g, st);   // (graph inputs are fp16)
+    return hipErrorInvalidValue;
 }
 
 template <typename E, int GS>
 hipError_t launch_e(const FcInt4Params &p, const FcInt4Geom &g, hipStream_t st) {
-    if (g.kgroups == 0) return launch_stream<E, GS>(p, g, st);
-    if (g.fm == 1 && g.waves == 2) return launch_tile<E, 1, 2, GS>(p, g, st);
-    if (g.fm == 1 && g.waves == 4) return launch_tile<E, 1, 4, GS>(p, g, st);
-    if (g.fm == 2 && g.waves == 2) return launch_tile<E, 2, 2, GS>(p, g, st);
-    if (g.fm == 4 && g.waves == 4) return launch_tile<E, 4, 4, GS>(p, g, st);
+    if (g.kgroups == 0 && p.xin && p.fp16_in) return launch_stream<E, GS, _Float16>(p, g, st);
+    if (g.kgroups == 0 && p.xin) return launch_stream<E, GS, float>(p, g, st);
+    if (g.kgroups == 0) return launch_stream<E, GS, void>(p, g, st);
+    if (g.fm == 1 && g.waves == 2) return launch_mode<E, 1, 2, GS>(p, g, st);
+    if (g.fm == 1 && g.waves == 4) return launch_mode<E, 1, 4, GS>(p, g, st);
+    if (g.fm == 2 && g.waves == 2) return launch_mode<E, 2, 2, GS>(p, g, st);
+    if (g.fm == 4 && g.waves == 4) return launch_mode<E, 4, 4, GS>(p, g, st);
     return hipErrorInvalidValue;
 }
 

@@ -112,8 +112,12 @@ size_t gemm_xs_lds_bytes(int ksp, int wm, int bn);
 // Fully connected layer with 4-bit weights (fcint4.hip), fp32 (M x cout) output.
 // K runs in blocks of 128 (four MFMA steps of 32); `gs` steps share a scale.
 struct FcInt4Params {
-    const h8 *x;             // as GemmParams: element (slice, row) at x[slice * xs + row * xp]
+    // activations, as GemmParams: element (slice, row) at x[slice * xs + row * xp];
+    // or (xin not null) a graph input as it is, M rows of cin fp32 or fp16 values
+    const h8 *x;
     int xs, xp;
+    const void *xin;
+    int cin, fp16_in;
     const h8 *zero;          // one zeroed element (read for slices past ksl)
     // blocks [nb16][kb]: codes [64 lanes][4 steps], eight to a word, then scales
     // [16 channels][4 / gs] in the storage type and, with zero points (else 8),
@@ -131,6 +135,7 @@ struct FcInt4Params {
 // gs: MFMA steps per scale.
 struct FcInt4Geom {
     int fm, waves, kgroups, gs;
+    bool reads_raw(int cin) const { return fm == 1 && cin >= 8; }   // takes xin
 };
 FcInt4Geom fcint4_geom(int M, int nb16, int kb, int group);
 hipError_t launch_fcint4(const FcInt4Params &p, const FcInt4Geom &g, hipStream_t st);

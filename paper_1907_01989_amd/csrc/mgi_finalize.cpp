@@ -1924,16 +1924,18 @@ void alias_concats(mgi_plan &p, const mgi_options &o) {
     }
 }
 
-// A graph input in whole slices whose readers can all read the NHWC array is
-// read in place by them (the ingest node stays in the list and launches
-// nothing, in runs where it can be so).  Depthwise kernels convert what they
-// read; the others take fp16 inputs of fp16 plans, whose 16-byte elements are
-// the same in both layouts.  Not with materialize_all.
+// A graph input whose readers can all read the NHWC array is read in place by
+// them (the ingest node stays in the list and launches nothing, in runs where it
+// can be so).  Depthwise kernels convert what they read, 4-bit layers of few
+// rows too, and need no whole slices; the others take fp16 inputs of fp16
+// plans in whole slices, whose 16-byte elements are the same in both layouts.
+// Not with materialize_all.
 void absorb_ingests(mgi_plan &p, const mgi_options &o) {
     int bits = 0;
     for (Node &in : p.nodes) {
-        if (in.kind != NodeKind::Ingest || p.bufs[in.out].shape.c % 8 != 0 || bits >= 64) continue;
-        const bool same = p.bufs[in.in[0]].in_dtype == MGI_DTYPE_FP16 && o.dtype == MGI_DTYPE_FP16;
+        if (in.kind != NodeKind::Ingest || bits >= 64) continue;
+        const bool whole = p.bufs[in.out].shape.c % 8 == 0;
+        const bool same = whole && p.bufs[in.in[0]].in_dtype == MGI_DTYPE_FP16 && o.dtype == MGI_DTYPE_FP16;
         std::vector<int> readers;
         bool all = true;
         for (size_t i = 0; i < p.nodes.size(); ++i) {
@@ -1945,14 +1947,14 @@ void absorb_ingests(mgi_plan &p, const mgi_options &o) {
             const Shape &os = p.bufs[r.out].shape;
             switch (r.kind) {
                 case NodeKind::Depthwise:
-                    all = all && kern::depthwise_reads_nhwc(c.kh, c.kw, c.stride_h, c.stride_w, c.dil_h, c.dil_w, os.n,
+                    all = all && whole && kern::depthwise_reads_nhwc(c.kh, c.kw, c.stride_h, c.stride_w, c.dil_h, c.dil_w, os.n,
                                                             slices(os.c), os.h, os.w);
                     break;
                 case NodeKind::Gemm:
                 case NodeKind::PwDw:
                 case NodeKind::GemmPool:
-                case NodeKind::FcInt4:
                 case NodeKind::Gap: all = all && same; break;
+                case NodeKind::FcInt4: all = all && (same || r.fq_geo.reads_raw(p.bufs[in.out].shape.c)); break;
                 default: all = false;
             }
         }

@@ -442,13 +442,19 @@ hipError_t launch_fcint4_node(const mgi_plan &p, const Node &nd, const Bases &B,
     FcInt4Params q{};
     const Operand x = operand(p, nd.in[0], B);
     q.x = x.x; q.xs = x.s; q.xp = x.p;
+    const Buf &xb = p.bufs[nd.in[0]];
+    if (x.in_place) {
+        q.cin = xb.shape.c;
+        q.fp16_in = p.bufs[xb.direct_src].in_dtype == MGI_DTYPE_FP16;
+        if (q.cin % 8 != 0 || !q.fp16_in || p.opt.dtype != MGI_DTYPE_FP16) q.xin = x.x;
+    }
     q.zero = (const h8 *)(wbase + p.zero_off);
     q.w = (const uint32_t *)(wbase + nd.w_off);
     q.zp = nd.zeros;
     q.mul = (const float *)(wbase + nd.e_off);
     q.bias = (const float *)(wbase + nd.b_off);
     q.y = (float *)y;
-    q.M = (int)p.bufs[nd.in[0]].shape.pixels();
+    q.M = (int)xb.shape.pixels();
     q.ksl = nd.ksl; q.kb = nd.ksp; q.nb16 = nd.nb16;
     q.cout = p.bufs[nd.out].shape.c;
     q.act = nd.act1;

@@ -209,3 +209,41 @@ def test_runs_repeat_and_replay(n, cin, cout):
         xs[0].neg_()
         torch.cuda.synchronize()
         assert not torch.equal(eager, first)
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("src", [DTYPE_FP16, DTYPE_FP32])
+@pytest.mark.parametrize("n,cin,cout", [(1, 7, 5), (1, 8, 20), (16, 9, 4200), (3, 15, 16), (5, 127, 4100), (9, 129, 33),
+                                        (13, 250, 4500), (16, 1027, 16), (7, 2001, 5003), (2, 1289, 16500)])
+def test_rows_read_as_they_are(n, cin, cout, src, dtype):
+    # few rows of fp32 or of odd fp16 length are converted by the layer itself:
+    # the same values as through a converted copy, also at the rows' ends
+    import torch
+    from paper_1907_01989_amd import engine
+    desc, t = layer(n, cin, cout, 64, True, dtype=src, seed=4)
+    if dtype == 1:
+        desc = workloads.as_bf16_graph(desc)
+    log(f"[case] {desc['name']} inputs {src}, storage type {dtype}")
+    plan = engine.Plan(desc, dtype=dtype)
+    (x,) = plan.input_tensors()
+    got = plan.run([x])[0].clone()
+    check(desc, t, got.cpu().numpy())
+    # an array off 16 bytes, and one that the output overlaps, are converted first
+    apart = torch.empty(x.numel() + 4, dtype=x.dtype, device=x.device)
+    off = apart[1:1 + x.numel()].view(x.shape)
+    off.copy_(x)
+    assert torch.equal(plan.run([off])[0], got)
+    room = torch.empty(max(x.numel() * x.element_size(), got.numel() * 4), dtype=torch.uint8, device=x.device)
+    same = room[:x.numel() * x.element_size()].view(x.dtype).view(x.shape)
+    same.copy_(x)
+    over = room[:got.numel() * 4].view(torch.float32).view(got.shape)
+    plan.run([same], [over])
+    assert torch.equal(over, got)
+    x[n - 1, ..., cin - 1] = float("inf")
+    last = plan.run([x])[0]
+    assert torch.equal(last[:n - 1], got[:n - 1])
+    op = desc["ops"][1]
+    codes = op["q"][:, (cin - 1) // 2] >> (4 * ((cin - 1) % 2)) & 15
+    w = torch.as_tensor((codes.astype(np.float64) - op["zeros"][:, -1]) * op["scales"][:, -1], device=x.device)
+    row = last[n - 1].reshape(-1).double()
+    assert torch.isnan(row[w == 0]).all() and torch.equal(row[w != 0], torch.sign(w[w != 0]) * float("inf"))
