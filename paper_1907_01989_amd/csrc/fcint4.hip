@@ -5,9 +5,9 @@
 // 16-bit type, so the inner sums run on the matrix cores with no rounding but
 // that of the fp32 accumulator, and the scale multiplies the group's sum, not
 // the weights.  Weights come as blocks of 16 output channels x 128 inputs (see
-// pack_fc_int4), a KiB of codes in the MFMA operand's own order.
+// pack_fc_int4), in the MFMA operand's own order.
 //
-// At few rows the bytes of the weights bound it, at many the vector work of
+// At few rows the bytes of the weights bound it, at more the vector work of
 // taking codes apart (bf16: 19 instructions for eight codes, fp16: 11) beside
 // the products.
 #include <type_traits>
@@ -74,10 +74,6 @@ __device__ __forceinline__ float scale_of(const uint32_t *s, int i) {
     if (E::bf) return __uint_as_float(i & 1 ? v & 0xFFFF0000u : v << 16);
     return (float)__builtin_bit_cast(_Float16, (uint16_t)(i & 1 ? v >> 16 : v));
 }
-
-// Bytes of a block of 16 output channels x 128 inputs: a wave's codes, then the
-// scales and zero points [16 channels][4 / gs].
-constexpr int block_bytes(int gs, bool zp) { return 1024 + (zp ? 48 : 32) * (4 / gs); }
 
 // Channels k .. k + 7 of a row of a graph input that is read as it is: fp32, or
 // fp16 in rows that are not whole slices or for a bf16 plan.  cin >= 8: near the
@@ -174,7 +170,7 @@ __global__ __launch_bounds__(512) void fcint4_kernel(FcInt4Params p) {
     f4 acc = f4{0.f, 0.f, 0.f, 0.f};
 
     auto load = [&](int b, St &st) {
-        const char *w = (const char *)p.w + ((size_t)nb * p.kb + b) * block_bytes(GS, ZP);
+        const char *w = (const char *)p.w + ((size_t)nb * p.kb + b) * fcint4_block_bytes(GS, ZP);
         st.w = *(const u4v *)(w + 16u * (uint32_t)lane);
         __builtin_memcpy(st.s, w + 1024u + (uint32_t)(8 * SG * kg), 8 * SG);
         if (ZP) {
@@ -262,9 +258,8 @@ __global__ __launch_bounds__(512) void fcint4_kernel(FcInt4Params p) {
 // for the same 16 FM rows, and a wave of its own fetches for it, block after
 // block, the rows' activations and the waves' codes into a ring of three stages
 // in LDS.  The waves that compute then read activations once per row tile and
-// spend no instructions on loads (256 x 4096 x 4096, bf16: 20.7 us where every
-// wave fetched its share, 17.1 with the fetching wave; 16 x 8192 x 8192 13.4 and
-// 10.3).  kgroups such groups share K.
+// spend no instructions on loads (16 x 8192 x 8192: 13.4 us where every wave
+// fetches for itself, 10.3 so).  kgroups such groups share K.
 template <int FM, int NW>
 struct TileLds {
     static constexpr int X = FM * 4096, W = 1280, STAGE = X + NW * W, STAGES = 3;
@@ -278,6 +273,41 @@ __device__ __forceinline__ void ring_barrier() {
     asm volatile("" ::: "memory");
 }
 __device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
+// A block of activations, 16 FM rows x 16 slices of 16 bytes, to LDS by one
+// wave.  NHWC: a load is four rows of 256 bytes, slices swapped by the row so
+// that the reads meet no bank twice; sliced: slice after slice.  Addresses are
+// uniform bases plus lane offsets that do not change.
+template <int FM, bool NHWC>
+struct RowFetch {
+    static constexpr int XL = FM * 4;      // loads of a block
+    uint32_t ofs[XL];
+    int slice[XL];
+    const h8 *base;
+    __device__ __forceinline__ RowFetch(const FcInt4Params &p, int m0, int lane) {
+        const int rows = min(16 * FM, p.M - m0);
+#pragma unroll
+        for (int q = 0; q < XL; ++q) {
+            const int slot = q * 64 + lane;
+            const int row = NHWC ? slot >> 4 : slot % (16 * FM);
+            slice[q] = NHWC ? (slot & 15) ^ (row & 15) : slot / (16 * FM);
+            ofs[q] = 16u * (uint32_t)(min(row, rows - 1) * p.xp + slice[q] * p.xs);
+        }
+        base = p.x + (size_t)m0 * p.xp;
+    }
+    __device__ __forceinline__ void issue(const FcInt4Params &p, int b, char *st) const {
+        const h8 *x = base + (size_t)(b * 16) * p.xs;
+        if (b * 16 + 16 <= p.ksl) {
+#pragma unroll
+            for (int q = 0; q < XL; ++q) load_lds16(x, ofs[q], (const h8 *)(st + q * 1024));
+        } else {                           // slices past the last: zeros
+#pragma unroll
+            for (int q = 0; q < XL; ++q)
+                load_lds16(b * 16 + slice[q] < p.ksl ? (const h8 *)((const char *)x + ofs[q]) : p.zero,
+                           (const h8 *)(st + q * 1024));
+        }
+    }
+};
 
 // The wave that fetches a raw graph input for a group of one row tile: through
 // registers, a block ahead of the ring, since the values are converted on the
@@ -335,7 +365,7 @@ template <typename E, int FM, int NW, int GS, bool ZP, int MODE>
 __global__ __launch_bounds__(MODE == kRaw ? 1024 : 768) void fcint4_tile_kernel(FcInt4Params p, int kgroups) {
     typedef TileLds<FM, NW> L;
     constexpr bool NHWC = MODE != kSliced;
-    constexpr int SG = 4 / GS, BLOCK = block_bytes(GS, ZP);
+    constexpr int SG = 4 / GS, BLOCK = fcint4_block_bytes(GS, ZP);
     extern __shared__ f4 red[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int t = xcd_tile(blockIdx.x, gridDim.x);
@@ -355,38 +385,15 @@ __global__ __launch_bounds__(MODE == kRaw ? 1024 : 768) void fcint4_tile_kernel(
         const int kq = wave - NW * kgroups;
         const int b0 = (int)((long)p.kb * kq / kgroups), b1 = (int)((long)p.kb * (kq + 1) / kgroups);
         char *ring = (char *)red + (size_t)kq * L::STAGES * L::STAGE;
-        // Activations of a block: 16 FM rows x 16 slices of 16 bytes.  NHWC: a
-        // load is four rows of 256 bytes, slices swapped by the row so that the
-        // reads meet no bank twice; sliced: slice after slice.  Addresses are
-        // uniform bases plus lane offsets that do not change.
         constexpr int XL = MODE == kRaw ? 0 : FM * 4;
-        uint32_t xofs[XL ? XL : 1];
-        int xslice[XL ? XL : 1];
-        const int rows = min(16 * FM, p.M - m0);
-#pragma unroll
-        for (int q = 0; q < XL; ++q) {
-            const int slot = q * 64 + lane;
-            const int row = NHWC ? slot >> 4 : slot % (16 * FM);
-            xslice[q] = NHWC ? (slot & 15) ^ (row & 15) : slot / (16 * FM);
-            xofs[q] = 16u * (uint32_t)(min(row, rows - 1) * p.xp + xslice[q] * p.xs);
-        }
-        const h8 *xbase = p.x + (size_t)m0 * p.xp;
+        const RowFetch<FM, NHWC> rows(p, m0, lane);
         const char *wbase[NW];
 #pragma unroll
         for (int i = 0; i < NW; ++i)
             wbase[i] = (const char *)p.w + (size_t)__builtin_amdgcn_readfirstlane(min(nt * NW + i, p.nb16 - 1)) * p.kb * BLOCK;
         auto issue = [&](int i, char *st) {           // (past the range: its last block again)
             const int b = __builtin_amdgcn_readfirstlane(min(min(b0 + i, b1 - 1), p.kb - 1));
-            const h8 *x = xbase + (size_t)(b * 16) * p.xs;
-            if (b * 16 + 16 <= p.ksl) {
-#pragma unroll
-                for (int q = 0; q < XL; ++q) load_lds16(x, xofs[q], (const h8 *)(st + q * 1024));
-            } else {                                  // slices past the last: zeros
-#pragma unroll
-                for (int q = 0; q < XL; ++q)
-                    load_lds16(b * 16 + xslice[q] < p.ksl ? (const h8 *)((const char *)x + xofs[q]) : p.zero,
-                               (const h8 *)(st + q * 1024));
-            }
+            if constexpr (MODE != kRaw) rows.issue(p, b, st);
 #pragma unroll
             for (int n = 0; n < NW; ++n)
                 load_lds16((const h8 *)(wbase[n] + (size_t)b * BLOCK), 16u * (uint32_t)lane, (const h8 *)(st + L::X + n * L::W));
@@ -481,6 +488,155 @@ __global__ __launch_bounds__(MODE == kRaw ? 1024 : 768) void fcint4_tile_kernel(
     for (int j = 0; j < FM; ++j) store_tile(p, acc[j], nb, m0 + j * 16, lane);
 }
 
+// The differences code - z of a lane's 32 inputs, as 6-bit floats (sign, two bits
+// of exponent, three of mantissa; the patterns 0 .. 15 are 0 .. 15 eighths, so
+// all are exact), as four MFMA fragments: one instruction.
+typedef uint32_t u6v __attribute__((ext_vector_type(6)));
+struct Frags {
+    h8 a[4];
+};
+template <typename E>
+__device__ __forceinline__ Frags six_bit(u6v w) {
+    if constexpr (E::bf) return __builtin_bit_cast(Frags, __builtin_amdgcn_cvt_scalef32_pk32_bf16_fp6(w, 8.0f));
+    else return __builtin_bit_cast(Frags, __builtin_amdgcn_cvt_scalef32_pk32_f16_fp6(w, 8.0f));
+}
+
+// Many rows: 64 rows x 64 channels, K shared by four groups of two waves, each
+// with 32 channels of all rows, and a wave that fetches the group's activations
+// into a ring of two stages.  A fragment read from LDS feeds two products, the
+// next step's are read before a step's products, and codes, which no other wave
+// reads, go to registers, a block ahead.  Taking 4-bit codes apart would take
+// longer than the products, so the layer is kept as 6-bit differences for this
+// kernel (256 x 4096 x 4096 bf16 19.5 us with 16 channels to a wave, 18.3 with 32,
+16.2 so).  What bounds it is the traffic between L2 and LDS: 0.7 MB to a compute
+unit there.
+constexpr int kWideGroups = 4, kWideX = 64 * 256, kWideLds = kWideGroups * 2 * kWideX;
+template <typename E, int GS, bool NHWC>
+__global__ __launch_bounds__(768) void fcint4_wide_kernel(FcInt4Params p) {
+    constexpr int FM = 4, NB = 2, SG = 4 / GS, BLOCK = 1536 + 32 * SG;
+    extern __shared__ f4 red[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int t = xcd_tile(blockIdx.x, gridDim.x);
+    const int nt = t / p.mtiles, m0 = (t - nt * p.mtiles) * 16 * FM;
+    const int steps = (p.kb + kWideGroups - 1) / kWideGroups;
+    const bool fetches = wave >= 2 * kWideGroups;
+    const int kq = fetches ? wave - 2 * kWideGroups : wave >> 1;
+    const int b0 = (int)((long)p.kb * kq / kWideGroups), b1 = (int)((long)p.kb * (kq + 1) / kWideGroups);
+    char *const ring = (char *)red + kq * 2 * kWideX;
+
+    if (fetches) {
+        const RowFetch<FM, NHWC> rows(p, m0, lane);
+        rows.issue(p, b0, ring);
+        for (int i = 0; i < steps; ++i) {
+            // block i is whole; behind the barrier all waves are done with block i - 1
+            wait_vm_lds<0>();
+            ring_barrier();
+            rows.issue(p, min(b0 + i + 1, b1 - 1), ring + ((i + 1) & 1) * kWideX);   // (past the range: its last again)
+        }
+        wait_vm_lds<0>();
+        ring_barrier();
+        __syncthreads();
+        return;
+    }
+
+    struct Weights {
+        u4v lo;
+        uint2 hi;
+        uint32_t s[2 * SG];
+    };
+    const int ng = wave & 1, kg = lane >> 4, nb = nt * 4 + ng * NB;
+    const char *wbase[NB];
+#pragma unroll
+    for (int n = 0; n < NB; ++n) wbase[n] = (const char *)p.w + (size_t)min(nb + n, p.nb16 - 1) * p.kb * BLOCK;
+    auto load = [&](int b, Weights *v) {
+#pragma unroll
+        for (int n = 0; n < NB; ++n) {
+            const char *w = wbase[n] + (size_t)b * BLOCK;
+            v[n].lo = *(const u4v *)(w + 16u * (uint32_t)lane);
+            v[n].hi = *(const uint2 *)(w + 1024u + 8u * (uint32_t)lane);
+            __builtin_memcpy(v[n].s, w + 1536u + (uint32_t)(8 * SG * kg), 8 * SG);
+        }
+    };
+    int xoff[4];
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+        xoff[s] = NHWC ? (lane & 15) * 256 + ((s * 4 + kg) ^ (lane & 15)) * 16 : ((s * 4 + kg) * 16 * FM + (lane & 15)) * 16;
+    f4 acc[NB][FM];
+#pragma unroll
+    for (int n = 0; n < NB; ++n)
+#pragma unroll
+        for (int j = 0; j < FM; ++j) acc[n][j] = f4{0.f, 0.f, 0.f, 0.f};
+    auto compute = [&](const char *st, const Frags *w, const uint32_t (*sc)[2 * SG]) {
+        h8 x[2][FM];
+        auto read = [&](int s) {
+#pragma unroll
+            for (int j = 0; j < FM; ++j) x[s & 1][j] = *(const h8 *)(st + xoff[s] + j * (NHWC ? 4096 : 256));
+        };
+        read(0);
+        f4 g[NB][FM];
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            if (s < 3) read(s + 1);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int n = 0; n < NB; ++n)
+#pragma unroll
+                for (int j = 0; j < FM; ++j)
+                    g[n][j] = E::mma(w[n].a[s], x[s & 1][j], s % GS == 0 ? f4{0.f, 0.f, 0.f, 0.f} : g[n][j]);
+            if (s % GS != GS - 1) continue;
+#pragma unroll
+            for (int n = 0; n < NB; ++n)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    const float f = scale_of<E>(sc[n], c * SG + s / GS);
+#pragma unroll
+                    for (int j = 0; j < FM; ++j) acc[n][j][c] = fmaf(f, g[n][j][c], acc[n][j][c]);
+                }
+        }
+    };
+    Weights next[NB];
+    load(b0, next);
+    for (int i = 0; i < steps; ++i) {
+        Frags w[NB];
+        uint32_t sc[NB][2 * SG];
+#pragma unroll
+        for (int n = 0; n < NB; ++n) {
+            const u4v lo = next[n].lo;
+            w[n] = six_bit<E>(u6v{lo[0], lo[1], lo[2], lo[3], next[n].hi.x, next[n].hi.y});
+            __builtin_memcpy(sc[n], next[n].s, 8 * SG);
+        }
+        wait_lds();                     // (this wave's reads of the block before)
+        ring_barrier();
+        load(min(b0 + i + 1, b1 - 1), next);
+        if (b0 + i < b1) compute(ring + (i & 1) * kWideX, w, sc);
+    }
+    wait_lds();
+    ring_barrier();
+    // the groups' sums, in a fixed order
+#pragma unroll
+    for (int n = 0; n < NB; ++n)
+#pragma unroll
+        for (int j = 0; j < FM; ++j) red[((wave * NB + n) * FM + j) * 64 + lane] = acc[n][j];
+    __syncthreads();
+    // wave w stores row tile w % 4 of channel blocks w / 4 and 2 + w / 4
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        const int n = u * 2 + (wave >> 2), j = wave & 3;    // (block n is wave n / 2's n % 2)
+        f4 v = red[(n * FM + j) * 64 + lane];
+#pragma unroll
+        for (int q = 1; q < kWideGroups; ++q) v += red[((q * 4 + n) * FM + j) * 64 + lane];
+        store_tile(p, v, nt * 4 + n, m0 + j * 16, lane);
+    }
+}
+
+template <typename E, int GS, bool NHWC>
+hipError_t launch_wide(const FcInt4Params &p, hipStream_t st) {
+    static_assert(kWideLds >= 2 * kWideGroups * 2 * 4 * 1024, "the groups' sums fit into the ring");
+    const dim3 grid((unsigned)p.mtiles * ((p.nb16 + 3) / 4)), block(64 * 3 * kWideGroups);
+    launch(fcint4_wide_kernel<E, GS, NHWC>, grid, block, kWideLds, st, p);
+    return hipGetLastError();
+}
+
 template <typename E, int GS, typename T>
 hipError_t launch_stream(const FcInt4Params &p, const FcInt4Geom &g, hipStream_t st) {
     const dim3 grid((unsigned)p.mtiles * p.nb16), block(64 * g.waves);
@@ -519,7 +675,11 @@ hipError_t launch_e(const FcInt4Params &p, const FcInt4Geom &g, hipStream_t st) 
     if (g.fm == 1 && g.waves == 2) return launch_mode<E, 1, 2, GS>(p, g, st);
     if (g.fm == 1 && g.waves == 4) return launch_mode<E, 1, 4, GS>(p, g, st);
     if (g.fm == 2 && g.waves == 2) return launch_mode<E, 2, 2, GS>(p, g, st);
-    if (g.fm == 4 && g.waves == 4) return launch_mode<E, 4, 4, GS>(p, g, st);
+    if (g.six_bit()) {
+        if (p.xin) return hipErrorInvalidValue;
+        if (p.xp == 1) return launch_wide<E, GS, false>(p, st);
+        if constexpr (!E::bf) return launch_wide<E, GS, true>(p, st);
+    }
     return hipErrorInvalidValue;
 }
 
@@ -532,9 +692,8 @@ hipError_t launch_e(const FcInt4Params &p, const FcInt4Geom &g, hipStream_t st) 
 // streaming 5.8; 16 x 8192 x 8192 10.3 and 13.4), or, for more than 16384
 // channels, of 64 with two (1 x 4096 x 32000 bf16 18.0 us, 19.8).
 // More: tiles of 64 rows x 64 channels where they give every compute unit one
-// and K is long enough to be worth the fetching wave's start (256 x 4096 x 4096
-// bf16 17.1 us, 32 x 32 tiles 20.4), else of 32 x 32 (45 x 283 x 12291 5.6 us,
-// large ones 6.5; 64 x 1024 x 1000 4.7).
+// and each group two blocks of K (256 x 4096 x 4096 bf16 16.2 us, 32 x 32 tiles
+// 20.4), else of 32 x 32 (64 x 1024 x 1000 4.7 us).
 FcInt4Geom fcint4_geom(int M, int nb16, int kb, int group) {
     FcInt4Geom g{};
     g.gs = group % 128 == 0 ? 4 : group % 64 == 0 ? 2 : 1;
@@ -549,8 +708,8 @@ FcInt4Geom fcint4_geom(int M, int nb16, int kb, int group) {
     } else {
         const bool large = (size_t)((M + 63) / 64) * ((nb16 + 3) / 4) >= 256 && kb >= 8;
         g.fm = large ? 4 : 2;
-        g.waves = large ? 4 : 2;
-        g.kgroups = kb >= 8 ? 2 : 1;
+        g.waves = 2;
+        g.kgroups = large ? kWideGroups : kb >= 8 ? 2 : 1;
     }
     return g;
 }

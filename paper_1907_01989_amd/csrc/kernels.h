@@ -133,8 +133,13 @@ struct FcInt4Params {
 // The streaming kernel (kgroups 0): `waves` waves share K.  The tile kernel:
 // `waves` waves of 16 channels to a group, kgroups groups share K, 16 * fm rows.
 // gs: MFMA steps per scale.
+// Bytes of a block of 16 output channels x 128 inputs: a wave's codes, then the
+// scales and zero points [16 channels][4 / gs].
+constexpr int fcint4_block_bytes(int gs, bool zp) { return 1024 + (zp ? 48 : 32) * (4 / gs); }
 struct FcInt4Geom {
     int fm, waves, kgroups, gs;
+    bool six_bit() const { return fm == 4; }     // codes less zero points as 6-bit floats
+    int block_bytes(bool zp) const { return six_bit() ? 1536 + 32 * (4 / gs) : fcint4_block_bytes(gs, zp); }
     bool reads_raw(int cin) const { return fm == 1 && cin >= 8; }   // takes xin
 };
 FcInt4Geom fcint4_geom(int M, int nb16, int kb, int group);

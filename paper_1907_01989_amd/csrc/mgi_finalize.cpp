@@ -1655,7 +1655,11 @@ void plan_memory(mgi_plan &p, const mgi_options &o) {
 // MFMA A operand: word s of lane l holds channel l % 16's inputs 32 s + 8
 // (l / 16) .. + 7, input 2i at bits 4i and input 2i + 1 at bits 16 + 4i, so that
 // a shift and a mask give a pair of 16-bit values.  Its scales, then its zero
-// points, follow: [16 channels][scales per block].  Inputs past the last take their group's zero point: weight 0.
+// points, follow: [16 channels][scales per block].  Inputs past the last take
+// their group's zero point: weight 0.  For the kernel of many rows a code is its
+// difference from the zero point, sign and magnitude in six bits (see there):
+// 192 bits to a lane, its 32 inputs in order, the first 128 of all lanes and
+// then the other 64; no zero points follow.
 // Scales are divided by a power of two per output channel that brings the
 // channel's largest near 1 and are then rounded to the storage type (half a
 // unit in the last place, 2^-11 in fp16 and 2^-9 in bf16): in fp16 a scale below
@@ -1663,8 +1667,9 @@ void plan_memory(mgi_plan &p, const mgi_options &o) {
 template <typename Reserve, typename Bits>
 void pack_fc_int4(const GOp &op, int cin, Node &nd, std::vector<uint8_t> &blob, Reserve reserve, Bits to_bits) {
     const int cout = op.cout, kb = nd.ksp, gs = nd.fq_geo.gs, per = 4 / gs, groups = (cin + op.group - 1) / op.group;
-    nd.zeros = !op.zeros.empty();
-    const size_t row_bytes = ((size_t)cin + 1) / 2, block = 1024 + (nd.zeros ? 48 : 32) * (size_t)per;
+    const bool six = nd.fq_geo.six_bit();
+    nd.zeros = !op.zeros.empty() && !six;
+    const size_t row_bytes = ((size_t)cin + 1) / 2, block = (size_t)nd.fq_geo.block_bytes(nd.zeros);
     nd.w_bytes = (size_t)nd.nb16 * kb * block;
     nd.w_off = reserve(nd.w_bytes);
     nd.e_off = reserve((size_t)nd.nb16 * 16 * 4);
@@ -1673,17 +1678,21 @@ void pack_fc_int4(const GOp &op, int cin, Node &nd, std::vector<uint8_t> &blob, 
     uint8_t *wp = blob.data() + nd.w_off;
     float *ep = reinterpret_cast<float *>(blob.data() + nd.e_off);
     float *bp = reinterpret_cast<float *>(blob.data() + nd.b_off);
-    std::vector<uint8_t> code((size_t)kb * 128);
+    const size_t codes_bytes = six ? 1536 : 1024;
+    std::vector<uint8_t> code((size_t)kb * 128), zero((size_t)kb * 4);   // zero: of 32 inputs
     for (int co = 0; co < nd.nb16 * 16; ++co) {
         const int nb = co / 16, row = co % 16;
         if (co >= cout) {   // channels past the last: weight 0 (never stored, but in range)
             std::fill(code.begin(), code.end(), 8);
+            std::fill(zero.begin(), zero.end(), 8);
         } else {
             const uint8_t *src = op.codes.data() + (size_t)co * row_bytes;
             const float *sc = op.w.data() + (size_t)co * groups;
             for (int i = 0; i < cin; ++i) code[i] = (src[i >> 1] >> (i & 1 ? 4 : 0)) & 15;
             const uint8_t last = op.zeros.empty() ? 8 : op.zeros[(size_t)co * groups + groups - 1];
             std::fill(code.begin() + cin, code.end(), last);
+            for (int i = 0; i < kb * 4; ++i)
+                zero[i] = op.zeros.empty() ? 8 : op.zeros[(size_t)co * groups + std::min(i * 32 / op.group, groups - 1)];
             float top = 0.0f;
             for (int gi = 0; gi < groups; ++gi) top = std::max(top, std::fabs(sc[gi]));
             // (exponents as far as both powers of two stay normal numbers)
@@ -1694,13 +1703,26 @@ void pack_fc_int4(const GOp &op, int cin, Node &nd, std::vector<uint8_t> &blob, 
             for (int b = 0; b < kb; ++b)
                 for (int q = 0; q < per; ++q) {
                     const int gi = std::min((b * 128 + q * gs * 32) / op.group, groups - 1);
-                    uint8_t *at = wp + ((size_t)nb * kb + b) * block + 1024;
+                    uint8_t *at = wp + ((size_t)nb * kb + b) * block + codes_bytes;
                     const uint16_t bits = to_bits(std::ldexp(sc[gi], -e));
                     std::memcpy(at + 2 * (row * per + q), &bits, 2);
                     if (nd.zeros) at[32 * per + row * per + q] = op.zeros[(size_t)co * groups + gi];
                 }
         }
-        for (int b = 0; b < kb; ++b)
+        for (int b = 0; six && b < kb; ++b)
+            for (int q = 0; q < 4; ++q) {
+                uint32_t v[6] = {};
+                for (int i = 0; i < 32; ++i) {
+                    const int s = i / 8, d = (int)code[(size_t)b * 128 + s * 32 + q * 8 + i % 8] - zero[(size_t)b * 4 + s];
+                    const uint64_t bits = (uint64_t)(d < 0 ? 32 - d : d) << (6 * i % 32);
+                    v[6 * i / 32] |= (uint32_t)bits;
+                    if (bits >> 32) v[6 * i / 32 + 1] |= (uint32_t)(bits >> 32);
+                }
+                uint8_t *at = wp + ((size_t)nb * kb + b) * block;
+                std::memcpy(at + (q * 16 + row) * 16, v, 16);
+                std::memcpy(at + 1024 + (q * 16 + row) * 8, v + 4, 8);
+            }
+        for (int b = 0; !six && b < kb; ++b)
             for (int s = 0; s < 4; ++s)
                 for (int q = 0; q < 4; ++q) {
                     const uint8_t *c = code.data() + (size_t)b * 128 + s * 32 + q * 8;

@@ -247,3 +247,22 @@ def test_rows_read_as_they_are(n, cin, cout, src, dtype):
     w = torch.as_tensor((codes.astype(np.float64) - op["zeros"][:, -1]) * op["scales"][:, -1], device=x.device)
     row = last[n - 1].reshape(-1).double()
     assert torch.isnan(row[w == 0]).all() and torch.equal(row[w != 0], torch.sign(w[w != 0]) * float("inf"))
+
+
+@pytest.mark.parametrize("src,dtype", [(DTYPE_FP16, 0), (DTYPE_FP32, 0), (DTYPE_FP32, 1)])
+@pytest.mark.parametrize("n,cin,cout,group,zeros", [(1000, 1030, 1030, 64, True), (1030, 1024, 1000, 128, False),
+                                                    (2050, 1288, 500, 96, True), (70, 1152, 8200, 32, False),
+                                                    (321, 2000, 3000, 256, True)])
+def test_many_rows(n, cin, cout, group, zeros, src, dtype):
+    import torch
+    from paper_1907_01989_amd import engine
+    desc, t = layer(n, cin, cout, group, zeros, dtype=src, seed=5)
+    if dtype == 1:
+        desc = workloads.as_bf16_graph(desc)
+    log(f"[case] {desc['name']} inputs {src}, storage type {dtype}")
+    plan = engine.Plan(desc, dtype=dtype)
+    xs = plan.input_tensors()
+    got = plan.run(xs)[0].clone()
+    check(desc, t, got.cpu().numpy())
+    for _ in range(3):
+        assert torch.equal(plan.run(xs)[0], got)
