@@ -508,8 +508,8 @@ __device__ __forceinline__ Frags six_bit(u6v w) {
 // reads, go to registers, a block ahead.  Taking 4-bit codes apart would take
 // longer than the products, so the layer is kept as 6-bit differences for this
 // kernel (256 x 4096 x 4096 bf16 19.5 us with 16 channels to a wave, 18.3 with 32,
-16.2 so).  What bounds it is the traffic between L2 and LDS: 0.7 MB to a compute
-unit there.
+// 16.2 so).  What bounds it is the traffic from the L2 caches: 0.7 MB to a compute
+// unit there.
 constexpr int kWideGroups = 4, kWideX = 64 * 256, kWideLds = kWideGroups * 2 * kWideX;
 template <typename E, int GS, bool NHWC>
 __global__ __launch_bounds__(768) void fcint4_wide_kernel(FcInt4Params p) {
