@@ -157,9 +157,9 @@ struct Held {
     }
 };
 
-// Adds the values of at least `th` to the candidates.  A lane marks its own and
-// then takes them one after the other, reading them again from memory (the
-// cache): few lanes have more than two or three, but among a wave's lanes
+// Adds the values of at least `th` to the candidates.  Of many a lane marks its
+// own and then takes them one after the other, reading them again from memory
+// (the cache): few lanes have more than two or three, but among a wave's lanes
 // nearly every register has one.
 template <int W, typename T, typename H>
 __device__ __forceinline__ void push(Shared<W> &sh, const H &h, const T *x, float th) {
@@ -172,6 +172,15 @@ __device__ __forceinline__ void push(Shared<W> &sh, const H &h, const T *x, floa
     for (uint32_t m : mark) n += __popc(m);
     int slot = take_slots(&sh.n, n);
     if (slot < 0) return;
+    if constexpr (PER <= 8) {
+#pragma unroll
+        for (int q = 0; q < PER; ++q)
+            if (mark[0] >> q & 1) {
+                if (slot < kCap) sh.cand[slot] = key_of(h.v[q], h.at(q / H::VEC) + q % H::VEC);
+                ++slot;
+            }
+        return;
+    }
 #pragma unroll
     for (int w = 0; w < (PER + 31) / 32; ++w)
 #pragma unroll 1
@@ -293,7 +302,7 @@ template <typename T, int NT, int PER, bool MORE>
 __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(PER == 64 ? 4 : 1))) void answers_kernel(AnswersParams p, int segs, int rounds, int seglen) {
     constexpr int W = NT / 64;
     __shared__ Shared<W> sh;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int row = blockIdx.x / segs, seg = blockIdx.x - row * segs;
     const T *x = (const T *)p.x + (size_t)row * p.cols;
     // channels of the lists, their values next, both long before they are used
@@ -312,19 +321,21 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(PER == 64 ? 
     float m = -FLT_MAX, s = 0.0f, t = 0.0f;    // (rows of -inf only: s = 0)
     int k = 0;                                 // keys in sh.best
     for (int round = 0;;) {
-        // The k-th largest value is at least the smallest of the waves' r-th
-        // largest lane maxima, r = ceil(k / waves): few values pass it.  (Waves
-        // past the end of a short row hold nothing and do not count.)  Of a
+        // Where at least k lanes hold values, the k-th largest is at least the
+        // smallest of the waves' r-th largest lane maxima, each wave with its
+        // share r of k by its lanes that hold some: few values pass it.  Of a
         // later stretch of the row only what reaches the k-th so far does.
-        const int len = hi - lo, kc = min(p.k, len), held = min(W, (len + 64 * h.VEC - 1) / (64 * h.VEC));
+        const int len = hi - lo, kc = min(p.k, len);
+        const int vecs = min(NT, (len + h.VEC - 1) / h.VEC), lanes = min(64, max(0, vecs - wave * 64));
+        const int r = kc <= vecs ? (kc * lanes + vecs - 1) / vecs : 0;
         float mx = -INFINITY;
 #pragma unroll
         for (int q = 0; q < PER; ++q) mx = fmaxf(mx, h.v[q]);
         const float wm = wave_max(mx);
-        float bound = wave_rth(mx, -INFINITY, (kc + held - 1) / held, [](float a, float b) { return fmaxf(a, b); });
+        float bound = wave_rth(mx, -INFINITY, r, [](float a, float b) { return fmaxf(a, b); });
         if (lane == 0) {
             sh.m[wave] = wm;
-            sh.bound[wave] = wave < held ? bound : INFINITY;
+            sh.bound[wave] = lanes > 0 ? bound : INFINITY;
         }
         __syncthreads();
         if (round == 0) {
