@@ -401,7 +401,8 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(PER == 64 ? 
         clear(sh);
     }
     if (segs > 1) {
-        for (int r = tid; r < p.k; r += NT) put(p.part_keys + ((size_t)row * segs + seg) * p.k + r, r < k ? sh.best[r] : 0ull);
+        const int stride = answers_stride(p.k);
+        for (int r = tid; r < stride; r += NT) put(p.part_keys + ((size_t)row * segs + seg) * stride + r, r < k ? sh.best[r] : 0ull);
         float *st = p.part_stats + (size_t)row * segs * 4;
         if (tid == 0) {
             put((unsigned long long *)(st + 4 * seg), (unsigned long long)__float_as_uint(s) << 32 | __float_as_uint(m));
@@ -409,26 +410,29 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(PER == 64 ? 
         }
         if (!arrive_last(p.cnt + row, segs, &sh.last)) return;
         constexpr int C = kCap / NT;
-        const int n = segs * p.k;
+        const int n = segs * stride;
         unsigned long long key[C];
         // (a segment to a lane: there are at most 64)
         f4 found = *(const f4 *)(st + 4 * min(lane, segs - 1));
         if (lane >= segs) found = f4{-FLT_MAX, 0.0f, 0.0f, 0.0f};
         if (p.k > 0) {
-            // as above: a bound from the lanes' largest, of the waves that
-            // hold keys; then what reaches it
+            // as above: a bound from the lanes' largest, then what reaches it.
+            // Waves take eight keys in turn, so that each has some of the first
+            // and some of the last of the segments' (33 x 49999, k = 50: 268
+            // candidates if each took one stretch, 141 so).
+            const int at = ((lane >> 3) * W + wave) * 8 + (lane & 7);
             uint32_t top = 0;
 #pragma unroll
-            for (int c = 0; c < C; ++c) key[c] = p.part_keys[(size_t)row * n + min(c * NT + tid, n - 1)];
+            for (int c = 0; c < C; ++c) key[c] = p.part_keys[(size_t)row * n + min(c * NT + at, n - 1)];
             clear(sh);
 #pragma unroll
             for (int c = 0; c < C; ++c) {
-                if (c * NT + tid >= n) key[c] = 0;
+                if (c * NT + at >= n) key[c] = 0;
                 top = max(top, (uint32_t)(key[c] >> 32));
             }
-            const int have = min(W, (n + 63) / 64);
-            const uint32_t bound = wave_rth(top, 0u, (p.k + have - 1) / have, [](uint32_t a, uint32_t b) { return max(a, b); });
-            if (lane == 0) sh.key_bound[wave] = wave < have ? bound : 0xFFFFFFFFu;
+            const int all = min(n, NT), units = all / 8, lanes = 8 * (units / W + (wave < units % W ? 1 : 0));
+            const uint32_t bound = wave_rth(top, 0u, (p.k * lanes + all - 1) / all, [](uint32_t a, uint32_t b) { return max(a, b); });
+            if (lane == 0) sh.key_bound[wave] = lanes > 0 ? bound : 0xFFFFFFFFu;
         }
         if (stats) {
             m = wave_max(found[0]);
@@ -484,7 +488,7 @@ hipError_t launch_t(const AnswersParams &p, const AnswersGeom &g, hipStream_t st
         return hipGetLastError();                                                                       \
     }
     MGI_ANSWERS(64, 8, false) MGI_ANSWERS(256, 8, false) MGI_ANSWERS(256, 16, false) MGI_ANSWERS(256, 32, false)
-    MGI_ANSWERS(512, 32, false) MGI_ANSWERS(512, 64, false) MGI_ANSWERS(512, 64, true)
+    MGI_ANSWERS(512, 16, false) MGI_ANSWERS(512, 32, false) MGI_ANSWERS(512, 64, false) MGI_ANSWERS(512, 64, true)
 #undef MGI_ANSWERS
     return hipErrorInvalidValue;
 }
@@ -494,10 +498,12 @@ hipError_t launch_t(const AnswersParams &p, const AnswersGeom &g, hipStream_t st
 // Segments: more than one where rows alone would leave compute units idle, none
 // shorter than 2048 columns, and no more than the last workgroup can rank.  A
 // workgroup takes its segment in as many rounds as its registers make
-// necessary (668 x 68012, k = 20: three segments with a join 128 us).
+// necessary (668 x 68012, k = 20: 64 us; as three segments with a join 128).  The
+// more there is to rank, the more a workgroup's waves help (33 x 49999 fp16, k =
+// 50: eight waves save 1.8 of 18.2 us; 23 x 69767, k = 3: they cost 2.7 on 12.4).
 AnswersGeom answers_geom(int rows, int cols, int k) {
     AnswersGeom g{};
-    const int most = k > 0 ? std::min(kCap / k, 64) : 64;
+    const int most = k > 0 ? std::min(kCap / answers_stride(k), 64) : 64;
     g.segs = std::max(1, std::min({256 / std::max(rows, 1), (cols + 2047) / 2048, most}));
     const int len = (cols + g.segs - 1) / g.segs;
     g.rounds = (len + 32767) / 32768;
@@ -509,6 +515,10 @@ AnswersGeom answers_geom(int rows, int cols, int k) {
         g.per = s[1];
         if (g.nt * g.per >= g.seglen) break;
     }
+    if (g.nt == 256 && g.per == 32 && k > 16) {
+        g.nt = 512;
+        g.per = 16;
+    }
     return g;
 }
 
@@ -517,7 +527,7 @@ hipError_t launch_answers(const AnswersParams &p, const AnswersGeom &g, hipStrea
     const long len = (long)g.rounds * g.seglen;
     if (g.segs < 1 || g.rounds < 1 || (long)g.nt * g.per < g.seglen || g.segs * len < p.cols || (g.segs - 1) * len >= p.cols ||
         (g.rounds > 1 && g.seglen < kMaxTopK) ||
-        g.segs > 64 || (long)g.segs * p.k > kCap || p.k > kMaxTopK || (g.segs > 1 && (!p.cnt || !p.part_stats)) ||
+        g.segs > 64 || (long)g.segs * answers_stride(p.k) > kCap || p.k > kMaxTopK || (g.segs > 1 && (!p.cnt || !p.part_stats)) ||
         (size_t)p.rows * g.segs > 0x7fffffffu)
         return hipErrorInvalidValue;
     AnswersParams q = p;

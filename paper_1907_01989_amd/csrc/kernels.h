@@ -161,15 +161,20 @@ struct AnswersParams {
     int list_given[kAnswerLists];    // list_n where there is a list, else 0 (set by the launcher)
     // rows split into segments: what each found, and arrival counters per row
     // (zero before and after)
-    unsigned long long *part_keys;   // [row][segment][k]
+    unsigned long long *part_keys;   // [row][segment][answers_stride(k)], on a 64-byte boundary
     float *part_stats;               // [row][segment][4]: max, sum, weighted sum
     int *cnt;
 };
+// Keys of a segment, in whole 64-byte units: no two workgroups write into one.
+constexpr int answers_stride(int k) { return (k + 7) / 8 * 8; }
 // threads per workgroup, values per thread, segments per row (workgroups), and
 // the stretches of seglen columns that each takes one after the other
 struct AnswersGeom {
     int nt, per, segs, rounds, seglen;
-    size_t part_bytes(int rows, int k) const { return segs > 1 ? (size_t)rows * segs * (8 * k + 16) : 0; }
+    size_t stats_bytes(int rows) const { return ((size_t)rows * segs * 16 + 63) / 64 * 64; }
+    size_t part_bytes(int rows, int k) const {
+        return segs > 1 ? stats_bytes(rows) + (size_t)rows * segs * answers_stride(k) * 8 : 0;
+    }
 };
 AnswersGeom answers_geom(int rows, int cols, int k);
 hipError_t launch_answers(const AnswersParams &p, const AnswersGeom &g, hipStream_t st);

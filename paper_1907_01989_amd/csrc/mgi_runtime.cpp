@@ -483,7 +483,7 @@ hipError_t launch_answers_node(const mgi_plan &p, const Node &nd, const Bases &B
     if (nd.cnt_bytes) {
         char *part = (char *)buf_ptr(p, nd.scratch, B);
         q.part_stats = (float *)part;
-        q.part_keys = (unsigned long long *)(part + (size_t)q.rows * nd.an_geo.segs * 16);
+        q.part_keys = (unsigned long long *)(part + nd.an_geo.stats_bytes(q.rows));
         q.cnt = (int *)(B.ws + nd.cnt_off);
     }
     return launch_answers(q, nd.an_geo, st);
