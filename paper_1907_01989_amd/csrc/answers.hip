@@ -299,7 +299,7 @@ __device__ __noinline__ void push_exact(Shared<NT / 64> &sh, const T *x, int lo,
 }
 
 template <typename T, int NT, int PER, bool MORE>
-__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(PER == 64 ? 4 : 1))) void answers_kernel(AnswersParams p, int segs, int rounds, int seglen) {
+__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(PER == 64 ? 4 : MORE ? 6 : 1))) void answers_kernel(AnswersParams p, int segs, int rounds, int seglen) {
     constexpr int W = NT / 64;
     __shared__ Shared<W> sh;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -488,7 +488,7 @@ hipError_t launch_t(const AnswersParams &p, const AnswersGeom &g, hipStream_t st
         return hipGetLastError();                                                                       \
     }
     MGI_ANSWERS(64, 8, false) MGI_ANSWERS(256, 8, false) MGI_ANSWERS(256, 16, false) MGI_ANSWERS(256, 32, false)
-    MGI_ANSWERS(512, 16, false) MGI_ANSWERS(512, 32, false) MGI_ANSWERS(512, 64, false) MGI_ANSWERS(512, 64, true)
+    MGI_ANSWERS(512, 16, false) MGI_ANSWERS(512, 32, false) MGI_ANSWERS(512, 64, false) MGI_ANSWERS(512, 32, true)
 #undef MGI_ANSWERS
     return hipErrorInvalidValue;
 }
@@ -497,16 +497,19 @@ hipError_t launch_t(const AnswersParams &p, const AnswersGeom &g, hipStream_t st
 
 // Segments: more than one where rows alone would leave compute units idle, none
 // shorter than 2048 columns, and no more than the last workgroup can rank.  A
-// workgroup takes its segment in as many rounds as its registers make
-// necessary (668 x 68012, k = 20: 64 us; as three segments with a join 128).  The
-// more there is to rank, the more a workgroup's waves help (33 x 49999 fp16, k =
-// 50: eight waves save 1.8 of 18.2 us; 23 x 69767, k = 3: they cost 2.7 on 12.4).
+// workgroup takes a segment that its registers cannot hold in rounds (668 x
+// 68012, k = 20: 50 us; as three segments with a join 128), of half of what they
+// could hold: three workgroups to a compute unit then read while others compute
+// (3269 x 38521, k = 5: 126 us; two with rounds of twice the length 157, four,
+// whose registers spill, 142).  The more there is to rank, the more waves help
+// (33 x 49999 fp16, k = 50: eight save 1.8 of 18.2 us; 23 x 69767, k = 3: they
+// cost 2.7 on 12.4).
 AnswersGeom answers_geom(int rows, int cols, int k) {
     AnswersGeom g{};
     const int most = k > 0 ? std::min(kCap / answers_stride(k), 64) : 64;
     g.segs = std::max(1, std::min({256 / std::max(rows, 1), (cols + 2047) / 2048, most}));
     const int len = (cols + g.segs - 1) / g.segs;
-    g.rounds = (len + 32767) / 32768;
+    g.rounds = len <= 32768 ? 1 : (len + 16383) / 16384;
     g.seglen = ((len + g.rounds - 1) / g.rounds + 7) / 8 * 8;
     g.segs = (cols + g.rounds * g.seglen - 1) / (g.rounds * g.seglen);
     const int sizes[6][2] = {{64, 8}, {256, 8}, {256, 16}, {256, 32}, {512, 32}, {512, 64}};
