@@ -163,6 +163,7 @@ class Plan:
         self.workspace_bytes = B.mgi_plan_workspace_bytes(self.handle)
         self.weight_bytes = B.mgi_plan_weight_bytes(self.handle)
         self.bound = False
+        self._io = None            # what _io_ok compares with
         if bind:
             self.bind()
 
@@ -222,17 +223,21 @@ class Plan:
     def _io_ok(self, inputs, outputs):
         """The conditions of check_io, as quickly as Python allows (a run of
         two kernels takes about 8 us in the library)."""
-        import torch
         if len(inputs) != self.n_inputs or len(outputs) != self.n_outputs:
             return False
-        dev = torch.device(self.device).index
+        if self._io is None:
+            import torch
+            types = _torch_types()
+            self._io = (torch.Tensor, torch.device(self.device).index, torch.cuda.current_device,
+                        [(types[dt], nbytes) for _, dt, nbytes in self.inputs_info],
+                        [(types[dt], nbytes) for _, dt, nbytes in self.outputs_info])
+        tensor, dev, current, need_in, need_out = self._io
         if dev is None:
-            dev = torch.cuda.current_device()
-        types = _torch_types()
-        for ts, info in ((inputs, self.inputs_info), (outputs, self.outputs_info)):
-            for x, (_, dt, nbytes) in zip(ts, info):
-                if not (isinstance(x, torch.Tensor) and x.is_cuda and x.get_device() == dev and
-                        x.dtype is types[dt] and x.is_contiguous() and x.nbytes == nbytes):
+            dev = current()
+        for ts, need in ((inputs, need_in), (outputs, need_out)):
+            for x, (dtype, nbytes) in zip(ts, need):
+                if not (isinstance(x, tensor) and x.is_cuda and x.get_device() == dev and
+                        x.dtype is dtype and x.is_contiguous() and x.nbytes == nbytes):
                     return False
         return True
 
