@@ -387,7 +387,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(PER == 64 ? 
                 n = kc;
             }
             if (MORE && k > 0) {                       // and the best so far
-                if (tid < k) sh.cand[n + tid] = sh.best[tid];
+                if (tid < k + 8) sh.cand[n + tid] = tid < k ? sh.best[tid] : 0;   // (push_exact leaves what it dropped)
                 n += k;
                 __syncthreads();
             }

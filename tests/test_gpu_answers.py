@@ -297,3 +297,16 @@ def test_writes_stay_inside_the_buffers():
     plan, outs, raw, ws, lead = guarded_plan(b.graph("fc"))
     plan.run(plan.input_tensors(), outs)
     check_guards(plan, raw, ws, lead, "fc_int4")
+
+
+@pytest.mark.parametrize("k", [1, 13, 41, 64])
+def test_crowds_in_a_later_stretch(k):
+    # rows that a workgroup reads in rounds: a later one holds more equal values,
+    # larger than all before them, than there is room for
+    x = np.random.default_rng(k).standard_normal((300, 70001)) * 0.1
+    x[:, 20000:50000] = 2.0
+    x[1, 40000:] = 3.0
+    x[2, 60000:60020] = 2.0
+    x[3:, 14008:] = 2.0                             # (from the second of five stretches on)
+    log(f"[case] crowds, k {k}")
+    ask(x, k)
