@@ -238,10 +238,13 @@ mgi_status mgi_graph_add_argmax(mgi_graph *g, int in, int *out);
  * and zeros: cout x ceil(cin / group) values, the last group may be shorter;
  * zeros: 0..15, NULL = 8 throughout; bias: cout floats, NULL = zeros.
  * group: a positive multiple of 32 (MGI_ERR_UNSUPPORTED otherwise), scales
- * finite.  Products of codes and activations are summed exactly as the 16-bit
- * layer sums them; scales are kept in the plan's 16-bit storage type, each
- * output channel's around a power of two of its own, so that none underflows
- * beside the channel's largest.  fp32 output (n, 1, 1, cout), like fc. */
+ * finite; n at most 2^24 (MGI_ERR_UNSUPPORTED).  Products of codes and
+ * activations are summed exactly as the 16-bit layer sums them; scales are kept
+ * in the plan's 16-bit storage type, each output channel's around a power of
+ * two of its own, so that none underflows beside the channel's largest.  A
+ * weight takes half a byte in the plan, and in plans of many images (64-row
+ * tiles enough for every compute unit) three quarters.  fp32 output
+ * (n, 1, 1, cout), like fc. */
 mgi_status mgi_graph_add_fc_int4(mgi_graph *g, int in, int cout, int group,
                                  const unsigned char *codes, const float *scales,
                                  const unsigned char *zeros, const float *bias, int *out);

@@ -133,6 +133,8 @@ struct FcInt4Params {
 // The streaming kernel (kgroups 0): `waves` waves share K.  The tile kernel:
 // `waves` waves of 16 channels to a group, kgroups groups share K, 16 * fm rows.
 // gs: MFMA steps per scale.
+// 32-bit offsets of a block of sixteen slices
+constexpr int kMaxFcInt4Rows = 1 << 24;
 // Bytes of a block of 16 output channels x 128 inputs: a wave's codes, then the
 // scales and zero points [16 channels][4 / gs].
 constexpr int fcint4_block_bytes(int gs, bool zp) { return 1024 + (zp ? 48 : 32) * (4 / gs); }

@@ -380,6 +380,8 @@ extern "C" mgi_status mgi_graph_add_fc_int4(mgi_graph *g, int in, int cout, int 
     const Shape x = g->ops[in].out;
     if (x.h != 1 || x.w != 1)
         return fail(MGI_ERR_UNSUPPORTED, std::string(who) + ": input must be 1x1 spatially");
+    if (x.n > kern::kMaxFcInt4Rows)
+        return fail(MGI_ERR_UNSUPPORTED, std::string(who) + ": at most " + std::to_string(kern::kMaxFcInt4Rows) + " images");
     const size_t groups = ((size_t)x.c + group - 1) / group, n = (size_t)cout * groups;
     for (size_t i = 0; i < n; ++i)
         if (!std::isfinite(scales[i])) return fail(MGI_ERR_INVALID_ARG, std::string(who) + ": scales must be finite");

@@ -56,6 +56,8 @@ def test_fc_int4_refusals(graph):
     assert "mgi_graph_add_fc_int4" in B.mgi_last_error()
     assert B.mgi_graph_add_fc_int4(g, x, 5, 32, q, s) == 3
     assert B.mgi_graph_add_fc_int4(g, x, 5, 64, q, np.ones((5, 1), np.float32), np.full((5, 1), 15, np.uint8)) == 4
+    many = B.mgi_graph_add_input(g, 2 ** 24 + 1, 1, 1, 40)
+    assert add(many, 5, 32, q, s) == 3                    # more images than offsets reach
 
 
 def test_fc_int4_array_sizes_are_checked_by_the_engine():
