@@ -88,6 +88,21 @@ __device__ __forceinline__ T wave_rth(T v, T none, int r, F join) {
     return top;
 }
 
+// A bound of at most the r-th largest of a wave's keys (order_of) and within
+// 2^-7 of it: the key's upper half, two bits at a time from counts of lanes.  As
+// long as five rounds of wave_rth, whatever r.
+__device__ __forceinline__ uint32_t wave_rth_near(uint32_t key, int r) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int b = 30; b >= 16; b -= 2) {
+        int n = 0;
+#pragma unroll
+        for (uint32_t q = 1; q < 4; ++q) n += __popcll(__ballot(key >= (top | q << b))) >= r;
+        top |= (uint32_t)n << b;
+    }
+    return top;
+}
+
 __device__ __forceinline__ int lanes_below(unsigned long long mask) {
     return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
 }
@@ -332,7 +347,13 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(PER == 64 ? 
 #pragma unroll
         for (int q = 0; q < PER; ++q) mx = fmaxf(mx, h.v[q]);
         const float wm = wave_max(mx);
-        float bound = wave_rth(mx, -INFINITY, r, [](float a, float b) { return fmaxf(a, b); });
+        float bound = -INFINITY;
+        if (r <= 5) {
+            bound = wave_rth(mx, -INFINITY, r, [](float a, float b) { return fmaxf(a, b); });
+        } else {
+            const uint32_t near = wave_rth_near(order_of(mx), r);
+            if (near >= order_of(-FLT_MAX)) bound = value_of(near);
+        }
         if (lane == 0) {
             sh.m[wave] = wm;
             sh.bound[wave] = lanes > 0 ? bound : INFINITY;
@@ -417,10 +438,10 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(PER == 64 ? 
         if (lane >= segs) found = f4{-FLT_MAX, 0.0f, 0.0f, 0.0f};
         if (p.k > 0) {
             // as above: a bound from the lanes' largest, then what reaches it.
-            // Waves take eight keys in turn, so that each has some of the first
+            // Waves take eight keys in turns that shift by one, so that each has some of the first
             // and some of the last of the segments' (33 x 49999, k = 50: 268
             // candidates if each took one stretch, 141 so).
-            const int at = ((lane >> 3) * W + wave) * 8 + (lane & 7);
+            const int at = ((lane >> 3) * W + ((wave + (lane >> 3)) & (W - 1))) * 8 + (lane & 7);
             uint32_t top = 0;
 #pragma unroll
             for (int c = 0; c < C; ++c) key[c] = p.part_keys[(size_t)row * n + min(c * NT + at, n - 1)];
@@ -430,8 +451,9 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(PER == 64 ? 
                 if (c * NT + at >= n) key[c] = 0;
                 top = max(top, (uint32_t)(key[c] >> 32));
             }
-            const int all = min(n, NT), units = all / 8, lanes = 8 * (units / W + (wave < units % W ? 1 : 0));
-            const uint32_t bound = wave_rth(top, 0u, (p.k * lanes + all - 1) / all, [](uint32_t a, uint32_t b) { return max(a, b); });
+            const int all = min(n, NT), units = all / 8, lanes = 8 * (units / W + (((wave + units / W) & (W - 1)) < units % W ? 1 : 0));
+            const int r = (p.k * lanes + all - 1) / all;
+            const uint32_t bound = r <= 5 ? wave_rth(top, 0u, r, [](uint32_t a, uint32_t b) { return max(a, b); }) : wave_rth_near(top, r);
             if (lane == 0) sh.key_bound[wave] = lanes > 0 ? bound : 0xFFFFFFFFu;
         }
         if (stats) {
