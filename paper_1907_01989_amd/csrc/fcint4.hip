@@ -706,10 +706,11 @@ FcInt4Geom fcint4_geom(int M, int nb16, int kb, int group) {
         g.waves = nb16 > 1024 ? 4 : 2;
         g.kgroups = std::max(1, std::min(nb16 > 1024 ? 2 : 4, kb / 2));
     } else {
-        const bool large = (size_t)((M + 63) / 64) * ((nb16 + 3) / 4) >= 256 && kb >= 8;
+        const bool large = M > 32 && (size_t)((M + 63) / 64) * ((nb16 + 3) / 4) >= 256 && kb >= 8;
         g.fm = large ? 4 : 2;
         g.waves = 2;
-        g.kgroups = large ? kWideGroups : kb >= 8 ? 2 : 1;
+        const bool few = (size_t)((M + 31) / 32) * ((nb16 + 1) / 2) <= 256;
+        g.kgroups = large ? kWideGroups : kb >= 16 && few ? 4 : kb >= 8 ? 2 : 1;
     }
     return g;
 }
