@@ -691,9 +691,11 @@ hipError_t launch_e(const FcInt4Params &p, const FcInt4Geom &g, hipStream_t st) 
 // else tiles of 32 channels with four groups along K (7 x 2001 x 5003 5.1 us,
 // streaming 5.8; 16 x 8192 x 8192 10.3 and 13.4), or, for more than 16384
 // channels, of 64 with two (1 x 4096 x 32000 bf16 18.0 us, 19.8).
-// More: tiles of 64 rows x 64 channels where they give every compute unit one
-// and each group two blocks of K (256 x 4096 x 4096 bf16 16.2 us, 32 x 32 tiles
-// 20.4), else of 32 x 32 (64 x 1024 x 1000 4.7 us).
+// More: tiles of 64 rows x 64 channels where half of them is used, every compute
+// unit gets one and each group two blocks of K (256 x 4096 x 4096 bf16 16.2 us,
+// 32 x 32 tiles 20.4; 256 x 1024 x 8192 13.0 and 21.0; but 25 x 3545 x 32821 bf16
+// 48.3 and 32.1), else of 32 x 32, with up to four groups along K where a compute
+// unit gets no second tile (64 x 4096 x 1000 7.8 us, two groups 9.4).
 FcInt4Geom fcint4_geom(int M, int nb16, int kb, int group) {
     FcInt4Geom g{};
     g.gs = group % 128 == 0 ? 4 : group % 64 == 0 ? 2 : 1;
