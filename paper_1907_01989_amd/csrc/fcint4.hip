@@ -685,10 +685,10 @@ hipError_t launch_e(const FcInt4Params &p, const FcInt4Geom &g, hipStream_t st) 
 
 }  // namespace
 
-// Up to 16 rows: the streaming kernel while each compute unit gets at most one
-// block of 16 channels (1 x 4096 x 4096 4.8 us, the tile kernel 6.0; 5 x 6816 x
-// 1424 6.8 and 10.0), with up to eight waves of at least two blocks of K each;
-// else tiles of 32 channels with four groups along K (7 x 2001 x 5003 5.1 us,
+// (Times are of inputs in the storage type.)  Up to 16 rows: the streaming kernel
+// while each compute unit gets at most one block of 16 channels (1 x 4096 x 4096
+// 4.8 us, the tile kernel 6.0; 5 x 6816 x 1424 6.8 and 10.0), with up to eight
+// waves of at least two blocks of K each; else tiles of 32 channels with four groups along K (7 x 2001 x 5003 5.1 us,
 // streaming 5.8; 16 x 8192 x 8192 10.3 and 13.4), or, for more than 16384
 // channels, of 64 with two (1 x 4096 x 32000 bf16 18.0 us, 19.8).
 // More: tiles of 64 rows x 64 channels where half of them is used, every compute
