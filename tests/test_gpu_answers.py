@@ -310,3 +310,46 @@ def test_crowds_in_a_later_stretch(k):
     x[3:, 14008:] = 2.0                             # (from the second of five stretches on)
     log(f"[case] crowds, k {k}")
     ask(x, k)
+
+
+def test_two_captured_heads_replayed_on_two_streams_and_tuned():
+    # plans of the same description share nothing but their inputs
+    import torch
+    from paper_1907_01989_amd import engine
+    b = NetBuilder(seed=11)
+    x = b.input(3, 1, 1, 203, -1, 1, dtype=DTYPE_FP32)
+    z = b.fc_int4(x, 30000, 96, True)
+    top = b.topk(z, 33)
+    for t in (top, b.log_prob(z, top), b.entropy(z)):
+        b.mark_output(t)
+    desc = b.graph("twice")
+    log("[case] two captured heads")
+    plans = [engine.Plan(desc) for _ in range(2)]
+    xs = plans[0].input_tensors()
+    want = [o.clone() for o in plans[0].run(xs)]
+    plans[1].autotune(xs)
+    outs = [p.capture(xs) for p in plans]
+    streams = [torch.cuda.Stream() for _ in plans]
+    torch.cuda.synchronize()
+    for rep in range(6):
+        for o in outs[0] + outs[1]:
+            o.fill_(-1)
+        torch.cuda.synchronize()
+        for p, s in zip(plans, streams):
+            p.replay(s)
+        torch.cuda.synchronize()
+        for got in outs:
+            assert all(torch.equal(a, w) for a, w in zip(got, want)), rep
+        assert torch.equal(plans[rep % 2].run(xs)[0], want[0])
+        torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("cols", [1, 3, 57, 64])
+def test_every_channel_is_asked_for(cols):
+    rng = np.random.default_rng(cols)
+    x = rng.standard_normal((70, cols))
+    x[3] = np.nan
+    x[5, cols // 2] = np.inf
+    x[7, : cols // 2] = -np.inf
+    log(f"[case] all {cols} channels")
+    ask(x, cols, rng.integers(-2, cols + 2, (70, 700)))
