@@ -1666,7 +1666,7 @@ void plan_memory(mgi_plan &p, const mgi_options &o) {
 // 6e-5 would lose bits, and one below 6e-8 vanish, without it.
 template <typename Reserve, typename Bits>
 void pack_fc_int4(const GOp &op, int cin, Node &nd, std::vector<uint8_t> &blob, Reserve reserve, Bits to_bits) {
-    const int cout = op.cout, kb = nd.ksp, gs = nd.fq_geo.gs, per = 4 / gs, groups = (cin + op.group - 1) / op.group;
+    const int cout = op.cout, kb = nd.ksp, gs = nd.fq_geo.gs, per = 4 / gs, groups = (cin - 1) / op.group + 1;
     const bool six = nd.fq_geo.six_bit();
     nd.zeros = !op.zeros.empty() && !six;
     const size_t row_bytes = ((size_t)cin + 1) / 2, block = (size_t)nd.fq_geo.block_bytes(nd.zeros);

@@ -266,3 +266,15 @@ def test_many_rows(n, cin, cout, group, zeros, src, dtype):
     check(desc, t, got.cpu().numpy())
     for _ in range(3):
         assert torch.equal(plan.run(xs)[0], got)
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+def test_a_group_far_longer_than_the_rows(dtype):
+    # one scale per channel, whatever multiple of 32 the group is
+    desc, t = layer(3, 100, 40, 128, True, seed=6)
+    if dtype == 1:
+        desc = workloads.as_bf16_graph(desc)
+    desc["ops"][1]["group"] = 2 ** 31 - 32
+    log(f"[case] group 2^31 - 32, storage type {dtype}")
+    _, outs, _ = run_gpu(desc, materialize_all=False, dtype=dtype)
+    check(desc, t, outs[0])

@@ -74,6 +74,21 @@ def test_fc_int4_array_sizes_are_checked_by_the_engine():
             engine.Plan(desc, bind=False)
 
 
+def one_group(group, cout=300):
+    b = NetBuilder()
+    x = b.input(2, 1, 1, 64, -1, 1)
+    t = b.fc_int4(x, cout, 64, zeros=True)
+    b.ops[t]["group"] = group
+    b.mark_output(t)
+    return b.graph(f"group_{group}"), t
+
+
+def test_a_group_may_be_far_longer_than_the_rows():
+    # (the number of groups is counted without adding to the largest int)
+    plans = [engine.Plan(one_group(g)[0], bind=False) for g in (96, 2 ** 31 - 32)]
+    assert plans[0].weight_bytes == plans[1].weight_bytes
+
+
 def test_question_refusals(graph):
     g, L = graph, B.lib()
     x = B.mgi_graph_add_input(g, 2, 1, 1, 100)
