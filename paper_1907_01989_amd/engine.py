@@ -52,6 +52,8 @@ def _channels(ops, t):
 def _add_fc_int4(g, ops, op):
     """The library receives raw pointers: arrays of other sizes are refused here."""
     cin, cout, group = _channels(ops, op["in"]), op["cout"], op["group"]
+    if not -2 ** 31 <= group < 2 ** 31:
+        raise ValueError(f"fc_int4: group {group} is no 32-bit int")
     groups = -(-cin // group) if group > 0 else 0
     for name, size in (("q", cout * ((cin + 1) // 2)), ("scales", cout * groups), ("zeros", cout * groups), ("b", cout)):
         a = op.get(name)

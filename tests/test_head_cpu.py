@@ -89,6 +89,13 @@ def test_a_group_may_be_far_longer_than_the_rows():
     assert plans[0].weight_bytes == plans[1].weight_bytes
 
 
+@pytest.mark.parametrize("group", [2 ** 32 + 32, 2 ** 32 + 64, -2 ** 32 + 64])
+def test_a_group_that_no_int_holds_is_refused(group):
+    # (as a C int these are groups of 32 and 64: other sizes than the arrays were checked for)
+    with pytest.raises(ValueError, match="group"):
+        engine.Plan(one_group(group)[0], bind=False)
+
+
 def test_question_refusals(graph):
     g, L = graph, B.lib()
     x = B.mgi_graph_add_input(g, 2, 1, 1, 100)
