@@ -50,10 +50,15 @@ def _channels(ops, t):
 
 
 def _add_fc_int4(g, ops, op):
-    """The library receives raw pointers: arrays of other sizes are refused here."""
-    cin, cout, group = _channels(ops, op["in"]), op["cout"], op["group"]
+    """The library receives raw pointers: arrays of other sizes are refused here.
+    ``ops``: the operators before this one (the library refuses other operands
+    before it reads an array)."""
+    cout, group = op["cout"], op["group"]
     if not -2 ** 31 <= group < 2 ** 31:
         raise ValueError(f"fc_int4: group {group} is no 32-bit int")
+    if not 0 <= op["in"] < len(ops):
+        return B.mgi_graph_add_fc_int4(g, op["in"], cout, group, op["q"], op["scales"], op.get("zeros"), op.get("b"))
+    cin = _channels(ops, op["in"])
     groups = -(-cin // group) if group > 0 else 0
     for name, size in (("q", cout * ((cin + 1) // 2)), ("scales", cout * groups), ("zeros", cout * groups), ("b", cout)):
         a = op.get(name)
@@ -105,7 +110,7 @@ def build_graph(desc):
             elif k == "argmax":
                 t = B.mgi_graph_add_argmax(g, op["in"])
             elif k == "fc_int4":
-                t = _add_fc_int4(g, desc["ops"], op)
+                t = _add_fc_int4(g, desc["ops"][:i], op)
             elif k == "index_input":
                 n, h, w, c = op["shape"]
                 t = B.mgi_graph_add_index_input(g, n, h, w, c)

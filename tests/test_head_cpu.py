@@ -96,6 +96,14 @@ def test_a_group_that_no_int_holds_is_refused(group):
         engine.Plan(one_group(group)[0], bind=False)
 
 
+@pytest.mark.parametrize("operand", [1, 2, 100, -1])
+def test_an_operand_that_is_no_earlier_tensor_is_refused_by_the_library(operand):
+    desc, t = one_group(64)
+    desc["ops"] = [dict(op) for op in desc["ops"]]
+    desc["ops"][t]["in"] = operand
+    assert status(engine.Plan, desc, bind=False) == 1
+
+
 def test_question_refusals(graph):
     g, L = graph, B.lib()
     x = B.mgi_graph_add_input(g, 2, 1, 1, 100)
