@@ -241,10 +241,10 @@ mgi_status mgi_graph_add_argmax(mgi_graph *g, int in, int *out);
  * finite; n at most 2^24 (MGI_ERR_UNSUPPORTED).  Products of codes and
  * activations are summed exactly as the 16-bit layer sums them; scales are kept
  * in the plan's 16-bit storage type, each output channel's around a power of
- * two of its own, so that none underflows beside the channel's largest.  A
- * weight takes half a byte in the plan, and in plans of many images (64-row
- * tiles enough for every compute unit) three quarters.  fp32 output
- * (n, 1, 1, cout), like fc. */
+ * two of its own: fp16 keeps their 11 bits down to 2^-28 of the channel's
+ * largest (below 2^-40 of it they are zero), bf16 their 8 bits.  A weight takes
+ * half a byte in the plan, and in plans of many images (64-row tiles enough for
+ * every compute unit) three quarters.  fp32 output (n, 1, 1, cout), like fc. */
 mgi_status mgi_graph_add_fc_int4(mgi_graph *g, int in, int cout, int group,
                                  const unsigned char *codes, const float *scales,
                                  const unsigned char *zeros, const float *bias, int *out);

@@ -1660,12 +1660,14 @@ void plan_memory(mgi_plan &p, const mgi_options &o) {
 // difference from the zero point, sign and magnitude in six bits (see there):
 // 192 bits to a lane, its 32 inputs in order, the first 128 of all lanes and
 // then the other 64; no zero points follow.
-// Scales are divided by a power of two per output channel that brings the
-// channel's largest near 1 and are then rounded to the storage type (half a
-// unit in the last place, 2^-11 in fp16 and 2^-9 in bf16): in fp16 a scale below
-// 6e-5 would lose bits, and one below 6e-8 vanish, without it.
+// Scales are divided by a power of two per output channel and are then rounded
+// to the storage type (half a unit in the last place, 2^-11 in fp16 and 2^-8 in
+// bf16).  In fp16 it brings the channel's largest to 2^14 .. 2^15, the last
+// power of two whose values cannot round to infinity, so that the others keep
+// their bits down to 2^-28 of it (they lose bits below 6e-5, and vanish below
+// 3e-8); in bf16 near 1.
 template <typename Reserve, typename Bits>
-void pack_fc_int4(const GOp &op, int cin, Node &nd, std::vector<uint8_t> &blob, Reserve reserve, Bits to_bits) {
+void pack_fc_int4(const GOp &op, int cin, bool bf16, Node &nd, std::vector<uint8_t> &blob, Reserve reserve, Bits to_bits) {
     const int cout = op.cout, kb = nd.ksp, gs = nd.fq_geo.gs, per = 4 / gs, groups = (cin - 1) / op.group + 1;
     const bool six = nd.fq_geo.six_bit();
     nd.zeros = !op.zeros.empty() && !six;
@@ -1697,7 +1699,7 @@ void pack_fc_int4(const GOp &op, int cin, Node &nd, std::vector<uint8_t> &blob, 
             for (int gi = 0; gi < groups; ++gi) top = std::max(top, std::fabs(sc[gi]));
             // (exponents as far as both powers of two stay normal numbers)
             int e = 0;
-            if (top > 0.0f) e = std::min(std::max(std::ilogb(top), -126), 126);
+            if (top > 0.0f) e = std::min(std::max(std::ilogb(top) - (bf16 ? 0 : 14), -126), 126);
             ep[co] = std::ldexp(1.0f, e);
             bp[co] = op.b[co];
             for (int b = 0; b < kb; ++b)
@@ -1752,7 +1754,8 @@ void pack_weights(const mgi_graph &g, mgi_plan &p, const mgi_options &o) {
     p.zero_off = reserve(256);  // zeroed block read by kernels for out-of-range taps
     for (Node &nd : p.nodes) {
         const GOp &op = g.ops[nd.op >= 0 ? nd.op : 0];
-        if (nd.kind == NodeKind::FcInt4) pack_fc_int4(op, g.ops[op.in[0]].out.c, nd, blob, reserve, to_bits);
+        if (nd.kind == NodeKind::FcInt4)
+            pack_fc_int4(op, g.ops[op.in[0]].out.c, o.dtype == MGI_DTYPE_BF16, nd, blob, reserve, to_bits);
         if (nd.kind == NodeKind::DwPw) {
             // depthwise taps of the absorbed op, laid out as for a depthwise node
             const GOp &dop = g.ops[nd.dw_op];

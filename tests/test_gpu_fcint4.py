@@ -278,3 +278,28 @@ def test_a_group_far_longer_than_the_rows(dtype):
     log(f"[case] group 2^31 - 32, storage type {dtype}")
     _, outs, _ = run_gpu(desc, materialize_all=False, dtype=dtype)
     check(desc, t, outs[0])
+
+
+@pytest.mark.parametrize("n,cout,group", [(3, 40, 32), (20, 50, 64), (9, 4200, 128)])
+@pytest.mark.parametrize("dtype", [0, 1])
+def test_scales_far_apart_within_a_channel(dtype, n, cout, group):
+    # groups of one channel with scales 2^24 apart, and features that make up for
+    # it: every group counts in the sum.  Scales of 24 bits, so each group's part
+    # is off by half a step of the storage type (2^-11, 2^-8).
+    desc, t = layer(n, 4 * group, cout, group, True, seed=7)
+    if dtype == 1:
+        desc = workloads.as_bf16_graph(desc)
+    rng = np.random.default_rng(cout)
+    op, x = desc["ops"][1], desc["ops"][0]["data"]
+    order = rng.permuted(np.tile(np.arange(4), (cout, 1)), axis=1)
+    order[::2] = np.arange(4)
+    op["scales"] = (op["scales"] / 16 * (1 + rng.random((cout, 4)) * 0.01) * 2.0 ** (-8 * order)).astype(np.float32)
+    x[:] = (x.reshape(n, 4, group) * 2.0 ** (8 * np.arange(4) - 12)[:, None]).reshape(x.shape)
+    x[:] = x.astype(np.float16)
+    op["b"] = np.zeros(cout)
+    log(f"[case] {desc['name']}, scales 2^24 apart, storage type {dtype}")
+    _, outs, _ = run_gpu(desc, materialize_all=False, dtype=dtype)
+    ref = oracle.run_graph(desc, keep=[t])[t].reshape(outs[0].shape)
+    full = bound(desc)
+    step = full / ((4 * group / 32 + 64) * 2.0 ** -23) * 2.0 ** (-8 if dtype else -11)
+    assert (np.abs(outs[0] - ref) <= full + step).all()
