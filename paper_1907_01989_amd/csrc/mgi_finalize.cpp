@@ -1665,7 +1665,11 @@ void plan_memory(mgi_plan &p, const mgi_options &o) {
 // bf16).  In fp16 it brings the channel's largest to 2^14 .. 2^15, the last
 // power of two whose values cannot round to infinity, so that the others keep
 // their bits down to 2^-28 of it (they lose bits below 6e-5, and vanish below
-// 3e-8); in bf16 near 1.
+// 3e-8).  In bf16, whose exponents are those of fp32, a channel keeps its scales
+// as they are unless the largest is outside 2^-60 .. 2^60, so that the sum over
+// the groups, which the kernels scale group by group, is no larger than the
+// result's own: only what one scale's inputs of a block (at most 128) sum to
+// comes before it.
 template <typename Reserve, typename Bits>
 void pack_fc_int4(const GOp &op, int cin, bool bf16, Node &nd, std::vector<uint8_t> &blob, Reserve reserve, Bits to_bits) {
     const int cout = op.cout, kb = nd.ksp, gs = nd.fq_geo.gs, per = 4 / gs, groups = (cin - 1) / op.group + 1;
@@ -1699,7 +1703,10 @@ void pack_fc_int4(const GOp &op, int cin, bool bf16, Node &nd, std::vector<uint8
             for (int gi = 0; gi < groups; ++gi) top = std::max(top, std::fabs(sc[gi]));
             // (exponents as far as both powers of two stay normal numbers)
             int e = 0;
-            if (top > 0.0f) e = std::min(std::max(std::ilogb(top) - (bf16 ? 0 : 14), -126), 126);
+            if (top > 0.0f) {
+                const int l = std::ilogb(top);
+                e = bf16 ? l - std::min(std::max(l, -60), 60) : std::max(l - 14, -126);
+            }
             ep[co] = std::ldexp(1.0f, e);
             bp[co] = op.b[co];
             for (int b = 0; b < kb; ++b)

@@ -303,3 +303,42 @@ def test_scales_far_apart_within_a_channel(dtype, n, cout, group):
     full = bound(desc)
     step = full / ((4 * group / 32 + 64) * 2.0 ** -23) * 2.0 ** (-8 if dtype else -11)
     assert (np.abs(outs[0] - ref) <= full + step).all()
+
+
+@pytest.mark.parametrize("n,cin,cout,group", [(3, 2048, 40, 128), (20, 2048, 50, 64), (9, 2000, 4200, 32),
+                                              (700, 2048, 1500, 128)])
+def test_large_bf16_features(n, cin, cout, group):
+    # features up to 2^116 of one sign and the largest codes: what one scale's
+    # stretch of at most 128 inputs sums to stays below 128 * 15 * 2^116 < 2^127,
+    # and the scales bring that back before more is added
+    desc, t = layer(n, cin, cout, group, True, dtype=DTYPE_FP32, seed=8)
+    desc = workloads.as_bf16_graph(desc)
+    op, x = desc["ops"][1], desc["ops"][0]["data"]
+    x[:] = workloads.bf16_round(2.0 ** 115 * (1 + np.abs(x) / 2.1))
+    op["q"][:] = 0xFF
+    op["zeros"][:] = 0
+    op["scales"] = (op["scales"] * 2.0 ** -30).astype(np.float32)
+    log(f"[case] {desc['name']}, features of 2^115")
+    _, outs, _ = run_gpu(desc, materialize_all=False, dtype=1)
+    check(desc, t, outs[0])
+
+
+def test_scales_at_the_ends_of_the_range():
+    # the largest floats do not round to infinity, the smallest not to zero
+    for dtype in (0, 1):
+        desc, t = layer(2, 160, 64, 32, True, seed=9)
+        if dtype == 1:
+            desc = workloads.as_bf16_graph(desc)
+        op = desc["ops"][1]
+        op["b"] = np.zeros(64)
+        big = np.float32(np.finfo(np.float32).max) / 2 ** 12
+        small = np.float32(2.0 ** -120)
+        op["scales"][:32], op["scales"][32:] = big, small
+        desc["ops"][0]["data"][:] *= 2.0 ** -5
+        log(f"[case] scales of 8e34 and 2^-120, storage type {dtype}")
+        _, outs, _ = run_gpu(desc, materialize_all=False, dtype=dtype)
+        ref = oracle.run_graph(desc, keep=[t])[t].reshape(outs[0].shape)
+        full = bound(desc)
+        # (half a step of each scale; results below the normal numbers in steps of 2^-149)
+        step = full / ((160 / 32 + 64) * 2.0 ** -23) * 2.0 ** (-8 if dtype else -11) + 2.0 ** -149
+        assert np.isfinite(outs[0]).all() and (np.abs(outs[0] - ref) <= full + step).all()
