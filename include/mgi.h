@@ -266,7 +266,8 @@ mgi_status mgi_graph_add_index_input(mgi_graph *g, int n, int h, int w, int c, i
 
 /* The k channels with the largest values of each pixel, largest first, equal
  * values by ascending channel: int32 (n, h, w, k), 1 <= k <= 64, k at most the
- * channels (MGI_ERR_SHAPE).  NaN ranks with -inf.  At most 2^19 channels. */
+ * channels (MGI_ERR_SHAPE).  NaN ranks with -inf.  At most 2^19 channels and
+ * 2^28 - 1 pixels (MGI_ERR_UNSUPPORTED), as for log_prob and entropy. */
 mgi_status mgi_graph_add_topk(mgi_graph *g, int in, int k, int *out);
 
 /* The logarithm of the softmax of each pixel's channels, for the channels that

@@ -19,6 +19,9 @@ namespace {
 
 constexpr int kCap = 1024;            // candidates a workgroup ranks
 constexpr float kLog2e = 1.44269504088896341f;
+// Workgroups along x of a grid that has more than one along y: threads along one
+// dimension have to stay below 2^32, which 2^26 rows of one wave each reach.
+constexpr int kGridBits = 22;
 
 // unsigned integers in the order of the values (-0 as +0)
 __device__ __forceinline__ uint32_t order_of(float v) {
@@ -318,7 +321,9 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(PER == 64 ? 
     constexpr int W = NT / 64;
     __shared__ Shared<W> sh;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int row = blockIdx.x / segs, seg = blockIdx.x - row * segs;
+    const unsigned block = blockIdx.y << kGridBits | blockIdx.x;
+    const int row = block / segs, seg = block - row * segs;
+    if (row >= p.rows) return;
     const T *x = (const T *)p.x + (size_t)row * p.cols;
     // channels of the lists, their values next, both long before they are used
     int listed[kAnswerLists];
@@ -503,7 +508,8 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(PER == 64 ? 
 
 template <typename T>
 hipError_t launch_t(const AnswersParams &p, const AnswersGeom &g, hipStream_t st) {
-    const dim3 grid((unsigned)p.rows * (unsigned)g.segs);
+    const unsigned blocks = (unsigned)p.rows * (unsigned)g.segs;
+    const dim3 grid(std::min(blocks, 1u << kGridBits), (blocks + (1u << kGridBits) - 1) >> kGridBits);
 #define MGI_ANSWERS(NT_, PER_, MORE_)                                                                   \
     if (g.nt == NT_ && g.per == PER_ && (g.rounds > 1) == MORE_) {                                       \
         launch(answers_kernel<T, NT_, PER_, MORE_>, grid, dim3(NT_), 0, st, p, g.segs, g.rounds, g.seglen); \

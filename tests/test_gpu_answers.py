@@ -353,3 +353,25 @@ def test_every_channel_is_asked_for(cols):
     x[7, : cols // 2] = -np.inf
     log(f"[case] all {cols} channels")
     ask(x, cols, rng.integers(-2, cols + 2, (70, 700)))
+
+
+def test_more_rows_than_one_grid_dimension_has_threads_for():
+    # 2^26 rows of one wave each: 2^32 threads
+    import torch
+    from paper_1907_01989_amd import engine
+    rows = 2 ** 26 + 5
+    desc = {"ops": [{"op": "input", "shape": (rows, 1, 1, 2), "dtype": DTYPE_FP16}, {"op": "topk", "in": 0, "k": 1},
+                    {"op": "log_prob", "in": 0, "index": 1}, {"op": "entropy", "in": 0}], "outputs": [1, 2, 3]}
+    log(f"[case] {rows} x 2")
+    plan = engine.Plan(desc)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    x = torch.randn((rows, 1, 1, 2), generator=g, device="cuda", dtype=torch.float16)
+    top, lp, h = plan.run([x], [o.fill_(-7) for o in plan.alloc_outputs()])
+    torch.cuda.synchronize()
+    for r in range(0, rows, 2 ** 24):
+        z = x[r:r + 2 ** 24].reshape(-1, 2).double()
+        assert torch.equal(top[r:r + 2 ** 24, 0], (z[:, 1] > z[:, 0]).int()), r
+        p = torch.log_softmax(z, 1)
+        assert ((lp[r:r + 2 ** 24, 0] - p.amax(1)).abs() <= 2e-5).all(), r
+        assert ((h[r:r + 2 ** 24, 0] + (p.exp() * p).sum(1)).abs() <= 5e-5).all(), r
