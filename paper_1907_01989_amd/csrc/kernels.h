@@ -19,10 +19,15 @@ struct LaunchEvents {
 };
 LaunchEvents &launch_events();
 
+// Set by a launch that this thread has been refused: 2^32 threads or more along
+// a grid dimension, of which the device would run the remainder without an error.
+bool &launch_refused();
+
 template <typename F, typename... Args>
 inline void launch(F kernel, dim3 grid, dim3 block, unsigned lds, hipStream_t st, Args... args) {
     const LaunchEvents &ev = launch_events();
-    if (ev.start || ev.stop)
+    if ((uint64_t)grid.x * block.x >> 32) launch_refused() = true;
+    else if (ev.start || ev.stop)
         hipExtLaunchKernelGGL(kernel, grid, block, lds, st, ev.start, ev.stop, 0, args...);
     else
         hipLaunchKernelGGL(kernel, grid, block, lds, st, args...);

@@ -675,6 +675,13 @@ hipError_t launch_node(const mgi_plan &p, const Node &nd, const Bases &B, hipStr
 
 namespace {
 
+// launch_node, with an error for a launch that was refused
+hipError_t run_node(const mgi_plan &p, const Node &nd, const Bases &B, hipStream_t st) {
+    launch_refused() = false;
+    const hipError_t e = launch_node(p, nd, B, st);
+    return e == hipSuccess && launch_refused() ? hipErrorInvalidConfiguration : e;
+}
+
 void release_graph(mgi_plan &p) {
     if (p.graph_exec) (void)hipGraphExecDestroy(static_cast<hipGraphExec_t>(p.graph_exec));
     if (p.graph) (void)hipGraphDestroy(static_cast<hipGraph_t>(p.graph));
@@ -753,7 +760,7 @@ mgi_status run_plan(mgi_plan *p, const void *const *dev_inputs, void *const *dev
     for (size_t i = 0; i < p->nodes.size(); ++i) {
         ev.start = start_ev ? static_cast<hipEvent_t>(start_ev[i]) : nullptr;
         ev.stop = stop_ev ? static_cast<hipEvent_t>(stop_ev[i]) : nullptr;
-        hipError_t e = launch_node(*p, p->nodes[i], B, st);
+        hipError_t e = run_node(*p, p->nodes[i], B, st);
         ev.start = ev.stop = nullptr;
         if (e != hipSuccess)
             return hip_fail(e, (std::string(who) + ": node " + std::to_string(i) + " (" +
@@ -966,7 +973,7 @@ extern "C" mgi_status mgi_plan_autotune(mgi_plan *p, const void *const *dev_inpu
                     const size_t k = std::find(timed.begin(), timed.end(), j) - timed.begin();
                     ev.start = k < timed.size() ? evs[2 * (pairs * r + k)] : nullptr;
                     ev.stop = k < timed.size() ? evs[2 * (pairs * r + k) + 1] : nullptr;
-                    e = launch_node(*p, p->nodes[j], B, st);
+                    e = run_node(*p, p->nodes[j], B, st);
                     ev.start = ev.stop = nullptr;
                     if (e == hipSuccess) continue;
                     if (j != ni) result = hip_fail(e, "mgi_plan_autotune: run");

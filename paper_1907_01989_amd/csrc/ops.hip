@@ -32,6 +32,11 @@ LaunchEvents &launch_events() {
     return ev;
 }
 
+bool &launch_refused() {
+    static thread_local bool refused;
+    return refused;
+}
+
 // ---------------------------------------------------------------------------
 // Depthwise 3x3 convolution, column strips.  A thread owns one output column
 // of one 8-channel slice of one image and R consecutive output rows: it reads

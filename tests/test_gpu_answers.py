@@ -375,3 +375,17 @@ def test_more_rows_than_one_grid_dimension_has_threads_for():
         p = torch.log_softmax(z, 1)
         assert ((lp[r:r + 2 ** 24, 0] - p.amax(1)).abs() <= 2e-5).all(), r
         assert ((h[r:r + 2 ** 24, 0] + (p.exp() * p).sum(1)).abs() <= 5e-5).all(), r
+
+
+def test_a_launch_of_too_many_threads_is_an_error():
+    # (a softmax takes a wave to a row too; only the count of threads is wrong, no access is)
+    import torch
+    from paper_1907_01989_amd import _binding as B, engine
+    rows = 2 ** 26 + 5
+    desc = {"ops": [{"op": "input", "shape": (rows, 1, 1, 2), "dtype": DTYPE_FP16}, {"op": "softmax", "in": 0}], "outputs": [1]}
+    log(f"[case] softmax of {rows} x 2")
+    plan = engine.Plan(desc)
+    x = torch.zeros((rows, 1, 1, 2), device="cuda", dtype=torch.float16)
+    with pytest.raises(B.MgiError, match="softmax.*InvalidConfiguration"):
+        plan.run([x])
+    torch.cuda.synchronize()
