@@ -238,15 +238,16 @@ mgi_status mgi_graph_add_argmax(mgi_graph *g, int in, int *out);
  * and zeros: cout x ceil(cin / group) values, the last group may be shorter;
  * zeros: 0..15, NULL = 8 throughout; bias: cout floats, NULL = zeros.
  * group: a positive multiple of 32 (MGI_ERR_UNSUPPORTED otherwise), scales
- * finite; n at most 2^24 (MGI_ERR_UNSUPPORTED).  Products of codes (less zero
- * points) and activations are exact and summed in fp32, and sums of up to 128
- * of one group are then scaled: in bf16 plans they stay finite with activations
- * up to 2^116 (beyond, the 16-bit layer, which multiplies by scaled weights,
- * may have a finite result where this one has none).  Scales are kept in the
- * plan's 16-bit storage type: in bf16 with their 8 bits, in fp16 around a power
- * of two of each output channel's own with their 11 bits down to 2^-28 of the
- * channel's largest (below 2^-40 of it they are zero).  A weight takes half a
- * byte in the plan, and in plans of many images (64-row tiles enough for every
+ * finite; n at most 2^24 (MGI_ERR_UNSUPPORTED), and finalize may refuse an
+ * n x cout above 2^33 so, for which a launch has no threads.  Products of codes
+ * (less zero points) and activations are exact and summed in fp32, and sums of
+ * up to 128 of one group are then scaled: in bf16 plans they stay finite with
+ * activations up to 2^116 (beyond, the 16-bit layer, which multiplies by scaled
+ * weights, may have a finite result where this one has none).  Scales are kept
+ * in the plan's 16-bit storage type: in bf16 with their 8 bits, in fp16 around a
+ * power of two of each output channel's own with their 11 bits down to 2^-28 of
+ * the channel's largest (below 2^-40 of it they are zero).  A weight takes half
+ * a byte in the plan, and in plans of many images (64-row tiles enough for every
  * compute unit) three quarters.  fp32 output (n, 1, 1, cout), like fc. */
 mgi_status mgi_graph_add_fc_int4(mgi_graph *g, int in, int cout, int group,
                                  const unsigned char *codes, const float *scales,

@@ -148,6 +148,13 @@ struct FcInt4Geom {
     bool six_bit() const { return fm == 4; }     // codes less zero points as 6-bit floats
     int block_bytes(bool zp) const { return six_bit() ? 1536 + 32 * (4 / gs) : fcint4_block_bytes(gs, zp); }
     bool reads_raw(int cin) const { return fm == 1 && cin >= 8; }   // takes xin
+    // Threads of a launch at the most (a tile kernel has one or two waves to a group that fetch).
+    size_t threads(int M, int nb16) const {
+        const size_t mtiles = ((size_t)M + 16 * fm - 1) / (16 * fm);
+        if (six_bit()) return mtiles * ((nb16 + 3) / 4) * 768;
+        if (kgroups == 0) return mtiles * nb16 * 64 * waves;
+        return mtiles * ((nb16 + waves - 1) / waves) * 64 * (waves + (fm == 1 ? 2 : 1)) * kgroups;
+    }
 };
 FcInt4Geom fcint4_geom(int M, int nb16, int kb, int group);
 hipError_t launch_fcint4(const FcInt4Params &p, const FcInt4Geom &g, hipStream_t st);

@@ -1347,6 +1347,8 @@ mgi_status Lowering::lower_other(const Group &G, const GOp &op, const Shape &out
             nd.out = new_buf(Layout::F32, out_shape, G.last);
             flat_buf[G.last] = nd.out;
             nd.fq_geo = kern::fcint4_geom(x.n, nd.nb16, nd.ksp, op.group);
+            if (nd.fq_geo.threads(x.n, nd.nb16) >> 32)
+                return fail(MGI_ERR_UNSUPPORTED, "fc_int4: images and output channels for more than 2^32 threads");
             return MGI_OK;
         }
         case OpKind::Softmax: {

@@ -104,6 +104,19 @@ def test_an_operand_that_is_no_earlier_tensor_is_refused_by_the_library(operand)
     assert status(engine.Plan, desc, bind=False) == 1
 
 
+@pytest.mark.parametrize("cin,n,cout,ok", [(32, 2 ** 24, 512, True), (32, 2 ** 24, 2000, False), (1024, 2 ** 23, 1024, True),
+                                           (1024, 2 ** 24, 2000, False), (32, 2 ** 22, 2 ** 11, True), (32, 2 ** 22, 2 ** 14, False)])
+def test_layers_that_no_launch_has_threads_for_are_refused(cin, n, cout, ok):
+    ops = [{"op": "input", "shape": (n, 1, 1, cin), "dtype": B.DTYPE_FP16},
+           {"op": "fc_int4", "in": 0, "cout": cout, "group": 32, "q": codes(cout, cin),
+            "scales": np.ones((cout, cin // 32), np.float32), "zeros": None, "b": None}]
+    desc = {"ops": ops, "outputs": [1]}
+    if ok:
+        assert kinds(engine.Plan(desc, bind=False))[-1] == "fc_int4"
+    else:
+        assert status(engine.Plan, desc, bind=False) == 3
+
+
 def test_question_refusals(graph):
     g, L = graph, B.lib()
     x = B.mgi_graph_add_input(g, 2, 1, 1, 100)
