@@ -265,3 +265,14 @@ def test_oracle_runs_a_head():
     r = oracle.run_graph(b.graph("head"), keep=outs)
     assert r[outs[3]].shape == (2, 1, 1, 5) and (np.diff(r[outs[1]], axis=-1) <= 0).all()
     assert workloads.NetBuilder is NetBuilder and (r[outs[2]] <= math.log(100)).all()
+
+
+def test_a_subset_of_the_batch_keeps_its_own_indices():
+    b, outs = head(n=4)
+    for op in b.ops:
+        if op["op"] == "index_input":
+            op["data"] = np.arange(8, dtype=np.int32).reshape(4, 1, 1, 2)
+    desc = b.graph("head")
+    full, part = oracle.run_graph(desc, keep=outs), oracle.run_graph(workloads.subset_batch(desc, [2, 0]), keep=outs)
+    for t in outs:
+        np.testing.assert_array_equal(part[t], full[t][[2, 0]])

@@ -362,7 +362,7 @@ def subset_batch(graph, images):
     are independent, so a sampled check can run the oracle on them alone)."""
     ops = []
     for op in graph["ops"]:
-        if op["op"] == "input":
+        if op["op"] in ("input", "index_input"):
             op = dict(op)
             op["data"] = op["data"][list(images)]
             op["shape"] = (len(images),) + tuple(op["shape"][1:])
