@@ -125,7 +125,7 @@ template <int W>
 struct Shared {
     alignas(16) unsigned long long cand[kCap + kMaxTopK + 8];   // zeros behind the candidates
     unsigned long long best[kMaxTopK];
-    int rank[kCap + kMaxTopK];
+    int rank[W > 1 ? kCap + kMaxTopK : 1];     // (one wave counts in registers)
     float m[W], bound[W], s[W], t[W];
     uint32_t key_bound[W];
     int cnt[W];
@@ -235,12 +235,13 @@ __device__ __forceinline__ void rank(Shared<W> &sh, int n, int k) {
     }
 }
 
-// Empty candidates and places (all threads of the workgroup; none may read the
-// old ones any more).
+// Empty candidates and places, which only a call that asks for the top columns
+// reads (all threads of the workgroup; none may read the old ones any more).
 template <int W>
-__device__ __forceinline__ void clear(Shared<W> &sh) {
+__device__ __forceinline__ void clear(Shared<W> &sh, int k) {
+    if (k == 0) return;
     for (int j = threadIdx.x; j < kCap + kMaxTopK + 8; j += 64 * W) sh.cand[j] = 0;
-    for (int j = threadIdx.x; j < kCap + kMaxTopK; j += 64 * W) sh.rank[j] = 0;
+    for (int j = threadIdx.x; W > 1 && j < kCap + kMaxTopK; j += 64 * W) sh.rank[j] = 0;
     if (threadIdx.x == 0) sh.n = 0;
 }
 
@@ -333,7 +334,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(PER == 64 ? 
         listed[l] = -1;
         if (tid < p.list_given[l]) listed[l] = p.list[l][(size_t)row * p.list_given[l] + tid];
     }
-    clear(sh);
+    clear(sh, p.k);
     const bool stats = p.n_lists > 0 || p.entropy;
     int lo = seg * rounds * seglen, hi = min(p.cols, lo + seglen);
     Held<T, NT, PER> h;
@@ -424,7 +425,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(PER == 64 ? 
         lo = hi;
         hi = min(p.cols, hi + seglen);
         h.load(x, lo, hi);
-        clear(sh);
+        clear(sh, p.k);
     }
     if (segs > 1) {
         const int stride = answers_stride(p.k);
@@ -450,7 +451,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(PER == 64 ? 
             uint32_t top = 0;
 #pragma unroll
             for (int c = 0; c < C; ++c) key[c] = p.part_keys[(size_t)row * n + min(c * NT + at, n - 1)];
-            clear(sh);
+            clear(sh, p.k);
 #pragma unroll
             for (int c = 0; c < C; ++c) {
                 if (c * NT + at >= n) key[c] = 0;
