@@ -7,7 +7,9 @@
 // other.  Sums are fp32.
 //
 // One workgroup owns a row, or a segment of one, and holds it in registers, so
-// the row is read once whatever is asked: a call is bound by the row's bytes.
+// the row is read once whatever is asked: a call about long rows is bound by their
+// bytes (4096 x 32000 fp32 5.0 TB/s), one about many short ones by the workgroups'
+// starts (513 x 513 x 21 244 us, of which the bytes take 5).
 // Where rows are few or long they are split into segments; each leaves its
 // (m, s, t) and its own k best, and the workgroup that arrives last joins them.
 #include "device.h"
@@ -93,7 +95,9 @@ __device__ __forceinline__ T wave_rth(T v, T none, int r, F join) {
 
 // A bound of at most the r-th largest of a wave's keys (order_of) and within
 // 2^-7 of it: the key's upper half, two bits at a time from counts of lanes.  As
-// long as five rounds of wave_rth, whatever r.
+// long as five rounds of wave_rth, whatever r.  (Where the values are far from
+// zero beside their spread most of them pass it and push_exact is called: 512 x
+// 32000, k = 50, about zero 19 us, about 1000 +- 1 238.)
 __device__ __forceinline__ uint32_t wave_rth_near(uint32_t key, int r) {
     uint32_t top = 0;
 #pragma unroll
@@ -529,8 +533,8 @@ hipError_t launch_t(const AnswersParams &p, const AnswersGeom &g, hipStream_t st
 // workgroup takes a segment that its registers cannot hold in rounds (668 x
 // 68012, k = 20: 50 us; as three segments with a join 128), of half of what they
 // could hold: three workgroups to a compute unit then read while others compute
-// (3269 x 38521, k = 5: 126 us; two with rounds of twice the length 157, four,
-// whose registers spill, 142).  The more there is to rank, the more waves help
+// (3269 x 38521, k = 5: 121 us; two with rounds of twice the length 157; four, for
+// which 24 registers spill in fp32 and 37 in fp16, 142; three spill 2 and 14).  The more there is to rank, the more waves help
 // (33 x 49999 fp16, k = 50: eight save 1.8 of 18.2 us; 23 x 69767, k = 3: they
 // cost 2.7 on 12.4).
 AnswersGeom answers_geom(int rows, int cols, int k) {
