@@ -31,8 +31,9 @@
  *   - A plan is not re-entrant: at most one mgi_plan_run per plan may be in
  *     flight on the device at a time unless the runs are ordered by the stream.
  *   - Tensor shapes are (n, h, w, c): batch, height, width, channels.  Graph
- *     inputs are NHWC arrays in fp32 or fp16 (or of int32 channel indices).
- *     Graph outputs are NHWC arrays of fp32 values (an output of
+ *     inputs are NHWC arrays in fp32 or fp16, in bf16 plans also bf16 (or of
+ *     int32 indices).  Graph outputs are NHWC arrays of fp32 values, or of the
+ *     plan's 16-bit storage type where asked (mgi_graph_mark_output_as; an output of
  *     global_avgpool / fc / softmax is (n, c)); argmax outputs are int32 arrays
  *     of shape (n, h, w), topk outputs of shape (n, h, w, k).
  *   - Tensor ids are assigned in call order, starting at 0, one per
@@ -172,7 +173,9 @@ const char *mgi_last_error(void);
 mgi_status mgi_graph_create(mgi_graph **g);
 mgi_status mgi_graph_destroy(mgi_graph *g); /* NULL is accepted */
 
-/* A graph input: an NHWC array of `dtype` (FP32 or FP16) supplied to run. */
+/* A graph input: an NHWC array of `dtype` supplied to run: FP32, FP16 or, in
+ * plans with bf16 storage only (MGI_ERR_UNSUPPORTED from finalize elsewhere),
+ * BF16. */
 mgi_status mgi_graph_add_input(mgi_graph *g, int n, int h, int w, int c, int dtype, int *out);
 
 /* 2D convolution (Sec. 4.1, convolution over a kernel_height x kernel_width
@@ -261,8 +264,9 @@ mgi_status mgi_graph_add_fc_int4(mgi_graph *g, int in, int cout, int group,
  * inputs in place: its outputs must not overlap its inputs
  * (MGI_ERR_INVALID_ARG from the run).
  * ------------------------------------------------------------------------- */
-/* A graph input of channel indices: an (n, h, w, c) int32 array supplied to
- * run, for mgi_graph_add_log_prob only (MGI_ERR_UNSUPPORTED elsewhere). */
+/* A graph input of indices: an (n, h, w, c) int32 array supplied to run: the
+ * channels for mgi_graph_add_log_prob, the positions for mgi_graph_add_rotary or
+ * the bounds for mgi_graph_add_attention (MGI_ERR_UNSUPPORTED elsewhere). */
 mgi_status mgi_graph_add_index_input(mgi_graph *g, int n, int h, int w, int c, int *out);
 
 /* The k channels with the largest values of each pixel, largest first, equal
@@ -284,9 +288,105 @@ mgi_status mgi_graph_add_log_prob(mgi_graph *g, int in, int index, int *out);
  * +inf. */
 mgi_status mgi_graph_add_entropy(mgi_graph *g, int in, int *out);
 
+/* ---------------------------------------------------------------------------
+ * attention blocks: the pixels of an image (or of any (n, h, w, c) tensor, in
+ * order) are tokens, their channels hold heads of equal size one after the
+ * other.  Tensors are stored in the plan's 16-bit type between operators,
+ * sums, statistics and products are fp32.
+ * ------------------------------------------------------------------------- */
+/* Root-mean-square norm of each pixel's channels:
+ *     y = x * weight / sqrt(mean over channels of x^2 + eps)
+ * weight: c floats (NULL = ones); eps: at least 0, finite.  With fusion on, an
+ * add whose sum this reads runs in the same kernel (the norm is of the sum as
+ * stored, rounded to 16 bits, as without fusion).  to8 = 1: the output is an
+ * 8-bit tensor as mgi_graph_add_quantize makes, rounded once from fp32.  The
+ * squares are summed in fp32: rows whose sum of squares passes 3.4e38 give
+ * zeros.  At most 2^14 channels (MGI_ERR_UNSUPPORTED). */
+mgi_status mgi_graph_add_rms_norm(mgi_graph *g, int in, const float *weight, float eps, int to8,
+                                  int *out);
+
+/* The tensor in 8-bit floating point (e4m3: 3 bits behind the leading one, up
+ * to 448), with a power of two 2^e for each pixel and block of 128 channels
+ * (the last may be shorter): e is the smallest, at least -126, with
+ * max |x| <= 448 * 2^e over the block's finite values; values are rounded to
+ * the nearest code, ties to even.  Infinities and NaN become NaN.  An 8-bit
+ * tensor feeds mgi_graph_add_pointwise_fp8 or is a graph output, which holds
+ * the values that it stands for (elsewhere MGI_ERR_UNSUPPORTED).  At most 2^14
+ * channels (MGI_ERR_UNSUPPORTED). */
+mgi_status mgi_graph_add_quantize(mgi_graph *g, int in, int *out);
+
+/* Pointwise (1x1) layer in 8-bit floating point, of an 8-bit tensor (other
+ * operands: MGI_ERR_UNSUPPORTED):
+ *     y[o] = act(b[o] + sum_i scales[o / 128][i / 128] * code[o][i] * x[i])
+ * codes: cout x cin bytes in e4m3 (a code of NaN, 0x7f or 0xff, gives
+ * MGI_ERR_INVALID_ARG); scales: ceil(cout / 128) x ceil(cin / 128) finite
+ * floats, rows first; bias: cout floats, NULL = zeros.  Products are exact; those
+ * of eight inputs, 8i .. 8i + 7, are added with what lies 2^-13 below the largest
+ * of them dropped (the matrix instruction's own sum), all else in fp32, block by
+ * block.  Output (n, h, w, cout). */
+mgi_status mgi_graph_add_pointwise_fp8(mgi_graph *g, int in, int cout, const unsigned char *codes,
+                                       const float *scales, const float *bias, int act, int *out);
+
+/* Rotary positions.  Of each of `heads` heads of head_dim channels, the first
+ * beginning at channel `from`, the first 2 * pairs channels are rotated pair by
+ * pair: pair i is the channels (i, i + pairs), or with adjacent = 1
+ * (2i, 2i + 1), and
+ *     (a, b) -> (a cos t - b sin t, a sin t + b cos t),
+ *     t = freqs[i] * position along axis axes[i];
+ * the other channels of the heads are copied.  head_dim and from are multiples
+ * of 8 (MGI_ERR_UNSUPPORTED).  axes, freqs: `pairs` values each, freqs finite,
+ * in radians per position (angles keep their fraction of a turn for any 32-bit
+ * position).  positions: an index input (n, h, w, axes) with each pixel's
+ * position along every axis (any axis count up to 8), or -1: the axes are 0 the
+ * image's number in the batch, 1 the pixel's row, 2 its column.
+ * Output (n, h, w, heads * head_dim). */
+typedef struct {
+    int heads, head_dim;
+    int from;
+    int pairs;
+    int adjacent;
+} mgi_rotary_desc;
+mgi_status mgi_graph_add_rotary(mgi_graph *g, int in, const mgi_rotary_desc *d, const int *axes,
+                                const double *freqs, int positions, int *out);
+
+/* Attention of q's pixels on those of k and v: for each head and query pixel
+ *     y = sum_j p_j v_j / sum_j p_j,  p_j = exp(scale * q.k_j - max)
+ * over the keys j that it sees.  `heads` query heads share kv_heads heads of
+ * keys and values (heads a multiple of kv_heads; head a uses a / (heads /
+ * kv_heads)); head_dim is a multiple of 8, at most 128 (MGI_ERR_UNSUPPORTED).
+ * The heads begin at channels q_from, k_from and v_from (multiples of 8), so
+ * q, k and v may be one tensor.  scale 0 stands for 1 / sqrt(head_dim).
+ * Sequences: without bounds (-1) image n of q sees image n of k and v, which
+ * may have another size.  bounds: an index input of at least two values; sequence
+ * s is pixels bounds[s] .. bounds[s + 1] - 1 of q, all images in one row, and
+ * the same (or, with k_bounds, an index input of as many values, those of its)
+ * pixels of k and v.  Values are read up to the pixel count and not below their
+ * predecessors (or 0): what runs back or past the end is an empty sequence's.  At
+ * most 2^16 sequences (MGI_ERR_UNSUPPORTED).
+ * causal = 1: of a sequence's nk keys query i of nq sees 0 .. i + nk - nq.
+ * Queries of no sequence, or that see no key, give zeros.  Keys and values
+ * that a query does not see have no part in its result, also if infinite or
+ * NaN.  Output (n, h, w, heads * head_dim), q's n, h and w.  The weights p are
+ * rounded to the storage type for the product with v, their sum is not. */
+typedef struct {
+    int heads, kv_heads, head_dim;
+    int q_from, k_from, v_from;
+    int causal;
+    float scale;
+} mgi_attention_desc;
+mgi_status mgi_graph_add_attention(mgi_graph *g, int q, int k, int v, const mgi_attention_desc *d,
+                                   int bounds, int k_bounds, int *out);
+
 /* Mark a tensor as a graph output (in call order: output index 0, 1, ...).
  * Graph inputs cannot be outputs. */
 mgi_status mgi_graph_mark_output(mgi_graph *g, int id);
+
+/* The same, with the array's element type: FP32 as mgi_graph_mark_output, or
+ * the plan's storage type (FP16 or BF16; finalize gives MGI_ERR_UNSUPPORTED for
+ * the other one): the tensor as stored, without widening.  Tensors that are not
+ * stored in 16 bits (logits, probabilities, labels, indices) have no such form
+ * (MGI_ERR_UNSUPPORTED). */
+mgi_status mgi_graph_mark_output_as(mgi_graph *g, int id, int dtype);
 
 /* ---------------------------------------------------------------------------
  * planning (pure host code; no device call)
@@ -314,7 +414,7 @@ mgi_status mgi_plan_memory_report(const mgi_plan *p, size_t *naive, size_t *plan
 
 /* Graph inputs and outputs of the plan, in declaration / marking order. */
 mgi_status mgi_plan_num_io(const mgi_plan *p, int *n_inputs, int *n_outputs);
-/* Shape and element type (FP32 / FP16 / INT32 for inputs, FP32 / INT32 for outputs)
+/* Shape and element type (FP32 / FP16 / BF16 / INT32 for inputs and outputs)
  * of input or output `index` (is_output selects which); bytes = total size. */
 mgi_status mgi_plan_io_info(const mgi_plan *p, int is_output, int index, int *n, int *h, int *w,
                             int *c, int *dtype, size_t *bytes);

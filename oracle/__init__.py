@@ -250,6 +250,111 @@ def entropy(x):
         return -np.where(np.isneginf(y), 0.0, np.exp(y) * y).sum(-1, keepdims=True)
 
 
+def rms_norm(x, w, eps):
+    """x * w / sqrt(mean over channels of x^2 + eps); w None: ones."""
+    y = x / np.sqrt((x * x).mean(-1, keepdims=True) + eps)
+    return y if w is None else y * np.asarray(w, np.float64)
+
+
+def e4m3_round(x):
+    """The nearest e4m3 value (ties to even) of each element, of magnitudes up to 448."""
+    step = np.exp2(np.maximum(np.frexp(np.abs(x))[1] - 1, -6) - 3.0)
+    return np.rint(x / step) * step
+
+
+def block_exponents(x):
+    """For each pixel and block of 128 channels the least e >= -126 with max |x| <= 448 * 2^e, over finite values."""
+    c = x.shape[-1]
+    a = np.where(np.isfinite(x), np.abs(x), 0.0)
+    top = np.stack([a[..., i:i + 128].max(-1) for i in range(0, c, 128)], -1)
+    m, e = np.frexp(top / 448.0)            # top / 448 = m 2^e, 0.5 <= m < 1
+    e = np.where(m == 0.5, e - 1, e)        # exactly a power of two
+    return np.maximum(np.where(top == 0, -126, e), -126)
+
+
+def quantize(x, exponents=None):
+    """The values that an 8-bit tensor of x stands for; NaN where x is not finite."""
+    e = block_exponents(x) if exponents is None else exponents
+    up = np.exp2(np.repeat(e, 128, -1)[..., :x.shape[-1]].astype(np.float64))
+    with np.errstate(invalid="ignore"):
+        return np.where(np.isfinite(x), e4m3_round(np.where(np.isfinite(x), x, 0.0) / up) * up, np.nan)
+
+
+def e4m3_values(codes):
+    """The values of e4m3 codes (no NaN among them)."""
+    c = np.asarray(codes).astype(np.int64)
+    e, m = c >> 3 & 15, c & 7
+    v = np.where(e > 0, (8 + m) * np.exp2(e - 10.0), m * 2.0 ** -9)
+    return np.where(c > 127, -v, v)
+
+
+def pointwise_fp8_weights(codes, scales, cout, cin):
+    s = np.asarray(scales, np.float64).reshape(-(-cout // 128), -(-cin // 128))
+    s = np.repeat(np.repeat(s, 128, 0)[:cout], 128, 1)[:, :cin]
+    return e4m3_values(codes).reshape(cout, cin) * s
+
+
+def pointwise_fp8(x, codes, scales, b, cout):
+    """Layer over an 8-bit tensor's values: sum of weights times x, plus bias."""
+    w = pointwise_fp8_weights(codes, scales, cout, x.shape[-1])
+    y = x.reshape(-1, x.shape[-1]) @ w.T
+    return (y if b is None else y + np.asarray(b, np.float64)).reshape(x.shape[:-1] + (cout,))
+
+
+def rotary(x, heads, head_dim, axes, freqs, positions=None, first=0, adjacent=False):
+    """Pairs of each head's channels turned by position * frequency; positions None: image, row, column."""
+    n, h, w, _ = x.shape
+    if positions is None:
+        positions = np.stack(np.meshgrid(np.arange(n), np.arange(h), np.arange(w), indexing="ij"), -1)
+    y = x[..., first:first + heads * head_dim].copy().reshape(n, h, w, heads, head_dim)
+    for i, (axis, f) in enumerate(zip(axes, freqs)):
+        t = positions[..., axis].astype(np.float64)[..., None] * f
+        p, q = (2 * i, 2 * i + 1) if adjacent else (i, i + len(axes))
+        a, b = y[..., p].copy(), y[..., q].copy()
+        y[..., p], y[..., q] = a * np.cos(t) - b * np.sin(t), a * np.sin(t) + b * np.cos(t)
+    return y.reshape(n, h, w, heads * head_dim)
+
+
+def attention_spans(nq, nk, n, bounds=None, k_bounds=None):
+    """(first query, end, first key, end) of each sequence."""
+    if bounds is None:
+        a, b = nq // n, nk // n
+        return [(i * a, i * a + a, i * b, i * b + b) for i in range(n)]
+
+    def edges(values, most):
+        return np.maximum.accumulate(np.clip(np.asarray(values, np.int64).reshape(-1), 0, most))
+
+    q = edges(bounds, nq)
+    k = edges(bounds if k_bounds is None else k_bounds, nk)
+    return [(q[i], q[i + 1], k[i], k[i + 1]) for i in range(len(q) - 1)]
+
+
+def attention(q, k, v, heads, kv_heads, head_dim, causal=False, scale=0.0, bounds=None, k_bounds=None, weight_of=None):
+    """Softmax attention of q's pixels on k's and v's, zeros where a query sees no key.  ``weight_of``: also the sum of
+    its weights times that function of the values."""
+    scale = scale or 1.0 / np.sqrt(head_dim)
+    shape = q.shape[:-1] + (heads * head_dim,)
+    qs, ks, vs = (t.reshape(-1, m, head_dim) for t, m in ((q, heads), (k, kv_heads), (v, kv_heads)))
+    out, more = np.zeros_like(qs), np.zeros_like(qs)
+    for q0, q1, k0, k1 in attention_spans(len(qs), len(ks), q.shape[0], bounds, k_bounds):
+        for i in range(q0, q1):
+            end = min(max(i - q0 + 1 + (k1 - k0) - (q1 - q0), 0), k1 - k0) if causal else k1 - k0
+            if end <= 0:
+                continue
+            for a in range(heads):
+                g = a // (heads // kv_heads)
+                with np.errstate(invalid="ignore", over="ignore"):
+                    s = ks[k0:k0 + end, g] @ qs[i, a] * scale
+                    top = s.max()
+                    p = np.exp(s - (0.0 if np.isneginf(top) else top))
+                    total = p.sum()
+                    if total != 0:
+                        out[i, a] = p @ vs[k0:k0 + end, g] / total
+                        if weight_of is not None:
+                            more[i, a] = p @ weight_of(vs[k0:k0 + end, g]) / total
+    return out.reshape(shape) if weight_of is None else (out.reshape(shape), more.reshape(shape))
+
+
 # ----------------------------------------------------------------------------
 # graphs
 # ----------------------------------------------------------------------------
@@ -296,6 +401,12 @@ def tensor_shapes(graph):
             shapes.append(shapes[op["in"]][:3] + (op["k"],))
         elif k == "log_prob":
             shapes.append(shapes[op["index"]])
+        elif k in ("rms_norm", "quantize"):
+            shapes.append(shapes[op["in"]])
+        elif k == "pointwise_fp8":
+            shapes.append(shapes[op["in"]][:3] + (op["cout"],))
+        elif k in ("rotary", "attention"):
+            shapes.append(shapes[op["in" if k == "rotary" else "q"]][:3] + (op["heads"] * op["head_dim"],))
         else:
             raise ValueError(f"unknown op {k}")
     return shapes
@@ -311,12 +422,17 @@ def op_inputs(op):
         return [op["a"], op["b"]]
     if k == "concat":
         return list(op["ins"])
+    if k == "rotary":
+        return [op["in"]] + ([op["positions"]] if op.get("positions", -1) >= 0 else [])
+    if k == "attention":
+        return [op["q"], op["k"], op["v"]] + [op[b] for b in ("bounds", "k_bounds") if op.get(b, -1) >= 0]
     return [op["in"]]
 
 
 # ops whose output the paper's engine keeps in fp16 storage (everything but
 # the fp32 logits / probabilities and the integer labels)
-FP16_STORED = {"conv2d", "depthwise", "add", "activation", "gap", "concat", "resize_bilinear", "pad"}
+FP16_STORED = {"conv2d", "depthwise", "add", "activation", "gap", "concat", "resize_bilinear", "pad", "rms_norm",
+               "pointwise_fp8", "rotary", "attention"}
 
 
 def eval_op(op, operands):
@@ -359,6 +475,22 @@ def eval_op(op, operands):
         return log_prob(operands[0], operands[1])
     if k == "entropy":
         return entropy(operands[0])
+    if k == "rms_norm":
+        y = rms_norm(operands[0], op.get("w"), op.get("eps", 1e-6))
+        return quantize(y) if op.get("to8") else y
+    if k == "quantize":
+        return quantize(operands[0])
+    if k == "pointwise_fp8":
+        return activation(pointwise_fp8(operands[0], op["q"], op["scales"], op.get("b"), op["cout"]), op.get("act", 0))
+    if k == "rotary":
+        return rotary(operands[0], op["heads"], op["head_dim"], op["axes"], op["freqs"],
+                      operands[1] if len(operands) > 1 else None, op.get("from", 0), op.get("adjacent", False))
+    if k == "attention":
+        width = op["head_dim"]
+        q, k_, v = (np.asarray(t)[..., op.get(f, 0):op.get(f, 0) + op[n] * width]
+                    for t, f, n in zip(operands, ("q_from", "k_from", "v_from"), ("heads", "kv_heads", "kv_heads")))
+        return attention(q, k_, v, op["heads"], op["kv_heads"], width, op.get("causal", False), op.get("scale", 0.0),
+                         *operands[3:])
     raise ValueError(f"unknown op {k}")
 
 
@@ -389,9 +521,9 @@ def run_graph(graph, keep=None, store_fp16=False, store_bf16=False):
     vals: dict[int, np.ndarray] = {}
     for i, op in enumerate(ops):
         y = eval_op(op, [vals[t] for t in op_inputs(op)])
-        if store_fp16 and op["op"] in FP16_STORED:
+        if store_fp16 and op["op"] in FP16_STORED and not op.get("to8"):
             y = y.astype(np.float16).astype(np.float64)
-        if store_bf16 and op["op"] in FP16_STORED:
+        if store_bf16 and op["op"] in FP16_STORED and not op.get("to8"):
             y = _round_bf16(y)
         vals[i] = y
         for t in op_inputs(op):

@@ -44,6 +44,15 @@ class Options(ctypes.Structure):
                 ("fuse_irb", ctypes.c_int)]
 
 
+class RotaryDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in ("heads", "head_dim", "from_", "pairs", "adjacent")]
+
+
+class AttentionDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in ("heads", "kv_heads", "head_dim", "q_from", "k_from", "v_from",
+                                           "causal")] + [("scale", ctypes.c_float)]
+
+
 _lib = None
 P = ctypes.c_void_p
 I = ctypes.c_int
@@ -51,6 +60,7 @@ IP = ctypes.POINTER(ctypes.c_int)
 SP = ctypes.POINTER(ctypes.c_size_t)
 FP = ctypes.POINTER(ctypes.c_float)
 UP = ctypes.POINTER(ctypes.c_ubyte)
+DP = ctypes.POINTER(ctypes.c_double)
 
 _SIGS = {
     "mgi_status_str": ([I], ctypes.c_char_p),
@@ -74,7 +84,13 @@ _SIGS = {
     "mgi_graph_add_topk": ([P, I, I, IP], I),
     "mgi_graph_add_log_prob": ([P, I, I, IP], I),
     "mgi_graph_add_entropy": ([P, I, IP], I),
+    "mgi_graph_add_rms_norm": ([P, I, FP, ctypes.c_float, I, IP], I),
+    "mgi_graph_add_quantize": ([P, I, IP], I),
+    "mgi_graph_add_pointwise_fp8": ([P, I, I, UP, FP, FP, I, IP], I),
+    "mgi_graph_add_rotary": ([P, I, ctypes.POINTER(RotaryDesc), IP, DP, I, IP], I),
+    "mgi_graph_add_attention": ([P, I, I, I, ctypes.POINTER(AttentionDesc), I, I, IP], I),
     "mgi_graph_mark_output": ([P, I], I),
+    "mgi_graph_mark_output_as": ([P, I, I], I),
     "mgi_options_default": ([ctypes.POINTER(Options)], None),
     "mgi_graph_finalize": ([P, ctypes.POINTER(Options), ctypes.POINTER(P)], I),
     "mgi_plan_destroy": ([P], I),
@@ -252,8 +268,40 @@ def mgi_graph_add_entropy(g, x):
     return _out(lib().mgi_graph_add_entropy, g, x)
 
 
+def mgi_graph_add_rms_norm(g, x, w=None, eps=1e-6, to8=False):
+    w = _f32(w)
+    return _out(lib().mgi_graph_add_rms_norm, g, x, _fptr(w), eps, int(to8))
+
+
+def mgi_graph_add_quantize(g, x):
+    return _out(lib().mgi_graph_add_quantize, g, x)
+
+
+def mgi_graph_add_pointwise_fp8(g, x, cout, codes, scales, b=None, act=ACT_NONE):
+    codes, scales, b = _u8(codes), _f32(scales), _f32(b)
+    return _out(lib().mgi_graph_add_pointwise_fp8, g, x, cout, codes.ctypes.data_as(UP) if codes is not None else None,
+                _fptr(scales), _fptr(b), act)
+
+
+def mgi_graph_add_rotary(g, x, heads, head_dim, axes, freqs, positions=-1, first=0, adjacent=False):
+    d = RotaryDesc(heads, head_dim, first, len(axes), int(adjacent))
+    a = (ctypes.c_int * max(1, len(axes)))(*axes)
+    f = (ctypes.c_double * max(1, len(axes)))(*freqs)
+    return _out(lib().mgi_graph_add_rotary, g, x, ctypes.byref(d), a, f, positions)
+
+
+def mgi_graph_add_attention(g, q, k, v, heads, kv_heads, head_dim, causal=False, scale=0.0, bounds=-1, k_bounds=-1,
+                            q_from=0, k_from=0, v_from=0):
+    d = AttentionDesc(heads, kv_heads, head_dim, q_from, k_from, v_from, int(causal), scale)
+    return _out(lib().mgi_graph_add_attention, g, q, k, v, ctypes.byref(d), bounds, k_bounds)
+
+
 def mgi_graph_mark_output(g, t):
     _check(lib().mgi_graph_mark_output(g, t))
+
+
+def mgi_graph_mark_output_as(g, t, dtype):
+    _check(lib().mgi_graph_mark_output_as(g, t, dtype))
 
 
 def mgi_options_default():

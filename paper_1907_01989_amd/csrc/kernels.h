@@ -423,5 +423,105 @@ hipError_t launch_ingest(const void *x, bool fp16_in, h8 *y, int M, int C, bool 
 hipError_t launch_zero_words(unsigned *dst, size_t words, hipStream_t st);
 hipError_t launch_export(const h8 *x, float *y, int M, int C, bool bf16, hipStream_t st);
 
+// ---------------------------------------------------------------------------
+// attention blocks
+// ---------------------------------------------------------------------------
+// A 16-bit operand: 8 channels of (slice, pixel) at x[slice * s + pixel * p]
+// (sliced: s = pixels, p = 1; an NHWC array: s = 1, p = its slices).
+struct TokenIn {
+    const h8 *x;
+    int s, p;
+};
+// An output, by groups of 8 channels at slice * s + pixel * p: 16-bit or fp32;
+// y null: not written.
+struct TokenOut {
+    void *y;
+    int s, p;
+    int f32;
+};
+// An 8-bit tensor: codes of 16 channels at codes[(slice16 * M + pixel) * 16],
+// exponents of four blocks of 128 channels at exps[word * M + pixel].
+struct Tensor8 {
+    uint8_t *codes;
+    uint32_t *exps;
+    static size_t codes_bytes(size_t pixels, int c) { return pixels * (((size_t)c + 127) / 128) * 128; }
+    static size_t bytes(size_t pixels, int c) { return codes_bytes(pixels, c) + pixels * (((size_t)c + 511) / 512) * 4; }
+};
+
+// rms_norm and quantize
+constexpr int kMaxNormChannels = 1 << 14;
+struct NormParams {
+    TokenIn a, b;        // b.x null: one operand
+    int act;             // of the sum
+    TokenOut sum;        // y null: not stored
+    const float *w;      // [whole blocks of 128 channels], zero past the last; null: no norm
+    float eps, inv_c;
+    TokenOut out;        // 16-bit output, or the values of the 8-bit one; or
+    Tensor8 q;           // codes null: `out` is written
+    int to8;
+    int M, S, KB;        // pixels, slices, blocks of 128 channels
+    int bf16;
+};
+hipError_t launch_norm(const NormParams &p, hipStream_t st);
+// sliced or 8-bit tensor -> NHWC fp32 or 16-bit output; NHWC 16-bit input -> sliced
+hipError_t launch_export16(const h8 *x, void *y, int M, int C, hipStream_t st);
+hipError_t launch_ingest16(const void *x, h8 *y, int M, int C, hipStream_t st);
+hipError_t launch_export8(const Tensor8 &x, void *y, bool f32, int M, int C, bool bf16, hipStream_t st);
+
+constexpr int kMaxAxes = 8;
+struct RotaryParams {
+    TokenIn x;           // from the first head's first slice on
+    TokenOut y;
+    const int *pos;      // [M][axes], or null: image, row and column of the pixel
+    int axes;
+    const uint64_t *freq;  // turns per position, as a fraction of 2^64
+    const int *axis;
+    int M, H, W;
+    int heads, d8, pairs, adjacent;
+    double inv_w, inv_h;
+    int bf16;
+};
+hipError_t launch_rotary(const RotaryParams &p, hipStream_t st);
+
+constexpr int kMaxHeadDim = 128, kMaxSequences = 1 << 16;
+// Rows of a tile, keys of a chunk (all where keys are not split), chunks, and
+// what the chunks leave behind
+struct AttentionGeom {
+    int tiles;           // row tiles of one head of keys (an upper bound for packed sequences)
+    int chunks, chunk;
+    int wr;              // waves along the rows of a tile (the others take other keys)
+    size_t part_bytes, cnt_bytes;
+};
+AttentionGeom attention_geom(int q_tokens, int k_tokens, int n, int nseq, int group, int kv_heads, int d8);
+struct AttentionParams {
+    TokenIn q, k, v;     // from the first head's first slice on
+    TokenOut y;
+    const int *bq, *bk;  // bounds of packed sequences, or null
+    int nseq;            // sequences (images where no bounds)
+    int tq, tk;          // pixels of an image, or of all
+    int kv_heads, group, d8, causal;
+    float scale;         // of the scores, times log2(e)
+    float *part;
+    int *cnt;
+    int bf16;
+};
+hipError_t launch_attention(const AttentionParams &p, const AttentionGeom &g, hipStream_t st);
+
+// Pointwise layer in 8 bits: weights [nb16][kb][2][64 lanes][16 bytes] in the
+// MFMA A operand's order, scales [ceil(nb16 / 8)][kb]
+struct PwFp8Geom {
+    int variant;
+};
+PwFp8Geom pwfp8_geom(size_t M, int nb16, int kb);
+struct PwFp8Params {
+    Tensor8 x;
+    const uint8_t *w;
+    const float *scales, *bias;
+    TokenOut y;
+    int M, kb, nb16, ns, act;
+    int bf16;
+};
+hipError_t launch_pwfp8(const PwFp8Params &p, const PwFp8Geom &g, hipStream_t st);
+
 }  // namespace kern
 }  // namespace mgi

@@ -66,6 +66,15 @@ uint16_t f32_to_bf16_bits(float f) {
     return (uint16_t)(u >> 16);
 }
 
+size_t element_bytes(int dtype) { return dtype == MGI_DTYPE_FP16 || dtype == MGI_DTYPE_BF16 ? 2 : 4; }
+
+// An angle in radians as a fraction of a turn, times 2^64.
+uint64_t turn_fraction(double radians) {
+    const long double turns = (long double)radians / (2.0L * 3.14159265358979323846264338327950288L);
+    const long double f = turns - std::floor(turns);
+    return f >= 1.0L ? 0 : (uint64_t)std::ldexp(f, 64);
+}
+
 struct Group {
     int head = -1;          // heavy op
     int last = -1;          // last absorbed op (position and output tensor)
@@ -822,8 +831,34 @@ void fuse_answers(mgi_plan &p) {
     p.nodes.swap(kept);
 }
 
+// A norm and the add whose sum it reads are one kernel, in the add's place (the
+// norm waits for nothing else).
+void fuse_add_into_norm(mgi_plan &p) {
+    std::vector<int> producer(p.bufs.size(), -1);
+    for (size_t i = 0; i < p.nodes.size(); ++i) producer[p.nodes[i].out] = (int)i;
+    std::vector<char> drop(p.nodes.size(), 0);
+    for (size_t i = 0; i < p.nodes.size(); ++i) {
+        Node &nm = p.nodes[i];
+        if (nm.kind != NodeKind::Norm || !nm.norm || producer[nm.in[0]] < 0) continue;
+        Node &add = p.nodes[producer[nm.in[0]]];
+        if (add.kind != NodeKind::Add) continue;
+        nm.in = add.in;
+        nm.out_sum = add.out;
+        nm.act1 = add.act1;
+        nm.n_fused += add.n_fused;
+        nm.kname = "add_rms_norm";
+        drop[i] = 1;
+        add = std::move(nm);
+    }
+    std::vector<Node> kept;
+    for (size_t i = 0; i < p.nodes.size(); ++i)
+        if (!drop[i]) kept.push_back(std::move(p.nodes[i]));
+    p.nodes.swap(kept);
+}
+
 // Geometry of the Answers kernels, the scratch tensors and counters of those
-// that split rows over workgroups, and whether questions are about graph inputs.
+// that split rows over workgroups (attention: keys), and whether questions are
+// about graph inputs or a kernel reads indices from one.
 void plan_splits(mgi_plan &p) {
     for (Node &nd : p.nodes) {
         size_t part = 0;
@@ -834,6 +869,13 @@ void plan_splits(mgi_plan &p) {
             nd.cnt_bytes = part ? s.pixels() * sizeof(int) : 0;
             for (int b : nd.in) p.reads_inputs_late = p.reads_inputs_late || p.bufs[b].loc == Loc::Input;
         }
+        if (nd.kind == NodeKind::Attention) {
+            part = nd.at_geo.part_bytes;
+            nd.cnt_bytes = nd.at_geo.cnt_bytes;
+        }
+        // (the positions of rotary, the bounds of attention)
+        if (nd.kind == NodeKind::Attention || nd.kind == NodeKind::Rotary)
+            for (int b : nd.in) p.reads_inputs_late = p.reads_inputs_late || p.bufs[b].loc == Loc::Input;
         if (part == 0) continue;
         Buf b;
         b.layout = Layout::F32;
@@ -1141,6 +1183,7 @@ struct Lowering {
     int need_c8(int t);
     int export_f32(int c8, const Shape &s);
     mgi_status lower_answers(const Group &G, const GOp &op, const Shape &out_shape, Node &nd);
+    mgi_status lower_tokens(const Group &G, const GOp &op, const Shape &out_shape, Node &nd);
     mgi_status lower_conv(const Group &G, const GOp &op, const Shape &out_shape, Node &nd);
     mgi_status lower_other(const Group &G, const GOp &op, const Shape &out_shape, Node &nd);
     mgi_status lower(const Group &G);
@@ -1157,7 +1200,7 @@ void Lowering::add_inputs() {
         b.layout = Layout::NHWC_IN;
         b.shape = g.ops[t].out;
         b.in_dtype = g.ops[t].in_dtype;
-        b.bytes = b.shape.elems() * (b.in_dtype == MGI_DTYPE_FP16 ? 2 : 4);
+        b.bytes = b.shape.elems() * element_bytes(b.in_dtype);
         b.loc = Loc::Input;
         b.index = (int)k;
         b.graph_tensor = t;
@@ -1175,9 +1218,10 @@ int Lowering::new_buf(Layout L, const Shape &s, int tensor) {
     b.layout = L;
     b.shape = s;
     if (L == Layout::C8) b.bytes = (size_t)slices(s.c) * 8 * s.pixels() * 2;
+    else if (L == Layout::Q8) b.bytes = kern::Tensor8::bytes(s.pixels(), s.c);
     else b.bytes = s.elems() * 4;
     b.graph_tensor = tensor;
-    if (tensor >= 0 && out_index[tensor] >= 0 && L != Layout::C8) {
+    if (tensor >= 0 && out_index[tensor] >= 0 && L != Layout::C8 && L != Layout::Q8) {
         b.loc = Loc::Output;
         b.index = out_index[tensor];
     }
@@ -1226,9 +1270,10 @@ mgi_status Lowering::lower_answers(const Group &G, const GOp &op, const Shape &o
     const int t = op.in[0];
     const Shape x = g.ops[t].out;
     int xb = flat_buf[t];
-    if (xb < 0) xb = in_buf[t];
+    // (bf16 inputs are widened as stored tensors are)
+    if (xb < 0 && g.ops[t].in_dtype != MGI_DTYPE_BF16) xb = in_buf[t];
     if (xb < 0) {
-        if (rows_buf[t] < 0 && c8_buf[t] >= 0) rows_buf[t] = export_f32(c8_buf[t], x);
+        if (rows_buf[t] < 0 && need_c8(t) >= 0) rows_buf[t] = export_f32(c8_buf[t], x);
         xb = rows_buf[t];
     }
     if (xb < 0 || p.bufs[xb].layout == Layout::I32)
@@ -1270,7 +1315,7 @@ mgi_status Lowering::lower_conv(const Group &G, const GOp &op, const Shape &out_
     const int rs = std::max(((ow - 1) * d.stride_w + (d.kw - 1) * d.dil_w + 1) * x.c,
                             (x.w + d.pad_l) * x.c);
     const size_t band1 = (size_t)((d.kh - 1) * d.dil_h + 1) * (rs + 7) * 2;
-    if (from_input && d.kh * d.kw * x.c <= 32 && d.cout <= 64 && band1 + kern::kStemStageBytes <= 65536) {
+    if (from_input && g.ops[op.in[0]].in_dtype != MGI_DTYPE_BF16 && d.kh * d.kw * x.c <= 32 && d.cout <= 64 && band1 + kern::kStemStageBytes <= 65536) {
         nd.kind = NodeKind::Stem;
         nd.kname = "conv_stem";
         nd.in = {in_buf[op.in[0]]};
@@ -1305,6 +1350,56 @@ mgi_status Lowering::lower_conv(const Group &G, const GOp &op, const Shape &out_
         nd.residual = rb;
     }
     nd.out = new_buf(Layout::C8, out_shape, G.last);
+    c8_buf[G.last] = nd.out;
+    return MGI_OK;
+}
+
+// An operator of an attention block.
+mgi_status Lowering::lower_tokens(const Group &G, const GOp &op, const Shape &out_shape, Node &nd) {
+    const size_t operands = op.kind == OpKind::Attention ? 3 : 1;
+    for (size_t k = 0; k < op.in.size(); ++k) {
+        const int t = op.in[k], b = k < operands ? (op.kind == OpKind::PointwiseFp8 ? c8_buf[t] : need_c8(t)) : in_buf[t];
+        if (b < 0) return fail(MGI_ERR_UNSUPPORTED, "operand of an attention block's operator has no sliced form");
+        nd.in.push_back(b);
+    }
+    Layout L = Layout::C8;
+    const Shape x = g.ops[op.in[0]].out;
+    switch (op.kind) {
+        case OpKind::RmsNorm:
+        case OpKind::Quantize:
+            nd.kind = NodeKind::Norm;
+            nd.norm = op.kind == OpKind::RmsNorm;
+            nd.to8 = !nd.norm || op.to8;
+            nd.kname = nd.norm ? "rms_norm" : "quantize";
+            nd.eps = op.eps;
+            if (nd.to8) L = Layout::Q8;
+            break;
+        case OpKind::PointwiseFp8:
+            nd.kind = NodeKind::PwFp8;
+            nd.kname = "pointwise_fp8";
+            nd.act1 = op.act;
+            nd.nb16 = (op.cout + 15) / 16;
+            nd.ksp = (x.c + 127) / 128;   // blocks of 128 input channels
+            nd.p8_geo = kern::pwfp8_geom(x.pixels(), nd.nb16, nd.ksp);
+            break;
+        case OpKind::Rotary:
+            nd.kind = NodeKind::Rotary;
+            nd.kname = "rotary";
+            nd.rotary = op.rotary;
+            break;
+        default: {
+            nd.kind = NodeKind::Attention;
+            nd.kname = "attention";
+            nd.attention = op.attention;
+            const mgi_attention_desc &d = op.attention;
+            const Shape k = g.ops[op.in[1]].out;
+            const int nseq = op.in.size() > 3 ? (int)g.ops[op.in[3]].out.elems() - 1 : 0;
+            nd.at_geo = kern::attention_geom((int)x.pixels(), (int)k.pixels(), x.n, nseq, d.heads / d.kv_heads, d.kv_heads,
+                                             d.head_dim / 8);
+            break;
+        }
+    }
+    nd.out = new_buf(L, out_shape, G.last);
     c8_buf[G.last] = nd.out;
     return MGI_OK;
 }
@@ -1495,6 +1590,15 @@ mgi_status Lowering::lower(const Group &G) {
             if (st != MGI_OK) return st;
             break;
         }
+        case OpKind::RmsNorm:
+        case OpKind::Quantize:
+        case OpKind::PointwiseFp8:
+        case OpKind::Rotary:
+        case OpKind::Attention: {
+            const mgi_status st = lower_tokens(G, op, out_shape, nd);
+            if (st != MGI_OK) return st;
+            break;
+        }
         case OpKind::FC:
         case OpKind::FcInt4:
         case OpKind::Softmax:
@@ -1512,8 +1616,8 @@ mgi_status Lowering::lower(const Group &G) {
     add_node(std::move(nd));
     // a sliced tensor that is a graph output is exported right away
     const int t = G.last;
-    if (out_index[t] >= 0 && c8_buf[t] >= 0 && p.bufs[c8_buf[t]].layout == Layout::C8 &&
-        flat_buf[t] < 0) {
+    if (out_index[t] >= 0 && c8_buf[t] >= 0 &&
+        (p.bufs[c8_buf[t]].layout == Layout::C8 || p.bufs[c8_buf[t]].layout == Layout::Q8) && flat_buf[t] < 0) {
         Node ex;
         ex.kind = NodeKind::Export;
         ex.kname = "export";
@@ -1521,9 +1625,10 @@ mgi_status Lowering::lower(const Group &G) {
         ex.n_fused = 0;
         ex.in = {c8_buf[t]};
         Buf b;
-        b.layout = Layout::F32;
+        const int dtype = g.output_dtypes[out_index[t]];
+        b.layout = dtype == MGI_DTYPE_FP32 ? Layout::F32 : Layout::H16;
         b.shape = g.ops[t].out;
-        b.bytes = b.shape.elems() * 4;
+        b.bytes = b.shape.elems() * element_bytes(dtype);
         b.loc = Loc::Output;
         b.index = out_index[t];
         b.graph_tensor = t;
@@ -1550,7 +1655,7 @@ mgi_status Lowering::bind_outputs() {
         p.output_bufs[k] = b;
         Shape s = g.ops[t].out;
         p.output_shapes.push_back(s);
-        p.output_dtypes.push_back(p.bufs[b].layout == Layout::I32 ? MGI_DTYPE_INT32 : MGI_DTYPE_FP32);
+        p.output_dtypes.push_back(p.bufs[b].layout == Layout::I32 ? MGI_DTYPE_INT32 : g.output_dtypes[k]);
     }
 
     return MGI_OK;
@@ -1563,7 +1668,7 @@ void compute_lifetimes(mgi_plan &p) {
     for (size_t i = 0; i < p.nodes.size(); ++i) {
         const Node &nd = p.nodes[i];
         p.bufs[nd.out].producer = (int)i;
-        for (int b : {nd.out_top, nd.out_entropy})
+        for (int b : {nd.out_top, nd.out_entropy, nd.out_sum})
             if (b >= 0) p.bufs[b].producer = (int)i;
         for (int l = 0; l < nd.n_lists; ++l) p.bufs[nd.list_out[l]].producer = (int)i;
         for (int b : nd.in) p.bufs[b].last_use = (int)i;
@@ -1744,6 +1849,32 @@ void pack_fc_int4(const GOp &op, int cin, bool bf16, Node &nd, std::vector<uint8
     }
 }
 
+// Codes, scales and biases of an 8-bit layer, in blocks of 16 output channels x
+// 128 inputs, 2 KiB in the order of the MFMA A operand: 16 bytes to a lane with
+// inputs 16 (l / 16) .. + 15 of channel l % 16, then the same of inputs 64 on.
+// Channels past the last are zeros.
+template <typename Reserve>
+void pack_pw_fp8(const GOp &op, int cin, Node &nd, std::vector<uint8_t> &blob, Reserve reserve) {
+    const int kb = nd.ksp;
+    nd.w_bytes = (size_t)nd.nb16 * kb * 2048;
+    nd.w_off = reserve(nd.w_bytes);
+    // (whole tiles of 256 channels are read)
+    nd.s_off = reserve(((size_t)nd.nb16 + 15) / 16 * 2 * kb * 4);
+    nd.b_bytes = ((size_t)nd.nb16 + 15) / 16 * 256 * 4;
+    nd.b_off = reserve(nd.b_bytes);
+    uint8_t *wp = blob.data() + nd.w_off;
+    for (int co = 0; co < op.cout; ++co) {
+        const uint8_t *src = op.codes.data() + (size_t)co * cin;
+        for (int ci = 0; ci < cin; ++ci) {
+            const int in = ci % 128;
+            const size_t lane = (size_t)(in % 64 / 16) * 16 + co % 16;
+            wp[((size_t)(co / 16) * kb + ci / 128) * 2048 + in / 64 * 1024 + lane * 16 + in % 16] = src[ci];
+        }
+    }
+    std::memcpy(blob.data() + nd.s_off, op.w.data(), op.w.size() * 4);
+    std::memcpy(blob.data() + nd.b_off, op.b.data(), op.b.size() * 4);
+}
+
 // The packed weight blob, uploaded by mgi_plan_bind.
 void pack_weights(const mgi_graph &g, mgi_plan &p, const mgi_options &o) {
     auto to_bits = o.dtype == MGI_DTYPE_BF16 ? f32_to_bf16_bits : f32_to_f16_bits;
@@ -1765,6 +1896,25 @@ void pack_weights(const mgi_graph &g, mgi_plan &p, const mgi_options &o) {
         const GOp &op = g.ops[nd.op >= 0 ? nd.op : 0];
         if (nd.kind == NodeKind::FcInt4)
             pack_fc_int4(op, g.ops[op.in[0]].out.c, o.dtype == MGI_DTYPE_BF16, nd, blob, reserve, to_bits);
+        if (nd.kind == NodeKind::PwFp8) pack_pw_fp8(op, g.ops[op.in[0]].out.c, nd, blob, reserve);
+        if (nd.kind == NodeKind::Norm && nd.norm) {
+            nd.w_bytes = ((size_t)op.out.c + 127) / 128 * 128 * 4;   // zeros past the last channel
+            nd.w_off = reserve(nd.w_bytes);
+            std::memcpy(blob.data() + nd.w_off, op.w.data(), op.w.size() * 4);
+        }
+        if (nd.kind == NodeKind::Rotary) {
+            // turns per position, as a fraction of 2^64, and the axis of each pair
+            const size_t n = op.axes.size();
+            nd.w_bytes = n * 8;
+            nd.w_off = reserve(n * 8);
+            nd.b_bytes = n * 4;
+            nd.b_off = reserve(n * 4);
+            for (size_t i = 0; i < n; ++i) {
+                const uint64_t f = turn_fraction(op.freqs[i]);
+                std::memcpy(blob.data() + nd.w_off + i * 8, &f, 8);
+                std::memcpy(blob.data() + nd.b_off + i * 4, &op.axes[i], 4);
+            }
+        }
         if (nd.kind == NodeKind::DwPw) {
             // depthwise taps of the absorbed op, laid out as for a depthwise node
             const GOp &dop = g.ops[nd.dw_op];
@@ -1861,7 +2011,8 @@ void pack_weights(const mgi_graph &g, mgi_plan &p, const mgi_options &o) {
 }
 
 // An fp32 graph output whose sliced tensor a GEMM node produces is written by
-// that node's kernel (the export node stays in the list and launches nothing).
+// that node's kernel (the export node stays in the list and launches nothing),
+// and so is an fp32 or 16-bit one of an attention block's operator.
 // Not with materialize_all, where every sliced tensor is kept to be read.
 void absorb_exports(mgi_plan &p) {
     std::vector<int> readers(p.bufs.size(), 0), producer(p.bufs.size(), -1);
@@ -1870,13 +2021,21 @@ void absorb_exports(mgi_plan &p) {
         for (int b : nd.in) readers[b]++;
         if (nd.residual >= 0) readers[nd.residual]++;
         producer[nd.out] = (int)i;
+        if (nd.out_sum >= 0) producer[nd.out_sum] = (int)i;
     }
     for (Node &ex : p.nodes) {
         if (ex.kind != NodeKind::Export || p.bufs[ex.out].loc != Loc::Output) continue;
         const int b = ex.in[0];
         if (producer[b] < 0) continue;
         Node &gm = p.nodes[producer[b]];
-        if (gm.kind != NodeKind::Gemm || gm.direct_out >= 0) continue;
+        if (gm.kind == NodeKind::Norm || gm.kind == NodeKind::PwFp8 || gm.kind == NodeKind::Rotary || gm.kind == NodeKind::Attention) {
+            // whole slices that nothing else reads (the sliced tensor is not stored)
+            if (p.bufs[b].shape.c % 8 != 0 || readers[b] > 1 || p.bufs[b].view_of >= 0) continue;
+            (b == gm.out ? gm.direct_out : gm.direct_sum) = ex.out;
+            ex.absorbed = ex.absorbed_aligned = true;
+            continue;
+        }
+        if (gm.kind != NodeKind::Gemm || gm.direct_out >= 0 || p.bufs[ex.out].layout != Layout::F32) continue;
         gm.direct_out = ex.out;
         gm.sliced_read = readers[b] > 1;
         ex.absorbed = true;
@@ -1962,14 +2121,15 @@ void alias_concats(mgi_plan &p, const mgi_options &o) {
 // them (the ingest node stays in the list and launches nothing, in runs where it
 // can be so).  Depthwise kernels convert what they read, 4-bit layers of few
 // rows too, and need no whole slices; the others take fp16 inputs of fp16
-// plans in whole slices, whose 16-byte elements are the same in both layouts.
+// plans (or bf16 ones of bf16 plans) in whole slices, whose 16-byte elements are the same in both layouts.
 // Not with materialize_all.
 void absorb_ingests(mgi_plan &p, const mgi_options &o) {
     int bits = 0;
     for (Node &in : p.nodes) {
         if (in.kind != NodeKind::Ingest || bits >= 64) continue;
         const bool whole = p.bufs[in.out].shape.c % 8 == 0;
-        const bool same = whole && p.bufs[in.in[0]].in_dtype == MGI_DTYPE_FP16 && o.dtype == MGI_DTYPE_FP16;
+        const bool bf16 = p.bufs[in.in[0]].in_dtype == MGI_DTYPE_BF16;   // (in bf16 plans only)
+        const bool same = whole && (bf16 || (p.bufs[in.in[0]].in_dtype == MGI_DTYPE_FP16 && o.dtype == MGI_DTYPE_FP16));
         std::vector<int> readers;
         bool all = true;
         for (size_t i = 0; i < p.nodes.size(); ++i) {
@@ -1981,14 +2141,17 @@ void absorb_ingests(mgi_plan &p, const mgi_options &o) {
             const Shape &os = p.bufs[r.out].shape;
             switch (r.kind) {
                 case NodeKind::Depthwise:
-                    all = all && whole && kern::depthwise_reads_nhwc(c.kh, c.kw, c.stride_h, c.stride_w, c.dil_h, c.dil_w, os.n,
+                    all = all && whole && !bf16 && kern::depthwise_reads_nhwc(c.kh, c.kw, c.stride_h, c.stride_w, c.dil_h, c.dil_w, os.n,
                                                             slices(os.c), os.h, os.w);
                     break;
                 case NodeKind::Gemm:
                 case NodeKind::PwDw:
                 case NodeKind::GemmPool:
+                case NodeKind::Norm:
+                case NodeKind::Rotary:
+                case NodeKind::Attention:
                 case NodeKind::Gap: all = all && same; break;
-                case NodeKind::FcInt4: all = all && (same || r.fq_geo.reads_raw(p.bufs[in.out].shape.c)); break;
+                case NodeKind::FcInt4: all = all && (same || (!bf16 && r.fq_geo.reads_raw(p.bufs[in.out].shape.c))); break;
                 default: all = false;
             }
         }
@@ -2003,6 +2166,12 @@ mgi_status build_plan_impl(const mgi_graph &g, const mgi_options &o, mgi_plan &p
     if (g.outputs.empty()) return fail(MGI_ERR_STATE, "mgi_graph_finalize: no output marked");
     mgi_status st = check_options(o);
     if (st != MGI_OK) return st;
+    for (int t : g.inputs)
+        if (g.ops[t].in_dtype == MGI_DTYPE_BF16 && o.dtype != MGI_DTYPE_BF16)
+            return fail(MGI_ERR_UNSUPPORTED, "mgi_graph_finalize: bf16 inputs need bf16 storage");
+    for (int d : g.output_dtypes)
+        if (d != MGI_DTYPE_FP32 && d != o.dtype)
+            return fail(MGI_ERR_UNSUPPORTED, "mgi_graph_finalize: 16-bit outputs are of the storage type");
     const std::vector<Group> groups = group_operators(g, o, live_ops(g));
     p.bufs.clear();
     p.nodes.clear();
@@ -2019,6 +2188,7 @@ mgi_status build_plan_impl(const mgi_graph &g, const mgi_options &o, mgi_plan &p
     if (o.fuse && o.fuse_softmax) fuse_softmax_into_fc(p);
     if (o.fuse && o.fuse_dwpw) fuse_dw_into_pw(p);
     if (o.fuse && !o.materialize_all) fuse_answers(p);
+    if (o.fuse && !o.materialize_all) fuse_add_into_norm(p);
     plan_splits(p);
     if (o.fuse && !o.materialize_all) {
         alias_concats(p, o);
@@ -2114,7 +2284,7 @@ extern "C" mgi_status mgi_plan_io_info(const mgi_plan *p, int is_output, int ind
     if (w) *w = s.w;
     if (c) *c = s.c;
     if (dtype) *dtype = types[index];
-    if (bytes) *bytes = s.elems() * (types[index] == MGI_DTYPE_FP16 ? 2 : 4);
+    if (bytes) *bytes = s.elems() * element_bytes(types[index]);
     return MGI_OK;
     MGI_ABI_CATCH("mgi_plan_io_info")
 }

@@ -74,10 +74,15 @@ bool is_index(const GOp &op) {
            (op.kind == OpKind::Input && op.in_dtype == MGI_DTYPE_INT32);
 }
 
+// an 8-bit tensor: only the 8-bit layer reads one
+bool is_8bit(const GOp &op) { return op.kind == OpKind::Quantize || (op.kind == OpKind::RmsNorm && op.to8); }
+
 // an operand that holds values: not the indices of topk or of an index input
 mgi_status check_values(const mgi_graph *g, int id, const char *who) {
     const mgi_status s = check_tensor(g, id, who);
     if (s) return s;
+    if (is_8bit(g->ops[id]))
+        return fail(MGI_ERR_UNSUPPORTED, std::string(who) + ": tensor " + std::to_string(id) + " is held in 8 bits");
     if (is_index(g->ops[id]) && g->ops[id].kind != OpKind::Argmax)   // (argmax: finalize says so)
         return fail(MGI_ERR_UNSUPPORTED, std::string(who) + ": tensor " + std::to_string(id) + " holds indices");
     return MGI_OK;
@@ -93,6 +98,22 @@ mgi_status check_rows(const mgi_graph *g, int id, const char *who) {
     if (x.c > kern::kMaxAnswerCols || x.pixels() > (size_t)INT_MAX / 8)
         return fail(MGI_ERR_UNSUPPORTED, std::string(who) + ": at most 2^19 channels and 2^28 - 1 pixels");
     return MGI_OK;
+}
+
+// the operand of an attention block's operator, whose kernels count 16-byte
+// elements in an int
+mgi_status check_tokens(const mgi_graph *g, int id, const char *who) {
+    const mgi_status s = check_values(g, id, who);
+    if (s) return s;
+    if (is_index(g->ops[id]))
+        return fail(MGI_ERR_UNSUPPORTED, std::string(who) + ": tensor " + std::to_string(id) + " holds indices");
+    return MGI_OK;
+}
+
+// ... and whether a tensor of that shape can be counted so
+bool countable(const Shape &x) {
+    const unsigned __int128 e = (unsigned __int128)x.n * x.h * x.w;
+    return e <= INT_MAX && e * (((size_t)x.c + 127) / 128 * 16) <= INT_MAX;
 }
 
 mgi_status push(mgi_graph *g, GOp &&op, int *out) {
@@ -131,8 +152,8 @@ extern "C" mgi_status mgi_graph_add_input(mgi_graph *g, int n, int h, int w, int
     if (!g || !out) return fail(MGI_ERR_INVALID_ARG, "mgi_graph_add_input: null pointer");
     if (n <= 0 || h <= 0 || w <= 0 || c <= 0)
         return fail(MGI_ERR_INVALID_ARG, "mgi_graph_add_input: sizes must be positive");
-    if (dtype != MGI_DTYPE_FP32 && dtype != MGI_DTYPE_FP16)
-        return fail(MGI_ERR_UNSUPPORTED, "mgi_graph_add_input: inputs are fp32 or fp16");
+    if (dtype != MGI_DTYPE_FP32 && dtype != MGI_DTYPE_FP16 && dtype != MGI_DTYPE_BF16)
+        return fail(MGI_ERR_UNSUPPORTED, "mgi_graph_add_input: inputs are fp32, fp16 or bf16");
     GOp op;
     op.kind = OpKind::Input;
     op.out = {n, h, w, c};
@@ -472,17 +493,240 @@ extern "C" mgi_status mgi_graph_add_entropy(mgi_graph *g, int in, int *out) {
     MGI_ABI_CATCH("mgi_graph_add_entropy")
 }
 
-extern "C" mgi_status mgi_graph_mark_output(mgi_graph *g, int id) {
+namespace {
+
+mgi_status check_8bit_source(const mgi_graph *g, int in, const char *who) {
+    const mgi_status s = check_tokens(g, in, who);
+    if (s) return s;
+    const Shape x = g->ops[in].out;
+    if (x.c > kern::kMaxNormChannels)
+        return fail(MGI_ERR_UNSUPPORTED, std::string(who) + ": at most " + std::to_string(kern::kMaxNormChannels) + " channels");
+    if (!countable(x)) return fail(MGI_ERR_UNSUPPORTED, std::string(who) + ": tensor too large");
+    return MGI_OK;
+}
+
+mgi_status check_index_input(const mgi_graph *g, int id, const char *who, const char *what) {
+    const mgi_status s = check_tensor(g, id, who);
+    if (s) return s;
+    const GOp &ix = g->ops[id];
+    if (ix.kind != OpKind::Input || ix.in_dtype != MGI_DTYPE_INT32)
+        return fail(MGI_ERR_INVALID_ARG, std::string(who) + ": " + what + " is an index input");
+    return MGI_OK;
+}
+
+}  // namespace
+
+extern "C" mgi_status mgi_graph_add_rms_norm(mgi_graph *g, int in, const float *weight, float eps, int to8, int *out) {
     MGI_ABI_TRY
-    mgi_status s = check_tensor(g, id, "mgi_graph_mark_output");
+    const char *who = "mgi_graph_add_rms_norm";
+    const mgi_status s = check_8bit_source(g, in, who);
+    if (s) return s;
+    if (!out) return fail(MGI_ERR_INVALID_ARG, std::string(who) + ": null pointer");
+    if (!std::isfinite(eps) || eps < 0.0f) return fail(MGI_ERR_INVALID_ARG, std::string(who) + ": eps is at least 0 and finite");
+    if (to8 != 0 && to8 != 1) return fail(MGI_ERR_INVALID_ARG, std::string(who) + ": to8 is 0 or 1");
+    GOp op;
+    op.kind = OpKind::RmsNorm;
+    op.in = {in};
+    op.out = g->ops[in].out;
+    op.eps = eps;
+    op.to8 = to8 != 0;
+    try {
+        if (weight) op.w.assign(weight, weight + op.out.c); else op.w.assign(op.out.c, 1.0f);
+    } catch (const std::bad_alloc &) {
+        return fail(MGI_ERR_OOM_HOST, std::string(who) + ": out of host memory");
+    }
+    return push(g, std::move(op), out);
+    MGI_ABI_CATCH("mgi_graph_add_rms_norm")
+}
+
+extern "C" mgi_status mgi_graph_add_quantize(mgi_graph *g, int in, int *out) {
+    MGI_ABI_TRY
+    const char *who = "mgi_graph_add_quantize";
+    const mgi_status s = check_8bit_source(g, in, who);
+    if (s) return s;
+    if (!out) return fail(MGI_ERR_INVALID_ARG, std::string(who) + ": null pointer");
+    GOp op;
+    op.kind = OpKind::Quantize;
+    op.in = {in};
+    op.out = g->ops[in].out;
+    return push(g, std::move(op), out);
+    MGI_ABI_CATCH("mgi_graph_add_quantize")
+}
+
+extern "C" mgi_status mgi_graph_add_pointwise_fp8(mgi_graph *g, int in, int cout, const unsigned char *codes,
+                                                  const float *scales, const float *bias, int act, int *out) {
+    MGI_ABI_TRY
+    const char *who = "mgi_graph_add_pointwise_fp8";
+    const mgi_status s = check_tensor(g, in, who);
+    if (s) return s;
+    if (!out || !codes || !scales) return fail(MGI_ERR_INVALID_ARG, std::string(who) + ": null pointer");
+    if (cout <= 0) return fail(MGI_ERR_INVALID_ARG, std::string(who) + ": cout must be positive");
+    if (!valid_act(act)) return fail(MGI_ERR_INVALID_ARG, std::string(who) + ": bad activation");
+    if (!is_8bit(g->ops[in]))
+        return fail(MGI_ERR_UNSUPPORTED, std::string(who) + ": tensor " + std::to_string(in) + " is not held in 8 bits");
+    const Shape x = g->ops[in].out;
+    Shape y = x;
+    y.c = cout;
+    if (cout > (1 << 24) || !countable(y)) return fail(MGI_ERR_UNSUPPORTED, std::string(who) + ": tensor too large");
+    const size_t n = (size_t)cout * x.c, ns = (((size_t)cout + 127) / 128) * (((size_t)x.c + 127) / 128);
+    for (size_t i = 0; i < ns; ++i)
+        if (!std::isfinite(scales[i])) return fail(MGI_ERR_INVALID_ARG, std::string(who) + ": scales must be finite");
+    for (size_t i = 0; i < n; ++i)
+        if ((codes[i] & 0x7f) == 0x7f) return fail(MGI_ERR_INVALID_ARG, std::string(who) + ": a code is NaN");
+    GOp op;
+    op.kind = OpKind::PointwiseFp8;
+    op.in = {in};
+    op.cout = cout;
+    op.act = act;
+    op.out = y;
+    try {
+        op.codes.assign(codes, codes + n);
+        op.w.assign(scales, scales + ns);
+        if (bias) op.b.assign(bias, bias + cout); else op.b.assign(cout, 0.0f);
+    } catch (const std::bad_alloc &) {
+        return fail(MGI_ERR_OOM_HOST, std::string(who) + ": out of host memory");
+    }
+    return push(g, std::move(op), out);
+    MGI_ABI_CATCH("mgi_graph_add_pointwise_fp8")
+}
+
+extern "C" mgi_status mgi_graph_add_rotary(mgi_graph *g, int in, const mgi_rotary_desc *d, const int *axes,
+                                           const double *freqs, int positions, int *out) {
+    MGI_ABI_TRY
+    const char *who = "mgi_graph_add_rotary";
+    mgi_status s = check_tokens(g, in, who);
+    if (s) return s;
+    if (!out || !d) return fail(MGI_ERR_INVALID_ARG, std::string(who) + ": null pointer");
+    if (d->heads <= 0 || d->head_dim <= 0 || d->from < 0 || d->pairs < 0 || (d->adjacent != 0 && d->adjacent != 1))
+        return fail(MGI_ERR_INVALID_ARG, std::string(who) + ": heads and head_dim are positive, from and pairs at least 0, adjacent 0 or 1");
+    if (d->head_dim % 8 || d->from % 8)
+        return fail(MGI_ERR_UNSUPPORTED, std::string(who) + ": head_dim and from are multiples of 8");
+    if (d->pairs > d->head_dim / 2) return fail(MGI_ERR_SHAPE, std::string(who) + ": more pairs than half a head's channels");
+    if (d->pairs > 0 && (!axes || !freqs)) return fail(MGI_ERR_INVALID_ARG, std::string(who) + ": null pointer");
+    const Shape x = g->ops[in].out;
+    if ((long)d->from + (long)d->heads * d->head_dim > x.c)
+        return fail(MGI_ERR_SHAPE, std::string(who) + ": heads past the last channel");
+    int n_axes = 3;
+    if (positions != -1) {
+        if ((s = check_index_input(g, positions, who, "positions"))) return s;
+        const Shape ps = g->ops[positions].out;
+        if (ps.n != x.n || ps.h != x.h || ps.w != x.w)
+            return fail(MGI_ERR_SHAPE, std::string(who) + ": positions differ in n, h or w");
+        if (ps.c > kern::kMaxAxes)
+            return fail(MGI_ERR_UNSUPPORTED, std::string(who) + ": at most " + std::to_string(kern::kMaxAxes) + " axes");
+        n_axes = ps.c;
+    }
+    for (int i = 0; i < d->pairs; ++i) {
+        if (axes[i] < 0 || axes[i] >= n_axes) return fail(MGI_ERR_INVALID_ARG, std::string(who) + ": no such axis");
+        if (!std::isfinite(freqs[i])) return fail(MGI_ERR_INVALID_ARG, std::string(who) + ": freqs must be finite");
+    }
+    GOp op;
+    op.kind = OpKind::Rotary;
+    op.in = {in};
+    if (positions != -1) op.in.push_back(positions);
+    op.out = x;
+    op.out.c = d->heads * d->head_dim;
+    if (!countable(x) || !countable(op.out)) return fail(MGI_ERR_UNSUPPORTED, std::string(who) + ": tensor too large");
+    op.rotary = *d;
+    try {
+        op.axes.assign(axes, axes + d->pairs);
+        op.freqs.assign(freqs, freqs + d->pairs);
+    } catch (const std::bad_alloc &) {
+        return fail(MGI_ERR_OOM_HOST, std::string(who) + ": out of host memory");
+    }
+    return push(g, std::move(op), out);
+    MGI_ABI_CATCH("mgi_graph_add_rotary")
+}
+
+extern "C" mgi_status mgi_graph_add_attention(mgi_graph *g, int q, int k, int v, const mgi_attention_desc *d,
+                                              int bounds, int k_bounds, int *out) {
+    MGI_ABI_TRY
+    const char *who = "mgi_graph_add_attention";
+    mgi_status s;
+    for (int t : {q, k, v})
+        if ((s = check_tokens(g, t, who))) return s;
+    if (!out || !d) return fail(MGI_ERR_INVALID_ARG, std::string(who) + ": null pointer");
+    if (d->heads <= 0 || d->kv_heads <= 0 || d->head_dim <= 0 || d->heads % d->kv_heads)
+        return fail(MGI_ERR_INVALID_ARG, std::string(who) + ": heads, kv_heads and head_dim are positive, heads a multiple of kv_heads");
+    if (d->q_from < 0 || d->k_from < 0 || d->v_from < 0 || (d->causal != 0 && d->causal != 1) || !std::isfinite(d->scale))
+        return fail(MGI_ERR_INVALID_ARG, std::string(who) + ": first channels are at least 0, causal 0 or 1, scale finite");
+    if (d->head_dim % 8 || d->head_dim > kern::kMaxHeadDim || d->q_from % 8 || d->k_from % 8 || d->v_from % 8)
+        return fail(MGI_ERR_UNSUPPORTED, std::string(who) + ": head_dim and first channels are multiples of 8, head_dim at most " +
+                                             std::to_string(kern::kMaxHeadDim));
+    const Shape xq = g->ops[q].out, xk = g->ops[k].out, xv = g->ops[v].out;
+    const long dim = d->head_dim;
+    if (d->q_from + d->heads * dim > xq.c || d->k_from + d->kv_heads * dim > xk.c || d->v_from + d->kv_heads * dim > xv.c)
+        return fail(MGI_ERR_SHAPE, std::string(who) + ": heads past the last channel");
+    if (xk.n != xv.n || xk.h != xv.h || xk.w != xv.w)
+        return fail(MGI_ERR_SHAPE, std::string(who) + ": k and v differ in n, h or w");
+    GOp op;
+    op.kind = OpKind::Attention;
+    op.in = {q, k, v};
+    op.out = xq;
+    op.out.c = (int)(d->heads * dim);
+    if (!countable(xq) || !countable(xk) || !countable(xv) || !countable(op.out))
+        return fail(MGI_ERR_UNSUPPORTED, std::string(who) + ": tensor too large");
+    if (bounds == -1) {
+        if (k_bounds != -1) return fail(MGI_ERR_INVALID_ARG, std::string(who) + ": k_bounds without bounds");
+        if (xq.n != xk.n) return fail(MGI_ERR_SHAPE, std::string(who) + ": q and k differ in n");
+    } else {
+        if ((s = check_index_input(g, bounds, who, "bounds"))) return s;
+        const size_t nb = g->ops[bounds].out.elems();
+        if (nb < 2) return fail(MGI_ERR_SHAPE, std::string(who) + ": at least two bounds");
+        if (nb > (size_t)kern::kMaxSequences + 1)
+            return fail(MGI_ERR_UNSUPPORTED, std::string(who) + ": at most " + std::to_string(kern::kMaxSequences) + " sequences");
+        op.in.push_back(bounds);
+        if (k_bounds != -1) {
+            if ((s = check_index_input(g, k_bounds, who, "k_bounds"))) return s;
+            if (g->ops[k_bounds].out.elems() != nb) return fail(MGI_ERR_SHAPE, std::string(who) + ": as many k_bounds as bounds");
+            op.in.push_back(k_bounds);
+        } else if (xq.pixels() != xk.pixels()) {
+            return fail(MGI_ERR_SHAPE, std::string(who) + ": q and k differ in pixels, and there are no k_bounds");
+        }
+    }
+    op.attention = *d;
+    // (the kernel counts query rows of a group of heads in an int)
+    if ((unsigned __int128)xq.pixels() * (d->heads / d->kv_heads) > INT_MAX / 2)
+        return fail(MGI_ERR_UNSUPPORTED, std::string(who) + ": too many queries");
+    return push(g, std::move(op), out);
+    MGI_ABI_CATCH("mgi_graph_add_attention")
+}
+
+namespace {
+
+mgi_status mark_output(mgi_graph *g, int id, int dtype, const char *who) {
+    mgi_status s = check_tensor(g, id, who);
     if (s) return s;
     if (g->ops[id].kind == OpKind::Input)
-        return fail(MGI_ERR_UNSUPPORTED, "mgi_graph_mark_output: a graph input cannot be an output");
+        return fail(MGI_ERR_UNSUPPORTED, std::string(who) + ": a graph input cannot be an output");
     for (int t : g->outputs)
-        if (t == id) return fail(MGI_ERR_INVALID_ARG, "mgi_graph_mark_output: already an output");
+        if (t == id) return fail(MGI_ERR_INVALID_ARG, std::string(who) + ": already an output");
     g->outputs.push_back(id);
+    g->output_dtypes.push_back(dtype);
     return MGI_OK;
+}
+
+}  // namespace
+
+extern "C" mgi_status mgi_graph_mark_output(mgi_graph *g, int id) {
+    MGI_ABI_TRY
+    return mark_output(g, id, MGI_DTYPE_FP32, "mgi_graph_mark_output");
     MGI_ABI_CATCH("mgi_graph_mark_output")
+}
+
+extern "C" mgi_status mgi_graph_mark_output_as(mgi_graph *g, int id, int dtype) {
+    MGI_ABI_TRY
+    const char *who = "mgi_graph_mark_output_as";
+    if (dtype != MGI_DTYPE_FP32 && dtype != MGI_DTYPE_FP16 && dtype != MGI_DTYPE_BF16)
+        return fail(MGI_ERR_UNSUPPORTED, std::string(who) + ": outputs are fp32, fp16 or bf16");
+    mgi_status s = check_tensor(g, id, who);
+    if (s) return s;
+    const OpKind k = g->ops[id].kind;
+    if (dtype != MGI_DTYPE_FP32 && (k == OpKind::FC || k == OpKind::FcInt4 || k == OpKind::Softmax || k == OpKind::Argmax ||
+                                    k == OpKind::TopK || k == OpKind::LogProb || k == OpKind::Entropy))
+        return fail(MGI_ERR_UNSUPPORTED, std::string(who) + ": tensor " + std::to_string(id) + " is not stored in 16 bits");
+    return mark_output(g, id, dtype, who);
+    MGI_ABI_CATCH("mgi_graph_mark_output_as")
 }
 
 extern "C" void mgi_options_default(mgi_options *o) {

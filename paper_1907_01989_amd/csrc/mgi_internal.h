@@ -41,7 +41,8 @@ namespace mgi {
 
 enum class OpKind {
     Input, Conv2d, Depthwise, Add, Activation, GlobalAvgPool, FC, Softmax, Concat,
-    ResizeBilinear, Argmax, Pad, FcInt4, TopK, LogProb, Entropy
+    ResizeBilinear, Argmax, Pad, FcInt4, TopK, LogProb, Entropy, RmsNorm, Quantize, PointwiseFp8,
+    Rotary, Attention
 };
 
 struct Shape {
@@ -61,8 +62,14 @@ struct GOp {
     int oh = 0, ow = 0, align_corners = 1;  // ResizeBilinear
     int cout = 0;               // FC, FcInt4
     int group = 0;              // FcInt4: input channels per scale (the scales are in w)
-    std::vector<uint8_t> codes, zeros;  // FcInt4: packed codes as given, zero points (empty: 8)
+    std::vector<uint8_t> codes, zeros;  // FcInt4: packed codes as given, zero points (empty: 8); PointwiseFp8: codes
     int k = 0;                  // TopK
+    float eps = 0.0f;           // RmsNorm
+    bool to8 = false;           // RmsNorm: the output is held in 8 bits
+    mgi_rotary_desc rotary{};
+    std::vector<int> axes;      // Rotary: axis and frequency of each pair
+    std::vector<double> freqs;
+    mgi_attention_desc attention{};
     int pads[4] = {0, 0, 0, 0}; // Pad: top, bottom, left, right
     std::vector<float> w, b;    // weights as given (OHWI / CHW / COUT x CIN), bias
 };
@@ -72,13 +79,18 @@ struct GOp {
 struct mgi_graph {
     std::vector<mgi::GOp> ops;
     std::vector<int> outputs;
+    std::vector<int> output_dtypes;   // of each: FP32, or the 16-bit type asked for
     std::vector<int> inputs;  // tensor ids of Input ops, in declaration order
 };
 
 namespace mgi {
 
 // Storage classes of materialised tensors.
-enum class Layout { C8, F32, I32, NHWC_IN };
+// Q8: an 8-bit tensor, codes in slices of 16 channels [slices][pixels][16] (whole
+// blocks of 128 channels, zeros past the last channel), then the exponents, one
+// byte (e + 127) to a block, four blocks to a word: [words][pixels].
+// H16: a graph output in the storage type (NHWC).
+enum class Layout { C8, F32, I32, NHWC_IN, Q8, H16 };
 enum class Loc { Arena, Input, Output };
 
 struct Buf {
@@ -103,7 +115,8 @@ struct Buf {
 
 enum class NodeKind {
     Ingest, Stem, Gemm, Depthwise, Add, Act, Gap, FC, Softmax, Concat, Resize, Argmax,
-    ResizeArgmax, Export, Pad, DwPw, PwDw, StemDw, GemmPool, FcSoftmax, Irb, FcInt4, Answers
+    ResizeArgmax, Export, Pad, DwPw, PwDw, StemDw, GemmPool, FcSoftmax, Irb, FcInt4, Answers,
+    Norm, PwFp8, Rotary, Attention
 };
 
 // Tile shape of the MFMA GEMM (pointwise, implicit-GEMM convolution, FC).
@@ -129,13 +142,14 @@ struct Node {
     std::vector<int> in;    // buffer ids
     int out = -1;           // buffer id
     int residual = -1;      // buffer id (Gemm / Stem epilogue), -1 = none
-    // Gemm: the fp32 graph output (buffer id) of the Export node that this
+    // Gemm, Norm, PwFp8, Rotary, Attention: the graph output (buffer id) of the Export node that this
     // node's kernel writes itself, -1 = none; whether anything else reads the
     // sliced output (no: it is not stored)
     int direct_out = -1;
     bool sliced_read = true;
     // Export: absorbed that way; Concat: its operands are views of its output
     bool absorbed = false;
+    bool absorbed_aligned = false;   // Export: ... in runs whose output is on a 16-byte boundary
     // Ingest: the nodes that read its output, all of which can read the graph
     // input itself (in some configuration); the bit of the run's mask that says
     // whether they do
@@ -188,6 +202,19 @@ struct Node {
     // segments of a row found
     kern::AnswersGeom an_geo{};
     int k = 0, out_top = -1, out_entropy = -1;
+    // Norm (rms_norm, quantize): the buffer of the sum it makes of its two
+    // operands (-1: one operand, no sum), the fp32 or 16-bit graph output that
+    // its kernel writes itself, and whether anything else reads the sum;
+    // whether it norms, whether its output is in 8 bits
+    int out_sum = -1, direct_sum = -1;
+    bool sum_read = true, norm = false, to8 = false;
+    float eps = 0.0f;
+    // Rotary, Attention
+    mgi_rotary_desc rotary{};
+    mgi_attention_desc attention{};
+    kern::AttentionGeom at_geo{};
+    kern::PwFp8Geom p8_geo{};
+    size_t s_off = 0;           // PwFp8: the blocks' scales
     int n_lists = 0, list_in[kern::kAnswerLists] = {}, list_out[kern::kAnswerLists] = {};
     // Irb (a PwDw node that also runs the pointwise projection reading its
     // output): the projection's graph op, packed weights, GEMM geometry and

@@ -7,6 +7,7 @@
 // the caller's outputs.
 #include <hip/hip_runtime.h>
 
+#include <cmath>
 #include <cstdint>
 #include <cstring>
 
@@ -446,7 +447,8 @@ hipError_t launch_fcint4_node(const mgi_plan &p, const Node &nd, const Bases &B,
     if (x.in_place) {
         q.cin = xb.shape.c;
         q.fp16_in = p.bufs[xb.direct_src].in_dtype == MGI_DTYPE_FP16;
-        if (q.cin % 8 != 0 || !q.fp16_in || p.opt.dtype != MGI_DTYPE_FP16) q.xin = x.x;
+        const bool stored = p.bufs[xb.direct_src].in_dtype == p.opt.dtype;   // (in whole slices: 16-byte elements as stored)
+        if (q.cin % 8 != 0 || !stored) q.xin = x.x;
     }
     q.zero = (const h8 *)(wbase + p.zero_off);
     q.w = (const uint32_t *)(wbase + nd.w_off);
@@ -489,6 +491,120 @@ hipError_t launch_answers_node(const mgi_plan &p, const Node &nd, const Bases &B
     return launch_answers(q, nd.an_geo, st);
 }
 
+// The distances of a sliced operand of an attention block, from channel `from` on.
+TokenIn token_in(const mgi_plan &p, int b, const Bases &B, int from = 0) {
+    const Operand o = operand(p, b, B);
+    return {o.x + (size_t)(from / 8) * o.s, o.s, o.p};
+}
+
+// Whether an absorbed export's output is written by its producer in this run.
+bool writes_output(const mgi_plan &p, int out, const Bases &B) {
+    return out >= 0 && B.direct && ((uintptr_t)buf_ptr(p, out, B) & 15) == 0;
+}
+
+// Where a node's kernel writes buffer b: the graph output `direct`, or b itself.
+TokenOut token_out(const mgi_plan &p, int b, int direct, const Bases &B) {
+    const Shape s = p.bufs[b].shape;
+    if (writes_output(p, direct, B)) return {buf_ptr(p, direct, B), 1, slices(s.c), p.bufs[direct].layout == Layout::F32};
+    return {buf_ptr(p, b, B), (int)s.pixels(), 1, 0};
+}
+
+Tensor8 tensor8(const mgi_plan &p, int b, const Bases &B) {
+    uint8_t *at = (uint8_t *)buf_ptr(p, b, B);
+    const Shape s = p.bufs[b].shape;
+    return {at, (uint32_t *)(at + Tensor8::codes_bytes(s.pixels(), s.c))};
+}
+
+hipError_t launch_norm_node(const mgi_plan &p, const Node &nd, const Bases &B, hipStream_t st) {
+    const char *wbase = static_cast<const char *>(p.dev_w);
+    const Shape x = p.bufs[nd.out].shape;
+    NormParams q{};
+    q.a = token_in(p, nd.in[0], B);
+    if (nd.out_sum >= 0) {
+        q.b = token_in(p, nd.in[1], B);
+        q.act = nd.act1;
+        q.sum = token_out(p, nd.out_sum, nd.direct_sum, B);
+    }
+    if (nd.norm) q.w = (const float *)(wbase + nd.w_off);
+    q.eps = nd.eps;
+    q.inv_c = 1.0f / x.c;
+    q.to8 = nd.to8;
+    if (nd.to8 && !writes_output(p, nd.direct_out, B)) q.q = tensor8(p, nd.out, B);
+    else q.out = token_out(p, nd.out, nd.direct_out, B);
+    q.M = (int)x.pixels();
+    q.S = slices(x.c);
+    q.KB = (x.c + 127) / 128;
+    q.bf16 = p.opt.dtype == MGI_DTYPE_BF16;
+    return launch_norm(q, st);
+}
+
+hipError_t launch_pwfp8_node(const mgi_plan &p, const Node &nd, const Bases &B, hipStream_t st) {
+    const char *wbase = static_cast<const char *>(p.dev_w);
+    const Shape y = p.bufs[nd.out].shape;
+    PwFp8Params q{};
+    q.x = tensor8(p, nd.in[0], B);
+    q.w = (const uint8_t *)(wbase + nd.w_off);
+    q.scales = (const float *)(wbase + nd.s_off);
+    q.bias = (const float *)(wbase + nd.b_off);
+    q.y = token_out(p, nd.out, nd.direct_out, B);
+    q.M = (int)y.pixels();
+    q.kb = nd.ksp;
+    q.nb16 = nd.nb16;
+    q.ns = slices(y.c);
+    q.act = nd.act1;
+    q.bf16 = p.opt.dtype == MGI_DTYPE_BF16;
+    return launch_pwfp8(q, nd.p8_geo, st);
+}
+
+hipError_t launch_rotary_node(const mgi_plan &p, const Node &nd, const Bases &B, hipStream_t st) {
+    const char *wbase = static_cast<const char *>(p.dev_w);
+    const mgi_rotary_desc &d = nd.rotary;
+    const Shape y = p.bufs[nd.out].shape;
+    RotaryParams q{};
+    q.x = token_in(p, nd.in[0], B, d.from);
+    q.y = token_out(p, nd.out, nd.direct_out, B);
+    if (nd.in.size() > 1) {
+        q.pos = (const int *)buf_ptr(p, nd.in[1], B);
+        q.axes = p.bufs[nd.in[1]].shape.c;
+    }
+    q.freq = (const uint64_t *)(wbase + nd.w_off);
+    q.axis = (const int *)(wbase + nd.b_off);
+    q.M = (int)y.pixels(); q.H = y.h; q.W = y.w;
+    q.heads = d.heads; q.d8 = d.head_dim / 8; q.pairs = d.pairs; q.adjacent = d.adjacent;
+    q.inv_w = 1.0 / y.w; q.inv_h = 1.0 / y.h;
+    q.bf16 = p.opt.dtype == MGI_DTYPE_BF16;
+    return launch_rotary(q, st);
+}
+
+hipError_t launch_attention_node(const mgi_plan &p, const Node &nd, const Bases &B, hipStream_t st) {
+    const mgi_attention_desc &d = nd.attention;
+    const Shape y = p.bufs[nd.out].shape, k = p.bufs[nd.in[1]].shape;
+    AttentionParams q{};
+    q.q = token_in(p, nd.in[0], B, d.q_from);
+    q.k = token_in(p, nd.in[1], B, d.k_from);
+    q.v = token_in(p, nd.in[2], B, d.v_from);
+    q.y = token_out(p, nd.out, nd.direct_out, B);
+    q.nseq = y.n;
+    q.tq = y.h * y.w;
+    q.tk = k.h * k.w;
+    if (nd.in.size() > 3) {
+        q.bq = (const int *)buf_ptr(p, nd.in[3], B);
+        if (nd.in.size() > 4) q.bk = (const int *)buf_ptr(p, nd.in[4], B);
+        q.nseq = (int)p.bufs[nd.in[3]].shape.elems() - 1;
+        q.tq = (int)y.pixels();
+        q.tk = (int)k.pixels();
+    }
+    q.kv_heads = d.kv_heads; q.group = d.heads / d.kv_heads; q.d8 = d.head_dim / 8;
+    q.causal = d.causal;
+    q.scale = (float)((d.scale == 0.0f ? 1.0 / std::sqrt((double)d.head_dim) : (double)d.scale) * 1.4426950408889634);
+    if (nd.scratch >= 0) {
+        q.part = (float *)buf_ptr(p, nd.scratch, B);
+        q.cnt = (int *)(B.ws + nd.cnt_off);
+    }
+    q.bf16 = p.opt.dtype == MGI_DTYPE_BF16;
+    return launch_attention(q, nd.at_geo, st);
+}
+
 // A node that launches nothing in this run: a timed run's events are still
 // recorded.
 hipError_t mark_events(hipStream_t st) {
@@ -509,6 +625,8 @@ hipError_t launch_node(const mgi_plan &p, const Node &nd, const Bases &B, hipStr
         case NodeKind::Ingest: {
             if (operand(p, nd.out, B).in_place) return mark_events(st);
             const Buf &ib = p.bufs[nd.in[0]];
+            if (ib.in_dtype == MGI_DTYPE_BF16)
+                return launch_ingest16(buf_ptr(p, nd.in[0], B), (h8 *)y, (int)ib.shape.pixels(), ib.shape.c, st);
             return launch_ingest(buf_ptr(p, nd.in[0], B), ib.in_dtype == MGI_DTYPE_FP16, (h8 *)y,
                                  (int)ib.shape.pixels(), ib.shape.c, bf, st);
         }
@@ -615,6 +733,14 @@ hipError_t launch_node(const mgi_plan &p, const Node &nd, const Bases &B, hipStr
                               (const h8 *)(wbase + p.zero_off), ib.shape.n,
                               ib.shape.h * ib.shape.w, slices(ib.shape.c), bf, st);
         }
+        case NodeKind::Norm:
+            return launch_norm_node(p, nd, B, st);
+        case NodeKind::PwFp8:
+            return launch_pwfp8_node(p, nd, B, st);
+        case NodeKind::Rotary:
+            return launch_rotary_node(p, nd, B, st);
+        case NodeKind::Attention:
+            return launch_attention_node(p, nd, B, st);
         case NodeKind::FcInt4:
             return launch_fcint4_node(p, nd, B, y, st);
         case NodeKind::Answers:
@@ -662,8 +788,12 @@ hipError_t launch_node(const mgi_plan &p, const Node &nd, const Bases &B, hipStr
                                  (int)ib.shape.pixels(), slices(ib.shape.c), ib.shape.c, bf, st);
         }
         case NodeKind::Export: {
-            if (nd.absorbed && B.direct) return mark_events(st);
+            if (nd.absorbed && (nd.absorbed_aligned ? writes_output(p, nd.out, B) : B.direct)) return mark_events(st);
             const Buf &ib = p.bufs[nd.in[0]];
+            if (ib.layout == Layout::Q8)
+                return launch_export8(tensor8(p, nd.in[0], B), y, ob.layout == Layout::F32, (int)ib.shape.pixels(), ib.shape.c, bf, st);
+            if (ob.layout == Layout::H16)
+                return launch_export16((const h8 *)buf_ptr(p, nd.in[0], B), y, (int)ib.shape.pixels(), ib.shape.c, st);
             return launch_export((const h8 *)buf_ptr(p, nd.in[0], B), (float *)y,
                                  (int)ib.shape.pixels(), ib.shape.c, bf, st);
         }
@@ -1074,7 +1204,10 @@ extern "C" mgi_status mgi_plan_read_node(mgi_plan *p, int i, void *dev_dst, void
     if (b.loc == Loc::Input) return fail(MGI_ERR_STATE, "mgi_plan_read_node: input buffer");
     void *src = buf_ptr(*p, nd.out, B);
     hipError_t e;
-    if (b.layout == Layout::C8) {
+    if (b.layout == Layout::Q8) {
+        e = launch_export8(tensor8(*p, nd.out, B), dev_dst, true, (int)b.shape.pixels(), b.shape.c,
+                           p->opt.dtype == MGI_DTYPE_BF16, st);
+    } else if (b.layout == Layout::C8) {
         e = launch_export((const h8 *)src, (float *)dev_dst, (int)b.shape.pixels(), b.shape.c,
                           p->opt.dtype == MGI_DTYPE_BF16, st);
     } else {

@@ -31,7 +31,8 @@ def _torch_types():
     """Element type code -> torch dtype (torch is imported on first use)."""
     if not _TORCH_TYPES:
         import torch
-        _TORCH_TYPES.update({B.DTYPE_FP16: torch.float16, B.DTYPE_FP32: torch.float32, B.DTYPE_INT32: torch.int32})
+        _TORCH_TYPES.update({B.DTYPE_FP16: torch.float16, B.DTYPE_BF16: torch.bfloat16, B.DTYPE_FP32: torch.float32,
+                             B.DTYPE_INT32: torch.int32})
     return _TORCH_TYPES
 
 
@@ -46,6 +47,8 @@ def _channels(ops, t):
         return 1
     if op["op"] == "topk":
         return op["k"]
+    if op["op"] in ("rotary", "attention"):
+        return op["heads"] * op["head_dim"]
     return op["cout"] if "cout" in op else _channels(ops, op.get("index", op.get("in", op.get("a"))))
 
 
@@ -72,8 +75,48 @@ def _add_fc_int4(g, ops, op):
     return B.mgi_graph_add_fc_int4(g, op["in"], cout, group, op["q"], op["scales"], op.get("zeros"), op.get("b"))
 
 
+def _sized(name, key, a, size, dtype=None):
+    if np.size(a) != size:
+        raise ValueError(f"{name}: {key} must hold {size} values, got {np.size(a)}")
+    if dtype is not None and np.asarray(a).dtype != dtype:
+        raise ValueError(f"{name}: {key} must be {np.dtype(dtype).name}, got {np.asarray(a).dtype}")
+
+
+def _add_tokens(g, ops, op):
+    """An attention block's operator.  The library receives raw pointers: arrays of
+    other sizes are refused here, for operands that are earlier tensors (the library
+    refuses others before it reads an array)."""
+    k = op["op"]
+    known = 0 <= op.get("in", 0) < len(ops)
+    if k == "rms_norm":
+        if known and op.get("w") is not None:
+            _sized(k, "w", op["w"], _channels(ops, op["in"]))
+        return B.mgi_graph_add_rms_norm(g, op["in"], op.get("w"), op.get("eps", 1e-6), op.get("to8", False))
+    if k == "quantize":
+        return B.mgi_graph_add_quantize(g, op["in"])
+    if k == "pointwise_fp8":
+        cout = op["cout"]
+        if known and cout > 0:
+            cin = _channels(ops, op["in"])
+            _sized(k, "q", op["q"], cout * cin, np.uint8)
+            _sized(k, "scales", op["scales"], -(-cout // 128) * -(-cin // 128))
+            if op.get("b") is not None:
+                _sized(k, "b", op["b"], cout)
+        return B.mgi_graph_add_pointwise_fp8(g, op["in"], cout, op["q"], op["scales"], op.get("b"),
+                                             op.get("act", B.ACT_NONE))
+    if k == "rotary":
+        _sized(k, "freqs", op["freqs"], len(op["axes"]))
+        return B.mgi_graph_add_rotary(g, op["in"], op["heads"], op["head_dim"], list(op["axes"]), list(op["freqs"]),
+                                      op.get("positions", -1), op.get("from", 0), op.get("adjacent", False))
+    return B.mgi_graph_add_attention(g, op["q"], op["k"], op["v"], op["heads"], op["kv_heads"], op["head_dim"],
+                                     op.get("causal", False), op.get("scale", 0.0), op.get("bounds", -1),
+                                     op.get("k_bounds", -1), op.get("q_from", 0), op.get("k_from", 0),
+                                     op.get("v_from", 0))
+
+
 def build_graph(desc):
-    """Create an mgi graph from ``desc`` (dict with "ops" and "outputs").
+    """Create an mgi graph from ``desc`` (dict with "ops" and "outputs", and with
+    "output_dtypes", {tensor id: element type}, for outputs in the storage type).
     Returns the graph handle; tensor ids equal op indices."""
     g = B.mgi_graph_create()
     try:
@@ -120,12 +163,15 @@ def build_graph(desc):
                 t = B.mgi_graph_add_log_prob(g, op["in"], op["index"])
             elif k == "entropy":
                 t = B.mgi_graph_add_entropy(g, op["in"])
+            elif k in ("rms_norm", "quantize", "pointwise_fp8", "rotary", "attention"):
+                t = _add_tokens(g, desc["ops"][:i], op)
             else:
                 raise ValueError(f"unknown op {k}")
             if t != i:
                 raise RuntimeError(f"tensor id {t} != op index {i}")
+        types = desc.get("output_dtypes", {})
         for t in desc["outputs"]:
-            B.mgi_graph_mark_output(g, t)
+            B.mgi_graph_mark_output_as(g, t, types[t]) if t in types else B.mgi_graph_mark_output(g, t)
     except Exception:
         B.mgi_graph_destroy(g)
         raise
@@ -189,7 +235,7 @@ class Plan:
         outs = []
         for t, (shape, dt, _) in zip(self.desc["outputs"], self.outputs_info):
             n, h, w, c = shape
-            tdt = torch.int32 if dt == B.DTYPE_INT32 else torch.float32
+            tdt = _torch_types()[dt]
             if dt == B.DTYPE_INT32 and self.desc["ops"][t]["op"] == "argmax":
                 outs.append(torch.empty((n, h, w), dtype=tdt, device=self.device))
             elif h == 1 and w == 1:
@@ -211,10 +257,8 @@ class Plan:
             raise ValueError(f"plan takes {self.n_inputs} inputs and {self.n_outputs} outputs, "
                              f"got {len(inputs)} and {len(outputs)}")
         dev = torch.device(self.device)
-        in_types = {B.DTYPE_FP16: torch.float16, B.DTYPE_FP32: torch.float32, B.DTYPE_INT32: torch.int32}
-        out_types = {B.DTYPE_INT32: torch.int32, B.DTYPE_FP32: torch.float32}
-        for role, ts, info, types in (("input", inputs, self.inputs_info, in_types),
-                                      ("output", outputs, self.outputs_info, out_types)):
+        types = _torch_types()
+        for role, ts, info in (("input", inputs, self.inputs_info), ("output", outputs, self.outputs_info)):
             for i, (x, (shape, dt, nbytes)) in enumerate(zip(ts, info)):
                 if not isinstance(x, torch.Tensor):
                     raise ValueError(f"{role} {i}: expected a torch tensor, got {type(x).__name__}")
@@ -295,7 +339,7 @@ class Plan:
         xs = []
         for op in self.desc["ops"]:
             if op["op"] == "input":
-                dt = torch.float16 if op.get("dtype", B.DTYPE_FP32) == B.DTYPE_FP16 else torch.float32
+                dt = _torch_types()[op.get("dtype", B.DTYPE_FP32)]
                 xs.append(torch.from_numpy(np.ascontiguousarray(op["data"])).to(self.device, dt))
             elif op["op"] == "index_input":
                 xs.append(torch.from_numpy(np.ascontiguousarray(op["data"], dtype=np.int32)).to(self.device))

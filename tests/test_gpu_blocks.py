@@ -1,0 +1,217 @@
+"""The attention block's operators together, as a program has them: a norm in 8
+bits, one layer for queries, keys and values, rotary positions, attention, the
+layer behind it, the residual and the next norm; eager, captured and replayed, in
+the no-allocation workspace, on another stream, and with buffers of every kind."""
+import numpy as np
+import pytest
+
+import oracle
+from gpu_util import log
+
+pytestmark = pytest.mark.gpu
+
+HEADS, KV, DIM, C = 4, 2, 32, 96
+
+
+def block(dtype, n=2, h=5, w=7, src=None, bounds=None, seed=0):
+    from block_util import builder, given, stored
+    b = builder(seed + 5)
+    x = given(b, stored(np.random.default_rng(seed).standard_normal((n, h, w, C)), dtype), dtype if src is None else src)
+    tokens = b.rms_norm(x, to8=True)
+    qkv = b.pointwise_fp8(tokens, (HEADS + 2 * KV) * DIM)
+    b.ops[qkv]["scales"] = b.ops[qkv]["scales"] * 0.5
+    half = DIM // 2
+    turned = b.rotary(qkv, HEADS + KV, DIM, [1 + i % 2 for i in range(half)], [0.5 ** i for i in range(half)])
+    extra = {} if bounds is None else {"bounds": b.index_input(np.asarray(bounds).reshape(1, 1, 1, -1))}
+    y = b.attention(turned, turned, qkv, HEADS, KV, DIM, k_from=HEADS * DIM, v_from=(HEADS + KV) * DIM, **extra)
+    o = b.pointwise_fp8(b.quantize(y), C)
+    s = b.add(x, o, act=0)
+    z = b.rms_norm(s)
+    return b, dict(x=x, tokens=tokens, qkv=qkv, turned=turned, y=y, o=o, s=s, z=z)
+
+
+def plan_of(b, outputs, dtype, **kw):
+    from paper_1907_01989_amd import engine
+    return engine.Plan({"name": "block", "ops": b.ops, "outputs": outputs, "output_dtypes": {t: dtype for t in outputs}}, dtype=dtype, **kw)
+
+
+@pytest.mark.parametrize("dtype,src", [(0, 0), (1, 1), (1, 2)])
+def test_block(dtype, src):
+    from block_util import HALF, run
+    b, t = block(dtype, src=src)
+    log(f"[case] block type {dtype} from {src}")
+    want = [t[k] for k in ("qkv", "turned", "y", "o", "s", "z")]
+    got, plan = run(b, want, dtype)
+    # each operator on the operands that the plan itself made (the norm's codes are tested alone)
+    vals = dict(zip(want, got))
+    vals[t["x"]] = np.asarray(b.ops[t["x"]]["data"])
+    for k in ("turned", "y", "s", "z"):
+        op = b.ops[t[k]]
+        ref = oracle.eval_op(op, [vals[u] for u in oracle.op_inputs(op)])
+        # one rounding to 16 bits, one of the weights, and fp32
+        assert np.abs(vals[t[k]] - ref).max() <= (2 * HALF[dtype] + 2.0 ** -12) * np.abs(ref).max(), k
+    ref = oracle.eval_op(b.ops[t["o"]], [oracle.quantize(vals[t["y"]])])
+    assert np.abs(vals[t["o"]] - ref).max() <= 2 * HALF[dtype] * np.abs(ref).max()
+    assert [i["kind"] for i in plan.nodes() if i["kind"] not in ("export", "ingest")] == [
+        "rms_norm", "pointwise_fp8", "rotary", "attention", "quantize", "pointwise_fp8", "add_rms_norm"]
+    # unfused, with every tensor kept: the same bits
+    again, _ = run(b, want, dtype, fuse=False)
+    kept, plan = run(b, want, dtype, materialize_all=True)
+    for a, c, d in zip(got, again, kept):
+        np.testing.assert_array_equal(a, c)
+        np.testing.assert_array_equal(a, d)
+
+
+def test_packed_block_replayed_and_without_allocation():
+    import torch
+    from block_util import inputs
+    from paper_1907_01989_amd import _binding as B
+    # rows of keys long enough to be shared by several workgroups
+    b, t = block(0, 1, 1, 3001, bounds=[0, 2990, 2991, 2991, 3000])
+    outs = [t["z"], t["y"]]
+    plan = plan_of(b, outs, 0)
+    xs = inputs(plan)
+    log("[case] block replayed")
+    eager = [o.clone() for o in plan.run(xs)]
+    assert all(torch.isfinite(o).all() for o in eager) and (eager[1].reshape(3001, -1)[3000:] == 0).all()
+    g = plan.capture(xs)
+    other = plan_of(b, outs, 0)
+    xs2 = [x if x.dtype == torch.int32 else x * 0.5 for x in xs]
+    ref2 = [o.clone() for o in other.run(xs2)]
+    h = other.capture(xs2)
+    for _ in range(4):
+        for o in list(g) + list(h):
+            o.fill_(-3)
+        plan.replay()
+        other.replay()
+        more = plan.run(xs)
+        torch.cuda.synchronize()
+        for a, c, d in zip(g, eager, more):
+            assert torch.equal(a, c) and torch.equal(d, c)
+        for a, c in zip(h, ref2):
+            assert torch.equal(a, c)
+    # new values in the same buffers
+    xs[0].copy_(xs2[0])
+    plan.replay()
+    torch.cuda.synchronize()
+    for a, c in zip(g, ref2):
+        assert torch.equal(a, c)
+    outs = plan.alloc_outputs()
+    for _ in range(2):
+        for o in outs:
+            o.fill_(7)
+        B.mgi_plan_run_noalloc(plan.handle, [x.data_ptr() for x in xs], [o.data_ptr() for o in outs],
+                               torch.cuda.current_stream().cuda_stream)
+        torch.cuda.synchronize()
+        for a, c in zip(outs, ref2):
+            assert torch.equal(a, c)
+
+
+def test_another_stream_and_many_runs():
+    import torch
+    from block_util import inputs
+    b, t = block(1, 1, 1, 2500, seed=3)
+    plan = plan_of(b, [t["z"]], 1)
+    xs = inputs(plan)
+    ref = plan.run(xs)[0].clone()
+    torch.cuda.synchronize()
+    st = torch.cuda.Stream()
+    log("[case] block on another stream")
+    with torch.cuda.stream(st):
+        outs = [plan.run(xs)[0] for _ in range(5)]
+    st.synchronize()
+    for o in outs:
+        assert torch.equal(o, ref)
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+def test_buffers_off_16_bytes(dtype):
+    import torch
+    from block_util import inputs
+    b, t = block(dtype, 1, 6, 6)
+    outs = [t["y"], t["s"], t["z"], t["turned"]]
+    plan = plan_of(b, outs, dtype)
+    xs = inputs(plan)
+    ref = [o.clone() for o in plan.run(xs)]
+    log(f"[case] block, buffers off 16 bytes, type {dtype}")
+
+    def off(x, fill=None):
+        y = torch.full((x.numel() + 9,), 3.0, dtype=x.dtype, device=x.device)
+        v = y[1:x.numel() + 1].view(x.shape)
+        v.copy_(x if fill is None else torch.full_like(x, fill))
+        return y, v
+
+    ys = [off(r, -1) for r in ref]
+    plan.run([off(x)[1] for x in xs], [v for _, v in ys])
+    torch.cuda.synchronize()
+    for (whole, v), r in zip(ys, ref):
+        assert torch.equal(v, r)
+        assert (whole[:1] == 3).all() and (whole[r.numel() + 1:] == 3).all()
+
+
+def test_outputs_over_inputs():
+    import torch
+    from block_util import builder, given, inputs, stored
+    from paper_1907_01989_amd import _binding as B, engine
+    x = stored(np.random.default_rng(2).standard_normal((1, 4, 8, 64)), 0)
+    b = builder()
+    t = b.rms_norm(given(b, x, 0))
+    plan = engine.Plan({"ops": b.ops, "outputs": [t], "output_dtypes": {t: 0}})
+    xs = inputs(plan)
+    ref = plan.run(xs)[0].clone()
+    log("[case] in place")
+    plan.run(xs, [xs[0]])                                  # in place: by conversions
+    torch.cuda.synchronize()
+    assert torch.equal(xs[0], ref)
+    # positions and bounds are read while outputs are written: refused
+    b = builder()
+    xi = given(b, x, 0)
+    p = b.index_input(np.zeros((1, 4, 8, 1), np.int32))
+    t = b.rotary(xi, 1, 64, [0] * 32, [1.0] * 32, positions=p)
+    plan = engine.Plan({"ops": b.ops, "outputs": [t], "output_dtypes": {t: 0}})
+    xs = inputs(plan)
+    with pytest.raises(B.MgiError, match="overlaps"):
+        plan.run(xs, [xs[0]])
+
+
+def test_bf16_inputs_of_other_operators():
+    # a stem, a depthwise layer, a convolution, a 4-bit layer, a pool and questions, from bf16 and from fp32 arrays
+    import workloads
+    from workloads import NetBuilder
+    from gpu_util import run_gpu
+
+    def net(dtype):
+        b = NetBuilder(seed=4)
+        a = b.input(2, 12, 12, 3, -1, 1, dtype=dtype)
+        c = b.input(2, 8, 8, 24, -1, 1, dtype=dtype)
+        d = b.input(2, 1, 1, 64, -1, 1, dtype=dtype)
+        e = b.input(2, 1, 1, 37, -1, 1, dtype=dtype)
+        outs = [b.conv(a, 16, 3, 2), b.dw(c), b.conv(c, 40, 3), b.fc_int4(d, 50), b.fc_int4(e, 50), b.gap(c), b.topk(d, 3),
+                b.entropy(e), b.softmax(e)]
+        for o in outs:
+            b.mark_output(o)
+        return workloads.as_bf16_graph(b.graph("bf16_inputs"))
+
+    log("[case] bf16 inputs of other operators")
+    _, a, _ = run_gpu(net(1), materialize_all=False, dtype=1)
+    _, r, _ = run_gpu(net(2), materialize_all=False, dtype=1)
+    for x, y in zip(a, r):
+        np.testing.assert_array_equal(x, y)
+
+
+def test_16_bit_outputs_of_other_operators():
+    import torch
+    from workloads import NetBuilder
+    from paper_1907_01989_amd import engine
+    b = NetBuilder(seed=6)
+    x = b.input(2, 9, 9, 24, -1, 1)
+    outs = [b.conv(x, 30, 1), b.conv(x, 40, 3, 2), b.dw(x), b.add(x, x), b.gap(x)]
+    log("[case] 16-bit outputs of other operators")
+    for dtype, kind in ((0, torch.float16), (1, torch.bfloat16)):
+        desc = {"ops": b.ops, "outputs": outs}
+        wide = engine.Plan(desc, dtype=dtype)
+        narrow = engine.Plan({**desc, "output_dtypes": {t: dtype for t in outs}}, dtype=dtype)
+        a, c = wide.run(wide.input_tensors()), narrow.run(narrow.input_tensors())
+        torch.cuda.synchronize()
+        for p, q in zip(a, c):
+            assert q.dtype == kind and torch.equal(p, q.float())

@@ -1,0 +1,173 @@
+"""rms_norm, quantize and their fusion with add, against the oracle (64 bits).
+
+fp32 roundings of a norm: a thread adds at most 8 * 2 * 8 squares one after the
+other, then six steps across lanes and up to sixteen waves' sums, 150 half steps
+of 2^-24 relative to the sum, of which the root halves the effect; the root, the
+reciprocal and two products add less than eight: 2^-17 relative to the value
+holds them all (128 half steps).  Then one rounding to 16 bits.  A code of 8 bits
+may be that of any value within 2^-17 of the exact one.
+"""
+import numpy as np
+import pytest
+
+import oracle
+from gpu_util import log
+
+pytestmark = pytest.mark.gpu
+
+FP32 = 2.0 ** -17
+
+
+def case(n, h, w, c, seed=0, spread=1.0):
+    rng = np.random.default_rng([seed, n * h * w, c])
+    return rng.standard_normal((n, h, w, c)) * np.exp(rng.standard_normal((n, h, w, 1)) * spread)
+
+
+def check8(got, y, what):
+    """`got`: values of an 8-bit tensor of y, where y is known to FP32."""
+    lo, hi = None, None
+    for a in (1 - FP32, 1, 1 + FP32):
+        for e in (oracle.block_exponents(y * (1 - FP32)), oracle.block_exponents(y * (1 + FP32))):
+            v = oracle.quantize(y * a, e)
+            lo = v if lo is None else np.minimum(lo, v)
+            hi = v if hi is None else np.maximum(hi, v)
+    bad = ~((got >= lo) & (got <= hi))
+    assert not bad.any(), f"{what}: {int(bad.sum())} of {bad.size}, first at {np.argwhere(bad)[0]}"
+    # (nearly all are the exact one's codes)
+    assert (got != oracle.quantize(y)).mean() < 2e-3, what
+
+
+CASES = [(1, 1, 1, 8), (1, 1, 1, 1), (1, 7, 9, 24), (2, 5, 5, 136), (3, 1, 1, 128), (1, 9, 9, 1000), (1, 1, 63, 181),
+         (1, 1, 64, 120), (1, 8, 9, 2048), (1, 1, 3, 4096), (1, 1, 1, 8192), (1, 3, 25, 5000), (1, 1, 1, 16384), (1, 1, 66, 16384),
+         (5, 13, 7, 77)]
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("n,h,w,c", CASES)
+def test_norm(n, h, w, c, dtype):
+    from block_util import HALF, TINY, builder, given, run, stored, within
+    log(f"[case] norm {n}x{h}x{w}x{c} type {dtype}")
+    x = stored(case(n, h, w, c), dtype)
+    b = builder(c)
+    t = b.rms_norm(given(b, x, dtype))
+    ref = oracle.rms_norm(x, b.ops[t]["w"], b.ops[t]["eps"])
+    bound = (HALF[dtype] + FP32) * np.abs(ref) + TINY[dtype]
+    (a,), _ = run(b, [t], dtype, {t: dtype})
+    within(a, ref, bound, "16-bit output")
+    (f,), _ = run(b, [t], dtype)
+    np.testing.assert_array_equal(f, a)                  # fp32 output: the stored values
+    q = b.rms_norm(t - 1, to8=True)
+    b.ops[q]["w"] = b.ops[t]["w"]
+    (v,), _ = run(b, [q], dtype)
+    check8(v, ref, "8-bit output")
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("n,h,w,c", CASES[1::2])
+@pytest.mark.parametrize("act,to8", [(0, False), (1, True), (2, False), (0, True)])
+def test_sum_and_norm_in_one_kernel_or_two(n, h, w, c, dtype, act, to8):
+    from block_util import HALF, TINY, builder, given, run, stored, within
+    log(f"[case] sum and norm {n}x{h}x{w}x{c} type {dtype} act {act} to8 {to8}")
+    b = builder(c)
+    x, r = (stored(case(n, h, w, c, s), dtype) for s in (1, 2))
+    s = b.add(given(b, x, dtype), given(b, r, dtype))
+    b.ops[s]["act"] = act
+    t = b.rms_norm(s, to8=to8)
+    (hs, y), plan = run(b, [s, t], dtype, {s: dtype} if to8 else {s: dtype, t: dtype})
+    assert "add_rms_norm" in [i["kind"] for i in plan.nodes()]
+    total = oracle.activation(oracle.add(x, r), act)
+    within(hs, total, HALF[dtype] * (1 + FP32) * np.abs(total) + TINY[dtype], "sum")
+    ref = oracle.rms_norm(hs, b.ops[t]["w"], b.ops[t]["eps"])
+    if to8:
+        check8(y, ref, "8-bit norm")
+    else:
+        within(y, ref, (HALF[dtype] + FP32) * np.abs(ref) + TINY[dtype], "norm")
+    # the norm alone an output; no fusion: the same bits
+    (again,), _ = run(b, [t], dtype)
+    np.testing.assert_array_equal(again, y)
+    (h2, y2), plan = run(b, [s, t], dtype, fuse=False)
+    assert "rms_norm" in [i["kind"] for i in plan.nodes()]
+    np.testing.assert_array_equal(h2, hs)
+    np.testing.assert_array_equal(y2, y)
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("n,h,w,c", CASES)
+def test_quantize_is_exact(n, h, w, c, dtype):
+    from block_util import builder, given, run, stored
+    log(f"[case] quantize {n}x{h}x{w}x{c} type {dtype}")
+    x = stored(case(n, h, w, c, 3, 3.0), dtype)
+    x[..., ::5] *= 2.0 ** -9
+    x = stored(x, dtype)
+    x[..., c // 2:] = 0 if c > 300 else x[..., c // 2:]
+    b = builder()
+    t = b.quantize(given(b, x, dtype))
+    (a,), _ = run(b, [t], dtype)
+    np.testing.assert_array_equal(a, oracle.quantize(x))
+    (a,), _ = run(b, [t], dtype, materialize_all=True)
+    np.testing.assert_array_equal(a, oracle.quantize(x))
+
+
+def test_quantize_borders():
+    # blocks whose largest value is at, just under and just over 448 times a power of two; halves between codes;
+    # zeros, subnormals, the largest fp16 and values that are not finite
+    from block_util import builder, given, run, stored
+    rows = []
+    for e in (-20, -8, 0, 5):
+        for top in (448, 448.5, 447.5, 256, 224.1, 225):
+            row = np.zeros(128)
+            row[:30] = np.array([top] + [8.5, 9.5, 10.5, 11.5, 17, 19, 21, 0.015625 * 1.5, 2.0 ** -9, 2.0 ** -10, 3 * 2.0 ** -10]
+                                + list(np.linspace(-top, top, 18))) * 2.0 ** e
+            rows.append(row)
+    rows += [np.zeros(128), np.full(128, 2.0 ** -24), np.full(128, 65504.0)]
+    odd = np.linspace(-3, 3, 128)
+    odd[[3, 50]], odd[7], odd[100] = np.inf, -np.inf, np.nan
+    rows += [odd, np.full(128, np.inf)]
+    x = stored(np.stack(rows)[None, None], 0)
+    b = builder()
+    t = b.quantize(given(b, x, 0))
+    log("[case] quantize borders")
+    (a,), _ = run(b, [t], 0)
+    np.testing.assert_array_equal(a, oracle.quantize(x))
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+def test_rows_of_zeros_and_of_extremes(dtype):
+    from block_util import HALF, TINY, builder, given, run, stored, within
+    big = 60000.0 if dtype == 0 else 1e18
+    x = np.random.default_rng(5).standard_normal((1, 1, 70, 264))
+    x[0, 0, 0], x[0, 0, 1] = 0, big
+    x[0, 0, 2] *= 1e-6
+    x[0, 0, 3, 5] = np.nan
+    x[0, 0, 4, 6] = np.inf
+    x = stored(x, dtype)
+    b = builder()
+    t = b.rms_norm(given(b, x, dtype))
+    log(f"[case] extremes type {dtype}")
+    (y,), _ = run(b, [t], dtype)
+    with np.errstate(invalid="ignore"):
+        ref = oracle.rms_norm(x, b.ops[t]["w"], b.ops[t]["eps"])
+    assert (y[0, 0, 0] == 0).all()
+    # the other rows are their own
+    fine = [i for i in range(70) if i not in (3, 4)]
+    within(y[:, :, fine], ref[:, :, fine], (HALF[dtype] + FP32) * np.abs(ref[:, :, fine]) + TINY[dtype])
+    assert np.isnan(y[0, 0, 3]).all() and np.isnan(y[0, 0, 4, 6])
+
+
+def test_norm_of_tensors_inside_a_network():
+    # behind a convolution, from fp32 inputs, into a concatenation and an add
+    from block_util import HALF, builder, given, run, stored, within
+    b = builder(3)
+    x = given(b, stored(case(2, 6, 5, 24), 0), 2)
+    c = b.conv(x, 40, 1, act=0)
+    t = b.rms_norm(c)
+    o = b.concat([b.rms_norm(x), t])
+    s = b.add(t, c)
+    u = b.rms_norm(s)
+    log("[case] norms in a network")
+    (cv, tv, ov, sv, uv), _ = run(b, [c, t, o, s, u], 0)
+    ref = oracle.rms_norm(cv, b.ops[t]["w"], 1e-6)
+    within(tv, ref, (HALF[0] + FP32) * np.abs(ref) + 2.0 ** -25)
+    np.testing.assert_array_equal(ov[..., 24:], tv)
+    ref = oracle.rms_norm(sv, b.ops[u]["w"], 1e-6)
+    within(uv, ref, (HALF[0] + FP32) * np.abs(ref) + 2.0 ** -25)

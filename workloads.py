@@ -196,6 +196,37 @@ class NetBuilder:
         h, w, _ = self._hwc[x]
         return self._push({"op": "entropy", "name": name or f"entropy{len(self.ops)}", "in": x}, (h, w, 1))
 
+    def rms_norm(self, x, eps=1e-6, to8=False, name=None):
+        """Weights of one with a spread of a fifth."""
+        idx = len(self.ops)
+        w = (1 + 0.2 * rng_for(self.seed, idx).standard_normal(self._hwc[x][2])).astype(np.float32)
+        return self._push({"op": "rms_norm", "name": name or f"rms_norm{idx}", "in": x, "w": w, "eps": eps, "to8": to8},
+                          self._hwc[x])
+
+    def quantize(self, x, name=None):
+        return self._push({"op": "quantize", "name": name or f"quantize{len(self.ops)}", "in": x}, self._hwc[x])
+
+    def pointwise_fp8(self, x, cout, act=ACT_NONE, name=None):
+        """A pointwise layer in 8-bit floating point: codes of all magnitudes, a scale for each block of 128 x 128."""
+        h, w, cin = self._hwc[x]
+        idx = len(self.ops)
+        rng = rng_for(self.seed, idx)
+        codes = rng.integers(0, 0x7f, (cout, cin)).astype(np.uint8) | (rng.integers(0, 2, (cout, cin)) << 7).astype(np.uint8)
+        scales = np.exp(rng.standard_normal((-(-cout // 128), -(-cin // 128))) * 0.5) * 0.02 / np.sqrt(cin)
+        return self._push({"op": "pointwise_fp8", "name": name or f"pointwise_fp8_{idx}", "in": x, "cout": cout, "act": act,
+                           "q": codes, "scales": scales.astype(np.float32), "b": bias_normal(rng, cout)}, (h, w, cout))
+
+    def rotary(self, x, heads, head_dim, axes, freqs, positions=-1, first=0, adjacent=False, name=None):
+        h, w, _ = self._hwc[x]
+        return self._push({"op": "rotary", "name": name or f"rotary{len(self.ops)}", "in": x, "heads": heads,
+                           "head_dim": head_dim, "axes": list(axes), "freqs": list(freqs), "positions": positions,
+                           "from": first, "adjacent": adjacent}, (h, w, heads * head_dim))
+
+    def attention(self, q, k, v, heads, kv_heads, head_dim, name=None, **kw):
+        h, w, _ = self._hwc[q]
+        return self._push({"op": "attention", "name": name or f"attention{len(self.ops)}", "q": q, "k": k, "v": v,
+                           "heads": heads, "kv_heads": kv_heads, "head_dim": head_dim, **kw}, (h, w, heads * head_dim))
+
     def softmax(self, x, name=None):
         return self._push({"op": "softmax", "name": name or f"softmax{len(self.ops)}", "in": x},
                           self._hwc[x])
