@@ -11,6 +11,8 @@
 // registers.  m, the sums, the scores and O are fp32; P is rounded to 16 bits
 // for the product (an error of half a step relative to each weight, which the
 // sum over keys averages), its sum is taken before.
+#include <algorithm>
+
 #include "tokens.h"
 
 namespace mgi {
@@ -20,7 +22,13 @@ namespace {
 
 typedef float f16v __attribute__((ext_vector_type(16)));
 
-constexpr int kBM = 128, kBN = 64;   // rows and keys of a tile
+constexpr int kBN = 64;              // keys of a tile that waves share
+constexpr int kPrivate = 32;         // ... and of a wave's own
+constexpr float kSlack = 8.0f;       // log2 of how far weights may pass 1 before the base is moved
+
+// Rows of a tile: 32 to a wave; WR waves along the rows, the others of the four
+// along the keys.
+__host__ __device__ constexpr int tile_rows(int wr) { return 32 * wr; }
 
 template <typename E>
 __device__ __forceinline__ f16v mma32(h8 a, h8 b, f16v c) {
@@ -40,11 +48,12 @@ struct Tile {
 // Finds tile `t` among the tiles of all sequences.  Bounds are read up to the
 // token count and not below their predecessors.  Two more sequences without
 // keys take the queries before the first bound and behind the last.
+template <int BM>
 __device__ __forceinline__ Tile find_tile(const AttentionParams &p, int t) {
     Tile r;
     r.none = false;
     if (!p.bq) {
-        const int per = (p.tq * p.group + kBM - 1) / kBM, image = t / per;
+        const int per = (p.tq * p.group + BM - 1) / BM, image = t / per;
         r.q0 = image * p.tq;
         r.nq = p.tq;
         r.k0 = image * p.tk;
@@ -73,7 +82,7 @@ __device__ __forceinline__ Tile find_tile(const AttentionParams &p, int t) {
             qs = qmax;
             ks = kmax;
         }
-        const int n = i < p.nseq + 2 ? ((qe - qs) * p.group + kBM - 1) / kBM : 0;
+        const int n = i < p.nseq + 2 ? ((qe - qs) * p.group + BM - 1) / BM : 0;
         int upto = n;
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) {
@@ -99,24 +108,81 @@ __device__ __forceinline__ Tile find_tile(const AttentionParams &p, int t) {
     return r;
 }
 
-__device__ __forceinline__ bool finite16(uint16_t v, bool bf) { return bf ? (v & 0x7f80) != 0x7f80 : (v & 0x7c00) != 0x7c00; }
+// Where a 16-byte element (key k of 16, slice s of 4) of a block is, in elements:
+// the lane whose load brings it.  A wave loads a block, 1 KiB, at once, so that
+// memory is read in pieces of 64 bytes (NHWC: four slices of a key) or 256 (sliced:
+// 16 keys of a slice), and the exclusive ors spread what the matrix instructions'
+// operands take at a time, 8 keys of a slice or 4 keys of 4 slices, over all banks.
+template <bool NHWC>
+__device__ __forceinline__ int at_of(int k, int s) { return NHWC ? k * 4 + (s ^ (k >> 1 & 3)) : s * 16 + (k ^ (s & 1) << 2); }
+template <bool NHWC>
+__device__ __forceinline__ void of_lane(int lane, int &k, int &s) {
+    if (NHWC) {
+        k = lane >> 2;
+        s = (lane & 3) ^ (k >> 1 & 3);
+    } else {
+        s = lane >> 4;
+        k = (lane & 15) ^ (s & 1) << 2;
+    }
+}
 
-// ND: the head's channels in steps of 32
-template <typename E, int ND>
-__global__ __launch_bounds__(256) void attention_kernel(AttentionParams p, int tiles) {
-    __shared__ h8 kt[ND * 4][kBN], vt[ND * 4][kBN];
+typedef short s4 __attribute__((ext_vector_type(4)));
+
+// A column of V: 4 keys of a channel to each lane, out of 16 lanes' 4 keys x 16 channels
+__device__ __forceinline__ s4 read_column(const h8 *base, int bytes) {
+    return __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+        (__attribute__((address_space(3))) s4 *)((__attribute__((address_space(3))) char *)(size_t)(unsigned)(size_t)(
+                                                     __attribute__((address_space(3))) const void *)base + bytes));
+}
+
+__device__ __forceinline__ h8 with_zeros_for_odd(h8 v, bool bf) {
+    const uint16_t mask = bf ? 0x7f80 : 0x7c00;
+    u16x8 b = bits8(v);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) b[i] = (b[i] & mask) == mask ? 0 : b[i];
+    return __builtin_bit_cast(h8, b);
+}
+__device__ __forceinline__ bool any_odd(h8 v, bool bf) {
+    const uint16_t mask = bf ? 0x7f80 : 0x7c00;
+    const u16x8 b = bits8(v);
+    bool odd = false;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) odd = odd || (b[i] & mask) == mask;
+    return odd;
+}
+
+// ND: the head's channels in steps of 32.  WR = 4: four waves of 32 rows share
+// tiles of 64 keys; WR = 1: four waves have the same 32 rows and 32 keys each, by
+// themselves.  Two stages of LDS: the next tile's loads are in flight while a tile
+// is worked on.
+template <typename E, int ND, int WR, bool NHWC>
+__global__ __launch_bounds__(256, WR == 4 ? 2 : 1) void attention_kernel(AttentionParams p, AttentionGeom geo) {
+    constexpr int BM = tile_rows(WR), NK = WR == 4 ? 2 : 1;          // blocks of 32 keys of a wave's tile
+    constexpr int KEYS = 32 * NK, STEP = WR == 4 ? KEYS : 4 * KEYS;  // keys of a wave's tile, from one to the next
+    constexpr int PART = NK * 2 * ND * 64, STAGE = 2 * PART;         // elements of K (or V), of both
+    constexpr int OWN = WR == 4 ? 1 : 4;
+    __shared__ h8 lds[2 * OWN * STAGE];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
-    const int kvh = blockIdx.x / tiles;
-    const Tile t = find_tile(p, blockIdx.x - kvh * tiles);
+    const int item = xcd_tile(blockIdx.x, gridDim.x), chunk = item % geo.chunks, pair = item / geo.chunks;
+    const int kvh = pair / geo.tiles;
+    const Tile t = find_tile<BM>(p, pair - kvh * geo.tiles);
     if (t.none) return;
-    const int rows = t.nq * p.group, r0 = t.tile * kBM + wave * 32, row = r0 + (lane & 31), rc = min(row, rows - 1);
+    const int rows = t.nq * p.group, first = t.tile * BM, r0 = first + (WR == 4 ? wave * 32 : 0);
+    const int row = r0 + (lane & 31), rc = min(row, rows - 1);
     const int token = rc / p.group, head = kvh * p.group + rc - token * p.group;
-    // keys that a row sees, and the least and the most of the tile's rows
+    // keys that a row sees
     auto seen = [&](int r) {
         const int tok = min(r, rows - 1) / p.group;
         return p.causal ? min(max(tok + 1 + t.nk - t.nq, 0), t.nk) : t.nk;
     };
-    const int lim = seen(rc), least = seen(t.tile * kBM), most = seen(t.tile * kBM + kBM - 1);
+    const int from = chunk * geo.chunk;
+    const int most = __builtin_amdgcn_readfirstlane(min(seen(first + BM - 1), geo.chunks > 1 ? from + geo.chunk : t.nk));
+    if (chunk > 0 && from >= most) return;                           // (the first chunk writes rows that see nothing)
+    // the fewest that a row of the tile sees, the most that one of the wave does
+    const int least = __builtin_amdgcn_readfirstlane(seen(first)), mine = __builtin_amdgcn_readfirstlane(min(seen(r0 + 31), most));
+    const int lim = seen(rc);
+    const bool works = r0 < rows;
+
     h8 q[ND * 2];
 #pragma unroll
     for (int s = 0; s < ND * 2; ++s) {
@@ -129,71 +195,109 @@ __global__ __launch_bounds__(256) void attention_kernel(AttentionParams p, int t
 #pragma unroll
     for (int d = 0; d < ND; ++d) o[d] = f16v{};
     float m = -INFINITY, l = 0.0f;
-    const h8 *kp = p.k.x + (size_t)kvh * p.d8 * p.k.s, *vp = p.v.x + (size_t)kvh * p.d8 * p.v.s;
-    for (int j0 = 0; j0 < most; j0 += kBN) {
-        for (int e = tid; e < (ND + 1) / 2 * 8 * kBN; e += 256) {
-            const int key = (e & 7) | (e >> 6) % 8 << 3, sl = (e >> 3 & 7) | e >> 9 << 3;
-            const size_t j = (size_t)(t.k0 + min(j0 + key, t.nk - 1));
-            if (sl >= ND * 4) continue;
-            kt[sl][key] = sl < p.d8 ? kp[(size_t)sl * p.k.s + j * p.k.p] : zero_h8();
-            vt[sl][key] = sl < p.d8 ? vp[(size_t)sl * p.v.s + j * p.v.p] : zero_h8();
-        }
-        __syncthreads();
-        f16v s[2];
-        s[0] = s[1] = f16v{};
+
+    // this lane's element of the blocks that the wave loads; slices past the head's
+    // last come from a block of zeros
+    int lk, ls;
+    of_lane<NHWC>(lane, lk, ls);
+    const h8 *kp = p.k.x + (size_t)(kvh * p.d8 + ls) * p.k.s, *vp = p.v.x + (size_t)(kvh * p.d8 + ls) * p.v.s;
+    auto issue = [&](int j0, int stage) {
+        h8 *to = lds + (stage * OWN + (WR == 4 ? 0 : wave)) * STAGE;
 #pragma unroll
-        for (int k = 0; k < ND * 2; ++k)
+        for (int u = 0; u < (WR == 4 ? 1 : 2); ++u) {
+            const int b = WR == 4 ? wave : u;                        // block of 16 keys of the tile
+            const size_t j = (size_t)(t.k0 + min(j0 + b * 16 + lk, t.nk - 1));
+            const h8 *kj = kp + j * p.k.p, *vj = vp + j * p.v.p;
 #pragma unroll
-            for (int b = 0; b < 2; ++b) s[b] = mma32<E>(kt[2 * k + half][b * 32 + (lane & 31)], q[k], s[b]);
-        const bool masked = j0 + kBN > least;
-        if (masked) {
-            // hidden keys: no score, and values that are infinite or NaN are
-            // taken out of the tile (0 times them is NaN) and added to the rows
-            // that see them
-            bool odd = false;
-            for (int e = tid; e < ND * 4 * kBN; e += 256) {
-                const h8 v = vt[e / kBN][e % kBN];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) odd = odd || !finite16(bits8(v)[i], E::bf);
+            for (int g = 0; g < ND; ++g) {
+                const bool zero = g == ND - 1 && ls + 4 * g >= p.d8;
+                load_lds16(zero ? p.zero : kj + (size_t)(4 * g) * p.k.s, to + (b * ND + g) * 64);
+                load_lds16(zero ? p.zero : vj + (size_t)(4 * g) * p.v.s, to + PART + (b * ND + g) * 64);
             }
-            if (__syncthreads_or(odd)) {
-                for (int key = 0; key < kBN; ++key)
+        }
+    };
+    // the lane's places in a stage, in elements (K: of even and odd steps of 16
+    // channels) and bytes
+    const int key = lane & 15, kblock = (lane >> 4 & 1) * ND * 64;
+    const int ka[2] = {kblock + at_of<NHWC>(key, half), kblock + at_of<NHWC>(key, 2 + half)};
+    const int va = at_of<NHWC>(4 * half + (key >> 2), (lane >> 4 & 1) * 2 + (key >> 1 & 1)) * 16 + (key & 1) * 8;
+    constexpr int EIGHT = NHWC ? 512 : 128;                          // bytes from a key to the eighth after it
+
+    const int start = from + (WR == 4 ? 0 : wave * KEYS);
+    int stage = 0;
+    if (start < most) issue(start, 0);
+    for (int j0 = start; j0 < most; j0 += STEP, stage ^= 1) {
+        wait_vm_lds<0>();
+        if constexpr (WR == 4) __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");                               // (no LDS access moves over the wait)
+        if (j0 + STEP < most) issue(j0 + STEP, stage ^ 1);
+        h8 *kt = lds + (stage * OWN + (WR == 4 ? 0 : wave)) * STAGE, *vt = kt + PART;
+        const bool masked = j0 + KEYS > least;
+        f16v s[NK];
+        if (works && j0 < mine) {
+#pragma unroll
+            for (int b = 0; b < NK; ++b) s[b] = f16v{};
+#pragma unroll
+            for (int k = 0; k < ND * 2; ++k)
+#pragma unroll
+                for (int b = 0; b < NK; ++b) s[b] = mma32<E>(kt[ka[k & 1] + (b * 2 * ND + k / 2) * 64], q[k], s[b]);
+        }
+        if (masked) {
+            // hidden keys have no score; values that are infinite or NaN are taken
+            // out of the tile (0 times them is NaN) and added to the rows that see
+            // them
+            bool odd = false;
+            const int me = WR == 4 ? tid : lane, all = WR == 4 ? 256 : 64;
+            for (int e = me; e < PART; e += all) odd = odd || any_odd(vt[e], E::bf);
+            const bool found = WR == 4 ? __syncthreads_or(odd) : __any(odd);
+            if (found) {
+                for (int k = 0; k < KEYS; ++k)
 #pragma unroll
                     for (int d = 0; d < ND; ++d)
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const float v = E::get(vt[d * 4 + i / 4][key], half * 4 + i % 4);
-                            if (j0 + key < lim && !(fabsf(v) < INFINITY)) o[d][i] += v;
-                        }
-                __syncthreads();
-                for (int e = tid; e < ND * 4 * kBN; e += 256) {
-                    h8 v = vt[e / kBN][e % kBN];
+                        for (int g = 0; g < 4; ++g) {
+                            const h8 v = vt[(k / 16 * ND + d) * 64 + at_of<NHWC>(k % 16, g)];
 #pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        if (!finite16(bits8(v)[i], E::bf)) v[i] = (_Float16)0.0f;
-                    vt[e / kBN][e % kBN] = v;
-                }
-                __syncthreads();
+                            for (int i = 0; i < 4; ++i) {
+                                const float x = half ? E::get(v, 4 + i) : E::get(v, i);
+                                if (j0 + k < lim && !(fabsf(x) < INFINITY)) o[d][g * 4 + i] += x;
+                            }
+                        }
+                if constexpr (WR == 4) __syncthreads();
+                else __builtin_amdgcn_wave_barrier();
+                for (int e = me; e < PART; e += all) vt[e] = with_zeros_for_odd(vt[e], E::bf);
+                if constexpr (WR == 4) __syncthreads();
+                else __builtin_amdgcn_wave_barrier();
             }
 #pragma unroll
-            for (int b = 0; b < 2; ++b)
+            for (int b = 0; b < NK; ++b)
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
                     if (j0 + b * 32 + i / 4 * 8 + half * 4 + i % 4 >= lim) s[b][i] = -INFINITY;
         }
-        float top = m;
+        if (!works || j0 >= mine) continue;
+        float top = s[0][0];
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
+        for (int b = 0; b < NK; ++b)
 #pragma unroll
             for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
         top = fmaxf(top, __shfl_xor(top, 32, 64));
-        const float base = top == -INFINITY ? 0.0f : top * c;
-        const float keep = __builtin_amdgcn_exp2f(fmaf(m, c, -base));
-        m = top;
-        float sum = 0.0f;
-        h8 pr[4];
+        // the weights' base moves only when a score passes it by 2^kSlack
+        const bool move = fmaf(top, c, m == -INFINITY ? INFINITY : -m * c) > kSlack;
+        if (__any(move)) {
+            // (before the first weights there is nothing to scale but what hidden
+            // keys' infinities left)
+            const float to = move ? top : m, keep = move && m != -INFINITY ? __builtin_amdgcn_exp2f((m - to) * c) : 1.0f;
+            m = to;
+            l *= keep;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
+            for (int d = 0; d < ND; ++d) o[d] *= keep;
+        }
+        const float base = m == -INFINITY ? 0.0f : m * c;
+        float sum = 0.0f;
+        h8 pr[2 * NK];
+#pragma unroll
+        for (int k = 0; k < 2 * NK; ++k) {
             float w[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
@@ -202,50 +306,166 @@ __global__ __launch_bounds__(256) void attention_kernel(AttentionParams p, int t
             }
             pr[k] = E::pack(w);
         }
-        l = fmaf(l, keep, sum);
+        l += sum;
 #pragma unroll
-        for (int d = 0; d < ND; ++d) {
-            o[d] *= keep;
+        for (int k = 0; k < 2 * NK; ++k)
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                h8 v;
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    v[i] = vt[d * 4 + (lane & 31) / 8][k * 16 + i / 4 * 8 + half * 4 + i % 4][lane & 7];
+            for (int d = 0; d < ND; ++d) {
+                const int off = va + (k * ND + d) * 1024;
+                const s4 a = read_column(vt, off), b = read_column(vt, off + EIGHT);
+                const h8 v = __builtin_bit_cast(h8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
                 o[d] = mma32<E>(v, pr[k], o[d]);
             }
-        }
-        __syncthreads();
     }
     l += __shfl_xor(l, 32, 64);
-    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-    // a lane has 4 of a slice's 8 channels, lane ^ 32 the others: of two slices
-    // each completes one
+    const int d32 = ND * 32;
+    const size_t slot = (size_t)(pair * geo.chunks + chunk) * BM;    // this chunk's rows among all partial ones
+    if constexpr (WR == 4) {
+        if (!works) return;
+        if (geo.chunks > 1) {
+            if (row < rows) {
+                float *part = p.part + (slot + row - first) * (d32 + 2);
 #pragma unroll
-    for (int d = 0; d < ND; ++d)
+                for (int d = 0; d < ND; ++d)
 #pragma unroll
-        for (int g = 0; g < 4; g += 2) {
-            float v[8];
+                    for (int g = 0; g < 4; ++g)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float a = o[d][g * 4 + i] * inv, b = o[d][g * 4 + 4 + i] * inv;
-                const float other = __shfl_xor(half ? a : b, 32, 64);
-                v[i] = half ? other : a;
-                v[4 + i] = half ? b : other;
+                        for (int i = 0; i < 4; i += 2)
+                            *(float2 *)(part + d * 32 + g * 8 + half * 4 + i) = float2{o[d][g * 4 + i], o[d][g * 4 + i + 1]};
+                if (half == 0) *(float2 *)(part + d32) = float2{m, l};
             }
-            const int sl = d * 4 + g + half;
-            if (row < rows && sl < p.d8) store8<E>(p.y, head * p.d8 + sl, t.q0 + token, E::pack(v));
+            return;
         }
+        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+        // a lane has 4 of a slice's 8 channels, lane ^ 32 the others: of two slices
+        // each completes one
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+            for (int g = 0; g < 4; g += 2) {
+                float v[8];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float a = o[d][g * 4 + i] * inv, b = o[d][g * 4 + 4 + i] * inv;
+                    const float other = __shfl_xor(half ? a : b, 32, 64);
+                    v[i] = half ? other : a;
+                    v[4 + i] = half ? b : other;
+                }
+                const int sl = d * 4 + g + half;
+                if (row < rows && sl < p.d8) store8<E>(p.y, head * p.d8 + sl, t.q0 + token, E::pack(v));
+            }
+    } else {
+        // the four waves' parts of the rows, in turn in the order of the waves
+        constexpr int LINE = ND * 32 + 4;
+        float *sums = (float *)lds;                                  // [wave][row][LINE]
+        __shared__ float2 ml[4][32];
+        __syncthreads();                                             // (all have read their last tile)
+        if (half == 0) ml[wave][lane] = float2{m, l};
+        float *mine_ = sums + (wave * 32 + (lane & 31)) * LINE;
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                *(f4 *)(mine_ + d * 32 + g * 8 + half * 4) = f4{o[d][g * 4], o[d][g * 4 + 1], o[d][g * 4 + 2], o[d][g * 4 + 3]};
+        __syncthreads();
+        for (int e = tid; e < 32 * ND * 4; e += 256) {
+            const int r = e & 31, sl = e >> 5;
+            if (first + r >= rows || sl >= p.d8) continue;
+            float top = -INFINITY, total = 0.0f, v[8] = {};
+#pragma unroll
+            for (int w = 0; w < 4; ++w) top = fmaxf(top, ml[w][r].x);
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                if (ml[w][r].x == -INFINITY && ml[w][r].y == 0.0f) continue;
+                const float f = __builtin_amdgcn_exp2f((ml[w][r].x - top) * c);
+                total = fmaf(ml[w][r].y, f, total);
+                const f4 *from_ = (const f4 *)(sums + (w * 32 + r) * LINE + sl * 8);
+                const f4 lo = from_[0], hi = from_[1];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = fmaf(i < 4 ? lo[i & 3] : hi[i & 3], f, v[i]);
+            }
+            if (geo.chunks > 1) {
+                float *part = p.part + (slot + r) * (d32 + 2);
+#pragma unroll
+                for (int i = 0; i < 8; i += 2) *(float2 *)(part + sl * 8 + i) = float2{v[i], v[i + 1]};
+                if (sl == 0) *(float2 *)(part + d32) = float2{top, total};
+            } else {
+                const float inv = total == 0.0f ? 0.0f : 1.0f / total;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] *= inv;
+                const int tok = (first + r) / p.group, hd = kvh * p.group + first + r - tok * p.group;
+                store8<E>(p.y, hd * p.d8 + sl, t.q0 + tok, E::pack(v));
+            }
+        }
+    }
+}
+
+// Joins the chunks of the rows of a tile: a thread has 8 channels of a row.
+template <typename E, int BM>
+__global__ __launch_bounds__(256) void attention_join_kernel(AttentionParams p, AttentionGeom geo, int d32) {
+    const int per = (BM * p.d8 + 255) / 256, pair = blockIdx.x / per, kvh = pair / geo.tiles;
+    const Tile t = find_tile<BM>(p, pair - kvh * geo.tiles);
+    if (t.none) return;
+    const int e = (blockIdx.x - pair * per) * 256 + threadIdx.x, r = e / p.d8, sl = e - r * p.d8;
+    const int rows = t.nq * p.group, first = t.tile * BM, row = first + r;
+    if (r >= BM || row >= rows) return;
+    const int last = min(first + BM - 1, rows - 1) / p.group;
+    const int most = p.causal ? min(max(last + 1 + t.nk - t.nq, 0), t.nk) : t.nk;
+    const int n = min(max(1, (most + geo.chunk - 1) / geo.chunk), geo.chunks);
+    const float c = fabsf(p.scale);
+    const float *part = p.part + ((size_t)pair * geo.chunks * BM + r) * (d32 + 2);
+    const size_t step = (size_t)BM * (d32 + 2);
+    float top = -INFINITY, total = 0.0f, v[8] = {};
+    for (int k = 0; k < n; ++k) top = fmaxf(top, part[k * step + d32]);
+    for (int k = 0; k < n; ++k) {
+        const float2 ml = *(const float2 *)(part + k * step + d32);
+        if (ml.x == -INFINITY && ml.y == 0.0f) continue;
+        const float f = __builtin_amdgcn_exp2f((ml.x - top) * c);
+        total = fmaf(ml.y, f, total);
+#pragma unroll
+        for (int i = 0; i < 8; i += 2) {
+            const float2 x = *(const float2 *)(part + k * step + sl * 8 + i);
+            v[i] = fmaf(x.x, f, v[i]);
+            v[i + 1] = fmaf(x.y, f, v[i + 1]);
+        }
+    }
+    const float inv = total == 0.0f ? 0.0f : 1.0f / total;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] *= inv;
+    const int tok = row / p.group, hd = kvh * p.group + row - tok * p.group;
+    store8<E>(p.y, hd * p.d8 + sl, t.q0 + tok, E::pack(v));
+}
+
+template <typename E, int ND, int WR>
+void launch_attention_w(const AttentionParams &p, const AttentionGeom &g, hipStream_t st) {
+    const dim3 grid((unsigned)g.tiles * p.kv_heads * g.chunks);
+    // (a timed run stamps the first kernel's start and the last one's end)
+    LaunchEvents &ev = launch_events();
+    const LaunchEvents saved = ev;
+    if (g.chunks > 1) ev.stop = nullptr;
+    if (p.k.s == 1 && p.v.s == 1) launch(attention_kernel<E, ND, WR, true>, grid, dim3(256), 0, st, p, g);
+    else launch(attention_kernel<E, ND, WR, false>, grid, dim3(256), 0, st, p, g);
+    ev = saved;
+    if (g.chunks == 1) return;
+    const dim3 join((unsigned)g.tiles * p.kv_heads * ((tile_rows(WR) * p.d8 + 255) / 256));
+    ev.start = nullptr;
+    launch(attention_join_kernel<E, tile_rows(WR)>, join, dim3(256), 0, st, p, g, ND * 32);
+    ev = saved;
+}
+
+template <typename E, int ND>
+void launch_attention_n(const AttentionParams &p, const AttentionGeom &g, hipStream_t st) {
+    if (g.wr == 4) launch_attention_w<E, ND, 4>(p, g, st);
+    else launch_attention_w<E, ND, 1>(p, g, st);
 }
 
 template <typename E>
 hipError_t launch_attention_t(const AttentionParams &p, const AttentionGeom &g, hipStream_t st) {
-    const dim3 grid((unsigned)g.tiles * p.kv_heads);
     switch ((p.d8 + 3) / 4) {
-        case 1: launch(attention_kernel<E, 1>, grid, dim3(256), 0, st, p, g.tiles); break;
-        case 2: launch(attention_kernel<E, 2>, grid, dim3(256), 0, st, p, g.tiles); break;
-        case 3: launch(attention_kernel<E, 3>, grid, dim3(256), 0, st, p, g.tiles); break;
-        case 4: launch(attention_kernel<E, 4>, grid, dim3(256), 0, st, p, g.tiles); break;
+        case 1: launch_attention_n<E, 1>(p, g, st); break;
+        case 2: launch_attention_n<E, 2>(p, g, st); break;
+        case 3: launch_attention_n<E, 3>(p, g, st); break;
+        case 4: launch_attention_n<E, 4>(p, g, st); break;
         default: return hipErrorInvalidValue;
     }
     return hipGetLastError();
@@ -255,10 +475,20 @@ hipError_t launch_attention_t(const AttentionParams &p, const AttentionGeom &g, 
 
 AttentionGeom attention_geom(int q_tokens, int k_tokens, int n, int nseq, int group, int kv_heads, int d8) {
     AttentionGeom g{};
-    const long rows = (long)q_tokens * group;
-    g.tiles = (int)(nseq ? rows / kBM + nseq + 2 : (long)n * ((rows / n + kBM - 1) / kBM));
-    g.chunks = 1;
-    g.wr = 4;
+    const long rows = (long)q_tokens * group, sequences = nseq ? nseq : n;
+    // few rows to a sequence: the waves share the keys out instead
+    g.wr = rows <= 32 * sequences ? 1 : 4;
+    const int bm = tile_rows(g.wr);
+    g.tiles = (int)(nseq ? rows / bm + nseq + 2 : n * ((rows / n + bm - 1) / bm));
+    // fewer workgroups than the card holds (two to a compute unit of tiles that
+    // waves share, one of the others): the keys are split
+    const long keys = nseq ? k_tokens : k_tokens / n, items = (long)g.tiles * kv_heads, want = g.wr == 4 ? 512 : 256;
+    const int step = g.wr == 4 ? kBN : 4 * kPrivate;
+    long chunks = items < want ? want / items : 1;
+    chunks = std::min(chunks, (keys + 4 * step - 1) / (4 * step));
+    g.chunk = (int)((keys + chunks * step - 1) / (chunks * step)) * step;
+    g.chunks = (int)((keys + g.chunk - 1) / g.chunk);
+    if (g.chunks > 1) g.part_bytes = (size_t)items * g.chunks * bm * ((d8 + 3) / 4 * 32 + 2) * 4;
     return g;
 }
 

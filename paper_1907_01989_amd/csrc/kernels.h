@@ -484,13 +484,12 @@ struct RotaryParams {
 hipError_t launch_rotary(const RotaryParams &p, hipStream_t st);
 
 constexpr int kMaxHeadDim = 128, kMaxSequences = 1 << 16;
-// Rows of a tile, keys of a chunk (all where keys are not split), chunks, and
-// what the chunks leave behind
+// Row tiles, chunks that the keys are split into, and their keys
 struct AttentionGeom {
     int tiles;           // row tiles of one head of keys (an upper bound for packed sequences)
     int chunks, chunk;
     int wr;              // waves along the rows of a tile (the others take other keys)
-    size_t part_bytes, cnt_bytes;
+    size_t part_bytes;   // what the chunks leave behind (0: one chunk)
 };
 AttentionGeom attention_geom(int q_tokens, int k_tokens, int n, int nseq, int group, int kv_heads, int d8);
 struct AttentionParams {
@@ -501,8 +500,8 @@ struct AttentionParams {
     int tq, tk;          // pixels of an image, or of all
     int kv_heads, group, d8, causal;
     float scale;         // of the scores, times log2(e)
-    float *part;
-    int *cnt;
+    const h8 *zero;      // a block of zeros
+    float *part;         // chunks: [row tile][chunk][row][channels, then maximum and sum]
     int bf16;
 };
 hipError_t launch_attention(const AttentionParams &p, const AttentionGeom &g, hipStream_t st);

@@ -869,10 +869,7 @@ void plan_splits(mgi_plan &p) {
             nd.cnt_bytes = part ? s.pixels() * sizeof(int) : 0;
             for (int b : nd.in) p.reads_inputs_late = p.reads_inputs_late || p.bufs[b].loc == Loc::Input;
         }
-        if (nd.kind == NodeKind::Attention) {
-            part = nd.at_geo.part_bytes;
-            nd.cnt_bytes = nd.at_geo.cnt_bytes;
-        }
+        if (nd.kind == NodeKind::Attention) part = nd.at_geo.part_bytes;
         // (the positions of rotary, the bounds of attention)
         if (nd.kind == NodeKind::Attention || nd.kind == NodeKind::Rotary)
             for (int b : nd.in) p.reads_inputs_late = p.reads_inputs_late || p.bufs[b].loc == Loc::Input;

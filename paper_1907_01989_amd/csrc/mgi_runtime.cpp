@@ -597,10 +597,8 @@ hipError_t launch_attention_node(const mgi_plan &p, const Node &nd, const Bases 
     q.kv_heads = d.kv_heads; q.group = d.heads / d.kv_heads; q.d8 = d.head_dim / 8;
     q.causal = d.causal;
     q.scale = (float)((d.scale == 0.0f ? 1.0 / std::sqrt((double)d.head_dim) : (double)d.scale) * 1.4426950408889634);
-    if (nd.scratch >= 0) {
-        q.part = (float *)buf_ptr(p, nd.scratch, B);
-        q.cnt = (int *)(B.ws + nd.cnt_off);
-    }
+    q.zero = (const h8 *)(static_cast<const char *>(p.dev_w) + p.zero_off);
+    if (nd.scratch >= 0) q.part = (float *)buf_ptr(p, nd.scratch, B);
     q.bf16 = p.opt.dtype == MGI_DTYPE_BF16;
     return launch_attention(q, nd.at_geo, st);
 }
