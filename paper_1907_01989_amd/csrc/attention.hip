@@ -400,35 +400,49 @@ __global__ __launch_bounds__(256, WR == 4 ? 2 : 1) void attention_kernel(Attenti
     }
 }
 
-// Joins the chunks of the rows of a tile: a thread has 8 channels of a row.
+// Joins the chunks of a row: a thread has 8 channels of every 16th chunk, then 16
+// threads join what those found, in order.
 template <typename E, int BM>
 __global__ __launch_bounds__(256) void attention_join_kernel(AttentionParams p, AttentionGeom geo, int d32) {
-    const int per = (BM * p.d8 + 255) / 256, pair = blockIdx.x / per, kvh = pair / geo.tiles;
+    __shared__ float found[16][16][8];
+    __shared__ float2 ml[16][16];
+    const int pair = blockIdx.x / BM, r = blockIdx.x - pair * BM, kvh = pair / geo.tiles;
     const Tile t = find_tile<BM>(p, pair - kvh * geo.tiles);
-    if (t.none) return;
-    const int e = (blockIdx.x - pair * per) * 256 + threadIdx.x, r = e / p.d8, sl = e - r * p.d8;
     const int rows = t.nq * p.group, first = t.tile * BM, row = first + r;
-    if (r >= BM || row >= rows) return;
+    if (t.none || row >= rows) return;
     const int last = min(first + BM - 1, rows - 1) / p.group;
     const int most = p.causal ? min(max(last + 1 + t.nk - t.nq, 0), t.nk) : t.nk;
     const int n = min(max(1, (most + geo.chunk - 1) / geo.chunk), geo.chunks);
     const float c = fabsf(p.scale);
+    const int sl = threadIdx.x & 15, g = threadIdx.x >> 4;
     const float *part = p.part + ((size_t)pair * geo.chunks * BM + r) * (d32 + 2);
     const size_t step = (size_t)BM * (d32 + 2);
     float top = -INFINITY, total = 0.0f, v[8] = {};
-    for (int k = 0; k < n; ++k) top = fmaxf(top, part[k * step + d32]);
-    for (int k = 0; k < n; ++k) {
-        const float2 ml = *(const float2 *)(part + k * step + d32);
-        if (ml.x == -INFINITY && ml.y == 0.0f) continue;
-        const float f = __builtin_amdgcn_exp2f((ml.x - top) * c);
-        total = fmaf(ml.y, f, total);
+    auto add = [&](float m, float l, const float *x) {
+        if (m == -INFINITY && l == 0.0f) return;
+        const float to = fmaxf(top, m), keep = top == -INFINITY && total == 0.0f ? 0.0f : __builtin_amdgcn_exp2f((top - to) * c);
+        const float f = __builtin_amdgcn_exp2f((m - to) * c);
+        top = to;
+        total = fmaf(total, keep, l * f);
 #pragma unroll
-        for (int i = 0; i < 8; i += 2) {
-            const float2 x = *(const float2 *)(part + k * step + sl * 8 + i);
-            v[i] = fmaf(x.x, f, v[i]);
-            v[i + 1] = fmaf(x.y, f, v[i + 1]);
+        for (int i = 0; i < 8; ++i) v[i] = fmaf(x[i], f, v[i] * keep);
+    };
+    if (sl < p.d8) {
+        for (int k = g; k < n; k += 16) {
+            const float *at = part + k * step;
+            const float2 w = *(const float2 *)(at + d32);
+            float x[8];
+#pragma unroll
+            for (int i = 0; i < 8; i += 2) *(float2 *)(x + i) = *(const float2 *)(at + sl * 8 + i);
+            add(w.x, w.y, x);
         }
     }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) found[g][sl][i] = v[i];
+    ml[g][sl] = float2{top, total};
+    __syncthreads();
+    if (g > 0 || sl >= p.d8) return;
+    for (int k = 1; k < min(n, 16); ++k) add(ml[k][sl].x, ml[k][sl].y, found[k][sl]);
     const float inv = total == 0.0f ? 0.0f : 1.0f / total;
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] *= inv;
@@ -447,7 +461,7 @@ void launch_attention_w(const AttentionParams &p, const AttentionGeom &g, hipStr
     else launch(attention_kernel<E, ND, WR, false>, grid, dim3(256), 0, st, p, g);
     ev = saved;
     if (g.chunks == 1) return;
-    const dim3 join((unsigned)g.tiles * p.kv_heads * ((tile_rows(WR) * p.d8 + 255) / 256));
+    const dim3 join((unsigned)g.tiles * p.kv_heads * tile_rows(WR));
     ev.start = nullptr;
     launch(attention_join_kernel<E, tile_rows(WR)>, join, dim3(256), 0, st, p, g, ND * 32);
     ev = saved;

@@ -509,11 +509,14 @@ hipError_t launch_attention(const AttentionParams &p, const AttentionGeom &g, hi
 // Pointwise layer in 8 bits: weights [nb16][kb][2][64 lanes][16 bytes] in the
 // MFMA A operand's order, scales [ceil(nb16 / 8)][kb]
 struct PwFp8Geom {
-    int variant;
+    int variant;         // 0: few pixels; 1, 2, 3: 64 x 64, 128 x 128, 256 x 256 tiles
+    bool reads_raw(size_t M) const { return variant == 0 && M <= 16; }   // can bring 16-bit pixels into 8 bits itself
 };
 PwFp8Geom pwfp8_geom(size_t M, int nb16, int kb);
 struct PwFp8Params {
     Tensor8 x;
+    TokenIn raw;         // the 16-bit tensor (x null: the 8-bit one is read), and its slices
+    int raw_s;
     const uint8_t *w;
     const float *scales, *bias;
     TokenOut y;

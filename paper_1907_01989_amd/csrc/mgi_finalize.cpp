@@ -856,6 +856,31 @@ void fuse_add_into_norm(mgi_plan &p) {
     p.nodes.swap(kept);
 }
 
+// An 8-bit layer of few pixels brings them into 8 bits itself where nothing else
+// reads the 8-bit tensor.
+void fuse_quantize_into_pw(mgi_plan &p) {
+    std::vector<int> readers(p.bufs.size(), 0), producer(p.bufs.size(), -1);
+    for (size_t i = 0; i < p.nodes.size(); ++i) {
+        for (int b : p.nodes[i].in) readers[b]++;
+        producer[p.nodes[i].out] = (int)i;
+    }
+    std::vector<char> drop(p.nodes.size(), 0);
+    for (Node &pw : p.nodes) {
+        if (pw.kind != NodeKind::PwFp8 || producer[pw.in[0]] < 0 || readers[pw.in[0]] != 1) continue;
+        const Node &q = p.nodes[producer[pw.in[0]]];
+        if (q.kind != NodeKind::Norm || q.norm || !pw.p8_geo.reads_raw(p.bufs[q.out].shape.pixels())) continue;
+        p.bufs[pw.in[0]].dead = true;
+        drop[producer[pw.in[0]]] = 1;
+        pw.in[0] = q.in[0];
+        pw.n_fused += q.n_fused;
+        pw.kname = "quantize_pointwise_fp8";
+    }
+    std::vector<Node> kept;
+    for (size_t i = 0; i < p.nodes.size(); ++i)
+        if (!drop[i]) kept.push_back(std::move(p.nodes[i]));
+    p.nodes.swap(kept);
+}
+
 // Geometry of the Answers kernels, the scratch tensors and counters of those
 // that split rows over workgroups (attention: keys), and whether questions are
 // about graph inputs or a kernel reads indices from one.
@@ -2145,6 +2170,7 @@ void absorb_ingests(mgi_plan &p, const mgi_options &o) {
                 case NodeKind::PwDw:
                 case NodeKind::GemmPool:
                 case NodeKind::Norm:
+                case NodeKind::PwFp8:
                 case NodeKind::Rotary:
                 case NodeKind::Attention:
                 case NodeKind::Gap: all = all && same; break;
@@ -2185,7 +2211,10 @@ mgi_status build_plan_impl(const mgi_graph &g, const mgi_options &o, mgi_plan &p
     if (o.fuse && o.fuse_softmax) fuse_softmax_into_fc(p);
     if (o.fuse && o.fuse_dwpw) fuse_dw_into_pw(p);
     if (o.fuse && !o.materialize_all) fuse_answers(p);
-    if (o.fuse && !o.materialize_all) fuse_add_into_norm(p);
+    if (o.fuse && !o.materialize_all) {
+        fuse_add_into_norm(p);
+        fuse_quantize_into_pw(p);
+    }
     plan_splits(p);
     if (o.fuse && !o.materialize_all) {
         alias_concats(p, o);

@@ -542,7 +542,12 @@ hipError_t launch_pwfp8_node(const mgi_plan &p, const Node &nd, const Bases &B, 
     const char *wbase = static_cast<const char *>(p.dev_w);
     const Shape y = p.bufs[nd.out].shape;
     PwFp8Params q{};
-    q.x = tensor8(p, nd.in[0], B);
+    if (p.bufs[nd.in[0]].layout == Layout::Q8) {
+        q.x = tensor8(p, nd.in[0], B);
+    } else {
+        q.raw = token_in(p, nd.in[0], B);
+        q.raw_s = slices(p.bufs[nd.in[0]].shape.c);
+    }
     q.w = (const uint8_t *)(wbase + nd.w_off);
     q.scales = (const float *)(wbase + nd.s_off);
     q.bias = (const float *)(wbase + nd.b_off);

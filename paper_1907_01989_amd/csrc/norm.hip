@@ -14,14 +14,6 @@ namespace kern {
 
 namespace {
 
-// The exponent of a block whose largest finite magnitude is `top`: 448 = 1.75 * 2^8.
-__device__ __forceinline__ int block_exponent(float top) {
-    const uint32_t b = __float_as_uint(top);
-    return max((int)(b >> 23) - 127 - 8 + ((b & 0x7fffff) > 0x600000 ? 1 : 0), -126);
-}
-
-__device__ __forceinline__ float power2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
-
 // P pixels to a wave, 64 / P slices at a time.  P = 8: a wave's lanes cover 8
 // pixels x 8 slices, 128 bytes of either layout, twice to a block of 128
 // channels; P = 1: four blocks of one pixel.  R: times that a wave comes round.
@@ -93,7 +85,7 @@ __global__ __launch_bounds__(1024) void norm_kernel(NormParams p) {
             }
             if constexpr (TO8) {
 #pragma unroll
-                for (int c = 0; c < 8; ++c) top = fmaxf(top, fabsf(y[j][c]) < INFINITY ? fabsf(y[j][c]) : 0.0f);
+                for (int c = 0; c < 8; ++c) top = fmaxf(top, finite(y[j][c]));
             }
             if (!TO8 && s < p.S && m < p.M) store8<E>(p.out, s, m, E::pack(y[j]));
         }
@@ -105,26 +97,16 @@ __global__ __launch_bounds__(1024) void norm_kernel(NormParams p) {
 #pragma unroll
             for (int j = 0; j < NS; ++j) {
                 const int s = (wave + W * r) * CH + j * SUBS + sub;
-                float v[8];
-#pragma unroll
-                for (int c = 0; c < 8; ++c) v[c] = fabsf(y[j][c]) < INFINITY ? y[j][c] * down : NAN;
-                int q[2];
-                q[0] = __builtin_amdgcn_cvt_pk_fp8_f32(v[0], v[1], 0, false);
-                q[0] = __builtin_amdgcn_cvt_pk_fp8_f32(v[2], v[3], q[0], true);
-                q[1] = __builtin_amdgcn_cvt_pk_fp8_f32(v[4], v[5], 0, false);
-                q[1] = __builtin_amdgcn_cvt_pk_fp8_f32(v[6], v[7], q[1], true);
+                const uint2 q = codes8(y[j], down);
                 if (m >= p.M) continue;
                 if (p.q.codes) {
                     if (s < p.KB * 16) {
-                        *(uint2 *)(p.q.codes + ((size_t)(s >> 1) * p.M + m) * 16 + (s & 1) * 8) = uint2{(unsigned)q[0], (unsigned)q[1]};
+                        *(uint2 *)(p.q.codes + ((size_t)(s >> 1) * p.M + m) * 16 + (s & 1) * 8) = q;
                         if (s % 16 == 0) ((uint8_t *)(p.q.exps + (size_t)(s >> 6) * p.M + m))[s >> 4 & 3] = (uint8_t)(e + 127);
                     }
                 } else if (s < p.S) {
-#pragma unroll
-                    for (int c = 0; c < 8; c += 4) {
-                        const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(q[c / 4], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(q[c / 4], true);
-                        v[c] = lo[0] * up; v[c + 1] = lo[1] * up; v[c + 2] = hi[0] * up; v[c + 3] = hi[1] * up;
-                    }
+                    float v[8];
+                    values8(q, up, v);
                     store8<E>(p.out, s, m, v);
                 }
             }
@@ -193,12 +175,7 @@ __global__ __launch_bounds__(256) void export8_kernel(Tensor8 x, void *y, int f3
     const uint2 q = *(const uint2 *)(x.codes + ((size_t)(s >> 1) * M + m) * 16 + (s & 1) * 8);
     const float up = power2((int)(x.exps[(size_t)(s >> 6) * M + m] >> (8 * (s >> 4 & 3)) & 255) - 127);
     float v[8];
-#pragma unroll
-    for (int c = 0; c < 8; c += 4) {
-        const int w = (int)(c ? q.y : q.x);
-        const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
-        v[c] = lo[0] * up; v[c + 1] = lo[1] * up; v[c + 2] = hi[0] * up; v[c + 3] = hi[1] * up;
-    }
+    values8(q, up, v);
     const h8 r = E::pack(v);
 #pragma unroll
     for (int c = 0; c < 8; ++c) {

@@ -10,6 +10,8 @@
 // instructions do the same).  That is 2^-16 of a result of normal values, under
 // the 16-bit output's step; products in 16 bits, which would be exact, run at half
 // the rate and need the codes converted.
+#include <type_traits>
+
 #include "tokens.h"
 
 namespace mgi {
@@ -30,67 +32,292 @@ template <int Q>
 __device__ __forceinline__ f4 mma8(i8v w, i8v x, uint32_t e) {
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x, f4{}, 0, 0, 0, 0x7f7f7f7f, Q, (int)e);
 }
-__device__ __forceinline__ f4 mma8(i8v w, i8v x, uint32_t e, int q) {
-    switch (q & 3) {
-        case 0: return mma8<0>(w, x, e);
-        case 1: return mma8<1>(w, x, e);
-        case 2: return mma8<2>(w, x, e);
-        default: return mma8<3>(w, x, e);
+
+// A block of a pixel's inputs, 32 of them to each of the lanes l, l ^ 16, l ^ 32,
+// l ^ 48, in 8 bits: the codes in the operand's order and the exponent's byte.
+template <typename E>
+__device__ __forceinline__ uint32_t to_8_bits(const uint4 (&raw)[4], i8v &codes) {
+    float top = 0.0f;
+#pragma unroll
+    for (int h = 0; h < 4; ++h) top = fmaxf(top, finite_top<E>(__builtin_bit_cast(h8, raw[h])));
+    top = fmaxf(top, __shfl_xor(top, 16, 64));
+    top = fmaxf(top, __shfl_xor(top, 32, 64));
+    const int e = block_exponent(top);
+    const float down = power2(-e);
+#pragma unroll
+    for (int h = 0; h < 4; ++h) {
+        const uint2 q = codes8<E>(__builtin_bit_cast(h8, raw[h]), down);
+        codes[2 * h] = (int)q.x;
+        codes[2 * h + 1] = (int)q.y;
     }
+    return (uint32_t)(e + 127);
 }
 
-// A wave: 16 channels x 64 pixels
+// the same for the four blocks of a word of exponents
+template <typename F>
+__device__ __forceinline__ void four_blocks(int n, F f) {
+    f(std::integral_constant<int, 0>{});
+    if (n > 1) f(std::integral_constant<int, 1>{});
+    if (n > 2) f(std::integral_constant<int, 2>{});
+    if (n > 3) f(std::integral_constant<int, 3>{});
+}
+
+// Of two neighbouring blocks of 16 channels (a, b; channels 4 quad .. + 3 of a
+// pixel to a lane) each lane completes one slice: of the first where its quad is
+// even, of the second where it is odd.
 template <typename E>
-__global__ __launch_bounds__(256) void pwfp8_kernel(PwFp8Params p) {
-    __shared__ float stage[4][64][17];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, quad = lane >> 4;
-    const unsigned cg = (p.nb16 + 3) / 4;
-    const int nb = (int)(blockIdx.x % cg) * 4 + wave, m0 = (int)(blockIdx.x / cg) * 64;
-    if (nb < p.nb16) {
-        f4 acc[4];
+__device__ __forceinline__ void store_pair(const PwFp8Params &p, f4 a, f4 b, int nb, int m, int quad) {
+    float v[8];
+    const bool odd = quad & 1;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) acc[j] = *(const f4 *)(p.bias + nb * 16 + quad * 4);
-        for (int kb = 0; kb < p.kb; ++kb) {
-            const uint4 *wp = (const uint4 *)p.w + ((size_t)nb * p.kb + kb) * 128 + lane;
-            const i8v w = join(wp[0], wp[64]);
-            const float sw = p.scales[(nb >> 3) * p.kb + kb];
+    for (int r = 0; r < 4; ++r) {
+        a[r] = act_keep(a[r], p.act);
+        b[r] = act_keep(b[r], p.act);
+        const float other = __shfl_xor(odd ? a[r] : b[r], 16, 64);
+        v[r] = odd ? other : a[r];
+        v[4 + r] = odd ? b[r] : other;
+    }
+    const int s = (nb + odd) * 2 + (quad >> 1);
+    if (m < p.M && s < p.ns) store8<E>(p.y, s, m, E::pack(v));
+}
+
+// Few pixels: bound by the weights' bytes and latency.  A workgroup has 16 channels
+// and 16 * FM pixels; its eight waves take the blocks of inputs in turn, four at a
+// time with all loads in flight, and their sums are added in the order of the waves.
+// RAW: the pixels are 16-bit and are brought into 8 bits here, as the quantize
+// kernel does, for what that launch costs.
+template <typename E, int FM, bool RAW>
+__global__ __launch_bounds__(512) void pwfp8_few_kernel(PwFp8Params p) {
+    __shared__ f4 red[8][FM][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, quad = lane >> 4;
+    const int nb = blockIdx.x % p.nb16, m0 = blockIdx.x / p.nb16 * (16 * FM);
+    const uint4 *wp = (const uint4 *)p.w + (size_t)nb * p.kb * 128 + lane;
+    const float *sp = p.scales + (nb >> 3) * p.kb;
+    f4 acc[FM];
+    int m[FM];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int m = min(m0 + j * 16 + col, p.M - 1);
-                const uint4 *xp = (const uint4 *)p.x.codes + (size_t)(kb * 8 + quad) * p.M + m;
-                const i8v x = join(xp[0], xp[(size_t)4 * p.M]);
-                const f4 part = mma8(w, x, p.x.exps[(size_t)(kb >> 2) * p.M + m], kb);
+    for (int j = 0; j < FM; ++j) {
+        acc[j] = f4{};
+        m[j] = min(m0 + j * 16 + col, p.M - 1);
+    }
+    for (int k0 = wave * 4; k0 < p.kb; k0 += 32) {
+        uint4 w[4][2], x[FM][4][RAW ? 4 : 2];
+        uint32_t e[FM];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int kb = min(k0 + u, p.kb - 1);
+            w[u][0] = wp[(size_t)kb * 128];
+            w[u][1] = wp[(size_t)kb * 128 + 64];
+        }
+#pragma unroll
+        for (int j = 0; j < FM; ++j) {
+            if constexpr (!RAW) e[j] = p.x.exps[(size_t)(k0 >> 2) * p.M + m[j]];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int kb = min(k0 + u, p.kb - 1);
+                if constexpr (RAW) {
+#pragma unroll
+                    for (int h = 0; h < 4; ++h) {
+                        const int s = kb * 16 + (h >> 1) * 8 + quad * 2 + (h & 1);
+                        const h8 v = p.raw.x[(size_t)min(s, p.raw_s - 1) * p.raw.s + (size_t)m[j] * p.raw.p];
+                        x[j][u][h] = __builtin_bit_cast(uint4, s < p.raw_s ? v : zero_h8());
+                    }
+                } else {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+                        x[j][u][h] = *((const uint4 *)p.x.codes + (size_t)(kb * 8 + h * 4 + quad) * p.M + m[j]);
+                }
+            }
+        }
+        four_blocks(p.kb - k0, [&](auto q) {
+            constexpr int u = decltype(q)::value;
+            const float sw = sp[k0 + u];
+#pragma unroll
+            for (int j = 0; j < FM; ++j) {
+                i8v xv;
+                uint32_t ev;
+                if constexpr (RAW) {
+                    ev = to_8_bits<E>(x[j][u], xv) << (8 * u);
+                } else {
+                    xv = join(x[j][u][0], x[j][u][1]);
+                    ev = e[j];
+                }
+                const f4 part = mma8<u>(join(w[u][0], w[u][1]), xv, ev);
 #pragma unroll
                 for (int r = 0; r < 4; ++r) acc[j][r] = fmaf(part[r], sw, acc[j][r]);
             }
+        });
+    }
+#pragma unroll
+    for (int j = 0; j < FM; ++j) red[wave][j][lane] = acc[j];
+    __syncthreads();
+    for (int j = wave; j < FM; j += 8) {
+        f4 v = *(const f4 *)(p.bias + nb * 16 + quad * 4);
+#pragma unroll
+        for (int w = 0; w < 8; ++w) v += red[w][j][lane];
+        // (the quads' halves of a slice meet)
+        const int at = m0 + j * 16 + col, s = nb * 2 + (quad >> 1);
+        float y[8];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            v[r] = act_keep(v[r], p.act);
+            const float other = __shfl_xor(v[r], 16, 64);
+            y[r] = quad & 1 ? other : v[r];
+            y[4 + r] = quad & 1 ? v[r] : other;
+        }
+        if ((quad & 1) == 0 && at < p.M && s < p.ns) store8<E>(p.y, s, at, E::pack(y));
+    }
+}
+
+// Many pixels: PX x CO tiles, 2-stage ring of one block of 128 inputs each.  Both
+// operands come by direct loads in the order of the matrix operands, so that LDS is
+// written and read in whole KiB.  A wave has WPX x WCO of the tile.
+template <int PX, int CO, int NPX, int NCO>
+struct PwTile {
+    static constexpr int WAVES = NPX * NCO, FM = PX / NPX / 16, FN = CO / NCO / 16;
+    static constexpr int XE = PX * 8, WE = CO * 8;                // 16-byte elements of a stage
+    static constexpr int LOADS = (XE + WE) / 64 / WAVES;
+    static_assert((XE / 64) % WAVES == 0 && (WE / 64) % WAVES == 0 && FN % 2 == 0, "whole loads to a wave, pairs of channel blocks");
+};
+
+template <typename E, int PX, int CO, int NPX, int NCO>
+__global__ __launch_bounds__(64 * NPX * NCO, 2) void pwfp8_tile_kernel(PwFp8Params p) {
+    using T = PwTile<PX, CO, NPX, NCO>;
+    constexpr int FM = T::FM, FN = T::FN, XL = T::XE / 64 / T::WAVES, WL = T::WE / 64 / T::WAVES;
+    __shared__ h8 ring[2][T::XE + T::WE];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, quad = lane >> 4;
+    const int ct = (p.nb16 * 16 + CO - 1) / CO, tile = xcd_tile(blockIdx.x, gridDim.x);
+    const int m0 = tile / ct * PX, n0 = tile % ct * (CO / 16);
+    const int wm = wave % NPX * FM, wn = wave / NPX * FN;         // the wave's first pixel and channel block
+
+    // the wave's loads: 64 pixels of a slice of 16 channels; half a block of 16 channels
+    const h8 *xp[XL], *wp[WL];
+#pragma unroll
+    for (int i = 0; i < XL; ++i) {
+        const int e = wave * XL + i, s = e / (PX / 64), px = e % (PX / 64) * 64 + lane;
+        xp[i] = (const h8 *)p.x.codes + (size_t)s * p.M + min(m0 + px, p.M - 1);
+    }
+#pragma unroll
+    for (int i = 0; i < WL; ++i) {
+        const int e = wave * WL + i, nb = min(n0 + e / 2, p.nb16 - 1);
+        wp[i] = (const h8 *)p.w + (size_t)nb * p.kb * 128 + (e & 1) * 64 + lane;
+    }
+    const size_t xstep = (size_t)8 * p.M;
+    auto issue = [&](h8 *st) {
+#pragma unroll
+        for (int i = 0; i < XL; ++i) {
+            load_lds16(xp[i], st + (wave * XL + i) * 64);
+            xp[i] += xstep;
         }
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+        for (int i = 0; i < WL; ++i) {
+            load_lds16(wp[i], st + T::XE + (wave * WL + i) * 64);
+            wp[i] += 128;
+        }
+    };
+    f4 acc[FN][FM];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) stage[wave][j * 16 + col][quad * 4 + r] = act_keep(acc[j][r], p.act);
+    for (int i = 0; i < FN; ++i)
+#pragma unroll
+        for (int j = 0; j < FM; ++j) acc[i][j] = f4{};
+    const uint32_t *ep[FM];
+    uint32_t e[FM], next[FM];
+#pragma unroll
+    for (int j = 0; j < FM; ++j) {
+        ep[j] = p.x.exps + min(m0 + (wm + j) * 16 + col, p.M - 1);
+        e[j] = *ep[j];
     }
-    __syncthreads();
-    if (nb >= p.nb16) return;
+    const float *sp = p.scales + (size_t)((n0 + wn) >> 3) * p.kb;
+    static_assert(FN <= 8, "a wave's channels share a scale");
+    issue(ring[0]);
+    auto step = [&](auto q, int kb) {
+        constexpr int u = decltype(q)::value;
+        h8 *st = ring[u & 1];
+        wait_vm_lds<0>();
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        if (u == 0 && kb + 4 < p.kb) {
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        const int m = m0 + lane, s = nb * 2 + k;
-        float v[8];
+            for (int j = 0; j < FM; ++j) next[j] = *(ep[j] += p.M);
+        }
+        if (kb + 1 < p.kb) issue(ring[(u & 1) ^ 1]);
+        const float sw = sp[kb];
+        i8v x[FM];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = stage[wave][lane][k * 8 + i];
-        if (m < p.M && s < p.ns) store8<E>(p.y, s, m, E::pack(v));
+        for (int j = 0; j < FM; ++j) {
+            const h8 *at = st + quad * PX + (wm + j) * 16 + col;
+            x[j] = join(__builtin_bit_cast(uint4, at[0]), __builtin_bit_cast(uint4, at[4 * PX]));
+        }
+#pragma unroll
+        for (int i = 0; i < FN; ++i) {
+            const h8 *at = st + T::XE + (wn + i) * 128 + lane;
+            const i8v w = join(__builtin_bit_cast(uint4, at[0]), __builtin_bit_cast(uint4, at[64]));
+#pragma unroll
+            for (int j = 0; j < FM; ++j) {
+                const f4 part = mma8<u>(w, x[j], e[j]);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) acc[i][j][r] = fmaf(part[r], sw, acc[i][j][r]);
+            }
+        }
+    };
+    for (int kb = 0; kb < p.kb; kb += 4) {
+        four_blocks(p.kb - kb, [&](auto q) { step(q, kb + decltype(q)::value); });
+#pragma unroll
+        for (int j = 0; j < FM; ++j) e[j] = next[j];
     }
+#pragma unroll
+    for (int i = 0; i < FN; i += 2) {
+        const int nb = n0 + wn + i;
+        if (nb >= p.nb16) break;
+        const f4 b0 = *(const f4 *)(p.bias + nb * 16 + quad * 4), b1 = *(const f4 *)(p.bias + nb * 16 + 16 + quad * 4);
+#pragma unroll
+        for (int j = 0; j < FM; ++j) store_pair<E>(p, acc[i][j] + b0, acc[i + 1][j] + b1, nb, m0 + (wm + j) * 16 + col, quad);
+    }
+}
+
+template <typename E, int PX, int CO, int NPX, int NCO>
+void launch_tile(const PwFp8Params &p, hipStream_t st) {
+    const size_t tiles = ((size_t)p.M + PX - 1) / PX * ((p.nb16 * 16 + CO - 1) / CO);
+    launch(pwfp8_tile_kernel<E, PX, CO, NPX, NCO>, dim3((unsigned)tiles), dim3(64 * NPX * NCO), 0, st, p);
+}
+
+template <typename E, int FM>
+void launch_few(const PwFp8Params &p, hipStream_t st) {
+    const dim3 grid((unsigned)(((size_t)p.M + 16 * FM - 1) / (16 * FM) * p.nb16));
+    launch(pwfp8_few_kernel<E, FM, false>, grid, dim3(512), 0, st, p);
+}
+
+template <typename E>
+hipError_t launch_pwfp8_t(const PwFp8Params &p, const PwFp8Geom &g, hipStream_t st) {
+    switch (g.variant) {
+        case 0:
+            if (p.raw.x) launch(pwfp8_few_kernel<E, 1, true>, dim3((unsigned)((p.M + 15) / 16 * p.nb16)), dim3(512), 0, st, p);
+            else if (p.M <= 16) launch_few<E, 1>(p, st);
+            else if (p.M <= 32) launch_few<E, 2>(p, st);
+            else launch_few<E, 4>(p, st);
+            break;
+        case 1: launch_tile<E, 64, 64, 2, 2>(p, st); break;
+        case 2: launch_tile<E, 128, 128, 2, 2>(p, st); break;
+        case 3: launch_tile<E, 256, 256, 4, 2>(p, st); break;
+        default: return hipErrorInvalidValue;
+    }
+    return hipGetLastError();
 }
 
 }  // namespace
 
-PwFp8Geom pwfp8_geom(size_t, int, int) { return PwFp8Geom{0}; }
+PwFp8Geom pwfp8_geom(size_t M, int nb16, int kb) {
+    if (M <= 64) return {0};
+    auto tiles = [&](size_t px, size_t co) { return (M + px - 1) / px * ((nb16 * 16 + co - 1) / co); };
+    if (tiles(256, 256) >= 256) return {3};
+    if (tiles(128, 128) >= 256) return {2};
+    if (tiles(64, 64) < 128 && kb >= 16) return {0};
+    return {1};
+}
 
-hipError_t launch_pwfp8(const PwFp8Params &p, const PwFp8Geom &, hipStream_t st) {
+hipError_t launch_pwfp8(const PwFp8Params &p, const PwFp8Geom &g, hipStream_t st) {
     if (p.M <= 0) return hipSuccess;
-    const dim3 grid((unsigned)(((size_t)p.M + 63) / 64 * ((p.nb16 + 3) / 4)));
-    if (p.bf16) launch(pwfp8_kernel<BF16>, grid, dim3(256), 0, st, p);
-    else launch(pwfp8_kernel<F16>, grid, dim3(256), 0, st, p);
-    return hipGetLastError();
+    return p.bf16 ? launch_pwfp8_t<BF16>(p, g, st) : launch_pwfp8_t<F16>(p, g, st);
 }
 
 }  // namespace kern

@@ -68,6 +68,33 @@ def test_layer(m, cin, cout, dtype):
     np.testing.assert_array_equal(f, y)
 
 
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("m,cin,cout", [(2000, 200, 2110), (16500, 136, 1000), (4200, 1300, 4100), (300, 4000, 500), (150, 2048, 1024)])
+def test_tiles(m, cin, cout, dtype):
+    # every tile form; some of the rows against the oracle
+    from block_util import run, within
+    log(f"[case] pointwise_fp8 {m}x{cin}x{cout} type {dtype}")
+    b, t, x = layer(m, cin, cout, dtype)
+    (y,), _ = run(b, [t], dtype, {t: dtype})
+    some = sorted(set(list(range(0, m, m // 40)) + [m - 1, m - 2]))
+    ref, bound = expect(b, t, x[:, :, some], dtype)
+    within(y[:, :, some], ref, bound)
+
+
+def test_few_pixels_in_8_bits_by_the_layer_itself_or_before():
+    # the same bits with the 8-bit tensor an output, which keeps it
+    from block_util import run
+    for m, cin, cout in ((1, 4096, 256), (7, 1000, 130), (16, 136, 40)):
+        for dtype in (0, 1):
+            log(f"[case] pointwise_fp8 {m}x{cin}x{cout} type {dtype}, in one kernel and two")
+            b, t, _ = layer(m, cin, cout, dtype, seed=3)
+            (y,), plan = run(b, [t], dtype)
+            assert [i["kind"] for i in plan.nodes() if "fp8" in i["kind"] or i["kind"] == "quantize"] == ["quantize_pointwise_fp8"]
+            (z, _), plan = run(b, [t, t - 1], dtype)
+            assert "quantize" in [i["kind"] for i in plan.nodes()]
+            np.testing.assert_array_equal(y, z)
+
+
 @pytest.mark.parametrize("act", [1, 2])
 def test_activation_and_images(act):
     from block_util import run, within
