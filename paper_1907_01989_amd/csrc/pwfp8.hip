@@ -227,8 +227,11 @@ __global__ __launch_bounds__(64 * NPX * NCO, 2) void pwfp8_tile_kernel(PwFp8Para
         ep[j] = p.x.exps + min(m0 + (wm + j) * 16 + col, p.M - 1);
         e[j] = *ep[j];
     }
+    // the blocks' scales, one to a lane (read as a scalar in the loop they would wait
+    // for the ring's loads)
+    static_assert(FN <= 8 && kMaxNormChannels <= 128 * 128, "a wave's channels share a scale; two registers of scales");
     const float *sp = p.scales + (size_t)((n0 + wn) >> 3) * p.kb;
-    static_assert(FN <= 8, "a wave's channels share a scale");
+    const float s0 = sp[min(lane, p.kb - 1)], s1 = sp[min(64 + lane, p.kb - 1)];
     issue(ring[0]);
     auto step = [&](auto q, int kb) {
         constexpr int u = decltype(q)::value;
@@ -241,23 +244,36 @@ __global__ __launch_bounds__(64 * NPX * NCO, 2) void pwfp8_tile_kernel(PwFp8Para
             for (int j = 0; j < FM; ++j) next[j] = *(ep[j] += p.M);
         }
         if (kb + 1 < p.kb) issue(ring[(u & 1) ^ 1]);
-        const float sw = sp[kb];
-        i8v x[FM];
+        const float sw = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(kb < 64 ? s0 : s1), kb & 63));
+        auto weights = [&](int i) {
+            const h8 *at = st + T::XE + (wn + i) * 128 + lane;
+            return join(__builtin_bit_cast(uint4, at[0]), __builtin_bit_cast(uint4, at[64]));
+        };
+        i8v x[FM], w = weights(0);
 #pragma unroll
         for (int j = 0; j < FM; ++j) {
             const h8 *at = st + quad * PX + (wm + j) * 16 + col;
             x[j] = join(__builtin_bit_cast(uint4, at[0]), __builtin_bit_cast(uint4, at[4 * PX]));
         }
+        // the products of a block of channels run while those of the one before are
+        // scaled and added, and the next one's weights are read
+        f4 part[2][FM];
 #pragma unroll
-        for (int i = 0; i < FN; ++i) {
-            const h8 *at = st + T::XE + (wn + i) * 128 + lane;
-            const i8v w = join(__builtin_bit_cast(uint4, at[0]), __builtin_bit_cast(uint4, at[64]));
+        for (int i = 0; i <= FN; ++i) {
+            i8v wn_;
+            if (i + 1 < FN) wn_ = weights(i + 1);
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int j = 0; j < FM; ++j) {
-                const f4 part = mma8<u>(w, x[j], e[j]);
+                if (i < FN) part[i & 1][j] = mma8<u>(w, x[j], e[j]);
+                __builtin_amdgcn_sched_barrier(0);
+                if (i > 0) {
 #pragma unroll
-                for (int r = 0; r < 4; ++r) acc[i][j][r] = fmaf(part[r], sw, acc[i][j][r]);
+                    for (int r = 0; r < 4; ++r) acc[i - 1][j][r] = fmaf(part[(i & 1) ^ 1][j][r], sw, acc[i - 1][j][r]);
+                }
+                __builtin_amdgcn_sched_barrier(0);
             }
+            w = wn_;
         }
     };
     for (int kb = 0; kb < p.kb; kb += 4) {
