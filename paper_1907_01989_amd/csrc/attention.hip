@@ -151,6 +151,35 @@ __device__ __forceinline__ bool any_odd(h8 v, bool bf) {
     return odd;
 }
 
+// A workgroup's head of keys, row tile and chunk.  An XCD (every eighth workgroup)
+// gets whole heads, whose keys then stay in its L2, where there are enough of them,
+// and walks the tiles of its heads side by side, so that the long ones of all come
+// first.
+template <int WR>
+__device__ __forceinline__ void place(const AttentionGeom &geo, int kv_heads, int block, int &kvh, int &tile, int &chunk) {
+    int item;
+    if (WR == 1) {
+        item = xcd_tile(block, geo.tiles * kv_heads * geo.chunks);
+        kvh = item % kv_heads;
+        item /= kv_heads;
+        tile = item / geo.chunks;
+        chunk = item - tile * geo.chunks;
+        return;
+    }
+    if (kv_heads % 8 == 0) {
+        const int own = kv_heads >> 3;
+        item = block >> 3;
+        kvh = (block & 7) * own + item % own;
+        item /= own;
+    } else {
+        item = xcd_tile(block, geo.tiles * kv_heads * geo.chunks);
+        kvh = item / (geo.tiles * geo.chunks);
+        item -= kvh * geo.tiles * geo.chunks;
+    }
+    tile = item / geo.chunks;
+    chunk = item - tile * geo.chunks;
+}
+
 // ND: the head's channels in steps of 32.  WR = 4: four waves of 32 rows share
 // tiles of 64 keys; WR = 1: four waves have the same 32 rows and 32 keys each, by
 // themselves.  Two stages of LDS: the next tile's loads are in flight while a tile
@@ -163,9 +192,9 @@ __global__ __launch_bounds__(256, WR == 4 ? 2 : 1) void attention_kernel(Attenti
     constexpr int OWN = WR == 4 ? 1 : 4;
     __shared__ h8 lds[2 * OWN * STAGE];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
-    const int item = xcd_tile(blockIdx.x, gridDim.x), chunk = item % geo.chunks, pair = item / geo.chunks;
-    const int kvh = pair / geo.tiles;
-    const Tile t = find_tile<BM>(p, pair - kvh * geo.tiles);
+    int kvh, number, chunk;
+    place<WR>(geo, p.kv_heads, blockIdx.x, kvh, number, chunk);
+    const Tile t = find_tile<BM>(p, number);
     if (t.none) return;
     const int rows = t.nq * p.group, first = t.tile * BM, r0 = first + (WR == 4 ? wave * 32 : 0);
     const int row = r0 + (lane & 31), rc = min(row, rows - 1);
@@ -201,19 +230,17 @@ __global__ __launch_bounds__(256, WR == 4 ? 2 : 1) void attention_kernel(Attenti
     int lk, ls;
     of_lane<NHWC>(lane, lk, ls);
     const h8 *kp = p.k.x + (size_t)(kvh * p.d8 + ls) * p.k.s, *vp = p.v.x + (size_t)(kvh * p.d8 + ls) * p.v.s;
-    auto issue = [&](int j0, int stage) {
-        h8 *to = lds + (stage * OWN + (WR == 4 ? 0 : wave)) * STAGE;
+    constexpr int BLOCKS = WR == 4 ? 1 : 2, LOADS = BLOCKS * ND;     // blocks of 16 keys that a wave loads, loads of K (or V)
+    auto issue = [&](int j0, int stage, bool values) {
+        h8 *to = lds + (stage * OWN + (WR == 4 ? 0 : wave)) * STAGE + (values ? PART : 0);
+        const TokenIn &x = values ? p.v : p.k;
 #pragma unroll
-        for (int u = 0; u < (WR == 4 ? 1 : 2); ++u) {
-            const int b = WR == 4 ? wave : u;                        // block of 16 keys of the tile
-            const size_t j = (size_t)(t.k0 + min(j0 + b * 16 + lk, t.nk - 1));
-            const h8 *kj = kp + j * p.k.p, *vj = vp + j * p.v.p;
+        for (int u = 0; u < BLOCKS; ++u) {
+            const int b = WR == 4 ? wave : u;
+            const h8 *at = (values ? vp : kp) + (size_t)(t.k0 + min(j0 + b * 16 + lk, t.nk - 1)) * x.p;
 #pragma unroll
-            for (int g = 0; g < ND; ++g) {
-                const bool zero = g == ND - 1 && ls + 4 * g >= p.d8;
-                load_lds16(zero ? p.zero : kj + (size_t)(4 * g) * p.k.s, to + (b * ND + g) * 64);
-                load_lds16(zero ? p.zero : vj + (size_t)(4 * g) * p.v.s, to + PART + (b * ND + g) * 64);
-            }
+            for (int g = 0; g < ND; ++g)
+                load_lds16(g == ND - 1 && ls + 4 * g >= p.d8 ? p.zero : at + (size_t)(4 * g) * x.s, to + (b * ND + g) * 64);
         }
     };
     // the lane's places in a stage, in elements (K: of even and odd steps of 16
@@ -223,24 +250,50 @@ __global__ __launch_bounds__(256, WR == 4 ? 2 : 1) void attention_kernel(Attenti
     const int va = at_of<NHWC>(4 * half + (key >> 2), (lane >> 4 & 1) * 2 + (key >> 1 & 1)) * 16 + (key & 1) * 8;
     constexpr int EIGHT = NHWC ? 512 : 128;                          // bytes from a key to the eighth after it
 
+    // Shared tiles: the next one's loads are in flight while one is worked on.  A
+    // wave's own: each half of a stage is refilled as soon as it has been read, so that
+    // three halves are always in flight (one query on 32768 keys: 31 -> 25 us).
     const int start = from + (WR == 4 ? 0 : wave * KEYS);
     int stage = 0;
-    if (start < most) issue(start, 0);
+    if (start < most) {
+        issue(start, 0, false);
+        issue(start, 0, true);
+    }
+    if (WR == 1 && start + STEP < most) {
+        issue(start + STEP, 1, false);
+        issue(start + STEP, 1, true);
+    }
     for (int j0 = start; j0 < most; j0 += STEP, stage ^= 1) {
-        wait_vm_lds<0>();
+        const bool more = j0 + STEP < most, refill = WR == 1 && j0 + 2 * STEP < most;
+        if (WR == 4) wait_vm_lds<0>();
+        else if (more) wait_vm_lds<3 * LOADS>();
+        else wait_vm_lds<LOADS>();
         if constexpr (WR == 4) __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");                               // (no LDS access moves over the wait)
-        if (j0 + STEP < most) issue(j0 + STEP, stage ^ 1);
+        if (WR == 4 && more) {
+            issue(j0 + STEP, stage ^ 1, false);
+            issue(j0 + STEP, stage ^ 1, true);
+        }
         h8 *kt = lds + (stage * OWN + (WR == 4 ? 0 : wave)) * STAGE, *vt = kt + PART;
         const bool masked = j0 + KEYS > least;
         f16v s[NK];
-        if (works && j0 < mine) {
+        if (WR == 1 || (works && j0 < mine)) {
 #pragma unroll
             for (int b = 0; b < NK; ++b) s[b] = f16v{};
 #pragma unroll
             for (int k = 0; k < ND * 2; ++k)
 #pragma unroll
                 for (int b = 0; b < NK; ++b) s[b] = mma32<E>(kt[ka[k & 1] + (b * 2 * ND + k / 2) * 64], q[k], s[b]);
+        }
+        if constexpr (WR == 1) {
+            if (refill) {
+                wait_vm_lds<63>();                                   // (the wave has read the keys)
+                issue(j0 + 2 * STEP, stage, false);
+            }
+            if (refill) wait_vm_lds<3 * LOADS>();
+            else if (more) wait_vm_lds<2 * LOADS>();
+            else wait_vm_lds<0>();
+            asm volatile("" ::: "memory");
         }
         if (masked) {
             // hidden keys have no score; values that are infinite or NaN are taken
@@ -275,7 +328,7 @@ __global__ __launch_bounds__(256, WR == 4 ? 2 : 1) void attention_kernel(Attenti
                 for (int i = 0; i < 16; ++i)
                     if (j0 + b * 32 + i / 4 * 8 + half * 4 + i % 4 >= lim) s[b][i] = -INFINITY;
         }
-        if (!works || j0 >= mine) continue;
+        if (WR == 4 && (!works || j0 >= mine)) continue;
         float top = s[0][0];
 #pragma unroll
         for (int b = 0; b < NK; ++b)
@@ -316,10 +369,14 @@ __global__ __launch_bounds__(256, WR == 4 ? 2 : 1) void attention_kernel(Attenti
                 const h8 v = __builtin_bit_cast(h8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
                 o[d] = mma32<E>(v, pr[k], o[d]);
             }
+        if (refill) {
+            wait_vm_lds<63>();                                       // (the wave has read the values)
+            issue(j0 + 2 * STEP, stage, true);
+        }
     }
     l += __shfl_xor(l, 32, 64);
     const int d32 = ND * 32;
-    const size_t slot = (size_t)(pair * geo.chunks + chunk) * BM;    // this chunk's rows among all partial ones
+    const size_t slot = ((size_t)(kvh * geo.tiles + number) * geo.chunks + chunk) * BM;    // this chunk's rows among all partial ones
     if constexpr (WR == 4) {
         if (!works) return;
         if (geo.chunks > 1) {
