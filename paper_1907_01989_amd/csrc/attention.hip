@@ -185,7 +185,7 @@ __device__ __forceinline__ void place(const AttentionGeom &geo, int kv_heads, in
 // themselves.  Two stages of LDS: the next tile's loads are in flight while a tile
 // is worked on.
 template <typename E, int ND, int WR, bool NHWC>
-__global__ __launch_bounds__(256, WR == 4 ? 2 : 1) void attention_kernel(AttentionParams p, AttentionGeom geo) {
+__global__ __launch_bounds__(256, WR == 1 ? 1 : ND == 3 ? 3 : 2) void attention_kernel(AttentionParams p, AttentionGeom geo) {
     constexpr int BM = tile_rows(WR), NK = WR == 4 ? 2 : 1;          // blocks of 32 keys of a wave's tile
     constexpr int KEYS = 32 * NK, STEP = WR == 4 ? KEYS : 4 * KEYS;  // keys of a wave's tile, from one to the next
     constexpr int PART = NK * 2 * ND * 64, STAGE = 2 * PART;         // elements of K (or V), of both
