@@ -299,9 +299,8 @@ mgi_status mgi_graph_add_entropy(mgi_graph *g, int in, int *out);
  * weight: c floats (NULL = ones); eps: at least 0, finite.  With fusion on, an
  * add whose sum this reads runs in the same kernel (the norm is of the sum as
  * stored, rounded to 16 bits, as without fusion).  to8 = 1: the output is an
- * 8-bit tensor as mgi_graph_add_quantize makes, rounded once from fp32.  The
- * squares are summed in fp32: rows whose sum of squares passes 3.4e38 give
- * zeros.  At most 2^14 channels (MGI_ERR_UNSUPPORTED). */
+ * 8-bit tensor as mgi_graph_add_quantize makes, rounded once from fp32.  At most
+ * 2^14 channels (MGI_ERR_UNSUPPORTED). */
 mgi_status mgi_graph_add_rms_norm(mgi_graph *g, int in, const float *weight, float eps, int to8,
                                   int *out);
 

@@ -45,6 +45,21 @@ struct Tile {
     bool none;
 };
 
+// Over the lanes of a wave: sums and maxima up to each lane (values of at least 0),
+// the left neighbour's value
+template <typename F>
+__device__ __forceinline__ int scan(int v, F join) {
+    v = join(v, __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false));   // shifts within rows of 16
+    v = join(v, __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false));
+    v = join(v, __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false));
+    v = join(v, __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false));
+    v = join(v, __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false));   // a row's last lane to the next row
+    return join(v, __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false));   // ... to the upper half
+}
+__device__ __forceinline__ int scan_add(int v) { return scan(v, [](int a, int b) { return a + b; }); }
+__device__ __forceinline__ int scan_max(int v) { return scan(v, [](int a, int b) { return max(a, b); }); }
+__device__ __forceinline__ int from_left(int v, int first) { return __builtin_amdgcn_update_dpp(first, v, 0x138, 0xf, 0xf, false); }
+
 // Finds tile `t` among the tiles of all sequences.  Bounds are read up to the
 // token count and not below their predecessors.  Two more sequences without
 // keys take the queries before the first bound and behind the last.
@@ -64,45 +79,26 @@ __device__ __forceinline__ Tile find_tile(const AttentionParams &p, int t) {
     const int lane = threadIdx.x & 63;
     int qmax = 0, kmax = 0, before = 0;
     for (int base = 0; base < p.nseq + 2; base += 64) {
-        const int i = base + lane;
-        int qe = i <= p.nseq ? min(max(p.bq[min(i, p.nseq)], 0), p.tq) : p.tq;
-        int ke = i <= p.nseq ? min(max((p.bk ? p.bk : p.bq)[min(i, p.nseq)], 0), p.tk) : p.tk;
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) {
-            const int a = __shfl_up(qe, d, 64), b = __shfl_up(ke, d, 64);
-            if (lane >= d) {
-                qe = max(qe, a);
-                ke = max(ke, b);
-            }
-        }
-        qe = max(qe, qmax);
-        ke = max(ke, kmax);
-        int qs = __shfl_up(qe, 1, 64), ks = __shfl_up(ke, 1, 64);
-        if (lane == 0) {
-            qs = qmax;
-            ks = kmax;
-        }
-        const int n = i < p.nseq + 2 ? ((qe - qs) * p.group + BM - 1) / BM : 0;
-        int upto = n;
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) {
-            const int a = __shfl_up(upto, d, 64);
-            if (lane >= d) upto += a;
-        }
-        const uint64_t has = __ballot(before + upto > t);
+        const int i = base + lane, at = min(i, p.nseq);
+        const int qv = p.bq[at], kv = p.bk ? p.bk[at] : qv;
+        const int qe = max(scan_max(i <= p.nseq ? min(max(qv, 0), p.tq) : p.tq), qmax);
+        const int ke = max(scan_max(i <= p.nseq ? min(max(kv, 0), p.tk) : p.tk), kmax);
+        const int qs = from_left(qe, qmax), ks = from_left(ke, kmax);
+        const int upto = before + scan_add(i < p.nseq + 2 ? ((qe - qs) * p.group + BM - 1) / BM : 0);
+        const uint64_t has = __ballot(upto > t);
         if (has) {
             const int src = __builtin_ctzll(has);
             const bool keys = base + src != 0 && base + src != p.nseq + 1;
-            r.q0 = __shfl(qs, src, 64);
-            r.nq = __shfl(qe, src, 64) - r.q0;
-            r.k0 = __shfl(ks, src, 64);
-            r.nk = keys ? __shfl(ke, src, 64) - r.k0 : 0;
-            r.tile = before + __shfl(upto, src, 64) - 1 - t;
+            r.q0 = __builtin_amdgcn_readlane(qs, src);
+            r.nq = __builtin_amdgcn_readlane(qe, src) - r.q0;
+            r.k0 = __builtin_amdgcn_readlane(ks, src);
+            r.nk = keys ? __builtin_amdgcn_readlane(ke, src) - r.k0 : 0;
+            r.tile = __builtin_amdgcn_readlane(upto, src) - 1 - t;
             return r;
         }
-        before += __shfl(upto, 63, 64);
-        qmax = __shfl(qe, 63, 64);
-        kmax = __shfl(ke, 63, 64);
+        before = __builtin_amdgcn_readlane(upto, 63);
+        qmax = __builtin_amdgcn_readlane(qe, 63);
+        kmax = __builtin_amdgcn_readlane(ke, 63);
     }
     r.none = true;
     return r;
@@ -205,8 +201,9 @@ __global__ __launch_bounds__(256, WR == 1 ? 1 : ND == 3 ? 3 : 2) void attention_
         return p.causal ? min(max(tok + 1 + t.nk - t.nq, 0), t.nk) : t.nk;
     };
     const int from = chunk * geo.chunk;
-    const int most = __builtin_amdgcn_readfirstlane(min(seen(first + BM - 1), geo.chunks > 1 ? from + geo.chunk : t.nk));
+    const int whole = seen(first + BM - 1), most = __builtin_amdgcn_readfirstlane(min(whole, geo.chunks > 1 ? from + geo.chunk : t.nk));
     if (chunk > 0 && from >= most) return;                           // (the first chunk writes rows that see nothing)
+    const bool split = __builtin_amdgcn_readfirstlane(geo.chunks > 1 && whole > geo.chunk);
     // the fewest that a row of the tile sees, the most that one of the wave does
     const int least = __builtin_amdgcn_readfirstlane(seen(first)), mine = __builtin_amdgcn_readfirstlane(min(seen(r0 + 31), most));
     const int lim = seen(rc);
@@ -379,7 +376,7 @@ __global__ __launch_bounds__(256, WR == 1 ? 1 : ND == 3 ? 3 : 2) void attention_
     const size_t slot = ((size_t)(kvh * geo.tiles + number) * geo.chunks + chunk) * BM;    // this chunk's rows among all partial ones
     if constexpr (WR == 4) {
         if (!works) return;
-        if (geo.chunks > 1) {
+        if (split) {
             if (row < rows) {
                 float *part = p.part + (slot + row - first) * (d32 + 2);
 #pragma unroll
@@ -403,7 +400,7 @@ __global__ __launch_bounds__(256, WR == 1 ? 1 : ND == 3 ? 3 : 2) void attention_
                 float v[8];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const float a = o[d][g * 4 + i] * inv, b = o[d][g * 4 + 4 + i] * inv;
+                    const float a = pinned(o[d][g * 4 + i] * inv), b = pinned(o[d][g * 4 + 4 + i] * inv);
                     const float other = __shfl_xor(half ? a : b, 32, 64);
                     v[i] = half ? other : a;
                     v[4 + i] = half ? b : other;
@@ -441,7 +438,7 @@ __global__ __launch_bounds__(256, WR == 1 ? 1 : ND == 3 ? 3 : 2) void attention_
 #pragma unroll
                 for (int i = 0; i < 8; ++i) v[i] = fmaf(i < 4 ? lo[i & 3] : hi[i & 3], f, v[i]);
             }
-            if (geo.chunks > 1) {
+            if (split) {
                 float *part = p.part + (slot + r) * (d32 + 2);
 #pragma unroll
                 for (int i = 0; i < 8; i += 2) *(float2 *)(part + sl * 8 + i) = float2{v[i], v[i + 1]};
@@ -449,7 +446,7 @@ __global__ __launch_bounds__(256, WR == 1 ? 1 : ND == 3 ? 3 : 2) void attention_
             } else {
                 const float inv = total == 0.0f ? 0.0f : 1.0f / total;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] *= inv;
+                for (int i = 0; i < 8; ++i) v[i] = pinned(v[i] * inv);
                 const int tok = (first + r) / p.group, hd = kvh * p.group + first + r - tok * p.group;
                 store8<E>(p.y, hd * p.d8 + sl, t.q0 + tok, E::pack(v));
             }
@@ -457,21 +454,23 @@ __global__ __launch_bounds__(256, WR == 1 ? 1 : ND == 3 ? 3 : 2) void attention_
     }
 }
 
-// Joins the chunks of a row: a thread has 8 channels of every 16th chunk, then 16
-// threads join what those found, in order.
-template <typename E, int BM>
+// Joins the chunks of the rows that have several: a thread has 8 channels of every
+// CG-th chunk of a row, then what CG threads found is joined in order.
+template <typename E, int BM, int CG>
 __global__ __launch_bounds__(256) void attention_join_kernel(AttentionParams p, AttentionGeom geo, int d32) {
-    __shared__ float found[16][16][8];
-    __shared__ float2 ml[16][16];
-    const int pair = blockIdx.x / BM, r = blockIdx.x - pair * BM, kvh = pair / geo.tiles;
+    constexpr int ROWS = 16 / CG;                                    // of a workgroup
+    __shared__ float found[CG > 1 ? CG : 1][16][8];
+    __shared__ float2 ml[CG > 1 ? CG : 1][16];
+    const int pair = blockIdx.x / (BM / ROWS), kvh = pair / geo.tiles;
+    const int sl = threadIdx.x & 15, g = CG > 1 ? threadIdx.x >> 4 : 0, r = (blockIdx.x - pair * (BM / ROWS)) * ROWS + (CG > 1 ? 0 : threadIdx.x >> 4);
     const Tile t = find_tile<BM>(p, pair - kvh * geo.tiles);
     const int rows = t.nq * p.group, first = t.tile * BM, row = first + r;
-    if (t.none || row >= rows) return;
+    if (t.none || first >= rows) return;
     const int last = min(first + BM - 1, rows - 1) / p.group;
     const int most = p.causal ? min(max(last + 1 + t.nk - t.nq, 0), t.nk) : t.nk;
-    const int n = min(max(1, (most + geo.chunk - 1) / geo.chunk), geo.chunks);
+    const int n = min((most + geo.chunk - 1) / geo.chunk, geo.chunks);
+    if (n < 2) return;
     const float c = fabsf(p.scale);
-    const int sl = threadIdx.x & 15, g = threadIdx.x >> 4;
     const float *part = p.part + ((size_t)pair * geo.chunks * BM + r) * (d32 + 2);
     const size_t step = (size_t)BM * (d32 + 2);
     float top = -INFINITY, total = 0.0f, v[8] = {};
@@ -484,8 +483,8 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionParams p, 
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = fmaf(x[i], f, v[i] * keep);
     };
-    if (sl < p.d8) {
-        for (int k = g; k < n; k += 16) {
+    if (sl < p.d8 && row < rows) {
+        for (int k = g; k < n; k += CG) {
             const float *at = part + k * step;
             const float2 w = *(const float2 *)(at + d32);
             float x[8];
@@ -494,15 +493,18 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionParams p, 
             add(w.x, w.y, x);
         }
     }
+    if constexpr (CG > 1) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) found[g][sl][i] = v[i];
-    ml[g][sl] = float2{top, total};
-    __syncthreads();
-    if (g > 0 || sl >= p.d8) return;
-    for (int k = 1; k < min(n, 16); ++k) add(ml[k][sl].x, ml[k][sl].y, found[k][sl]);
+        for (int i = 0; i < 8; ++i) found[g][sl][i] = v[i];
+        ml[g][sl] = float2{top, total};
+        __syncthreads();
+        if (g > 0) return;
+        for (int k = 1; k < min(n, CG); ++k) add(ml[k][sl].x, ml[k][sl].y, found[k][sl]);
+    }
+    if (row >= rows || sl >= p.d8) return;
     const float inv = total == 0.0f ? 0.0f : 1.0f / total;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] *= inv;
+    for (int i = 0; i < 8; ++i) v[i] = pinned(v[i] * inv);
     const int tok = row / p.group, hd = kvh * p.group + row - tok * p.group;
     store8<E>(p.y, hd * p.d8 + sl, t.q0 + tok, E::pack(v));
 }
@@ -518,9 +520,10 @@ void launch_attention_w(const AttentionParams &p, const AttentionGeom &g, hipStr
     else launch(attention_kernel<E, ND, WR, false>, grid, dim3(256), 0, st, p, g);
     ev = saved;
     if (g.chunks == 1) return;
-    const dim3 join((unsigned)g.tiles * p.kv_heads * tile_rows(WR));
+    constexpr int CG = WR == 1 ? 16 : 1;                             // (many chunks of few rows, few of many)
+    const dim3 join((unsigned)g.tiles * p.kv_heads * (tile_rows(WR) * CG / 16));
     ev.start = nullptr;
-    launch(attention_join_kernel<E, tile_rows(WR)>, join, dim3(256), 0, st, p, g, ND * 32);
+    launch(attention_join_kernel<E, tile_rows(WR), CG>, join, dim3(256), 0, st, p, g, ND * 32);
     ev = saved;
 }
 
@@ -551,9 +554,10 @@ AttentionGeom attention_geom(int q_tokens, int k_tokens, int n, int nseq, int gr
     g.wr = rows <= 32 * sequences ? 1 : 4;
     const int bm = tile_rows(g.wr);
     g.tiles = (int)(nseq ? rows / bm + nseq + 2 : n * ((rows / n + bm - 1) / bm));
-    // fewer workgroups than the card holds (two to a compute unit of tiles that
-    // waves share, one of the others): the keys are split
-    const long keys = nseq ? k_tokens : k_tokens / n, items = (long)g.tiles * kv_heads, want = g.wr == 4 ? 512 : 256;
+    // fewer workgroups than twice what the card holds of tiles that waves share (two
+    // to a compute unit), whose longest would end alone, or than it holds of the
+    // others (one): the keys are split
+    const long keys = nseq ? k_tokens : k_tokens / n, items = (long)g.tiles * kv_heads, want = g.wr == 4 ? 1024 : 256;
     const int step = g.wr == 4 ? kBN : 4 * kPrivate;
     long chunks = items < want ? want / items : 1;
     chunks = std::min(chunks, (keys + 4 * step - 1) / (4 * step));

@@ -455,7 +455,7 @@ struct NormParams {
     int act;             // of the sum
     TokenOut sum;        // y null: not stored
     const float *w;      // [whole blocks of 128 channels], zero past the last; null: no norm
-    float eps, inv_c;
+    double eps, inv_c;
     TokenOut out;        // 16-bit output, or the values of the 8-bit one; or
     Tensor8 q;           // codes null: `out` is written
     int to8;

@@ -527,7 +527,7 @@ hipError_t launch_norm_node(const mgi_plan &p, const Node &nd, const Bases &B, h
     }
     if (nd.norm) q.w = (const float *)(wbase + nd.w_off);
     q.eps = nd.eps;
-    q.inv_c = 1.0f / x.c;
+    q.inv_c = 1.0 / x.c;
     q.to8 = nd.to8;
     if (nd.to8 && !writes_output(p, nd.direct_out, B)) q.q = tensor8(p, nd.out, B);
     else q.out = token_out(p, nd.out, nd.direct_out, B);

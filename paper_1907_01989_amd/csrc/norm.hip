@@ -3,6 +3,10 @@
 //   h = act(a + b) rounded to 16 bits (or a);  y = h w / sqrt(mean h^2 + eps) (or h)
 //   8-bit: e the smallest with max |y| <= 448 2^e over 128 channels, code = e4m3(y 2^-e)
 //
+// The squares are summed in 64 bits, which no 16-bit value overflows and which
+// leaves the two products with scale and weight as the only fp32 roundings (the
+// conversions hide behind the loads: 16384 x 2048 takes the same time).
+//
 // One pass: a pixel's channels stay in registers (as the 16-bit values they
 // are) between the sum of squares and the output, so that each operand is read
 // once.  Scaling by a power of two is exact, so a code differs from the
@@ -20,7 +24,7 @@ namespace {
 template <typename E, int P, int R, bool NORM, bool TO8>
 __global__ __launch_bounds__(1024) void norm_kernel(NormParams p) {
     constexpr int SUBS = 64 / P, NS = P == 8 ? 2 : 1, CH = SUBS * NS;   // slices of a wave's chunk
-    __shared__ float part[16][P];
+    __shared__ double part[16][P];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, W = blockDim.x >> 6;
     const int sub = lane / P, m = blockIdx.x * P + lane % P, mc = min(m, p.M - 1);
     h8 h[R][NS], b[R][NS];
@@ -32,7 +36,7 @@ __global__ __launch_bounds__(1024) void norm_kernel(NormParams p) {
             h[r][j] = p.a.x[(size_t)s * p.a.s + (size_t)mc * p.a.p];
             if (p.b.x) b[r][j] = p.b.x[(size_t)s * p.b.s + (size_t)mc * p.b.p];
         }
-    float squares = 0.0f;
+    double squares = 0.0;
 #pragma unroll
     for (int r = 0; r < R; ++r)
 #pragma unroll
@@ -41,14 +45,14 @@ __global__ __launch_bounds__(1024) void norm_kernel(NormParams p) {
             if (p.b.x) {
                 float v[8];
 #pragma unroll
-                for (int c = 0; c < 8; ++c) v[c] = act_apply(E::get(h[r][j], c) + E::get(b[r][j], c), p.act);
+                for (int c = 0; c < 8; ++c) v[c] = pinned(act_apply(E::get(h[r][j], c) + E::get(b[r][j], c), p.act));
                 h[r][j] = E::pack(v);
                 if (p.sum.y && s < p.S && m < p.M) store8<E>(p.sum, s, m, h[r][j]);
             }
             if (s >= p.S) h[r][j] = zero_h8();
             if constexpr (NORM) {
 #pragma unroll
-                for (int c = 0; c < 8; ++c) squares = fmaf(E::get(h[r][j], c), E::get(h[r][j], c), squares);
+                for (int c = 0; c < 8; ++c) squares = fma((double)E::get(h[r][j], c), (double)E::get(h[r][j], c), squares);
             }
         }
     float scale = 1.0f;
@@ -58,10 +62,10 @@ __global__ __launch_bounds__(1024) void norm_kernel(NormParams p) {
         if (W > 1) {
             if (sub == 0) part[wave][lane % P] = squares;
             __syncthreads();
-            squares = 0.0f;
+            squares = 0.0;
             for (int w = 0; w < W; ++w) squares += part[w][lane % P];
         }
-        scale = 1.0f / sqrtf(fmaf(squares, p.inv_c, p.eps));
+        scale = (float)(1.0 / sqrt(squares * p.inv_c + p.eps));
     }
 #pragma unroll
     for (int r = 0; r < R; ++r) {
@@ -73,7 +77,7 @@ __global__ __launch_bounds__(1024) void norm_kernel(NormParams p) {
                 const f4 *wp = (const f4 *)p.w + 2 * min(s, p.KB * 16 - 1);
                 const f4 lo = wp[0], hi = wp[1];
 #pragma unroll
-                for (int c = 0; c < 8; ++c) y[j][c] = E::get(h[r][j], c) * scale * (c < 4 ? lo[c & 3] : hi[c & 3]);
+                for (int c = 0; c < 8; ++c) y[j][c] = pinned(E::get(h[r][j], c) * scale * (c < 4 ? lo[c & 3] : hi[c & 3]));
             } else {
 #pragma unroll
                 for (int c = 0; c < 8; ++c) y[j][c] = E::get(h[r][j], c);
@@ -139,18 +143,37 @@ hipError_t launch_norm_p(const NormParams &p, hipStream_t st) {
     return hipGetLastError();
 }
 
+// Whether rows of C values of `size` bytes are whole 16-byte units from y on.
+__device__ __forceinline__ bool whole_rows(const void *y, int C) { return C % 8 == 0 && ((uintptr_t)y & 15) == 0; }
+
+// A wave's 8 pixels x 64 channels through LDS, so that memory sees a pixel's
+// channels side by side also where they are no whole 16-byte units (2115 x 6290:
+// 31 us by single stores from the sliced order).
+template <typename T>
+__device__ __forceinline__ void store_rows(T *tile, const T *v, T *y, int M, int C, int m, int s) {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) tile[(lane & 7) * 66 + (lane >> 3) * 8 + c] = v[c];
+    __builtin_amdgcn_wave_barrier();
+    const int m0 = m - (lane & 7), c = (s - (lane >> 3)) * 8 + lane;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (m0 + i < M && c < C) y[(size_t)(m0 + i) * C + c] = tile[i * 66 + lane];
+}
+
 __global__ __launch_bounds__(256) void export16_kernel(const h8 *x, uint16_t *y, int M, int C, int S) {
+    __shared__ uint16_t tile[4][8 * 66];
     int m, s;
-    if (!plane_place(M, S, m, s)) return;
-    const h8 v = x[(size_t)s * M + m];
-    uint16_t *d = y + (size_t)m * C + s * 8;
-    if (C % 8 == 0 && ((uintptr_t)y & 15) == 0) {
-        *(h8 *)d = v;
+    const bool in = plane_place(M, S, m, s);
+    const h8 v = x[(size_t)min(s, S - 1) * M + min(m, M - 1)];
+    if (whole_rows(y, C)) {
+        if (in) *(h8 *)(y + (size_t)m * C + s * 8) = v;
         return;
     }
+    uint16_t b[8];
 #pragma unroll
-    for (int c = 0; c < 8; ++c)
-        if (s * 8 + c < C) d[c] = bits8(v)[c];
+    for (int c = 0; c < 8; ++c) b[c] = bits8(v)[c];
+    store_rows(tile[threadIdx.x >> 6], b, y, M, C, m, s);
 }
 
 __global__ __launch_bounds__(256) void ingest16_kernel(const uint16_t *x, h8 *y, int M, int C, int S) {
@@ -158,7 +181,7 @@ __global__ __launch_bounds__(256) void ingest16_kernel(const uint16_t *x, h8 *y,
     if (!plane_place(M, S, m, s)) return;
     const uint16_t *d = x + (size_t)m * C + s * 8;
     h8 v = zero_h8();
-    if (C % 8 == 0 && ((uintptr_t)x & 15) == 0) {
+    if (whole_rows(x, C)) {
         v = *(const h8 *)d;
     } else {
 #pragma unroll
@@ -170,19 +193,22 @@ __global__ __launch_bounds__(256) void ingest16_kernel(const uint16_t *x, h8 *y,
 
 template <typename E>
 __global__ __launch_bounds__(256) void export8_kernel(Tensor8 x, void *y, int f32, int M, int C, int S) {
+    __shared__ float tile[4][8 * 66];
     int m, s;
-    if (!plane_place(M, S, m, s)) return;
-    const uint2 q = *(const uint2 *)(x.codes + ((size_t)(s >> 1) * M + m) * 16 + (s & 1) * 8);
-    const float up = power2((int)(x.exps[(size_t)(s >> 6) * M + m] >> (8 * (s >> 4 & 3)) & 255) - 127);
+    plane_place(M, S, m, s);
+    const int mc = min(m, M - 1), sc = min(s, S - 1);
+    const uint2 q = *(const uint2 *)(x.codes + ((size_t)(sc >> 1) * M + mc) * 16 + (sc & 1) * 8);
+    const float up = power2((int)(x.exps[(size_t)(sc >> 6) * M + mc] >> (8 * (sc >> 4 & 3)) & 255) - 127);
     float v[8];
     values8(q, up, v);
-    const h8 r = E::pack(v);
+    if (f32) {
+        store_rows(tile[threadIdx.x >> 6], v, (float *)y, M, C, m, s);
+    } else {
+        uint16_t b[8];
+        const u16x8 r = bits8(E::pack(v));
 #pragma unroll
-    for (int c = 0; c < 8; ++c) {
-        if (s * 8 + c >= C) break;
-        const size_t at = (size_t)m * C + s * 8 + c;
-        if (f32) ((float *)y)[at] = v[c];
-        else ((uint16_t *)y)[at] = bits8(r)[c];
+        for (int c = 0; c < 8; ++c) b[c] = r[c];
+        store_rows((uint16_t *)tile[threadIdx.x >> 6], b, (uint16_t *)y, M, C, m, s);
     }
 }
 
@@ -190,8 +216,10 @@ __global__ __launch_bounds__(256) void export8_kernel(Tensor8 x, void *y, int f3
 
 hipError_t launch_norm(const NormParams &p, hipStream_t st) {
     if (p.M <= 0) return hipSuccess;
-    // one pixel to a wave where there are few; eight else
-    if (p.M < 64) return p.bf16 ? launch_norm_p<BF16, 1>(p, st) : launch_norm_p<F16, 1>(p, st);
+    // one pixel to a wave where there are few, or where all is NHWC, whose pixels are
+    // whole lines; eight else, for the sliced side
+    const bool nhwc = p.a.s == 1 && (!p.b.x || p.b.s == 1) && (!p.sum.y || p.sum.s == 1) && !p.q.codes && p.out.s == 1;
+    if (p.M < 64 || nhwc) return p.bf16 ? launch_norm_p<BF16, 1>(p, st) : launch_norm_p<F16, 1>(p, st);
     return p.bf16 ? launch_norm_p<BF16, 8>(p, st) : launch_norm_p<F16, 8>(p, st);
 }
 

@@ -35,20 +35,55 @@ __device__ __forceinline__ f4 mma8(i8v w, i8v x, uint32_t e) {
 
 // A block of a pixel's inputs, 32 of them to each of the lanes l, l ^ 16, l ^ 32,
 // l ^ 48, in 8 bits: the codes in the operand's order and the exponent's byte.
+// Magnitudes are compared as 16-bit integers, and pairs are scaled and converted by
+// one instruction; blocks with infinities or NaN take the quantize kernel's way.
 template <typename E>
 __device__ __forceinline__ uint32_t to_8_bits(const uint4 (&raw)[4], i8v &codes) {
-    float top = 0.0f;
+    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+    const uint32_t *words = (const uint32_t *)raw;
+    u16x2 most{};
 #pragma unroll
-    for (int h = 0; h < 4; ++h) top = fmaxf(top, finite_top<E>(__builtin_bit_cast(h8, raw[h])));
-    top = fmaxf(top, __shfl_xor(top, 16, 64));
-    top = fmaxf(top, __shfl_xor(top, 32, 64));
-    const int e = block_exponent(top);
-    const float down = power2(-e);
+    for (int i = 0; i < 16; ++i) most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, words[i] & 0x7fff7fffu));
+    uint32_t top = max(most[0], most[1]);
+    top = max(top, (uint32_t)__shfl_xor((int)top, 16, 64));
+    top = max(top, (uint32_t)__shfl_xor((int)top, 32, 64));
+    if (__any(top >= (E::bf ? 0x7f80u : 0x7c00u))) {
+        float t = 0.0f;
 #pragma unroll
-    for (int h = 0; h < 4; ++h) {
-        const uint2 q = codes8<E>(__builtin_bit_cast(h8, raw[h]), down);
-        codes[2 * h] = (int)q.x;
-        codes[2 * h + 1] = (int)q.y;
+        for (int h = 0; h < 4; ++h) t = fmaxf(t, finite_top<E>(__builtin_bit_cast(h8, raw[h])));
+        t = fmaxf(t, __shfl_xor(t, 16, 64));
+        t = fmaxf(t, __shfl_xor(t, 32, 64));
+        const int e = block_exponent(t);
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+            const uint2 q = codes8<E>(__builtin_bit_cast(h8, raw[h]), power2(-e));
+            codes[2 * h] = (int)q.x;
+            codes[2 * h + 1] = (int)q.y;
+        }
+        return (uint32_t)(e + 127);
+    }
+    h8 one = zero_h8();
+    {
+        u16x8 b = bits8(one);
+        b[0] = (uint16_t)top;
+        one = __builtin_bit_cast(h8, b);
+    }
+    const int e = block_exponent(E::get(one, 0));
+    const float up = power2(e);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        typedef short s2 __attribute__((ext_vector_type(2)));
+        s2 q{};
+        if constexpr (E::bf) {
+            typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+            q = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(q, __builtin_bit_cast(b2, words[2 * i]), up, false);
+            q = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(q, __builtin_bit_cast(b2, words[2 * i + 1]), up, true);
+        } else {
+            typedef _Float16 f2 __attribute__((ext_vector_type(2)));
+            q = __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(q, __builtin_bit_cast(f2, words[2 * i]), up, false);
+            q = __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(q, __builtin_bit_cast(f2, words[2 * i + 1]), up, true);
+        }
+        codes[i] = __builtin_bit_cast(int, q);
     }
     return (uint32_t)(e + 127);
 }
@@ -71,8 +106,8 @@ __device__ __forceinline__ void store_pair(const PwFp8Params &p, f4 a, f4 b, int
     const bool odd = quad & 1;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-        a[r] = act_keep(a[r], p.act);
-        b[r] = act_keep(b[r], p.act);
+        a[r] = pinned(act_keep(a[r], p.act));
+        b[r] = pinned(act_keep(b[r], p.act));
         const float other = __shfl_xor(odd ? a[r] : b[r], 16, 64);
         v[r] = odd ? other : a[r];
         v[4 + r] = odd ? b[r] : other;
@@ -160,7 +195,7 @@ __global__ __launch_bounds__(512) void pwfp8_few_kernel(PwFp8Params p) {
         float y[8];
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            v[r] = act_keep(v[r], p.act);
+            v[r] = pinned(act_keep(v[r], p.act));
             const float other = __shfl_xor(v[r], 16, 64);
             y[r] = quad & 1 ? other : v[r];
             y[4 + r] = quad & 1 ? v[r] : other;
@@ -169,7 +204,7 @@ __global__ __launch_bounds__(512) void pwfp8_few_kernel(PwFp8Params p) {
     }
 }
 
-// Many pixels: PX x CO tiles, 2-stage ring of one block of 128 inputs each.  Both
+// Many pixels: PX x CO tiles, a ring of NST stages of one block of 128 inputs each.  Both
 // operands come by direct loads in the order of the matrix operands, so that LDS is
 // written and read in whole KiB.  A wave has WPX x WCO of the tile.
 template <int PX, int CO, int NPX, int NCO>
@@ -180,11 +215,12 @@ struct PwTile {
     static_assert((XE / 64) % WAVES == 0 && (WE / 64) % WAVES == 0 && FN % 2 == 0, "whole loads to a wave, pairs of channel blocks");
 };
 
-template <typename E, int PX, int CO, int NPX, int NCO>
+template <typename E, int PX, int CO, int NPX, int NCO, int NST>
 __global__ __launch_bounds__(64 * NPX * NCO, 2) void pwfp8_tile_kernel(PwFp8Params p) {
     using T = PwTile<PX, CO, NPX, NCO>;
     constexpr int FM = T::FM, FN = T::FN, XL = T::XE / 64 / T::WAVES, WL = T::WE / 64 / T::WAVES;
-    __shared__ h8 ring[2][T::XE + T::WE];
+    static_assert(NST == 2 || NST == 4, "a step's stage is known when it is compiled");
+    __shared__ h8 ring[NST][T::XE + T::WE];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, quad = lane >> 4;
     const int ct = (p.nb16 * 16 + CO - 1) / CO, tile = xcd_tile(blockIdx.x, gridDim.x);
     const int m0 = tile / ct * PX, n0 = tile % ct * (CO / 16);
@@ -232,18 +268,22 @@ __global__ __launch_bounds__(64 * NPX * NCO, 2) void pwfp8_tile_kernel(PwFp8Para
     static_assert(FN <= 8 && kMaxNormChannels <= 128 * 128, "a wave's channels share a scale; two registers of scales");
     const float *sp = p.scales + (size_t)((n0 + wn) >> 3) * p.kb;
     const float s0 = sp[min(lane, p.kb - 1)], s1 = sp[min(64 + lane, p.kb - 1)];
-    issue(ring[0]);
+#pragma unroll
+    for (int i = 0; i < NST - 1; ++i)
+        if (i < p.kb) issue(ring[i]);
     auto step = [&](auto q, int kb) {
         constexpr int u = decltype(q)::value;
-        h8 *st = ring[u & 1];
-        wait_vm_lds<0>();
+        h8 *st = ring[u % NST];
+        if (NST == 2 || kb + 1 >= p.kb) wait_vm_lds<0>();            // (stages issued after this one stay in flight)
+        else if (kb + 2 >= p.kb) wait_vm_lds<T::LOADS>();
+        else wait_vm_lds<2 * T::LOADS>();
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         if (u == 0 && kb + 4 < p.kb) {
 #pragma unroll
             for (int j = 0; j < FM; ++j) next[j] = *(ep[j] += p.M);
         }
-        if (kb + 1 < p.kb) issue(ring[(u & 1) ^ 1]);
+        if (kb + NST - 1 < p.kb) issue(ring[(u + NST - 1) % NST]);
         const float sw = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(kb < 64 ? s0 : s1), kb & 63));
         auto weights = [&](int i) {
             const h8 *at = st + T::XE + (wn + i) * 128 + lane;
@@ -291,10 +331,10 @@ __global__ __launch_bounds__(64 * NPX * NCO, 2) void pwfp8_tile_kernel(PwFp8Para
     }
 }
 
-template <typename E, int PX, int CO, int NPX, int NCO>
+template <typename E, int PX, int CO, int NPX, int NCO, int NST>
 void launch_tile(const PwFp8Params &p, hipStream_t st) {
     const size_t tiles = ((size_t)p.M + PX - 1) / PX * ((p.nb16 * 16 + CO - 1) / CO);
-    launch(pwfp8_tile_kernel<E, PX, CO, NPX, NCO>, dim3((unsigned)tiles), dim3(64 * NPX * NCO), 0, st, p);
+    launch(pwfp8_tile_kernel<E, PX, CO, NPX, NCO, NST>, dim3((unsigned)tiles), dim3(64 * NPX * NCO), 0, st, p);
 }
 
 template <typename E, int FM>
@@ -312,9 +352,9 @@ hipError_t launch_pwfp8_t(const PwFp8Params &p, const PwFp8Geom &g, hipStream_t 
             else if (p.M <= 32) launch_few<E, 2>(p, st);
             else launch_few<E, 4>(p, st);
             break;
-        case 1: launch_tile<E, 64, 64, 2, 2>(p, st); break;
-        case 2: launch_tile<E, 128, 128, 2, 2>(p, st); break;
-        case 3: launch_tile<E, 256, 256, 4, 2>(p, st); break;
+        case 1: launch_tile<E, 64, 64, 2, 2, 4>(p, st); break;
+        case 2: launch_tile<E, 128, 128, 2, 2, 4>(p, st); break;
+        case 3: launch_tile<E, 256, 256, 4, 2, 2>(p, st); break;
         default: return hipErrorInvalidValue;
     }
     return hipGetLastError();

@@ -69,8 +69,8 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryParams p, int units, 
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const float c = E::get(x, 2 * i), d = E::get(x, 2 * i + 1);
-                v[2 * i] = c * cs[i] - d * sn[i];
-                v[2 * i + 1] = c * sn[i] + d * cs[i];
+                v[2 * i] = pinned(c * cs[i] - d * sn[i]);
+                v[2 * i + 1] = pinned(c * sn[i] + d * cs[i]);
             }
             store8<E>(p.y, s + a, m, E::pack(v));
         } else {
@@ -79,8 +79,8 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryParams p, int units, 
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const float c = E::get(x, i), d = E::get(y, i);
-                v[i] = c * cs[i] - d * sn[i];
-                w[i] = c * sn[i] + d * cs[i];
+                v[i] = pinned(c * cs[i] - d * sn[i]);
+                w[i] = pinned(c * sn[i] + d * cs[i]);
             }
             store8<E>(p.y, s + a, m, E::pack(v));
             store8<E>(p.y, s + b, m, E::pack(w));
@@ -110,7 +110,7 @@ __global__ __launch_bounds__(256) void rotary_any_kernel(RotaryParams p) {
         other[0] = ((const _Float16 *)at)[o % 8];
         float sn, cs;
         turn(place[p.axis[pair]], p.freq[pair], sn, cs);
-        v[i] = first ? v[i] * cs - E::get(other, 0) * sn : E::get(other, 0) * sn + v[i] * cs;
+        v[i] = pinned(first ? v[i] * cs - E::get(other, 0) * sn : E::get(other, 0) * sn + v[i] * cs);
     }
     store8<E>(p.y, s, m, E::pack(v));
 }

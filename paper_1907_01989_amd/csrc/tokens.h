@@ -10,6 +10,15 @@ namespace kern {
 // v[i]), gives the first one's bits whatever i is)
 __device__ __forceinline__ u16x8 bits8(h8 v) { return __builtin_bit_cast(u16x8, v); }
 
+// An fp32 value as it is: without this the compiler may make one instruction of a
+// product or sum and its rounding to fp16 (v_fma_mixlo_f16), which rounds once
+// where fp32 and then fp16 rounds twice, in some instances of a kernel and not in
+// others, whose results then differ.
+__device__ __forceinline__ float pinned(float v) {
+    asm("" : "+v"(v));
+    return v;
+}
+
 // act_apply that leaves NaN a NaN
 __device__ __forceinline__ float act_keep(float v, int act) {
     if (act == MGI_ACT_NONE) return v;
@@ -96,6 +105,7 @@ __device__ __forceinline__ bool plane_place(int M, int S, int &m, int &s) {
     const unsigned wave = blockIdx.x * (blockDim.x >> 6) + (threadIdx.x >> 6), sg = (S + 7) / 8;
     m = (int)(wave / sg) * 8 + (lane & 7);
     s = (int)(wave % sg) * 8 + (lane >> 3);
+    // (waves past the last have a pixel past the last)
     return m < M && s < S;
 }
 inline unsigned plane_blocks(int M, int S) { return (unsigned)((((size_t)M + 7) / 8 * (((size_t)S + 7) / 8) + 3) / 4); }
