@@ -147,31 +147,13 @@ __device__ __forceinline__ bool any_odd(h8 v, bool bf) {
     return odd;
 }
 
-// A workgroup's head of keys, row tile and chunk.  An XCD (every eighth workgroup)
-// gets whole heads, whose keys then stay in its L2, where there are enough of them,
-// and walks the tiles of its heads side by side, so that the long ones of all come
-// first.
-template <int WR>
+// A workgroup's head of keys, row tile and chunk: the head fastest, so that an XCD
+// (every eighth workgroup) has few of them, whose keys then stay in its L2, and the
+// long tiles of all heads, which come first, are spread over all XCDs (8 heads on one
+// of keys, 3141 tokens of 96 channels: contiguous tiles to each XCD 62 us).
 __device__ __forceinline__ void place(const AttentionGeom &geo, int kv_heads, int block, int &kvh, int &tile, int &chunk) {
-    int item;
-    if (WR == 1) {
-        item = xcd_tile(block, geo.tiles * kv_heads * geo.chunks);
-        kvh = item % kv_heads;
-        item /= kv_heads;
-        tile = item / geo.chunks;
-        chunk = item - tile * geo.chunks;
-        return;
-    }
-    if (kv_heads % 8 == 0) {
-        const int own = kv_heads >> 3;
-        item = block >> 3;
-        kvh = (block & 7) * own + item % own;
-        item /= own;
-    } else {
-        item = xcd_tile(block, geo.tiles * kv_heads * geo.chunks);
-        kvh = item / (geo.tiles * geo.chunks);
-        item -= kvh * geo.tiles * geo.chunks;
-    }
+    const int item = block / kv_heads;
+    kvh = block - item * kv_heads;
     tile = item / geo.chunks;
     chunk = item - tile * geo.chunks;
 }
@@ -189,7 +171,7 @@ __global__ __launch_bounds__(256, WR == 1 ? 1 : ND == 3 ? 3 : 2) void attention_
     __shared__ h8 lds[2 * OWN * STAGE];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
     int kvh, number, chunk;
-    place<WR>(geo, p.kv_heads, blockIdx.x, kvh, number, chunk);
+    place(geo, p.kv_heads, blockIdx.x, kvh, number, chunk);
     const Tile t = find_tile<BM>(p, number);
     if (t.none) return;
     const int rows = t.nq * p.group, first = t.tile * BM, r0 = first + (WR == 4 ? wave * 32 : 0);
@@ -454,7 +436,10 @@ __global__ __launch_bounds__(256, WR == 1 ? 1 : ND == 3 ? 3 : 2) void attention_
     }
 }
 
-// Joins the chunks of the rows that have several: a thread has 8 channels of every
+// Joins the chunks of the rows that have several, in a launch of its own (by the
+// workgroup that is done last, as other kernels here do: its stores past the L2 and
+// its acquire take longer than the launch, 13 packed sequences 62 us against 41, one
+// query on 32768 keys the same 37).  A thread has 8 channels of every
 // CG-th chunk of a row, then what CG threads found is joined in order.
 template <typename E, int BM, int CG>
 __global__ __launch_bounds__(256) void attention_join_kernel(AttentionParams p, AttentionGeom geo, int d32) {
@@ -554,12 +539,16 @@ AttentionGeom attention_geom(int q_tokens, int k_tokens, int n, int nseq, int gr
     g.wr = rows <= 32 * sequences ? 1 : 4;
     const int bm = tile_rows(g.wr);
     g.tiles = (int)(nseq ? rows / bm + nseq + 2 : n * ((rows / n + bm - 1) / bm));
-    // fewer workgroups than twice what the card holds of tiles that waves share (two
-    // to a compute unit), whose longest would end alone, or than it holds of the
-    // others (one): the keys are split
-    const long keys = nseq ? k_tokens : k_tokens / n, items = (long)g.tiles * kv_heads, want = g.wr == 4 ? 1024 : 256;
+    // The keys are split where workgroups are few: below twice what the card holds of
+    // tiles that waves share (two to a compute unit), or what it holds of the others
+    // (one).  Packed sequences, whose lengths the host does not know, may have one that
+    // is much longer than the others and ends alone, so they are split further, unless
+    // that would be into halves (the joining launch costs 3 us where nothing is split).
+    const long keys = nseq ? k_tokens : k_tokens / n, items = (long)g.tiles * kv_heads;
+    const long want = g.wr == 1 ? 256 : nseq ? 2048 : 1024;
     const int step = g.wr == 4 ? kBN : 4 * kPrivate;
     long chunks = items < want ? want / items : 1;
+    if (nseq && g.wr == 4 && chunks < 3) chunks = 1;
     chunks = std::min(chunks, (keys + 4 * step - 1) / (4 * step));
     g.chunk = (int)((keys + chunks * step - 1) / (chunks * step)) * step;
     g.chunks = (int)((keys + g.chunk - 1) / g.chunk);

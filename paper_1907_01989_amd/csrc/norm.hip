@@ -20,7 +20,7 @@ namespace {
 
 // P pixels to a wave, 64 / P slices at a time.  P = 8: a wave's lanes cover 8
 // pixels x 8 slices, 128 bytes of either layout, twice to a block of 128
-// channels; P = 1: four blocks of one pixel.  R: times that a wave comes round.
+// channels; P = 4, 2, 1: one, two, four blocks of each.  R: times that a wave comes round.
 template <typename E, int P, int R, bool NORM, bool TO8>
 __global__ __launch_bounds__(1024) void norm_kernel(NormParams p) {
     constexpr int SUBS = 64 / P, NS = P == 8 ? 2 : 1, CH = SUBS * NS;   // slices of a wave's chunk
@@ -127,7 +127,7 @@ void launch_norm_r(const NormParams &p, dim3 grid, dim3 block, hipStream_t st) {
 
 template <typename E, int P>
 hipError_t launch_norm_p(const NormParams &p, hipStream_t st) {
-    constexpr int CH = P == 8 ? 16 : 64;
+    constexpr int CH = P == 8 ? 16 : 64 / P;
     const int chunks = (p.KB * 16 + CH - 1) / CH;
     int waves = 1, r = 1;
     while (waves < 16 && waves * 4 < chunks) waves *= 2;
@@ -218,9 +218,15 @@ hipError_t launch_norm(const NormParams &p, hipStream_t st) {
     if (p.M <= 0) return hipSuccess;
     // one pixel to a wave where there are few, or where all is NHWC, whose pixels are
     // whole lines; eight else, for the sliced side
+    // (half as many where that makes too few workgroups: 868 x 4929 11.8 us by eights)
     const bool nhwc = p.a.s == 1 && (!p.b.x || p.b.s == 1) && (!p.sum.y || p.sum.s == 1) && !p.q.codes && p.out.s == 1;
-    if (p.M < 64 || nhwc) return p.bf16 ? launch_norm_p<BF16, 1>(p, st) : launch_norm_p<F16, 1>(p, st);
-    return p.bf16 ? launch_norm_p<BF16, 8>(p, st) : launch_norm_p<F16, 8>(p, st);
+    const int P = p.M < 64 || nhwc ? 1 : p.M < 1024 ? 2 : p.M < 4096 ? 4 : 8;
+    switch (P) {
+        case 1: return p.bf16 ? launch_norm_p<BF16, 1>(p, st) : launch_norm_p<F16, 1>(p, st);
+        case 2: return p.bf16 ? launch_norm_p<BF16, 2>(p, st) : launch_norm_p<F16, 2>(p, st);
+        case 4: return p.bf16 ? launch_norm_p<BF16, 4>(p, st) : launch_norm_p<F16, 4>(p, st);
+        default: return p.bf16 ? launch_norm_p<BF16, 8>(p, st) : launch_norm_p<F16, 8>(p, st);
+    }
 }
 
 hipError_t launch_export16(const h8 *x, void *y, int M, int C, hipStream_t st) {

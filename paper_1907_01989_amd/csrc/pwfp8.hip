@@ -353,7 +353,7 @@ hipError_t launch_pwfp8_t(const PwFp8Params &p, const PwFp8Geom &g, hipStream_t 
             else launch_few<E, 4>(p, st);
             break;
         case 1: launch_tile<E, 64, 64, 2, 2, 4>(p, st); break;
-        case 2: launch_tile<E, 128, 128, 2, 2, 4>(p, st); break;
+        case 2: launch_tile<E, 128, 128, 2, 2, 2>(p, st); break;
         case 3: launch_tile<E, 256, 256, 4, 2, 2>(p, st); break;
         default: return hipErrorInvalidValue;
     }
