@@ -222,8 +222,10 @@ __global__ __launch_bounds__(64 * NPX * NCO, 2) void pwfp8_tile_kernel(PwFp8Para
     static_assert(NST == 2 || NST == 4, "a step's stage is known when it is compiled");
     __shared__ h8 ring[NST][T::XE + T::WE];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, quad = lane >> 4;
-    const int ct = (p.nb16 * 16 + CO - 1) / CO, tile = xcd_tile(blockIdx.x, gridDim.x);
-    const int m0 = tile / ct * PX, n0 = tile % ct * (CO / 16);
+    // an XCD's tiles are neighbours: of all pixels where those are fewer tiles, so that
+    // its weights are read into its L2 once, else of all channels
+    const int ct = (p.nb16 * 16 + CO - 1) / CO, mt = (p.M + PX - 1) / PX, tile = xcd_tile(blockIdx.x, gridDim.x);
+    const int m0 = (mt < ct ? tile % mt : tile / ct) * PX, n0 = (mt < ct ? tile / mt : tile % ct) * (CO / 16);
     const int wm = wave % NPX * FM, wn = wave / NPX * FN;         // the wave's first pixel and channel block
 
     // the wave's loads: 64 pixels of a slice of 16 channels; half a block of 16 channels
