@@ -509,7 +509,7 @@ hipError_t launch_attention(const AttentionParams &p, const AttentionGeom &g, hi
 // Pointwise layer in 8 bits: weights [nb16][kb][2][64 lanes][16 bytes] in the
 // MFMA A operand's order, scales [ceil(nb16 / 8)][kb]
 struct PwFp8Geom {
-    int variant;         // 0: few pixels; 1, 2, 3: 64 x 64, 128 x 128, 256 x 256 tiles
+    int variant;         // 0: few pixels; 1 to 4: 64 x 64, 64 x 128, 128 x 128, 256 x 256 tiles
     bool reads_raw(size_t M) const { return variant == 0 && M <= 16; }   // can bring 16-bit pixels into 8 bits itself
 };
 PwFp8Geom pwfp8_geom(size_t M, int nb16, int kb);

@@ -216,7 +216,7 @@ struct PwTile {
 };
 
 template <typename E, int PX, int CO, int NPX, int NCO, int NST>
-__global__ __launch_bounds__(64 * NPX * NCO, 2) void pwfp8_tile_kernel(PwFp8Params p) {
+__global__ __launch_bounds__(64 * NPX * NCO, PX == 128 ? 4 : 2) void pwfp8_tile_kernel(PwFp8Params p) {
     using T = PwTile<PX, CO, NPX, NCO>;
     constexpr int FM = T::FM, FN = T::FN, XL = T::XE / 64 / T::WAVES, WL = T::WE / 64 / T::WAVES;
     static_assert(NST == 2 || NST == 4, "a step's stage is known when it is compiled");
@@ -355,8 +355,9 @@ hipError_t launch_pwfp8_t(const PwFp8Params &p, const PwFp8Geom &g, hipStream_t 
             else launch_few<E, 4>(p, st);
             break;
         case 1: launch_tile<E, 64, 64, 2, 2, 4>(p, st); break;
-        case 2: launch_tile<E, 128, 128, 2, 2, 2>(p, st); break;
-        case 3: launch_tile<E, 256, 256, 4, 2, 2>(p, st); break;
+        case 2: launch_tile<E, 64, 128, 2, 2, 2>(p, st); break;
+        case 3: launch_tile<E, 128, 128, 2, 4, 2>(p, st); break;
+        case 4: launch_tile<E, 256, 256, 4, 2, 2>(p, st); break;
         default: return hipErrorInvalidValue;
     }
     return hipGetLastError();
@@ -364,11 +365,17 @@ hipError_t launch_pwfp8_t(const PwFp8Params &p, const PwFp8Geom &g, hipStream_t 
 
 }  // namespace
 
+// The largest tile that fills the card: of 256 x 256 one to a compute unit, of
+// 128 x 128 two, of 64 x 128 one (315 x 1960 x 12032: 16.7 us, by 128 x 128 20.1, by
+// 64 x 64 24.0; 2115 x 96 x 6290: 13.4 by 128 x 128, 14.9 by 64 x 128; 8192 x 4096 x
+// 4096 133 by 256 x 256).  Few tiles and many inputs: the kernel of few pixels, which
+// shares the inputs out.
 PwFp8Geom pwfp8_geom(size_t M, int nb16, int kb) {
     if (M <= 64) return {0};
     auto tiles = [&](size_t px, size_t co) { return (M + px - 1) / px * ((nb16 * 16 + co - 1) / co); };
-    if (tiles(256, 256) >= 256) return {3};
-    if (tiles(128, 128) >= 256) return {2};
+    if (tiles(256, 256) >= 256) return {4};
+    if (tiles(128, 128) >= 512) return {3};
+    if (tiles(64, 128) >= 256) return {2};
     if (tiles(64, 64) < 128 && kb >= 16) return {0};
     return {1};
 }

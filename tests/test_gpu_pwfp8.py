@@ -69,7 +69,7 @@ def test_layer(m, cin, cout, dtype):
 
 
 @pytest.mark.parametrize("dtype", [0, 1])
-@pytest.mark.parametrize("m,cin,cout", [(2000, 200, 2110), (16500, 136, 1000), (4200, 1300, 4100), (300, 4000, 500), (150, 2048, 1024)])
+@pytest.mark.parametrize("m,cin,cout", [(2000, 200, 2110), (2900, 300, 2900), (16500, 136, 1000), (4200, 1300, 4100), (300, 4000, 500), (150, 2048, 1024)])
 def test_tiles(m, cin, cout, dtype):
     # every tile form; some of the rows against the oracle
     from block_util import run, within
