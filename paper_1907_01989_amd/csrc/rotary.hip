@@ -59,31 +59,43 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryParams p, int units, 
     }
     const int a = ADJ || rot ? u : u + turned, b = a + turned;
     const int end = min(p.heads, (int)(blockIdx.y + 1) * per);
-    for (int h = blockIdx.y * per + n / units; h < end; h += lanes) {
-        const int s = h * p.d8;
-        const h8 x = p.x.x[(size_t)(s + a) * p.x.s + (size_t)m * p.x.p];
-        if (!rot) {
-            store8<E>(p.y, s + a, m, x);
-        } else if constexpr (ADJ) {
-            float v[8];
+    const h8 *xa = p.x.x + (size_t)a * p.x.s + (size_t)m * p.x.p, *xb = p.x.x + (size_t)b * p.x.s + (size_t)m * p.x.p;
+    const bool two = !ADJ && rot;
+    // four heads' loads in flight together (29952 x 32 x 128: 110 us by one)
+    for (int h0 = blockIdx.y * per + n / units; h0 < end; h0 += 4 * lanes) {
+        h8 x[4], y[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float c = E::get(x, 2 * i), d = E::get(x, 2 * i + 1);
-                v[2 * i] = pinned(c * cs[i] - d * sn[i]);
-                v[2 * i + 1] = pinned(c * sn[i] + d * cs[i]);
-            }
-            store8<E>(p.y, s + a, m, E::pack(v));
-        } else {
-            const h8 y = p.x.x[(size_t)(s + b) * p.x.s + (size_t)m * p.x.p];
-            float v[8], w[8];
+        for (int i = 0; i < 4; ++i) {
+            const size_t at = (size_t)min(h0 + i * lanes, end - 1) * p.d8 * p.x.s;
+            x[i] = xa[at];
+            if (two) y[i] = xb[at];
+        }
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float c = E::get(x, i), d = E::get(y, i);
-                v[i] = pinned(c * cs[i] - d * sn[i]);
-                w[i] = pinned(c * sn[i] + d * cs[i]);
+        for (int i = 0; i < 4; ++i) {
+            const int h = h0 + i * lanes, s = h * p.d8;
+            if (h >= end) break;
+            if (!rot) {
+                store8<E>(p.y, s + a, m, x[i]);
+            } else if constexpr (ADJ) {
+                float v[8];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const float c = E::get(x[i], 2 * k), d = E::get(x[i], 2 * k + 1);
+                    v[2 * k] = pinned(c * cs[k] - d * sn[k]);
+                    v[2 * k + 1] = pinned(c * sn[k] + d * cs[k]);
+                }
+                store8<E>(p.y, s + a, m, E::pack(v));
+            } else {
+                float v[8], w[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const float c = E::get(x[i], k), d = E::get(y[i], k);
+                    v[k] = pinned(c * cs[k] - d * sn[k]);
+                    w[k] = pinned(c * sn[k] + d * cs[k]);
+                }
+                store8<E>(p.y, s + a, m, E::pack(v));
+                store8<E>(p.y, s + b, m, E::pack(w));
             }
-            store8<E>(p.y, s + a, m, E::pack(v));
-            store8<E>(p.y, s + b, m, E::pack(w));
         }
     }
 }
