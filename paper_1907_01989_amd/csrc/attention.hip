@@ -229,92 +229,54 @@ __global__ __launch_bounds__(256, WR == 1 ? 1 : ND == 3 ? 3 : 2) void attention_
     const int va = at_of<NHWC>(4 * half + (key >> 2), (lane >> 4 & 1) * 2 + (key >> 1 & 1)) * 16 + (key & 1) * 8;
     constexpr int EIGHT = NHWC ? 512 : 128;                          // bytes from a key to the eighth after it
 
-    // Shared tiles: the next one's loads are in flight while one is worked on.  A
-    // wave's own: each half of a stage is refilled as soon as it has been read, so that
-    // three halves are always in flight (one query on 32768 keys: 31 -> 25 us).
-    const int start = from + (WR == 4 ? 0 : wave * KEYS);
-    int stage = 0;
-    if (start < most) {
-        issue(start, 0, false);
-        issue(start, 0, true);
-    }
-    if (WR == 1 && start + STEP < most) {
-        issue(start + STEP, 1, false);
-        issue(start + STEP, 1, true);
-    }
-    for (int j0 = start; j0 < most; j0 += STEP, stage ^= 1) {
-        const bool more = j0 + STEP < most, refill = WR == 1 && j0 + 2 * STEP < most;
-        if (WR == 4) wait_vm_lds<0>();
-        else if (more) wait_vm_lds<3 * LOADS>();
-        else wait_vm_lds<LOADS>();
-        if constexpr (WR == 4) __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");                               // (no LDS access moves over the wait)
-        if (WR == 4 && more) {
-            issue(j0 + STEP, stage ^ 1, false);
-            issue(j0 + STEP, stage ^ 1, true);
-        }
-        h8 *kt = lds + (stage * OWN + (WR == 4 ? 0 : wave)) * STAGE, *vt = kt + PART;
-        const bool masked = j0 + KEYS > least;
-        f16v s[NK];
-        if (WR == 1 || (works && j0 < mine)) {
+    auto scores = [&](const h8 *kt, f16v (&s)[NK]) {
 #pragma unroll
-            for (int b = 0; b < NK; ++b) s[b] = f16v{};
+        for (int b = 0; b < NK; ++b) s[b] = f16v{};
 #pragma unroll
-            for (int k = 0; k < ND * 2; ++k)
+        for (int k = 0; k < ND * 2; ++k)
 #pragma unroll
-                for (int b = 0; b < NK; ++b) s[b] = mma32<E>(kt[ka[k & 1] + (b * 2 * ND + k / 2) * 64], q[k], s[b]);
-        }
-        if constexpr (WR == 1) {
-            if (refill) {
-                wait_vm_lds<63>();                                   // (the wave has read the keys)
-                issue(j0 + 2 * STEP, stage, false);
-            }
-            if (refill) wait_vm_lds<3 * LOADS>();
-            else if (more) wait_vm_lds<2 * LOADS>();
-            else wait_vm_lds<0>();
-            asm volatile("" ::: "memory");
-        }
-        if (masked) {
-            // hidden keys have no score; values that are infinite or NaN are taken
-            // out of the tile (0 times them is NaN) and added to the rows that see
-            // them
-            bool odd = false;
-            const int me = WR == 4 ? tid : lane, all = WR == 4 ? 256 : 64;
-            for (int e = me; e < PART; e += all) odd = odd || any_odd(vt[e], E::bf);
-            const bool found = WR == 4 ? __syncthreads_or(odd) : __any(odd);
-            if (found) {
-                for (int k = 0; k < KEYS; ++k)
+            for (int b = 0; b < NK; ++b) s[b] = mma32<E>(kt[ka[k & 1] + (b * 2 * ND + k / 2) * 64], q[k], s[b]);
+    };
+    // Hidden keys have no score; values that are infinite or NaN are taken out of the
+    // tile (0 times them is NaN) and added to the rows that see them.
+    auto hide = [&](int j0, h8 *vt, f16v (&s)[NK]) {
+        bool odd = false;
+        const int me = WR == 4 ? tid : lane, all = WR == 4 ? 256 : 64;
+        for (int e = me; e < PART; e += all) odd = odd || any_odd(vt[e], E::bf);
+        const bool found = WR == 4 ? __syncthreads_or(odd) : __any(odd);
+        if (found) {
+            for (int k = 0; k < KEYS; ++k)
 #pragma unroll
-                    for (int d = 0; d < ND; ++d)
+                for (int d = 0; d < ND; ++d)
 #pragma unroll
-                        for (int g = 0; g < 4; ++g) {
-                            const h8 v = vt[(k / 16 * ND + d) * 64 + at_of<NHWC>(k % 16, g)];
+                    for (int g = 0; g < 4; ++g) {
+                        const h8 v = vt[(k / 16 * ND + d) * 64 + at_of<NHWC>(k % 16, g)];
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                const float x = half ? E::get(v, 4 + i) : E::get(v, i);
-                                if (j0 + k < lim && !(fabsf(x) < INFINITY)) o[d][g * 4 + i] += x;
-                            }
+                        for (int i = 0; i < 4; ++i) {
+                            const float x = half ? E::get(v, 4 + i) : E::get(v, i);
+                            if (j0 + k < lim && !(fabsf(x) < INFINITY)) o[d][g * 4 + i] += x;
                         }
-                if constexpr (WR == 4) __syncthreads();
-                else __builtin_amdgcn_wave_barrier();
-                for (int e = me; e < PART; e += all) vt[e] = with_zeros_for_odd(vt[e], E::bf);
-                if constexpr (WR == 4) __syncthreads();
-                else __builtin_amdgcn_wave_barrier();
-            }
-#pragma unroll
-            for (int b = 0; b < NK; ++b)
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (j0 + b * 32 + i / 4 * 8 + half * 4 + i % 4 >= lim) s[b][i] = -INFINITY;
+                    }
+            if constexpr (WR == 4) __syncthreads();
+            else __builtin_amdgcn_wave_barrier();
+            for (int e = me; e < PART; e += all) vt[e] = with_zeros_for_odd(vt[e], E::bf);
+            if constexpr (WR == 4) __syncthreads();
+            else __builtin_amdgcn_wave_barrier();
         }
-        if (WR == 4 && (!works || j0 >= mine)) continue;
+#pragma unroll
+        for (int b = 0; b < NK; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (j0 + b * 32 + i / 4 * 8 + half * 4 + i % 4 >= lim) s[b][i] = -INFINITY;
+    };
+    // The rows' maxima: the weights' base moves only when a score passes it by 2^kSlack.
+    auto rebase = [&](const f16v (&s)[NK]) {
         float top = s[0][0];
 #pragma unroll
         for (int b = 0; b < NK; ++b)
 #pragma unroll
             for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
         top = fmaxf(top, __shfl_xor(top, 32, 64));
-        // the weights' base moves only when a score passes it by 2^kSlack
         const bool move = fmaf(top, c, m == -INFINITY ? INFINITY : -m * c) > kSlack;
         if (__any(move)) {
             // (before the first weights there is nothing to scale but what hidden
@@ -325,9 +287,10 @@ __global__ __launch_bounds__(256, WR == 1 ? 1 : ND == 3 ? 3 : 2) void attention_
 #pragma unroll
             for (int d = 0; d < ND; ++d) o[d] *= keep;
         }
-        const float base = m == -INFINITY ? 0.0f : m * c;
+        return m == -INFINITY ? 0.0f : m * c;
+    };
+    auto weights = [&](const f16v (&s)[NK], float base, h8 (&pr)[2 * NK]) {
         float sum = 0.0f;
-        h8 pr[2 * NK];
 #pragma unroll
         for (int k = 0; k < 2 * NK; ++k) {
             float w[8];
@@ -339,6 +302,8 @@ __global__ __launch_bounds__(256, WR == 1 ? 1 : ND == 3 ? 3 : 2) void attention_
             pr[k] = E::pack(w);
         }
         l += sum;
+    };
+    auto values = [&](const h8 *vt, const h8 (&pr)[2 * NK]) {
 #pragma unroll
         for (int k = 0; k < 2 * NK; ++k)
 #pragma unroll
@@ -348,10 +313,32 @@ __global__ __launch_bounds__(256, WR == 1 ? 1 : ND == 3 ? 3 : 2) void attention_
                 const h8 v = __builtin_bit_cast(h8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
                 o[d] = mma32<E>(v, pr[k], o[d]);
             }
-        if (refill) {
-            wait_vm_lds<63>();                                       // (the wave has read the values)
-            issue(j0 + 2 * STEP, stage, true);
+    };
+
+    const int start = from + (WR == 4 ? 0 : wave * KEYS);
+    int stage = 0;
+    if (start < most) {
+        issue(start, 0, false);
+        issue(start, 0, true);
+    }
+    for (int j0 = start; j0 < most; j0 += STEP, stage ^= 1) {
+        wait_vm_lds<0>();
+        if constexpr (WR == 4) __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");                           // (no LDS access moves over the wait)
+        if (j0 + STEP < most) {
+            issue(j0 + STEP, stage ^ 1, false);
+            issue(j0 + STEP, stage ^ 1, true);
         }
+        h8 *kt = lds + (stage * OWN + (WR == 4 ? 0 : wave)) * STAGE, *vt = kt + PART;
+        f16v s[NK];
+        const bool mute = !works || j0 >= mine;
+        if (!mute) scores(kt, s);
+        if (j0 + KEYS > least) hide(j0, vt, s);
+        if (mute) continue;
+        const float base = rebase(s);
+        h8 pr[2 * NK];
+        weights(s, base, pr);
+        values(vt, pr);
     }
     l += __shfl_xor(l, 32, 64);
     const int d32 = ND * 32;
