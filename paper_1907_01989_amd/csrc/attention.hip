@@ -526,13 +526,12 @@ AttentionGeom attention_geom(int q_tokens, int k_tokens, int n, int nseq, int gr
     g.wr = rows <= 32 * sequences ? 1 : 4;
     const int bm = tile_rows(g.wr);
     g.tiles = (int)(nseq ? rows / bm + nseq + 2 : n * ((rows / n + bm - 1) / bm));
-    // The keys are split where workgroups are few: below twice what the card holds of
-    // tiles that waves share (two to a compute unit), or what it holds of the others
-    // (one).  Packed sequences, whose lengths the host does not know, may have one that
+    // The keys are split where workgroups are few: below what the card holds of tiles
+    // that waves share (two to a compute unit) or of the others (one).  Packed sequences, whose lengths the host does not know, may have one that
     // is much longer than the others and ends alone, so they are split further, unless
     // that would be into halves (the joining launch costs 3 us where nothing is split).
     const long keys = nseq ? k_tokens : k_tokens / n, items = (long)g.tiles * kv_heads;
-    const long want = g.wr == 1 ? 256 : nseq ? 2048 : 1024;
+    const long want = g.wr == 1 ? 256 : nseq ? 2048 : 512;
     const int step = g.wr == 4 ? kBN : 4 * kPrivate;
     long chunks = items < want ? want / items : 1;
     if (nseq && g.wr == 4 && chunks < 3) chunks = 1;

@@ -129,10 +129,13 @@ template <typename E, int P>
 hipError_t launch_norm_p(const NormParams &p, hipStream_t st) {
     constexpr int CH = P == 8 ? 16 : 64 / P;
     const int chunks = (p.KB * 16 + CH - 1) / CH;
+    // at most four rounds of loads to a wave, fewer until the card has four waves to a
+    // SIMD
+    const int groups = (p.M + P - 1) / P;
     int waves = 1, r = 1;
-    while (waves < 16 && waves * 4 < chunks) waves *= 2;
+    while (waves < 16 && (waves * 4 < chunks || (waves < chunks && (size_t)groups * waves < 4096))) waves *= 2;
     while (waves * r < chunks) r *= 2;
-    const dim3 grid(((unsigned)p.M + P - 1) / P), block(64 * waves);
+    const dim3 grid((unsigned)groups), block(64 * waves);
     switch (r) {
         case 1: launch_norm_r<E, P, 1>(p, grid, block, st); break;
         case 2: launch_norm_r<E, P, 2>(p, grid, block, st); break;
@@ -177,18 +180,28 @@ __global__ __launch_bounds__(256) void export16_kernel(const h8 *x, uint16_t *y,
 }
 
 __global__ __launch_bounds__(256) void ingest16_kernel(const uint16_t *x, h8 *y, int M, int C, int S) {
+    __shared__ uint16_t tiles[4][8 * 66];
     int m, s;
-    if (!plane_place(M, S, m, s)) return;
-    const uint16_t *d = x + (size_t)m * C + s * 8;
+    const bool in = plane_place(M, S, m, s);
     h8 v = zero_h8();
     if (whole_rows(x, C)) {
-        v = *(const h8 *)d;
+        if (in) v = *(const h8 *)(x + (size_t)m * C + s * 8);
     } else {
+        // (the other way round; zeros past the last channel)
+        uint16_t *tile = tiles[threadIdx.x >> 6];
+        const int lane = threadIdx.x & 63, m0 = m - (lane & 7), c = (s - (lane >> 3)) * 8 + lane;
+        uint16_t row[8];
 #pragma unroll
-        for (int c = 0; c < 8; ++c)
-            if (s * 8 + c < C) v[c] = __builtin_bit_cast(_Float16, d[c]);
+        for (int i = 0; i < 8; ++i) row[i] = m0 + i < M && c < C ? x[(size_t)(m0 + i) * C + c] : 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) tile[i * 66 + lane] = row[i];
+        __builtin_amdgcn_wave_barrier();
+        u16x8 b;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) b[i] = tile[(lane & 7) * 66 + (lane >> 3) * 8 + i];
+        v = __builtin_bit_cast(h8, b);
     }
-    y[(size_t)s * M + m] = v;
+    if (in) y[(size_t)s * M + m] = v;
 }
 
 template <typename E>
