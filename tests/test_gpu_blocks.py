@@ -215,3 +215,95 @@ def test_16_bit_outputs_of_other_operators():
         torch.cuda.synchronize()
         for p, q in zip(a, c):
             assert q.dtype == kind and torch.equal(p, q.float())
+
+
+def test_operators_write_inside_their_buffers():
+    from block_util import inputs
+    from test_gpu_guards import check_guards, guarded_plan
+    # long rows (keys split over workgroups) and odd widths (sliced outputs that are exported)
+    for dtype, kw in ((0, dict(n=1, h=1, w=3001, bounds=[0, 2990, 2991, 2991, 3000])), (1, dict(n=3, h=5, w=7))):
+        b, t = block(dtype, **kw)
+        odd = b.pointwise_fp8(t["tokens"], 77)
+        b.ops[odd]["scales"] = b.ops[odd]["scales"] * 0.5
+        outs = [t["z"], t["y"], t["turned"], t["tokens"], odd, b.quantize(odd), b.rms_norm(odd)]
+        types = {o: dtype for o in outs[:2] + outs[4:]}
+        log(f"[case] block guards, type {dtype}")
+        for extra in ({}, {"materialize_all": True}, {"fuse": False}):
+            plan, ys, raw, ws, lead = guarded_plan({"name": "block", "ops": b.ops, "outputs": outs, "output_dtypes": types}, dtype=dtype, **extra)
+            xs = inputs(plan)
+            for _ in range(2):
+                plan.run(xs, ys)
+            check_guards(plan, raw, ws, lead, f"block {dtype} {extra}")
+
+
+def test_nodes_can_be_read_and_timed():
+    import torch
+    from block_util import inputs
+    from paper_1907_01989_amd import _binding as B
+    b, t = block(0, 1, 1, 2600)
+    want = ["tokens", "qkv", "turned", "y", "o", "s", "z"]
+    plan = plan_of(b, [t["z"]], 0, materialize_all=True)
+    xs = inputs(plan)
+    log("[case] block, nodes read and timed")
+    plan.run(xs)
+    read = {info["tensor"]: plan.read_node(i)[1] for i, info in enumerate(plan.nodes()) if info["tensor"] >= 0}
+    other = plan_of(b, [t[k] for k in want if k != "tokens"], 0)
+    ys = other.run(xs)
+    torch.cuda.synchronize()
+    for k, y in zip([k for k in want if k != "tokens"], ys):
+        assert torch.equal(read[t[k]].reshape(y.shape), y.float()), k
+    assert torch.isfinite(read[t["tokens"]]).all()
+    # every node's kernels between two events (attention's keys are split: two kernels)
+    kinds = [n["kind"] for n in other.nodes()]
+    events = [[torch.cuda.Event(enable_timing=True) for _ in kinds] for _ in range(2)]
+    for e in events[0] + events[1]:
+        e.record()
+    again = other.alloc_outputs()
+    B.mgi_plan_run_timed(other.handle, [x.data_ptr() for x in xs], [y.data_ptr() for y in again],
+                         [e.cuda_event for e in events[0]], [e.cuda_event for e in events[1]], torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    for y, z in zip(again, ys):
+        assert torch.equal(y, z)
+    times = {k: a.elapsed_time(z) for k, a, z in zip(kinds, *events)}
+    assert times["attention"] > 0.005 and all(v < 100 for v in times.values()), times
+
+
+def test_a_tensor_added_to_itself_and_one_sum_for_two_norms():
+    from block_util import HALF, builder, given, run, stored, within
+    x = stored(np.random.default_rng(3).standard_normal((1, 3, 5, 72)), 0)
+    b = builder()
+    s = b.add(given(b, x, 0), 0, act=0)
+    n, m = b.rms_norm(s), b.rms_norm(s, eps=0.5)
+    log("[case] a tensor added to itself")
+    (sv, nv, mv), _ = run(b, [s, n, m], 0, {s: 0})
+    np.testing.assert_array_equal(sv, 2 * x)
+    for t, v in ((n, nv), (m, mv)):
+        ref = oracle.rms_norm(sv, b.ops[t]["w"], b.ops[t]["eps"])
+        within(v, ref, (HALF[0] + 2.0 ** -17) * np.abs(ref) + 2.0 ** -25)
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+def test_channels_past_the_last_stay_zero(dtype):
+    import torch
+    from block_util import builder, given, inputs, stored
+    from paper_1907_01989_amd import _binding as B
+    b = builder()
+    x = given(b, stored(np.random.default_rng(4).standard_normal((2, 5, 9, 77)), dtype), dtype)
+    n = b.rms_norm(x)
+    p = b.pointwise_fp8(b.quantize(n), 45)
+    s = b.add(n, x, act=0)
+    plan = plan_of(b, [p, s], dtype, materialize_all=True)
+    plan.run(inputs(plan))
+    log(f"[case] padding lanes, type {dtype}")
+    seen = 0
+    for i, info in enumerate(plan.nodes()):
+        if info["tensor"] not in (n, p, s):
+            continue
+        c = info["shape"][3]
+        raw = torch.empty(B.mgi_plan_read_node_raw(plan.handle, i), dtype=torch.uint8, device="cuda:0")
+        B.mgi_plan_read_node_raw(plan.handle, i, raw.data_ptr(), torch.cuda.current_stream().cuda_stream)
+        torch.cuda.synchronize()
+        lanes = raw.view(torch.int16).reshape(-1, 90, 8)
+        assert (lanes[-1, :, c % 8:] == 0).all() and (lanes[-1, :, :c % 8] != 0).any()
+        seen += 1
+    assert seen == 3
