@@ -2,9 +2,10 @@
 //
 //   y[m][o] = act(b[o] + sum_kb sw[o / 128][kb] 2^e[m][kb] sum_{i in kb} cw[o][i] q[m][i])
 //
-// One matrix instruction multiplies a block of 128 inputs; its operand for the
-// pixels' exponents takes the powers of two, which scales exactly, and the
-// blocks' sums go into the fp32 result times the weights' scale.  The instruction
+// One matrix instruction multiplies a block of 128 inputs; its operands for
+// exponents take the pixels' powers of two and the weight scale's, which scales
+// exactly, and the blocks' sums go into the fp32 result times the rest of the scale,
+// 1 to 2: no sum leaves fp32's range whose share of the result does not.  The instruction
 // adds eight products at a time with their bits below 2^-13 of the largest's
 // leading one cut off, and those sums in fp32 (measured; the unscaled 8-bit
 // instructions do the same).  That is 2^-16 of a result of normal values, under
@@ -27,10 +28,17 @@ __device__ __forceinline__ i8v join(uint4 a, uint4 b) {
 
 // 16 channels x 16 pixels of a block of 128 inputs: lane l has inputs 16 (l / 16)
 // .. + 15 and the same + 64 of channel (or pixel) l % 16; `e`: the pixel's
-// exponents of four blocks
+// exponents of four blocks, `k`: the weights' exponent
 template <int Q>
-__device__ __forceinline__ f4 mma8(i8v w, i8v x, uint32_t e) {
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x, f4{}, 0, 0, 0, 0x7f7f7f7f, Q, (int)e);
+__device__ __forceinline__ f4 mma8(i8v w, i8v x, uint32_t k, uint32_t e) {
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x, f4{}, 0, 0, 0, (int)k, Q, (int)e);
+}
+
+// a scale is 2^(k - 127) times what is left in s, 1 to 2 (less where it is subnormal or zero)
+__device__ __forceinline__ uint32_t split_scale(float &s) {
+    const uint32_t bits = __float_as_uint(s), k = bits >> 23 & 255;
+    s = k ? __uint_as_float((bits & 0x807fffffu) | 0x3f800000u) : s * 0x1p126f;
+    return max(k, 1u);
 }
 
 // A block of a pixel's inputs, 32 of them to each of the lanes l, l ^ 16, l ^ 32,
@@ -166,7 +174,8 @@ __global__ __launch_bounds__(512) void pwfp8_few_kernel(PwFp8Params p) {
         }
         four_blocks(p.kb - k0, [&](auto q) {
             constexpr int u = decltype(q)::value;
-            const float sw = sp[k0 + u];
+            float sw = sp[k0 + u];
+            const uint32_t k = split_scale(sw);
 #pragma unroll
             for (int j = 0; j < FM; ++j) {
                 i8v xv;
@@ -177,7 +186,7 @@ __global__ __launch_bounds__(512) void pwfp8_few_kernel(PwFp8Params p) {
                     xv = join(x[j][u][0], x[j][u][1]);
                     ev = e[j];
                 }
-                const f4 part = mma8<u>(join(w[u][0], w[u][1]), xv, ev);
+                const f4 part = mma8<u>(join(w[u][0], w[u][1]), xv, k, ev);
 #pragma unroll
                 for (int r = 0; r < 4; ++r) acc[j][r] = fmaf(part[r], sw, acc[j][r]);
             }
@@ -269,7 +278,8 @@ __global__ __launch_bounds__(64 * NPX * NCO, PX == 128 ? 4 : 2) void pwfp8_tile_
     // for the ring's loads)
     static_assert(FN <= 8 && kMaxNormChannels <= 128 * 128, "a wave's channels share a scale; two registers of scales");
     const float *sp = p.scales + (size_t)((n0 + wn) >> 3) * p.kb;
-    const float s0 = sp[min(lane, p.kb - 1)], s1 = sp[min(64 + lane, p.kb - 1)];
+    float s0 = sp[min(lane, p.kb - 1)], s1 = sp[min(64 + lane, p.kb - 1)];
+    const uint32_t k0 = split_scale(s0), k1 = split_scale(s1);
 #pragma unroll
     for (int i = 0; i < NST - 1; ++i)
         if (i < p.kb) issue(ring[i]);
@@ -287,6 +297,7 @@ __global__ __launch_bounds__(64 * NPX * NCO, PX == 128 ? 4 : 2) void pwfp8_tile_
         }
         if (kb + NST - 1 < p.kb) issue(ring[(u + NST - 1) % NST]);
         const float sw = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(kb < 64 ? s0 : s1), kb & 63));
+        const uint32_t k = __builtin_amdgcn_readlane(kb < 64 ? k0 : k1, kb & 63);
         auto weights = [&](int i) {
             const h8 *at = st + T::XE + (wn + i) * 128 + lane;
             return join(__builtin_bit_cast(uint4, at[0]), __builtin_bit_cast(uint4, at[64]));
@@ -307,7 +318,7 @@ __global__ __launch_bounds__(64 * NPX * NCO, PX == 128 ? 4 : 2) void pwfp8_tile_
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int j = 0; j < FM; ++j) {
-                if (i < FN) part[i & 1][j] = mma8<u>(w, x[j], e[j]);
+                if (i < FN) part[i & 1][j] = mma8<u>(w, x[j], k, e[j]);
                 __builtin_amdgcn_sched_barrier(0);
                 if (i > 0) {
 #pragma unroll

@@ -95,6 +95,39 @@ def test_few_pixels_in_8_bits_by_the_layer_itself_or_before():
             np.testing.assert_array_equal(y, z)
 
 
+@pytest.mark.parametrize("dtype", [0, 1])
+def test_extreme_blocks_in_one_kernel_and_two(dtype):
+    # blocks of zeros, of the least and the largest values, of subnormals among others, with infinities and NaN
+    from block_util import builder, given, run, stored, within
+    rng = np.random.default_rng(9)
+    x = rng.standard_normal((1, 1, 13, 1024))
+    least, most = (2.0 ** -24, 65504.0) if dtype == 0 else (2.0 ** -133, 3.3e38)
+    x[0, 0, :, 128:256] = 0
+    x[0, 0, :, 256:384] = np.where(rng.random((13, 128)) < 0.5, least, -3 * least)
+    x[0, 0, :, 384:512] *= least * 100
+    x[0, 0, :, 512:640] = np.where(rng.random((13, 128)) < 0.3, most, -most / 3)
+    x[0, 0, :, 640:768] *= 2.0 ** rng.integers(-14, 14, (13, 128))
+    x[0, 0, 3, 700], x[0, 0, 5, 900], x[0, 0, 6, 1000] = np.nan, np.inf, -np.inf
+    x = stored(x, dtype)
+    b = builder(3)
+    q = b.quantize(given(b, x, dtype))
+    # (a product of the largest values passes fp32's range before the block's scale brings it back)
+    t = b.pointwise_fp8(q, 48)
+    b.ops[t]["scales"][:, 4] *= 1e-5 if dtype == 0 else 1e-38
+    log(f"[case] extreme blocks, type {dtype}")
+    (y,), plan = run(b, [t], dtype)
+    assert "quantize_pointwise_fp8" in [i["kind"] for i in plan.nodes()]
+    (z, v), _ = run(b, [t, q], dtype)
+    np.testing.assert_array_equal(y, z)
+    with np.errstate(over="ignore"):
+        np.testing.assert_array_equal(v, oracle.quantize(x).astype(np.float32))
+    bad = [3, 5, 6]
+    assert np.isnan(y[0, 0, bad]).all()
+    good = [i for i in range(13) if i not in bad]
+    ref, bound = expect(b, t, x[:, :, good], dtype)
+    within(y[:, :, good], ref, bound)
+
+
 @pytest.mark.parametrize("act", [1, 2])
 def test_activation_and_images(act):
     from block_util import run, within
