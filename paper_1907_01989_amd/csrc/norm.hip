@@ -158,6 +158,7 @@ __device__ __forceinline__ void store_rows(T *tile, const T *v, T *y, int M, int
 #pragma unroll
     for (int c = 0; c < 8; ++c) tile[(lane & 7) * 66 + (lane >> 3) * 8 + c] = v[c];
     __builtin_amdgcn_wave_barrier();
+    asm volatile("" ::: "memory");                   // (a wave's LDS accesses are in order as they are written)
     const int m0 = m - (lane & 7), c = (s - (lane >> 3)) * 8 + lane;
 #pragma unroll
     for (int i = 0; i < 8; ++i)
@@ -196,6 +197,7 @@ __global__ __launch_bounds__(256) void ingest16_kernel(const uint16_t *x, h8 *y,
 #pragma unroll
         for (int i = 0; i < 8; ++i) tile[i * 66 + lane] = row[i];
         __builtin_amdgcn_wave_barrier();
+        asm volatile("" ::: "memory");
         u16x8 b;
 #pragma unroll
         for (int i = 0; i < 8; ++i) b[i] = tile[(lane & 7) * 66 + (lane >> 3) * 8 + i];
@@ -229,11 +231,19 @@ __global__ __launch_bounds__(256) void export8_kernel(Tensor8 x, void *y, int f3
 
 hipError_t launch_norm(const NormParams &p, hipStream_t st) {
     if (p.M <= 0) return hipSuccess;
-    // one pixel to a wave where there are few, or where all is NHWC, whose pixels are
-    // whole lines; eight else, for the sliced side
-    // (half as many where that makes too few workgroups: 868 x 4929 11.8 us by eights)
-    const bool nhwc = p.a.s == 1 && (!p.b.x || p.b.s == 1) && (!p.sum.y || p.sum.s == 1) && !p.q.codes && p.out.s == 1;
-    const int P = p.M < 64 || nhwc ? 1 : p.M < 1024 ? 2 : p.M < 4096 ? 4 : 8;
+    // Sliced tensors want many pixels to a wave, for whole lines of a slice (2048 x 2048
+    // sliced to sliced, 1 / 2 / 4 / 8: 16.8, 9.8, 6.8, 5.2 us), few pixels many waves (300
+    // x 2048: 6.2, 4.6, 4.0, 4.6).  NHWC ones are lines by themselves: enough pixels to
+    // give all lanes channels (100000 x 64: 27.6, 15.6, 10.0, 8.4; 8192 x 1000: 7.8, 7.6,
+    // 7.8, 7.7).  Codes alone, 16 bytes of a pixel, are between (norm 197 x 4096: 3.9, 4.5,
+    // 5.8, 7.6; 5000 x 4096: 23.5, 18.1, 17.6, 20.3; without the norm 8192 x 4096: 49.5,
+    // 39.2, 28.9, 25).
+    const bool nhwc = p.a.s == 1 && (!p.b.x || p.b.s == 1) && (!p.sum.y || p.sum.s == 1) && (p.q.codes || p.out.s == 1);
+    int P;
+    if (p.M < 64) P = 1;
+    else if (!nhwc) P = p.M < 256 ? 2 : p.M < 1024 ? 4 : 8;
+    else if (p.q.codes) P = p.M < 300 ? 1 : p.M < 2048 ? 2 : p.w ? 4 : 8;
+    else P = p.KB == 1 ? 8 : p.KB == 2 ? 4 : 2;
     switch (P) {
         case 1: return p.bf16 ? launch_norm_p<BF16, 1>(p, st) : launch_norm_p<F16, 1>(p, st);
         case 2: return p.bf16 ? launch_norm_p<BF16, 2>(p, st) : launch_norm_p<F16, 2>(p, st);

@@ -63,6 +63,33 @@ def test_norm(n, h, w, c, dtype):
 
 
 @pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("c", [72, 130, 256, 1000, 2304])
+def test_a_row_is_the_same_among_few_and_many(c, dtype):
+    # (pixels are shared out over lanes by their number, the layouts and the type of the output)
+    from block_util import builder, given, run, stored
+    x = stored(case(1, 1, 2200, c, 5), dtype)
+
+    def outputs(x):
+        b = builder(c)
+        t = given(b, x, dtype)
+        n = b.rms_norm(t)
+        s = b.rms_norm(b.add(n, t), to8=True)
+        q = b.quantize(n)
+        layers = [b.pointwise_fp8(s, 24), b.pointwise_fp8(q, 24)]   # (readers, whose sums have an order of their own)
+        return b, [b.rms_norm(t, eps=1e-3), b.rms_norm(b.rms_norm(n), eps=1e-4), s, q] + layers
+
+    rows = [0, 1, 7, 40, 62, 254]
+    b, outs = outputs(x[:, :, rows])
+    few = run(b, outs, dtype, {t: dtype for t in outs})[0]
+    for m in (65, 255, 299, 1023, 1025, 2200):
+        some = rows[:5] if m < 255 else rows
+        log(f"[case] norm of {m} x {c} type {dtype}")
+        b, outs = outputs(x[:, :, :m])
+        for y, z in zip(run(b, outs, dtype, {t: dtype for t in outs})[0][:4], few):
+            np.testing.assert_array_equal(y[:, :, some], z[:, :, :len(some)])
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
 @pytest.mark.parametrize("n,h,w,c", CASES[1::2])
 @pytest.mark.parametrize("act,to8", [(0, False), (1, True), (2, False), (0, True)])
 def test_sum_and_norm_in_one_kernel_or_two(n, h, w, c, dtype, act, to8):
