@@ -259,9 +259,11 @@ __global__ __launch_bounds__(256, WR == 1 ? 1 : ND == 3 ? 3 : 2) void attention_
                     }
             if constexpr (WR == 4) __syncthreads();
             else __builtin_amdgcn_wave_barrier();
+            asm volatile("" ::: "memory");
             for (int e = me; e < PART; e += all) vt[e] = with_zeros_for_odd(vt[e], E::bf);
             if constexpr (WR == 4) __syncthreads();
             else __builtin_amdgcn_wave_barrier();
+            asm volatile("" ::: "memory");
         }
 #pragma unroll
         for (int b = 0; b < NK; ++b)

@@ -688,6 +688,12 @@ extern "C" mgi_status mgi_graph_add_attention(mgi_graph *g, int q, int k, int v,
     // (the kernel counts query rows of a group of heads in an int)
     if ((unsigned __int128)xq.pixels() * (d->heads / d->kv_heads) > INT_MAX / 2)
         return fail(MGI_ERR_UNSUPPORTED, std::string(who) + ": too many queries");
+    // (... and a launch has fewer than 2^24 workgroups of 256 threads)
+    const kern::AttentionGeom geo = kern::attention_geom((int)xq.pixels(), (int)xk.pixels(), xq.n,
+                                                         bounds == -1 ? 0 : (int)g->ops[bounds].out.elems() - 1,
+                                                         d->heads / d->kv_heads, d->kv_heads, d->head_dim / 8);
+    if ((uint64_t)geo.tiles * d->kv_heads * geo.chunks >= 1u << 24)
+        return fail(MGI_ERR_UNSUPPORTED, std::string(who) + ": too many sequences and heads");
     return push(g, std::move(op), out);
     MGI_ABI_CATCH("mgi_graph_add_attention")
 }

@@ -106,7 +106,7 @@ def _add_tokens(g, ops, op):
                                              op.get("act", B.ACT_NONE))
     if k == "rotary":
         _sized(k, "freqs", op["freqs"], len(op["axes"]))
-        return B.mgi_graph_add_rotary(g, op["in"], op["heads"], op["head_dim"], list(op["axes"]), list(op["freqs"]),
+        return B.mgi_graph_add_rotary(g, op["in"], op["heads"], op["head_dim"], [int(a) for a in op["axes"]], list(op["freqs"]),
                                       op.get("positions", -1), op.get("from", 0), op.get("adjacent", False))
     return B.mgi_graph_add_attention(g, op["q"], op["k"], op["v"], op["heads"], op["kv_heads"], op["head_dim"],
                                      op.get("causal", False), op.get("scale", 0.0), op.get("bounds", -1),

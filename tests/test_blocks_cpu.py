@@ -120,6 +120,26 @@ def test_rotary_refusals(g):
     assert B.lib().mgi_graph_add_rotary(g, x, ctypes.byref(d), axes, freqs, -1, ctypes.byref(out)) == 0
 
 
+def test_more_workgroups_than_a_launch_has_are_refused(g):
+    # (sequences or images times heads of keys)
+    wide = B.mgi_graph_add_input(g, 1, 1, 1, 2 ** 23, 0)
+    most = B.mgi_graph_add_index_input(g, 1, 1, 1, 2 ** 16 + 1)
+    few = B.mgi_graph_add_index_input(g, 1, 1, 1, 2)
+    assert status(B.mgi_graph_add_attention, g, wide, wide, wide, 2 ** 20, 2 ** 20, 8, bounds=most) == 3
+    assert B.mgi_graph_add_attention(g, wide, wide, wide, 2 ** 20, 2 ** 20, 8, bounds=few) == 3
+    many = B.mgi_graph_add_input(g, 2 ** 23, 1, 1, 16, 0)
+    assert status(B.mgi_graph_add_attention, g, many, many, many, 2, 2, 8) == 3
+    assert B.mgi_graph_add_attention(g, many, many, many, 2, 1, 8) == 5
+
+
+def test_rotary_takes_arrays():
+    from paper_1907_01989_amd import engine
+    ops = [{"op": "input", "shape": (1, 2, 2, 16)},
+           {"op": "rotary", "in": 0, "heads": 1, "head_dim": 16, "axes": np.array([0, 1, 2]),
+            "freqs": np.array([1, 0.5, 0.25], np.float32)}]
+    B.mgi_graph_destroy(engine.build_graph({"ops": ops, "outputs": [1]}))
+
+
 def test_attention_refusals(g):
     q = B.mgi_graph_add_input(g, 2, 4, 4, 64)
     k = B.mgi_graph_add_input(g, 2, 2, 2, 32)
