@@ -96,7 +96,7 @@ __device__ __forceinline__ uint32_t to_8_bits(const uint4 (&raw)[4], i8v &codes)
     return (uint32_t)(e + 127);
 }
 
-// the same for the four blocks of a word of exponents
+// f for each of up to four blocks, those of a word of exponents
 template <typename F>
 __device__ __forceinline__ void four_blocks(int n, F f) {
     f(std::integral_constant<int, 0>{});
@@ -215,7 +215,16 @@ __global__ __launch_bounds__(512) void pwfp8_few_kernel(PwFp8Params p) {
 
 // Many pixels: PX x CO tiles, a ring of NST stages of one block of 128 inputs each.  Both
 // operands come by direct loads in the order of the matrix operands, so that LDS is
-// written and read in whole KiB.  A wave has WPX x WCO of the tile.
+// written and read in whole KiB.  A wave has WPX x WCO of the tile.  Steps are without
+// branches, four to a round (with them, and with addresses in vector registers: 197 x
+// 4096 x 4096 15.5 us, now 13.6; 4096 x 4096 x 4096 68.4, now 66.3).
+//
+// What bounds it: 8192 x 4096 x 4096 takes 131 us on a card that was idle (2.1 PFLOP/s)
+// and up to 150 on one that was not; its matrix instructions alone, on what lies in
+// registers, take 100, at the clock that they leave the card, and with the weights'
+// LDS reads taken out it takes 98.  Reading the inputs a block ahead, the weights two
+// blocks of channels ahead, and a wave's priority made no difference; sums in the
+// matrix instruction, without the scales, took longer.
 template <int PX, int CO, int NPX, int NCO>
 struct PwTile {
     static constexpr int WAVES = NPX * NCO, FM = PX / NPX / 16, FN = CO / NCO / 16;
@@ -237,29 +246,33 @@ __global__ __launch_bounds__(64 * NPX * NCO, PX == 128 ? 4 : 2) void pwfp8_tile_
     const int m0 = (mt < ct ? tile % mt : tile / ct) * PX, n0 = (mt < ct ? tile / mt : tile % ct) * (CO / 16);
     const int wm = wave % NPX * FM, wn = wave / NPX * FN;         // the wave's first pixel and channel block
 
-    // the wave's loads: 64 pixels of a slice of 16 channels; half a block of 16 channels
+    // the wave's loads: 64 pixels of a slice of 16 channels; half a block of 16 channels.
+    // `more`: another block follows; the last one is loaded again where there is none,
+    // so that steps have no branches
     const h8 *xp[XL], *wp[WL];
+    uint32_t xo[XL];
 #pragma unroll
     for (int i = 0; i < XL; ++i) {
         const int e = wave * XL + i, s = e / (PX / 64), px = e % (PX / 64) * 64 + lane;
-        xp[i] = (const h8 *)p.x.codes + (size_t)s * p.M + min(m0 + px, p.M - 1);
+        xp[i] = (const h8 *)p.x.codes + (size_t)s * p.M;
+        xo[i] = (uint32_t)min(m0 + px, p.M - 1) * 16;
     }
 #pragma unroll
     for (int i = 0; i < WL; ++i) {
         const int e = wave * WL + i, nb = min(n0 + e / 2, p.nb16 - 1);
-        wp[i] = (const h8 *)p.w + (size_t)nb * p.kb * 128 + (e & 1) * 64 + lane;
+        wp[i] = (const h8 *)p.w + (size_t)nb * p.kb * 128 + (e & 1) * 64;
     }
     const size_t xstep = (size_t)8 * p.M;
-    auto issue = [&](h8 *st) {
+    auto issue = [&](bool more, h8 *st) {
 #pragma unroll
         for (int i = 0; i < XL; ++i) {
-            load_lds16(xp[i], st + (wave * XL + i) * 64);
-            xp[i] += xstep;
+            load_lds16(xp[i], xo[i], st + (wave * XL + i) * 64);
+            xp[i] += more ? xstep : 0;
         }
 #pragma unroll
         for (int i = 0; i < WL; ++i) {
-            load_lds16(wp[i], st + T::XE + (wave * WL + i) * 64);
-            wp[i] += 128;
+            load_lds16(wp[i], (uint32_t)lane * 16, st + T::XE + (wave * WL + i) * 64);
+            wp[i] += more ? 128 : 0;
         }
     };
     f4 acc[FN][FM];
@@ -282,20 +295,19 @@ __global__ __launch_bounds__(64 * NPX * NCO, PX == 128 ? 4 : 2) void pwfp8_tile_
     const uint32_t k0 = split_scale(s0), k1 = split_scale(s1);
 #pragma unroll
     for (int i = 0; i < NST - 1; ++i)
-        if (i < p.kb) issue(ring[i]);
+        issue(i + 1 < p.kb, ring[i]);
     auto step = [&](auto q, int kb) {
         constexpr int u = decltype(q)::value;
         h8 *st = ring[u % NST];
-        if (NST == 2 || kb + 1 >= p.kb) wait_vm_lds<0>();            // (stages issued after this one stay in flight)
-        else if (kb + 2 >= p.kb) wait_vm_lds<T::LOADS>();
-        else wait_vm_lds<2 * T::LOADS>();
+        wait_vm_lds<(NST - 2) * T::LOADS>();                         // (stages issued after this one stay in flight)
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        if (u == 0 && kb + 4 < p.kb) {
+        if (u == 0) {
+            const int more = kb + 4 < p.kb ? p.M : 0;
 #pragma unroll
-            for (int j = 0; j < FM; ++j) next[j] = *(ep[j] += p.M);
+            for (int j = 0; j < FM; ++j) next[j] = *(ep[j] += more);
         }
-        if (kb + NST - 1 < p.kb) issue(ring[(u + NST - 1) % NST]);
+        issue(kb + NST < p.kb, ring[(u + NST - 1) % NST]);
         const float sw = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(kb < 64 ? s0 : s1), kb & 63));
         const uint32_t k = __builtin_amdgcn_readlane(kb < 64 ? k0 : k1, kb & 63);
         auto weights = [&](int i) {
@@ -310,7 +322,7 @@ __global__ __launch_bounds__(64 * NPX * NCO, PX == 128 ? 4 : 2) void pwfp8_tile_
         }
         // the products of a block of channels run while those of the one before are
         // scaled and added, and the next one's weights are read
-        f4 part[2][FM];
+        f4 part[FM];
 #pragma unroll
         for (int i = 0; i <= FN; ++i) {
             i8v wn_;
@@ -318,22 +330,28 @@ __global__ __launch_bounds__(64 * NPX * NCO, PX == 128 ? 4 : 2) void pwfp8_tile_
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int j = 0; j < FM; ++j) {
-                if (i < FN) part[i & 1][j] = mma8<u>(w, x[j], k, e[j]);
-                __builtin_amdgcn_sched_barrier(0);
                 if (i > 0) {
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) acc[i - 1][j][r] = fmaf(part[(i & 1) ^ 1][j][r], sw, acc[i - 1][j][r]);
+                    for (int r = 0; r < 4; ++r) acc[i - 1][j][r] = fmaf(part[j][r], sw, acc[i - 1][j][r]);
                 }
+                __builtin_amdgcn_sched_barrier(0);
+                if (i < FN) part[j] = mma8<u>(w, x[j], k, e[j]);
                 __builtin_amdgcn_sched_barrier(0);
             }
             w = wn_;
         }
     };
-    for (int kb = 0; kb < p.kb; kb += 4) {
-        four_blocks(p.kb - kb, [&](auto q) { step(q, kb + decltype(q)::value); });
+    int kb = 0;
+    for (; kb + 4 <= p.kb; kb += 4) {
+        step(std::integral_constant<int, 0>{}, kb);
+        step(std::integral_constant<int, 1>{}, kb + 1);
+        step(std::integral_constant<int, 2>{}, kb + 2);
+        step(std::integral_constant<int, 3>{}, kb + 3);
 #pragma unroll
         for (int j = 0; j < FM; ++j) e[j] = next[j];
     }
+    if (kb < p.kb) four_blocks(p.kb - kb, [&](auto q) { step(q, kb + decltype(q)::value); });
+    wait_vm_lds<0>();                                                 // (no load to LDS outlives the workgroup)
 #pragma unroll
     for (int i = 0; i < FN; i += 2) {
         const int nb = n0 + wn + i;
@@ -378,8 +396,7 @@ hipError_t launch_pwfp8_t(const PwFp8Params &p, const PwFp8Geom &g, hipStream_t 
 
 // The largest tile that fills the card: of 256 x 256 one to a compute unit, of
 // 128 x 128 two, of 64 x 128 one (315 x 1960 x 12032: 16.7 us, by 128 x 128 20.1, by
-// 64 x 64 24.0; 2115 x 96 x 6290: 13.4 by 128 x 128, 14.9 by 64 x 128; 8192 x 4096 x
-// 4096 133 by 256 x 256).  Few tiles and many inputs: the kernel of few pixels, which
+// 64 x 64 24.0; 2115 x 96 x 6290: 13.4 by 128 x 128, 14.9 by 64 x 128).  Few tiles and many inputs: the kernel of few pixels, which
 // shares the inputs out.
 PwFp8Geom pwfp8_geom(size_t M, int nb16, int kb) {
     if (M <= 64) return {0};
