@@ -489,7 +489,7 @@ mgi_status mgi_plan_read_node(mgi_plan *p, int i, void *dev_dst, void *stream);
  * (ceil(c/8) * n*h*w * 16 bytes) on `stream`; *bytes receives that size (it
  * may be queried with dev_dst NULL).  For checking that padding lanes hold
  * zeros.  Requires materialize_all and an enqueued run (MGI_ERR_STATE), and a
- * node whose output is stored sliced (MGI_ERR_UNSUPPORTED for fp32 logits,
+ * node whose output is stored sliced (MGI_ERR_UNSUPPORTED for fp32 logits, 8-bit tensors,
  * probabilities and labels). */
 mgi_status mgi_plan_read_node_raw(mgi_plan *p, int i, void *dev_dst, size_t *bytes, void *stream);
 

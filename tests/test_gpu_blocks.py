@@ -307,3 +307,47 @@ def test_channels_past_the_last_stay_zero(dtype):
         assert (lanes[-1, :, c % 8:] == 0).all() and (lanes[-1, :, :c % 8] != 0).any()
         seen += 1
     assert seen == 3
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+def test_a_trunk_before_and_a_head_behind_tuned_and_captured(dtype):
+    # convolutions before the block, its tensors in a concatenation, a depthwise layer, a resize and a head
+    from block_util import builder, given, inputs, run, stored
+    from paper_1907_01989_amd import engine
+    b = builder(11)
+    x = given(b, stored(np.random.default_rng(4).uniform(0, 1, (2, 33, 29, 3)), dtype), dtype)
+    p = b.conv(b.dw(b.conv(x, 32, 3, 2)), 64)
+    n = b.rms_norm(p, to8=True)
+    qkv = b.pointwise_fp8(n, 3 * 64)
+    r = b.rotary(qkv, 4, 32, [1 + i % 2 for i in range(12)], [0.7 ** i for i in range(12)])
+    y = b.attention(r, r, qkv, 2, 2, 32, k_from=64, v_from=128)
+    o = b.pointwise_fp8(b.quantize(y), 64, 1)
+    s = b.add(p, o)
+    z = b.rms_norm(s)
+    joined = b.concat([y, z, s])
+    d = b.dw(joined)
+    small = b.resize(y, 9, 9)
+    label = b.argmax(b.conv(small, 24, act=0))
+    logits = b.fc(b.gap(b.conv(d, 128)), 40)
+    outs = [logits, label, y, z, small, joined]
+    log(f"[case] block between a trunk and a head, type {dtype}")
+    want, _ = run(b, outs, dtype, fuse=False)
+    kept, _ = run(b, outs, dtype, materialize_all=True)
+    plan = engine.Plan({"name": "trunk", "ops": b.ops, "outputs": outs}, dtype=dtype)
+    xs = inputs(plan)
+
+    def same(ys):
+        for a, c in zip(ys, want):
+            np.testing.assert_array_equal(a.double().cpu().numpy().reshape(c.shape), c)
+
+    for a, c in zip(kept, want):
+        np.testing.assert_array_equal(a, c)
+    same(plan.run(xs))
+    plan.autotune(xs, reps=2)
+    same(plan.run(xs))
+    held = plan.capture(xs)
+    for _ in range(3):
+        for o in held:
+            o.fill_(-3)
+        plan.replay()
+        same(held)
