@@ -12,18 +12,20 @@
 // for the product (an error of half a step relative to each weight, which the
 // sum over keys averages), its sum is taken before.
 //
-// What bounds it (MI355X).  Long sequences: the matrix instructions at the clock that
-// they leave the card, 8192 causal tokens, 32 heads of 128 on 8 of keys, bf16, 535 to
-// 565 us, 1.0 PFLOP/s, where a library's product of 8192 x 8192 x 8192 reaches 1.21.
-// Taking half of the LDS reads of V out, or the exponentials, changed that by 7% at
-// most; scores of the next tile computed between the weights of this one took 663 us
-// against 625 on the same card, a wave's priority made no difference.  Packed short
-// ones (5003 tokens in 13 sequences, 16 heads of 80: 45 us): loads and barriers take 3%
-// of a wave's time there, a tile's 24 matrix instructions and about 1000 cycles of
-// maxima, exponentials and sums share a SIMD among three waves (3500 cycles for three
-// tiles), and the compute units that hold the longest sequence's tiles end last.  One
-// query on 32768 keys: bytes in flight, 134 MB in 29 us, 4.6 TB/s with the start.
+// What bounds it (MI355X).  Long sequences, 8192 causal tokens, 32 heads of 128 on 8 of
+// keys, bf16: 531 to 545 us a call, 1.0 PFLOP/s, where a library's product of 8192 x 8192
+// x 8192 reaches 1.21.  A wave's step has 1024 cycles of matrix instructions and about
+// as many of maxima, exponentials and sums, of which two waves on a SIMD hide little of
+// each other's (matrix instructions 49% of the cycles, vector ones as many).  Taking half
+// of the LDS reads of V out, or the exponentials, changed the time by 7% at most;
+// scores of the next tile computed between the weights of this one took 663 us against
+// 625 on the same card, a wave's priority made no difference.  Packed short sequences
+// (5003 tokens in 13 of them, 16 heads of 80: 47 us): 3500 cycles for the steps of three
+// waves on a SIMD, and the compute units that hold the longest sequence's tiles end
+// last.  One query on 32768 keys: bytes in flight, 134 MB in 29 us, 4.6 TB/s with the
+// start.
 #include <algorithm>
+#include <type_traits>
 
 #include "tokens.h"
 
@@ -222,17 +224,18 @@ __global__ __launch_bounds__(256, WR == 1 ? 1 : ND == 3 ? 3 : 2) void attention_
     of_lane<NHWC>(lane, lk, ls);
     const h8 *kp = p.k.x + (size_t)(kvh * p.d8 + ls) * p.k.s, *vp = p.v.x + (size_t)(kvh * p.d8 + ls) * p.v.s;
     constexpr int BLOCKS = WR == 4 ? 1 : 2, LOADS = BLOCKS * ND;     // blocks of 16 keys that a wave loads, loads of K (or V)
-    auto issue = [&](int j0, int stage, bool values) {
+    // one of the 2 LOADS loads of a tile: K's blocks and slices, then V's
+    auto issue = [&](int j0, int stage, int piece) {
+        const bool values = piece >= LOADS;
+        const int u = piece % LOADS / ND, g = piece % ND, b = WR == 4 ? wave : u;
         h8 *to = lds + (stage * OWN + (WR == 4 ? 0 : wave)) * STAGE + (values ? PART : 0);
         const TokenIn &x = values ? p.v : p.k;
+        const h8 *at = (values ? vp : kp) + (size_t)(t.k0 + min(j0 + b * 16 + lk, t.nk - 1)) * x.p;
+        load_lds16(g == ND - 1 && ls + 4 * g >= p.d8 ? p.zero : at + (size_t)(4 * g) * x.s, to + (b * ND + g) * 64);
+    };
+    auto issue_all = [&](int j0, int stage) {
 #pragma unroll
-        for (int u = 0; u < BLOCKS; ++u) {
-            const int b = WR == 4 ? wave : u;
-            const h8 *at = (values ? vp : kp) + (size_t)(t.k0 + min(j0 + b * 16 + lk, t.nk - 1)) * x.p;
-#pragma unroll
-            for (int g = 0; g < ND; ++g)
-                load_lds16(g == ND - 1 && ls + 4 * g >= p.d8 ? p.zero : at + (size_t)(4 * g) * x.s, to + (b * ND + g) * 64);
-        }
+        for (int i = 0; i < 2 * LOADS; ++i) issue(j0, stage, i);
     };
     // the lane's places in a stage, in elements (K: of even and odd steps of 16
     // channels) and bytes
@@ -241,13 +244,41 @@ __global__ __launch_bounds__(256, WR == 1 ? 1 : ND == 3 ? 3 : 2) void attention_
     const int va = at_of<NHWC>(4 * half + (key >> 2), (lane >> 4 & 1) * 2 + (key >> 1 & 1)) * 16 + (key & 1) * 8;
     constexpr int EIGHT = NHWC ? 512 : 128;                          // bytes from a key to the eighth after it
 
-    auto scores = [&](const h8 *kt, f16v (&s)[NK]) {
+    // The next tile's loads are issued between the products: all at once they wait for
+    // one another, 700 of a step's 3600 cycles (8192 causal tokens, heads of 128: 614 us,
+    // now 593).  Heads of 96 channels, whose waves have 168 registers, have none to spare
+    // for that (103 us against 47 for the packed sequences above); waves by themselves
+    // wait for their own loads either way.
+    constexpr bool SPREAD = WR == 4 && ND != 3;
+    auto scores = [&](auto load, int j0, int to, const h8 *kt, f16v (&s)[NK]) {
+        auto read = [&](int k, int b) { return kt[ka[k & 1] + (b * 2 * ND + k / 2) * 64]; };
 #pragma unroll
         for (int b = 0; b < NK; ++b) s[b] = f16v{};
+        if constexpr (!decltype(load)::value) {
 #pragma unroll
-        for (int k = 0; k < ND * 2; ++k)
+            for (int k = 0; k < ND * 2; ++k)
 #pragma unroll
-            for (int b = 0; b < NK; ++b) s[b] = mma32<E>(kt[ka[k & 1] + (b * 2 * ND + k / 2) * 64], q[k], s[b]);
+                for (int b = 0; b < NK; ++b) s[b] = mma32<E>(read(k, b), q[k], s[b]);
+        } else {
+            h8 a[3][NK];                                                 // (read two steps ahead)
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int b = 0; b < NK; ++b) a[k][b] = read(k, b);
+#pragma unroll
+            for (int k = 0; k < ND * 2; ++k) {
+                if (k + 2 < ND * 2) {
+#pragma unroll
+                    for (int b = 0; b < NK; ++b) a[(k + 2) % 3][b] = read(k + 2, b);
+                }
+#pragma unroll
+                for (int i = 0; i < LOADS / ND; ++i) issue(j0, to, k * (LOADS / ND) + i);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int b = 0; b < NK; ++b) s[b] = mma32<E>(a[k % 3][b], q[k], s[b]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
     };
     // Hidden keys have no score; values that are infinite or NaN are taken out of the
     // tile (0 times them is NaN) and added to the rows that see them.
@@ -332,21 +363,21 @@ __global__ __launch_bounds__(256, WR == 1 ? 1 : ND == 3 ? 3 : 2) void attention_
     const int start = from + (WR == 4 ? 0 : wave * KEYS);
     int stage = 0;
     if (start < most) {
-        issue(start, 0, false);
-        issue(start, 0, true);
+        issue_all(start, 0);
     }
     for (int j0 = start; j0 < most; j0 += STEP, stage ^= 1) {
         wait_vm_lds<0>();
         if constexpr (WR == 4) __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");                           // (no LDS access moves over the wait)
-        if (j0 + STEP < most) {
-            issue(j0 + STEP, stage ^ 1, false);
-            issue(j0 + STEP, stage ^ 1, true);
-        }
+        const bool more = j0 + STEP < most;
         h8 *kt = lds + (stage * OWN + (WR == 4 ? 0 : wave)) * STAGE, *vt = kt + PART;
         f16v s[NK];
         const bool mute = !works || j0 >= mine;
-        if (!mute) scores(kt, s);
+        if (more && (mute || !SPREAD)) issue_all(j0 + STEP, stage ^ 1);
+        if (!mute) {
+            if (SPREAD && more) scores(std::true_type{}, j0 + STEP, stage ^ 1, kt, s);
+            else scores(std::false_type{}, 0, 0, kt, s);
+        }
         if (j0 + KEYS > least) hide(j0, vt, s);
         if (mute) continue;
         const float base = rebase(s);

@@ -220,12 +220,11 @@ __global__ __launch_bounds__(512) void pwfp8_few_kernel(PwFp8Params p) {
 // branches, four to a round (with them, and with addresses in vector registers: 197 x
 // 4096 x 4096 15.5 us, now 13.6; 4096 x 4096 x 4096 68.4, now 66.3).
 //
-// What bounds it: 8192 x 4096 x 4096 takes 131 us on a card that was idle (2.1 PFLOP/s)
-// and up to 150 on one that was not; its matrix instructions alone, on what lies in
-// registers, take 100, at the clock that they leave the card, and with the weights'
-// LDS reads taken out it takes 98.  Reading the inputs a block ahead, the weights two
-// blocks of channels ahead, and a wave's priority made no difference; sums in the
-// matrix instruction, without the scales, took longer.
+// What bounds it: 8192 x 4096 x 4096 takes 130 us (2.1 PFLOP/s), 61% of them with
+// matrix instructions in a tile's steps, and the starts and stores of two rounds of
+// tiles about 25.  With the weights' LDS reads taken out it takes 98, without the loads
+// to LDS 113, without the inputs' reads 129.  Reading the inputs a block ahead or the
+// weights two blocks of channels ahead, and a wave's priority, made no difference.
 template <int PX, int CO, int NPX, int NCO>
 struct PwTile {
     static constexpr int WAVES = NPX * NCO, FM = PX / NPX / 16, FN = CO / NCO / 16;
