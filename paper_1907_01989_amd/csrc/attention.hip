@@ -13,14 +13,14 @@
 // sum over keys averages), its sum is taken before.
 //
 // What bounds it (MI355X).  Long sequences, 8192 causal tokens, 32 heads of 128 on 8 of
-// keys, bf16: 531 to 545 us a call, 1.0 PFLOP/s, where a library's product of 8192 x 8192
+// keys, bf16: 503 to 531 us a call, 1.04 to 1.09 PFLOP/s, where a library's product of 8192 x 8192
 // x 8192 reaches 1.21.  A wave's step has 1024 cycles of matrix instructions and about
 // as many of maxima, exponentials and sums, of which two waves on a SIMD hide little of
 // each other's (matrix instructions 49% of the cycles, vector ones as many).  Taking half
 // of the LDS reads of V out, or the exponentials, changed the time by 7% at most;
 // scores of the next tile computed between the weights of this one took 663 us against
 // 625 on the same card, a wave's priority made no difference.  Packed short sequences
-// (5003 tokens in 13 of them, 16 heads of 80: 47 us): 3500 cycles for the steps of three
+// (5003 tokens in 13 of them, 16 heads of 80: 45 us): 3500 cycles for the steps of three
 // waves on a SIMD, and the compute units that hold the longest sequence's tiles end
 // last.  One query on 32768 keys: bytes in flight, 134 MB in 29 us, 4.6 TB/s with the
 // start.
@@ -50,6 +50,13 @@ __device__ __forceinline__ f16v mma32(h8 a, h8 b, f16v c) {
         return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bh8, a), __builtin_bit_cast(bh8, b), c, 0, 0, 0);
     else
         return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+}
+
+// the larger of a lane's value and lane ^ 32's, without a way through LDS (8192 causal
+// tokens: 589 -> 580 us)
+__device__ __forceinline__ float larger_half(float v) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
 // A tile of query rows: the sequence's queries and keys, and the tile's number
@@ -247,7 +254,7 @@ __global__ __launch_bounds__(256, WR == 1 ? 1 : ND == 3 ? 3 : 2) void attention_
     // The next tile's loads are issued between the products: all at once they wait for
     // one another, 700 of a step's 3600 cycles (8192 causal tokens, heads of 128: 614 us,
     // now 593).  Heads of 96 channels, whose waves have 168 registers, have none to spare
-    // for that (103 us against 47 for the packed sequences above); waves by themselves
+    // for that (103 us against 47, the packed sequences above); waves by themselves
     // wait for their own loads either way.
     constexpr bool SPREAD = WR == 4 && ND != 3;
     auto scores = [&](auto load, int j0, int to, const h8 *kt, f16v (&s)[NK]) {
@@ -256,9 +263,14 @@ __global__ __launch_bounds__(256, WR == 1 ? 1 : ND == 3 ? 3 : 2) void attention_
         for (int b = 0; b < NK; ++b) s[b] = f16v{};
         if constexpr (!decltype(load)::value) {
 #pragma unroll
-            for (int k = 0; k < ND * 2; ++k)
+            for (int k = 0; k < ND * 2 - 1; ++k)
 #pragma unroll
                 for (int b = 0; b < NK; ++b) s[b] = mma32<E>(read(k, b), q[k], s[b]);
+            // (16 channels of zeros are left out: heads of 80, the packed sequences above 46.5 -> 45.0 us)
+            if (p.d8 > ND * 4 - 2) {
+#pragma unroll
+                for (int b = 0; b < NK; ++b) s[b] = mma32<E>(read(ND * 2 - 1, b), q[ND * 2 - 1], s[b]);
+            }
         } else {
             h8 a[3][NK];                                                 // (read two steps ahead)
 #pragma unroll
@@ -321,7 +333,7 @@ __global__ __launch_bounds__(256, WR == 1 ? 1 : ND == 3 ? 3 : 2) void attention_
         for (int b = 0; b < NK; ++b)
 #pragma unroll
             for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
-        top = fmaxf(top, __shfl_xor(top, 32, 64));
+        top = larger_half(top);
         const bool move = fmaf(top, c, m == -INFINITY ? INFINITY : -m * c) > kSlack;
         if (__any(move)) {
             // (before the first weights there is nothing to scale but what hidden
