@@ -13,14 +13,14 @@
 // sum over keys averages), its sum is taken before.
 //
 // What bounds it (MI355X).  Long sequences, 8192 causal tokens, 32 heads of 128 on 8 of
-// keys, bf16: 503 to 531 us a call, 1.04 to 1.09 PFLOP/s, where a library's product of 8192 x 8192
+// keys, bf16: 503 to 548 us a call on different cards, 1.0 to 1.09 PFLOP/s, where a library's product of 8192 x 8192
 // x 8192 reaches 1.21.  A wave's step has 1024 cycles of matrix instructions and about
 // as many of maxima, exponentials and sums, of which two waves on a SIMD hide little of
 // each other's (matrix instructions 49% of the cycles, vector ones as many).  Taking half
 // of the LDS reads of V out, or the exponentials, changed the time by 7% at most;
 // scores of the next tile computed between the weights of this one took 663 us against
 // 625 on the same card, a wave's priority made no difference.  Packed short sequences
-// (5003 tokens in 13 of them, 16 heads of 80: 45 us): 3500 cycles for the steps of three
+// (5003 tokens in 13 of them, 16 heads of 80: 42 us): 3500 cycles for the steps of three
 // waves on a SIMD, and the compute units that hold the longest sequence's tiles end
 // last.  One query on 32768 keys: bytes in flight, 134 MB in 29 us, 4.6 TB/s with the
 // start.
@@ -361,15 +361,30 @@ __global__ __launch_bounds__(256, WR == 1 ? 1 : ND == 3 ? 3 : 2) void attention_
         l += sum;
     };
     auto values = [&](const h8 *vt, const h8 (&pr)[2 * NK]) {
+        auto read = [&](int i) {
+            const int off = va + i * 1024;
+            const s4 a = read_column(vt, off), b = read_column(vt, off + EIGHT);
+            return __builtin_bit_cast(h8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+        };
+        constexpr int N = 2 * NK * ND;
+        if constexpr (WR == 4 && ND < 4) {
+            // (read ahead, which the compiler does not do by itself here: the packed
+            // sequences above 44.7 -> 42.3 us; heads of 128 channels do not gain)
+            constexpr int D = 2;                                         // (heads of 96 keep two registers in memory for it)
+            h8 v[D + 1];
 #pragma unroll
-        for (int k = 0; k < 2 * NK; ++k)
+            for (int i = 0; i < D; ++i) v[i] = read(i);
 #pragma unroll
-            for (int d = 0; d < ND; ++d) {
-                const int off = va + (k * ND + d) * 1024;
-                const s4 a = read_column(vt, off), b = read_column(vt, off + EIGHT);
-                const h8 v = __builtin_bit_cast(h8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
-                o[d] = mma32<E>(v, pr[k], o[d]);
+            for (int i = 0; i < N; ++i) {
+                if (i + D < N) v[(i + D) % (D + 1)] = read(i + D);
+                __builtin_amdgcn_sched_barrier(0);
+                o[i % ND] = mma32<E>(v[i % (D + 1)], pr[i / ND], o[i % ND]);
+                __builtin_amdgcn_sched_barrier(0);
             }
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) o[i % ND] = mma32<E>(read(i), pr[i / ND], o[i % ND]);
+        }
     };
 
     const int start = from + (WR == 4 ? 0 : wave * KEYS);
