@@ -13,8 +13,8 @@
 // sum over keys averages), its sum is taken before.
 //
 // What bounds it (MI355X).  Long sequences, 8192 causal tokens, 32 heads of 128 on 8 of
-// keys, bf16: 503 to 548 us a call on different cards, 1.0 to 1.09 PFLOP/s, where a library's product of 8192 x 8192
-// x 8192 reaches 1.21.  A wave's step has 1024 cycles of matrix instructions and about
+// keys, bf16: 503 to 548 us a call on different cards, 1.0 to 1.09 PFLOP/s, where a
+// library's product of 8192 x 8192 x 8192 reaches 1.21.  A wave's step has 1024 cycles of matrix instructions and about
 // as many of maxima, exponentials and sums, of which two waves on a SIMD hide little of
 // each other's (matrix instructions 49% of the cycles, vector ones as many).  Taking half
 // of the LDS reads of V out, or the exponentials, changed the time by 7% at most;
