@@ -70,6 +70,17 @@ def test_images(n, q, k, heads, kv, dim, causal, dtype):
     np.testing.assert_array_equal(f, y)
 
 
+@pytest.mark.parametrize("dim", range(8, 129, 8))
+def test_every_head_size_over_several_tiles(dim):
+    from block_util import run
+    for q, k in (((1, 140), (1, 333)), ((1, 1), (1, 700))):
+        log(f"[case] attention {q} on {k} heads of {dim}")
+        t = tensors(np.random.default_rng(dim), (2,) + q, (2,) + k, 2, 1, dim, dim // 8 % 2)
+        b, a = graph(*t, dim // 8 % 2, 2, 1, dim, causal=dim % 3 == 0)
+        (y,), _ = run(b, [a], dim // 8 % 2, {a: dim // 8 % 2})
+        check(*t, dim // 8 % 2, 2, 1, dim, y, causal=dim % 3 == 0)
+
+
 PACKED = [
     # bounds, k_bounds, pixels, k pixels
     ([0, 5], None, 5, 5), ([0, 64, 128, 129, 129, 300], None, 300, 300), ([3, 10, 10, 200], None, 210, 210),
