@@ -384,7 +384,7 @@ mgi_status mgi_graph_mark_output(mgi_graph *g, int id);
  * the plan's storage type (FP16 or BF16; finalize gives MGI_ERR_UNSUPPORTED for
  * the other one): the tensor as stored, without widening.  Tensors that are not
  * stored in 16 bits (logits, probabilities, labels, indices) have no such form
- * (MGI_ERR_UNSUPPORTED). */
+ * (MGI_ERR_UNSUPPORTED; from finalize for activations of logits, which are logits). */
 mgi_status mgi_graph_mark_output_as(mgi_graph *g, int id, int dtype);
 
 /* ---------------------------------------------------------------------------

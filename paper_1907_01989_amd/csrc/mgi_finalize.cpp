@@ -1674,6 +1674,11 @@ mgi_status Lowering::bind_outputs() {
         if (b < 0 || p.bufs[b].loc != Loc::Output)
             return fail(MGI_ERR_UNSUPPORTED, "output tensor " + std::to_string(t) +
                                                  " was fused away or cannot be exported");
+        // (what a layer of logits absorbed is fp32 as the logits are: its kernel would write
+        // twice the bytes of a 16-bit array)
+        if (g.output_dtypes[k] != MGI_DTYPE_FP32 && p.bufs[b].layout != Layout::H16)
+            return fail(MGI_ERR_UNSUPPORTED, "mgi_graph_finalize: output tensor " + std::to_string(t) +
+                                                 " is not stored in 16 bits");
         p.output_bufs[k] = b;
         Shape s = g.ops[t].out;
         p.output_shapes.push_back(s);

@@ -237,6 +237,25 @@ def test_16_bit_outputs_are_refused_for_tensors_of_32(g):
     assert status(B.mgi_graph_mark_output_as, g, 77, B.DTYPE_FP16) == 1
 
 
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("form", ["relu", "none", "two", "behind one", "int4"])
+def test_16_bit_outputs_are_refused_for_activations_of_logits(form, dtype):
+    # (the layer takes the activation along and writes fp32 values: twice the bytes of such an output)
+    b = NetBuilder()
+    x = b.input(2, 1, 1, 64, -1, 1)
+    f = b.fc_int4(x, 8) if form == "int4" else b.fc(x, 8)
+    if form == "behind one":
+        f = b.concat([f])
+    if form == "two":
+        f = b.activation(f, 0)
+    a = b.activation(f, 0 if form == "none" else 1)
+    wide = engine.Plan({"ops": b.ops, "outputs": [a]}, bind=False, dtype=dtype)
+    assert wide.outputs_info[0][1:] == (B.DTYPE_FP32, 64)
+    with pytest.raises(B.MgiError, match="16 bits") as e:
+        engine.Plan({"ops": b.ops, "outputs": [a], "output_dtypes": {a: dtype}}, bind=False, dtype=dtype)
+    assert e.value.status == 3
+
+
 def kinds(b, outputs, **kw):
     plan = engine.Plan({"ops": b.ops, "outputs": outputs}, bind=False, **kw)
     return [n["kind"] for n in plan.nodes() if n["kind"] not in ("ingest", "export")]
