@@ -463,9 +463,11 @@ struct NormParams {
     int bf16;
 };
 hipError_t launch_norm(const NormParams &p, hipStream_t st);
-// sliced or 8-bit tensor -> NHWC fp32 or 16-bit output; NHWC 16-bit input -> sliced
+// sliced or 8-bit tensor -> NHWC fp32 or 16-bit output; NHWC 16-bit input -> sliced;
+// 16-bit output -> fp32
 hipError_t launch_export16(const h8 *x, void *y, int M, int C, hipStream_t st);
 hipError_t launch_ingest16(const void *x, h8 *y, int M, int C, hipStream_t st);
+hipError_t launch_widen16(const void *x, float *y, size_t n, bool bf16, hipStream_t st);
 hipError_t launch_export8(const Tensor8 &x, void *y, bool f32, int M, int C, bool bf16, hipStream_t st);
 
 constexpr int kMaxAxes = 8;

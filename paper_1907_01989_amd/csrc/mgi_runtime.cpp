@@ -1215,6 +1215,8 @@ extern "C" mgi_status mgi_plan_read_node(mgi_plan *p, int i, void *dev_dst, void
     } else if (b.layout == Layout::C8) {
         e = launch_export((const h8 *)src, (float *)dev_dst, (int)b.shape.pixels(), b.shape.c,
                           p->opt.dtype == MGI_DTYPE_BF16, st);
+    } else if (b.layout == Layout::H16) {
+        e = launch_widen16(src, (float *)dev_dst, b.shape.elems(), p->opt.dtype == MGI_DTYPE_BF16, st);
     } else {
         e = hipMemcpyAsync(dev_dst, src, b.bytes, hipMemcpyDeviceToDevice, st);
     }

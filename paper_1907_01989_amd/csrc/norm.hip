@@ -231,6 +231,16 @@ __global__ __launch_bounds__(256) void export8_kernel(Tensor8 x, void *y, int f3
     }
 }
 
+// an array's 16-bit values as fp32
+template <typename E>
+__global__ __launch_bounds__(256) void widen16_kernel(const uint16_t *x, float *y, size_t n) {
+    const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= n) return;
+    u16x8 b{};
+    b[0] = x[i];
+    y[i] = E::get(__builtin_bit_cast(h8, b), 0);
+}
+
 }  // namespace
 
 hipError_t launch_norm(const NormParams &p, hipStream_t st) {
@@ -265,6 +275,13 @@ hipError_t launch_export16(const h8 *x, void *y, int M, int C, hipStream_t st) {
 hipError_t launch_ingest16(const void *x, h8 *y, int M, int C, hipStream_t st) {
     const int S = (C + 7) / 8;
     launch(ingest16_kernel, dim3(plane_blocks(M, S)), dim3(256), 0, st, (const uint16_t *)x, y, M, C, S);
+    return hipGetLastError();
+}
+
+hipError_t launch_widen16(const void *x, float *y, size_t n, bool bf16, hipStream_t st) {
+    const dim3 grid((unsigned)((n + 255) / 256));
+    if (bf16) launch(widen16_kernel<BF16>, grid, dim3(256), 0, st, (const uint16_t *)x, y, n);
+    else launch(widen16_kernel<F16>, grid, dim3(256), 0, st, (const uint16_t *)x, y, n);
     return hipGetLastError();
 }
 

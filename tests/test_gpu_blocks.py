@@ -351,3 +351,21 @@ def test_a_trunk_before_and_a_head_behind_tuned_and_captured(dtype):
             o.fill_(-3)
         plan.replay()
         same(held)
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+def test_nodes_that_write_16_bit_outputs_are_read_as_fp32(dtype):
+    import torch
+    from block_util import builder, given, inputs, stored
+    b = builder()
+    x = given(b, stored(np.random.default_rng(4).standard_normal((1, 3, 5, 77)), dtype), dtype)
+    s = b.add(x, x, act=0)
+    q = b.quantize(s)
+    plan = plan_of(b, [s, q], dtype, materialize_all=True)
+    ys = plan.run(inputs(plan))
+    log(f"[case] export nodes read, type {dtype}")
+    nodes = [i for i, n in enumerate(plan.nodes()) if n["kind"] == "export"]
+    assert len(nodes) == 2
+    for i, y in zip(nodes, ys):
+        assert y.dtype == (torch.float16, torch.bfloat16)[dtype]
+        assert torch.equal(plan.read_node(i)[1], y.float())
