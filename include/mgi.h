@@ -191,7 +191,9 @@ mgi_status mgi_graph_add_conv2d(mgi_graph *g, int in, const mgi_conv_desc *d,
 mgi_status mgi_graph_add_depthwise(mgi_graph *g, int in, const mgi_conv_desc *d,
                                    const float *w, const float *bias, int *out);
 
-/* Element-wise y = act(a + b); a and b have equal shapes (Sec. 3.1, ADD). */
+/* Element-wise y = act(a + b); a and b have equal shapes (Sec. 3.1, ADD).  NaN
+ * stays NaN, also where a norm runs the add; an add that a convolution absorbs
+ * clamps it to a bound of the activation, as convolutions do. */
 mgi_status mgi_graph_add_add(mgi_graph *g, int a, int b, int act, int *out);
 
 /* Standalone activation; finalize fuses it into its producer when it can

@@ -22,6 +22,13 @@ __device__ __forceinline__ float act_apply(float v, int act) {
     return __builtin_amdgcn_fmed3f(v, lo, hi);
 }
 
+// act_apply that leaves NaN a NaN (of a NaN the clamp makes a bound)
+__device__ __forceinline__ float act_keep(float v, int act) {
+    if (act == MGI_ACT_NONE) return v;
+    const float y = act_apply(v, act);
+    return v == v ? y : v;
+}
+
 __device__ __forceinline__ h8 zero_h8() {
     h8 z;
 #pragma unroll

@@ -49,7 +49,7 @@ __global__ __launch_bounds__(1024) void norm_kernel(NormParams p) {
             if (p.b.x) {
                 float v[8];
 #pragma unroll
-                for (int c = 0; c < 8; ++c) v[c] = pinned(act_apply(E::get(h[r][j], c) + E::get(b[r][j], c), p.act));
+                for (int c = 0; c < 8; ++c) v[c] = pinned(act_keep(E::get(h[r][j], c) + E::get(b[r][j], c), p.act));
                 h[r][j] = E::pack(v);
                 if (p.sum.y && s < p.S && m < p.M) store8<E>(p.sum, s, m, h[r][j]);
             }

@@ -489,7 +489,7 @@ __global__ __launch_bounds__(256) void add_kernel(const h8 *a, const h8 *b, h8 *
     const h8 u = a[i], v = b[i];
     float o[8];
 #pragma unroll
-    for (int c = 0; c < 8; ++c) o[c] = act_apply(E::get(u, c) + E::get(v, c), act);
+    for (int c = 0; c < 8; ++c) o[c] = act_keep(E::get(u, c) + E::get(v, c), act);
     y[i] = E::pack(o);
 }
 

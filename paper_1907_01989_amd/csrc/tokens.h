@@ -19,13 +19,6 @@ __device__ __forceinline__ float pinned(float v) {
     return v;
 }
 
-// act_apply that leaves NaN a NaN
-__device__ __forceinline__ float act_keep(float v, int act) {
-    if (act == MGI_ACT_NONE) return v;
-    v = v < 0.0f ? 0.0f : v;
-    return act == MGI_ACT_RELU6 && v > 6.0f ? 6.0f : v;
-}
-
 // 8 channels of (slice, pixel), rounded once to the output's type
 template <typename E>
 __device__ __forceinline__ void store8(const TokenOut &o, int slice, int pixel, const float *v) {

@@ -198,3 +198,35 @@ def test_norm_of_tensors_inside_a_network():
     np.testing.assert_array_equal(ov[..., 24:], tv)
     ref = oracle.rms_norm(sv, b.ops[u]["w"], 1e-6)
     within(uv, ref, (HALF[0] + FP32) * np.abs(ref) + 2.0 ** -25)
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("act", [0, 1, 2])
+@pytest.mark.parametrize("to8", [False, True])
+def test_a_sum_leaves_nan_and_infinities_as_they_are(act, to8, dtype):
+    # in either operand, and of infinities of both signs: one value of a row, whose norm it reaches
+    from block_util import HALF, TINY, builder, given, run, stored, within
+    rng = np.random.default_rng(8)
+    for m, c in ((9, 40), (1100, 72)):
+        x, r = (stored(rng.standard_normal((1, 1, m, c)), dtype) for _ in range(2))
+        x[0, 0, 1, 3], r[0, 0, 2, c - 1] = np.nan, np.nan
+        x[0, 0, 3, 0], r[0, 0, 4, 5] = np.inf, -np.inf
+        x[0, 0, 5, 7], r[0, 0, 5, 7] = np.inf, -np.inf
+        b = builder(c)
+        s = b.add(given(b, x, dtype), given(b, r, dtype))
+        b.ops[s]["act"] = act
+        t = b.rms_norm(s, to8=to8)
+        log(f"[case] {m} x {c}: a sum with NaN and infinities, type {dtype} act {act} to8 {to8}")
+        with np.errstate(invalid="ignore"):
+            total = x + r if act == 0 else np.clip(x + r, 0, (np.inf, 6)[act - 1])     # (which keeps NaN)
+            assert np.isnan(total[0, 0, [1, 2, 5]]).any(-1).all()
+            for kw in ({}, {"fuse": False}, {"materialize_all": True}):
+                (hs, y), _ = run(b, [s, t], dtype, **kw)
+                within(hs, total, np.where(np.isfinite(total), HALF[dtype] * (1 + FP32) * np.abs(total) + TINY[dtype], 0), f"sum {kw}")
+                ref = oracle.rms_norm(hs, b.ops[t]["w"], b.ops[t]["eps"])
+                if to8:
+                    np.testing.assert_array_equal(np.isnan(y), np.isnan(ref), err_msg=f"norm {kw}")
+                else:
+                    within(y, ref, np.where(np.isfinite(ref), (HALF[dtype] + FP32) * np.abs(ref) + TINY[dtype], 0), f"norm {kw}")
+                (alone,), _ = run(b, [t], dtype, **kw)
+                np.testing.assert_array_equal(alone, y)
