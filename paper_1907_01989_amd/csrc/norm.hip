@@ -4,8 +4,8 @@
 //   8-bit: e the smallest with max |y| <= 448 2^e over 128 channels, code = e4m3(y 2^-e)
 //
 // The squares are summed in 64 bits, which no 16-bit value overflows and which
-// leaves the two products with scale and weight as the only fp32 roundings (the
-// conversions hide behind the loads: 16384 x 2048 takes the same time).
+// leaves the root's own and the two products with it and the weight as the only fp32
+// roundings (the conversions hide behind the loads: 16384 x 2048 takes the same time).
 //
 // One pass: a pixel's channels stay in registers (as the 16-bit values they
 // are) between the sum of squares and the output, so that each operand is read
@@ -60,6 +60,7 @@ __global__ __launch_bounds__(1024) void norm_kernel(NormParams p) {
             }
         }
     float scale = 1.0f;
+    int power = 0;
     if constexpr (NORM) {
 #pragma unroll
         for (int d = P; d < 64; d *= 2) squares += __shfl_xor(squares, d, 64);
@@ -69,7 +70,12 @@ __global__ __launch_bounds__(1024) void norm_kernel(NormParams p) {
             squares = 0.0;
             for (int w = 0; w < W; ++w) squares += part[w][lane % P];
         }
-        scale = (float)(1.0 / sqrt(squares * p.inv_c + p.eps));
+        // the factor in two: an exact power of two, and 1/2 to 1 (infinite, zero and NaN
+        // factors as they are): of rows of the least and the largest bf16 values it is no
+        // normal fp32 value
+        const double factor = 1.0 / sqrt(squares * p.inv_c + p.eps);
+        scale = (float)__builtin_amdgcn_frexp_mant(factor);
+        power = __builtin_amdgcn_frexp_exp(factor);
     }
 #pragma unroll
     for (int r = 0; r < R; ++r) {
@@ -81,7 +87,7 @@ __global__ __launch_bounds__(1024) void norm_kernel(NormParams p) {
                 const f4 *wp = (const f4 *)p.w + 2 * min(s, p.KB * 16 - 1);
                 const f4 lo = wp[0], hi = wp[1];
 #pragma unroll
-                for (int c = 0; c < 8; ++c) y[j][c] = pinned(E::get(h[r][j], c) * scale * (c < 4 ? lo[c & 3] : hi[c & 3]));
+                for (int c = 0; c < 8; ++c) y[j][c] = pinned(ldexpf(E::get(h[r][j], c), power) * scale * (c < 4 ? lo[c & 3] : hi[c & 3]));
             } else {
 #pragma unroll
                 for (int c = 0; c < 8; ++c) y[j][c] = E::get(h[r][j], c);

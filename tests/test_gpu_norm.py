@@ -230,3 +230,46 @@ def test_a_sum_leaves_nan_and_infinities_as_they_are(act, to8, dtype):
                     within(y, ref, np.where(np.isfinite(ref), (HALF[dtype] + FP32) * np.abs(ref) + TINY[dtype], 0), f"norm {kw}")
                 (alone,), _ = run(b, [t], dtype, **kw)
                 np.testing.assert_array_equal(alone, y)
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("to8", [False, True])
+def test_rows_of_the_least_and_largest_values_without_eps(to8, dtype):
+    # (1 / rms passes fp32's range, or is none of its normal values; the norm is about 1 all the same).  The squares
+    # and their root are 64-bit: the factor's rounding and two products, three half steps of fp32, are 2^-22
+    from block_util import HALF, TINY, builder, given, run, stored, within
+    rng = np.random.default_rng(6)
+    least = (2.0 ** -24, 2.0 ** -133)[dtype]
+    for m, c in ((7, 72), (1100, 40), (3, 4100)):
+        x = rng.standard_normal((1, 1, m, c))
+        x[0, 0, 0] = least * rng.integers(-3, 4, c)                     # zeros among the least
+        x[0, 0, 1] = least * rng.choice([-1, 1], c)
+        x[0, 0, 2] = np.where(rng.random(c) < 0.5, 1, -0.6) * (6e4, 3.3e38)[dtype]
+        for i in range(3, m):
+            x[0, 0, i] *= 2.0 ** rng.integers((-14, -126)[dtype], (12, 124)[dtype])
+        x = stored(x, dtype)
+        b = builder(c)
+        t = b.rms_norm(given(b, x, dtype), eps=0.0, to8=to8)
+        b.ops[t]["w"] = np.exp(rng.standard_normal(c)).astype(np.float32)
+        ref = oracle.rms_norm(x, b.ops[t]["w"], 0.0)
+        log(f"[case] {m} x {c} of extremes, no eps, type {dtype} to8 {to8}")
+        (y,), _ = run(b, [t], dtype)
+        assert np.isfinite(ref).all()
+        if to8:
+            check8(y, ref, "8-bit")
+        else:
+            within(y, ref, (HALF[dtype] + 2.0 ** -22) * np.abs(ref) + TINY[dtype])
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("n,h,w,c", CASES)
+def test_norm_to_three_roundings(n, h, w, c, dtype):
+    # (as above: the squares and their root are 64-bit)
+    from block_util import HALF, TINY, builder, given, run, stored, within
+    log(f"[case] norm {n}x{h}x{w}x{c} type {dtype}, 2^-22")
+    x = stored(case(n, h, w, c, 11, 4.0), dtype)
+    b = builder(c)
+    t = b.rms_norm(given(b, x, dtype), eps=1e-5)
+    ref = oracle.rms_norm(x, b.ops[t]["w"], b.ops[t]["eps"])
+    (y,), _ = run(b, [t], dtype)
+    within(y, ref, (HALF[dtype] + 2.0 ** -22) * np.abs(ref) + TINY[dtype])
