@@ -459,7 +459,7 @@ struct NormParams {
     TokenOut out;        // 16-bit output, or the values of the 8-bit one; or
     Tensor8 q;           // codes null: `out` is written
     int to8;
-    int M, S, KB;        // pixels, slices, blocks of 128 channels
+    int M, C, S, KB;     // pixels, channels, slices, blocks of 128 channels
     int bf16;
 };
 hipError_t launch_norm(const NormParams &p, hipStream_t st);
@@ -522,7 +522,7 @@ struct PwFp8Params {
     const uint8_t *w;
     const float *scales, *bias;
     TokenOut y;
-    int M, kb, nb16, ns, act;
+    int M, kb, nb16, ns, cout, act;
     int bf16;
 };
 hipError_t launch_pwfp8(const PwFp8Params &p, const PwFp8Geom &g, hipStream_t st);

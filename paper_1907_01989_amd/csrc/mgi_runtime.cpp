@@ -532,6 +532,7 @@ hipError_t launch_norm_node(const mgi_plan &p, const Node &nd, const Bases &B, h
     if (nd.to8 && !writes_output(p, nd.direct_out, B)) q.q = tensor8(p, nd.out, B);
     else q.out = token_out(p, nd.out, nd.direct_out, B);
     q.M = (int)x.pixels();
+    q.C = x.c;
     q.S = slices(x.c);
     q.KB = (x.c + 127) / 128;
     q.bf16 = p.opt.dtype == MGI_DTYPE_BF16;
@@ -556,6 +557,7 @@ hipError_t launch_pwfp8_node(const mgi_plan &p, const Node &nd, const Bases &B, 
     q.kb = nd.ksp;
     q.nb16 = nd.nb16;
     q.ns = slices(y.c);
+    q.cout = y.c;
     q.act = nd.act1;
     q.bf16 = p.opt.dtype == MGI_DTYPE_BF16;
     return launch_pwfp8(q, nd.p8_geo, st);

@@ -92,10 +92,10 @@ __global__ __launch_bounds__(1024) void norm_kernel(NormParams p) {
 #pragma unroll
                 for (int c = 0; c < 8; ++c) y[j][c] = E::get(h[r][j], c);
             }
-            // (slices past the last hold zeros, which a scale of infinity would turn into NaN)
-            if (NORM && s >= p.S) {
+            // (channels past the last hold zeros, which a factor of infinity or NaN would turn into NaN)
+            if (NORM && s * 8 + 8 > p.C) {
 #pragma unroll
-                for (int c = 0; c < 8; ++c) y[j][c] = 0.0f;
+                for (int c = 0; c < 8; ++c) y[j][c] = s * 8 + c < p.C ? y[j][c] : 0.0f;
             }
             if constexpr (TO8) {
 #pragma unroll

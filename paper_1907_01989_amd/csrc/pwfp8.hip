@@ -105,6 +105,18 @@ __device__ __forceinline__ void four_blocks(int n, F f) {
     if (n > 3) f(std::integral_constant<int, 3>{});
 }
 
+// A slice of a pixel's results, one of those up to channel `end`.  Channels past the
+// last hold zeros, which the zero weights there do not give for a pixel with NaN.
+template <typename E>
+__device__ __forceinline__ void store_slice(const PwFp8Params &p, int end, int s, int m, float *v) {
+    if (m >= p.M || s >= p.ns) return;
+    if (end > p.cout) {
+#pragma unroll
+        for (int c = 0; c < 8; ++c) v[c] = s * 8 + c < p.cout ? v[c] : 0.0f;
+    }
+    store8<E>(p.y, s, m, E::pack(v));
+}
+
 // Of two neighbouring blocks of 16 channels (a, b; channels 4 quad .. + 3 of a
 // pixel to a lane) each lane completes one slice: of the first where its quad is
 // even, of the second where it is odd.
@@ -121,7 +133,7 @@ __device__ __forceinline__ void store_pair(const PwFp8Params &p, f4 a, f4 b, int
         v[4 + r] = odd ? b[r] : other;
     }
     const int s = (nb + odd) * 2 + (quad >> 1);
-    if (m < p.M && s < p.ns) store8<E>(p.y, s, m, E::pack(v));
+    store_slice<E>(p, nb * 16 + 32, s, m, v);
 }
 
 // Few pixels: bound by the weights' bytes and latency.  A workgroup has 16 channels
@@ -210,7 +222,7 @@ __global__ __launch_bounds__(512) void pwfp8_few_kernel(PwFp8Params p) {
             y[r] = quad & 1 ? other : v[r];
             y[4 + r] = quad & 1 ? v[r] : other;
         }
-        if ((quad & 1) == 0 && at < p.M && s < p.ns) store8<E>(p.y, s, at, E::pack(y));
+        if ((quad & 1) == 0) store_slice<E>(p, nb * 16 + 16, s, at, y);
     }
 }
 

@@ -369,3 +369,35 @@ def test_nodes_that_write_16_bit_outputs_are_read_as_fp32(dtype):
     for i, y in zip(nodes, ys):
         assert y.dtype == (torch.float16, torch.bfloat16)[dtype]
         assert torch.equal(plan.read_node(i)[1], y.float())
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("m", [12, 90, 1200])
+def test_channels_past_the_last_stay_zero_beside_nan(m, dtype):
+    # rows of zeros (whose factor without eps is infinite), with NaN and with infinities
+    import torch
+    from block_util import builder, given, inputs, stored
+    from paper_1907_01989_amd import _binding as B
+    b = builder()
+    x = stored(np.random.default_rng(4).standard_normal((1, 1, m, 77)), dtype)
+    x[0, 0, 1], x[0, 0, 2, 5], x[0, 0, 3, 76] = 0, np.nan, np.inf
+    x = given(b, x, dtype)
+    n, e = b.rms_norm(x), b.rms_norm(x, eps=0.0)
+    s = b.rms_norm(b.add(n, e))
+    ps = [b.pointwise_fp8(b.quantize(t), 45) for t in (x, n, e)]
+    log(f"[case] {m} rows, padding lanes beside NaN, type {dtype}")
+    for kw in ({"materialize_all": True}, {"materialize_all": True, "fuse": False}):
+        plan = plan_of(b, [s] + ps, dtype, **kw)
+        plan.run(inputs(plan))
+        seen = 0
+        for i, info in enumerate(plan.nodes()):
+            if info["tensor"] not in [n, e, s] + ps:
+                continue
+            c = info["shape"][3]
+            raw = torch.empty(B.mgi_plan_read_node_raw(plan.handle, i), dtype=torch.uint8, device="cuda:0")
+            B.mgi_plan_read_node_raw(plan.handle, i, raw.data_ptr(), torch.cuda.current_stream().cuda_stream)
+            torch.cuda.synchronize()
+            lanes = raw.view(torch.int16).reshape(-1, m, 8)
+            assert (lanes[-1, :, c % 8:] == 0).all(), (info, torch.nonzero(lanes[-1, :, c % 8:])[:5])
+            seen += 1
+        assert seen == 6
