@@ -832,10 +832,14 @@ void fuse_answers(mgi_plan &p) {
 }
 
 // A norm and the add whose sum it reads are one kernel, in the add's place (the
-// norm waits for nothing else).
+// norm waits for nothing else).  A sum that nothing else reads is not stored.
 void fuse_add_into_norm(mgi_plan &p) {
-    std::vector<int> producer(p.bufs.size(), -1);
-    for (size_t i = 0; i < p.nodes.size(); ++i) producer[p.nodes[i].out] = (int)i;
+    std::vector<int> readers(p.bufs.size(), 0), producer(p.bufs.size(), -1);
+    for (size_t i = 0; i < p.nodes.size(); ++i) {
+        for (int b : p.nodes[i].in) readers[b]++;
+        if (p.nodes[i].residual >= 0) readers[p.nodes[i].residual]++;
+        producer[p.nodes[i].out] = (int)i;
+    }
     std::vector<char> drop(p.nodes.size(), 0);
     for (size_t i = 0; i < p.nodes.size(); ++i) {
         Node &nm = p.nodes[i];
@@ -843,7 +847,8 @@ void fuse_add_into_norm(mgi_plan &p) {
         Node &add = p.nodes[producer[nm.in[0]]];
         if (add.kind != NodeKind::Add) continue;
         nm.in = add.in;
-        nm.out_sum = add.out;
+        if (readers[add.out] > 1) nm.out_sum = add.out;
+        else p.bufs[add.out].dead = true;
         nm.act1 = add.act1;
         nm.n_fused += add.n_fused;
         nm.kname = "add_rms_norm";
@@ -2111,7 +2116,10 @@ void unalias_concat(mgi_plan &p, Node &cc, std::vector<char> &parent) {
 // one 28 s, by halves 4.9, planned once 0.7).
 void alias_concats(mgi_plan &p, const mgi_options &o) {
     std::vector<int> producer(p.bufs.size(), -1);
-    for (size_t i = 0; i < p.nodes.size(); ++i) producer[p.nodes[i].out] = (int)i;
+    for (size_t i = 0; i < p.nodes.size(); ++i) {
+        producer[p.nodes[i].out] = (int)i;
+        if (p.nodes[i].out_sum >= 0) producer[p.nodes[i].out_sum] = (int)i;
+    }
     std::vector<char> parent(p.bufs.size(), 0);
     std::vector<Node *> concats;
     for (Node &nd : p.nodes)

@@ -203,11 +203,11 @@ struct Node {
     kern::AnswersGeom an_geo{};
     int k = 0, out_top = -1, out_entropy = -1;
     // Norm (rms_norm, quantize): the buffer of the sum it makes of its two
-    // operands (-1: one operand, no sum), the fp32 or 16-bit graph output that
-    // its kernel writes itself, and whether anything else reads the sum;
-    // whether it norms, whether its output is in 8 bits
+    // operands (-1: one operand, or a sum that nothing else reads), the fp32 or
+    // 16-bit graph output of it that its kernel writes itself; whether it norms,
+    // whether its output is in 8 bits
     int out_sum = -1, direct_sum = -1;
-    bool sum_read = true, norm = false, to8 = false;
+    bool norm = false, to8 = false;
     float eps = 0.0f;
     // Rotary, Attention
     mgi_rotary_desc rotary{};

@@ -520,11 +520,11 @@ hipError_t launch_norm_node(const mgi_plan &p, const Node &nd, const Bases &B, h
     const Shape x = p.bufs[nd.out].shape;
     NormParams q{};
     q.a = token_in(p, nd.in[0], B);
-    if (nd.out_sum >= 0) {
+    if (nd.in.size() > 1) {
         q.b = token_in(p, nd.in[1], B);
         q.act = nd.act1;
-        q.sum = token_out(p, nd.out_sum, nd.direct_sum, B);
     }
+    if (nd.out_sum >= 0) q.sum = token_out(p, nd.out_sum, nd.direct_sum, B);
     if (nd.norm) q.w = (const float *)(wbase + nd.w_off);
     q.eps = nd.eps;
     q.inv_c = 1.0 / x.c;

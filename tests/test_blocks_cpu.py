@@ -297,3 +297,38 @@ def test_oracle_definitions():
     z = oracle.attention(np.zeros((1, 1, 4, 8)), np.ones((1, 1, 3, 8)), v, 1, 1, 8, causal=True)
     np.testing.assert_allclose(z[0, 0], [np.zeros(8), v[0, 0, 0], v[0, 0, :2].mean(0), v[0, 0].mean(0)])
     assert oracle.attention_spans(10, 10, 1, [2, 5, 4, 99]) == [(2, 5, 2, 5), (5, 5, 5, 5), (5, 10, 5, 10)]
+
+
+@pytest.mark.parametrize("planner", [B.PLANNER_GREEDY, B.PLANNER_MCFP])
+@pytest.mark.parametrize("layer", ["rotary", "pointwise_fp8"])
+def test_the_workspace_does_not_grow_with_the_blocks(layer, planner):
+    # each block's sum feeds its norm alone: a fused sum is no tensor
+    def workspace(blocks, fuse):
+        b = NetBuilder()
+        h = b.input(1, 32, 32, 256, -1, 1, dtype=B.DTYPE_FP16)
+        for _ in range(blocks):
+            y = b.rotary(h, 4, 64, [1, 2] * 8, [0.5] * 16) if layer == "rotary" else b.pointwise_fp8(b.quantize(h), 256)
+            h = b.rms_norm(b.add(h, y))
+        plan = engine.Plan({"ops": b.ops, "outputs": [h]}, bind=False, fuse=fuse, planner=planner)
+        assert ("add_rms_norm" in [n["kind"] for n in plan.nodes()]) == fuse
+        return plan.workspace_bytes
+
+    assert workspace(12, True) == workspace(4, True) <= workspace(4, False) == workspace(12, False)
+    assert workspace(1, True) <= workspace(1, False)
+
+
+def test_a_fused_sum_in_a_concatenation_needs_no_copy():
+    def plan(fuse):
+        b = NetBuilder()
+        x = b.input(1, 32, 32, 64, -1, 1, dtype=B.DTYPE_FP16)
+        s = b.add(b.conv(x, 64, 1), b.conv(x, 64, 1, act=0))
+        t = b.add(b.dw(x), b.dw(x, act=0))
+        n = b.rms_norm(t)
+        return engine.Plan({"ops": b.ops, "outputs": [b.conv(b.concat([s, t, n]), 16)]}, bind=False, fuse=fuse)
+
+    p = plan(True)
+    assert "add_rms_norm" in [n["kind"] for n in p.nodes()]
+    # the three parts lie in the concatenation, beside it the input's sliced copy and the two summands: with one
+    # of the parts copied the workspace holds that twice
+    whole, part = 32 * 32 * 192 * 2, 32 * 32 * 64 * 2
+    assert p.workspace_bytes <= whole + 3 * part and p.memory_report()[1] <= plan(False).memory_report()[1]

@@ -273,3 +273,41 @@ def test_norm_to_three_roundings(n, h, w, c, dtype):
     ref = oracle.rms_norm(x, b.ops[t]["w"], b.ops[t]["eps"])
     (y,), _ = run(b, [t], dtype)
     within(y, ref, (HALF[dtype] + 2.0 ** -22) * np.abs(ref) + TINY[dtype])
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+def test_a_sum_that_only_its_norm_reads(dtype):
+    # (not stored) the same bits as where others read it: one or two of them, an output, a part of a concatenation
+    from block_util import builder, given, run, stored
+    rng = np.random.default_rng(12)
+    x, r = (stored(rng.standard_normal((2, 9, 11, 72)), dtype) for _ in range(2))
+
+    def net(more, to8):
+        b = builder(2)
+        s = b.add(given(b, x, dtype), given(b, r, dtype))
+        t = b.rms_norm(s, to8=to8)
+        y = b.pointwise_fp8(t, 40) if to8 else b.dw(t)
+        b.ops[t]["w"] = np.linspace(0.5, 1.5, 72).astype(np.float32)
+        outs = [y, t]
+        if more == "output":
+            outs.append(s)
+        elif more == "reader":
+            outs.append(b.conv(s, 16))
+        elif more == "concat":
+            outs.append(b.conv(b.concat([s, b.dw(s)]), 16))
+        if to8:
+            b.ops[y].update(q=np.full((40, 72), 0x38, np.uint8), scales=np.ones((1, 1), np.float32), b=None)
+        else:
+            b.ops[y].update(w=np.ones((72, 3, 3), np.float32), b=None)
+        return b, outs
+
+    for to8 in (False, True):
+        first = None
+        for more in ("nothing", "output", "reader", "concat"):
+            log(f"[case] a sum read by its norm and {more}, type {dtype} to8 {to8}")
+            for kw in ({}, {"fuse": False}):
+                got, plan = run(*net(more, to8), dtype, **kw)
+                assert ("add_rms_norm" in [i["kind"] for i in plan.nodes()]) == (not kw)
+                first = first or got[:2]
+                for a, c in zip(got, first):
+                    np.testing.assert_array_equal(a, c)
