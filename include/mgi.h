@@ -368,7 +368,11 @@ mgi_status mgi_graph_add_rotary(mgi_graph *g, int in, const mgi_rotary_desc *d, 
  * Queries of no sequence, or that see no key, give zeros.  Keys and values
  * that a query does not see have no part in its result, also if infinite or
  * NaN.  Output (n, h, w, heads * head_dim), q's n, h and w.  The weights p are
- * rounded to the storage type for the product with v, their sum is not. */
+ * rounded to the storage type for the product with v (fp16: to 2^-11 of their
+ * own, or to 2^-32 of the row's largest where that is more), their sum is
+ * not.  Sums of p v are divided in the end, with weights up to 2^8 (fp16: 2^15) in
+ * them: where bf16 values are so large that these pass fp32's range, above 2^119
+ * over the number of keys, results can be infinite. */
 typedef struct {
     int heads, kv_heads, head_dim;
     int q_from, k_from, v_from;

@@ -10,7 +10,8 @@
 // instruction they are the operand of O^T = V^T P^T, so P never leaves the
 // registers.  m, the sums, the scores and O are fp32; P is rounded to 16 bits
 // for the product (an error of half a step relative to each weight, which the
-// sum over keys averages), its sum is taken before.
+// sum over keys averages; in fp16 half of 2^-31 of the base where that is more),
+// its sum is taken before.
 //
 // What bounds it (MI355X).  Long sequences, 8192 causal tokens, 32 heads of 128 on 8 of
 // keys, bf16: 503 to 548 us a call on different cards, 1.0 to 1.09 PFLOP/s, where a
@@ -39,6 +40,12 @@ typedef float f16v __attribute__((ext_vector_type(16)));
 constexpr int kBN = 64;              // keys of a tile that waves share
 constexpr int kPrivate = 32;         // ... and of a wave's own
 constexpr float kSlack = 8.0f;       // log2 of how far weights may pass 1 before the base is moved
+// log2 of a factor of all of a row's weights, which its division takes out again: fp16
+// ends at 65504 and its last step is 2^-24, so that with weights of up to 2^15 only those
+// below 2^-32 of the base are lost, not those of 2^-25, of which a row may have tens of
+// thousands
+template <typename E>
+constexpr float kLift = E::bf ? 0.0f : 7.0f;
 
 // Rows of a tile: 32 to a wave; WR waves along the rows, the others of the four
 // along the keys.
@@ -344,7 +351,7 @@ __global__ __launch_bounds__(256, WR == 1 ? 1 : ND == 3 ? 3 : 2) void attention_
 #pragma unroll
             for (int d = 0; d < ND; ++d) o[d] *= keep;
         }
-        return m == -INFINITY ? 0.0f : m * c;
+        return m == -INFINITY ? 0.0f : m * c - kLift<E>;
     };
     auto weights = [&](const f16v (&s)[NK], float base, h8 (&pr)[2 * NK]) {
         float sum = 0.0f;

@@ -180,3 +180,70 @@ def test_one_tensor_for_queries_keys_and_values():
     log("[case] attention of one tensor")
     (y,), _ = run(b, [a], 0)
     check(x[..., 8:104], x[..., 104:152], x[..., 152:200], 0, 4, 2, 24, y)
+
+
+def tight(q, k, v, dtype, heads, kv, dim, got, bounds=None, k_bounds=None, causal=False, scale=0.0, what=""):
+    """``check`` with a bound of each row and channel's own: fp16 weights are off by half a step of 2^-11, or where
+    that is more by half of 2^-31 of the row's largest (they are kept as 2^7 times that and more, in steps of 2^-24):
+        |error| <= (half + 2 r + 2^-18) sum p |v| / S + 2^-32 sum |v| + half |y|, the sums over the keys that a row sees
+    (S, the weights' sum, is at least the largest's 1)."""
+    from block_util import HALF, TINY, within
+    args = (heads, kv, dim, causal)
+    ref, size = oracle.attention(q, k, v, *args, scale, bounds, k_bounds, weight_of=np.abs)
+    # (equal weights give means)
+    _, mean = oracle.attention(np.zeros_like(q), k, v, *args, scale, bounds, k_bounds, weight_of=np.abs)
+    count = np.zeros(ref.shape[:3]).reshape(-1)
+    nq, nk = int(np.prod(q.shape[:3])), int(np.prod(k.shape[:3]))
+    for q0, q1, k0, k1 in oracle.attention_spans(nq, nk, q.shape[0], bounds, k_bounds):
+        for i in range(q0, q1):
+            count[i] = min(max(i - q0 + 1 + (k1 - k0) - (q1 - q0), 0), k1 - k0) if causal else k1 - k0
+    norm = [np.sqrt(np.square(t.reshape(-1, dim)).sum(1)).max() for t in (q, k)]
+    r = (dim + 4) * 2.0 ** -24 * abs(scale or dim ** -0.5) * norm[0] * norm[1]
+    lost = 2.0 ** -32 * mean * count.reshape(ref.shape[:3] + (1,)) if dtype == 0 else 0.0
+    within(got, ref, (HALF[dtype] + 2 * r + 2.0 ** -18) * size + lost + HALF[dtype] * np.abs(ref) + TINY[dtype], what)
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("queries,heads", [(1, 1), (1024, 64)])
+@pytest.mark.parametrize("bits", [12, 20, 25, 27, 30])
+def test_many_keys_of_small_weights(bits, queries, heads, dtype):
+    # one key far above 50000 others, whose weights are 2^-bits of its own (keys split over workgroups or in one)
+    from block_util import run, stored
+    rng = np.random.default_rng(bits)
+    n, dim, top = 50000, 8, 777
+    q = np.zeros((1, 1, queries, heads * dim))
+    q[..., ::dim] = 1
+    k, v = np.zeros((1, 1, n, dim)), 1 + 0.2 * rng.standard_normal((1, 1, n, dim))
+    k[..., 0], v[..., top, :] = -16, 0
+    k[0, 0, top, 0] = -16 + bits                                       # (scores in units of log2: scale)
+    q, k, v = (stored(t, dtype) for t in (q, k, v))
+    scale = float(np.float32(np.log(2)))
+    b, a = graph(q, k, v, dtype, heads, 1, dim, scale=scale)
+    log(f"[case] attention on 50000 keys of weight 2^-{bits}, {queries} queries of {heads} heads, type {dtype}")
+    (y,), _ = run(b, [a], dtype)
+    one = y[:, :, :1, :dim]
+    tight(q[:, :, :1, :dim], k, v, dtype, 1, 1, dim, one, scale=scale)
+    np.testing.assert_array_equal(y.reshape(-1, dim), np.broadcast_to(one[0, 0], (queries * heads, dim)))
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("n,q,k,heads,kv,dim,causal", IMAGES)
+def test_images_to_their_own_bounds(n, q, k, heads, kv, dim, causal, dtype):
+    from block_util import run
+    log(f"[case] attention {n} x {q} on {k} heads {heads}/{kv} x {dim} causal {causal} type {dtype}, own bounds")
+    t = tensors(np.random.default_rng([n, heads, dim, 5]), (n,) + q, (n,) + k, heads, kv, dim, dtype, 1.5)
+    b, a = graph(*t, dtype, heads, kv, dim, causal=causal)
+    (y,), _ = run(b, [a], dtype, {a: dtype})
+    tight(*t, dtype, heads, kv, dim, y, causal=causal)
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("bounds,k_bounds,nq,nk", PACKED)
+def test_packed_to_their_own_bounds(bounds, k_bounds, nq, nk, causal, dtype):
+    from block_util import run
+    log(f"[case] attention packed {bounds} {k_bounds} of {nq}, {nk} causal {causal} type {dtype}, own bounds")
+    t = tensors(np.random.default_rng([nq, 7]), (1, 1, nq), (1, 1, nk), 4, 2, 64, dtype, 1.5)
+    b, a = graph(*t, dtype, 4, 2, 64, bounds, k_bounds, causal=causal)
+    (y,), _ = run(b, [a], dtype)
+    tight(*t, dtype, 4, 2, 64, y, bounds, k_bounds, causal)
