@@ -367,7 +367,8 @@ mgi_status mgi_graph_add_rotary(mgi_graph *g, int in, const mgi_rotary_desc *d, 
  * causal = 1: of a sequence's nk keys query i of nq sees 0 .. i + nk - nq.
  * Queries of no sequence, or that see no key, give zeros.  Keys and values
  * that a query does not see have no part in its result, also if infinite or
- * NaN.  Output (n, h, w, heads * head_dim), q's n, h and w.  The weights p are
+ * NaN; where one that it sees has an infinite or NaN value, so has the result in
+ * that channel, however small the key's weight.  Output (n, h, w, heads * head_dim), q's n, h and w.  The weights p are
  * rounded to the storage type for the product with v (fp16: to 2^-11 of their
  * own, or to 2^-32 of the row's largest where that is more), their sum is
  * not.  Sums of p v are divided in the end, with weights up to 2^8 (fp16: 2^15) in

@@ -159,6 +159,27 @@ __device__ __forceinline__ s4 read_column(const h8 *base, int bytes) {
                                                      __attribute__((address_space(3))) const void *)base + bytes));
 }
 
+// Infinite and NaN values that a row sees.  A channel in which one of its keys has
+// such a value is that (NaN of infinities of both signs), however small the key's
+// weight: the products have NaN of weights that are zero in 16 bits, and so has a sum
+// that was scaled by zero since.  Where a sum ended infinite or NaN, what there is of
+// these values is added up by itself.
+__device__ __forceinline__ bool ended_odd(const float *v) {
+    float top = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; i += 2)
+        top = __builtin_elementwise_maximum(__builtin_elementwise_maximum(fabsf(v[i]), fabsf(v[i + 1])), top);
+    return !(top < INFINITY);
+}
+__device__ __forceinline__ void add_odd(const float *x, float *odd) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) odd[i] += fabsf(x[i]) < INFINITY ? 0.0f : x[i];
+}
+__device__ __forceinline__ void take_odd(const float *odd, float *v) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = odd[i] != 0.0f ? odd[i] : v[i];
+}
+
 __device__ __forceinline__ h8 with_zeros_for_odd(h8 v, bool bf) {
     const uint16_t mask = bf ? 0x7f80 : 0x7c00;
     u16x8 b = bits8(v);
@@ -343,8 +364,7 @@ __global__ __launch_bounds__(256, WR == 1 ? 1 : ND == 3 ? 3 : 2) void attention_
         top = larger_half(top);
         const bool move = fmaf(top, c, m == -INFINITY ? INFINITY : -m * c) > kSlack;
         if (__any(move)) {
-            // (before the first weights there is nothing to scale but what hidden
-            // keys' infinities left)
+            // (before the first weights there is nothing to scale but infinities)
             const float to = move ? top : m, keep = move && m != -INFINITY ? __builtin_amdgcn_exp2f((m - to) * c) : 1.0f;
             m = to;
             l *= keep;
@@ -424,6 +444,31 @@ __global__ __launch_bounds__(256, WR == 1 ? 1 : ND == 3 ? 3 : 2) void attention_
     const size_t slot = ((size_t)(kvh * geo.tiles + number) * geo.chunks + chunk) * BM;    // this chunk's rows among all partial ones
     if constexpr (WR == 4) {
         if (!works) return;
+        float ended = 0.0f;
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; i += 2)
+                ended = __builtin_elementwise_maximum(__builtin_elementwise_maximum(fabsf(o[d][i]), fabsf(o[d][i + 1])), ended);
+        if (__any(!(ended < INFINITY) && l == l)) {                  // (the scores' NaN are the whole row's)
+#pragma unroll
+            for (int d = 0; d < ND; ++d) {
+                f16v odd = f16v{};
+                for (int j = from; j < most; ++j)
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        if (d * 4 + g >= p.d8) continue;
+                        const h8 v = p.v.x[(size_t)(kvh * p.d8 + d * 4 + g) * p.v.s + (size_t)(t.k0 + j) * p.v.p];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const float x = half ? E::get(v, 4 + i) : E::get(v, i);
+                            if (j < lim && !(fabsf(x) < INFINITY)) odd[g * 4 + i] += x;
+                        }
+                    }
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[d][i] = odd[i] != 0.0f ? odd[i] : o[d][i];
+            }
+        }
         if (split) {
             if (row < rows) {
                 float *part = p.part + (slot + row - first) * (d32 + 2);
@@ -438,7 +483,7 @@ __global__ __launch_bounds__(256, WR == 1 ? 1 : ND == 3 ? 3 : 2) void attention_
             }
             return;
         }
-        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+        const float inv = l == 0.0f ? 1.0f : 1.0f / l;               // (no weights: o is zero, infinite or NaN)
         // a lane has 4 of a slice's 8 channels, lane ^ 32 the others: of two slices
         // each completes one
 #pragma unroll
@@ -478,13 +523,24 @@ __global__ __launch_bounds__(256, WR == 1 ? 1 : ND == 3 ? 3 : 2) void attention_
             for (int w = 0; w < 4; ++w) top = fmaxf(top, ml[w][r].x);
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
-                if (ml[w][r].x == -INFINITY && ml[w][r].y == 0.0f) continue;
-                const float f = __builtin_amdgcn_exp2f((ml[w][r].x - top) * c);
+                const float f = ml[w][r].x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((ml[w][r].x - top) * c);
                 total = fmaf(ml[w][r].y, f, total);
                 const f4 *from_ = (const f4 *)(sums + (w * 32 + r) * LINE + sl * 8);
                 const f4 lo = from_[0], hi = from_[1];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) v[i] = fmaf(i < 4 ? lo[i & 3] : hi[i & 3], f, v[i]);
+            }
+            if (ended_odd(v) && total == total) {
+                float odd[8] = {};
+                const int end = min(seen(first + r), most);
+                for (int j = from; j < end; ++j) {
+                    const h8 x = p.v.x[(size_t)(kvh * p.d8 + sl) * p.v.s + (size_t)(t.k0 + j) * p.v.p];
+                    float w[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) w[i] = E::get(x, i);
+                    add_odd(w, odd);
+                }
+                take_odd(odd, v);
             }
             if (split) {
                 float *part = p.part + (slot + r) * (d32 + 2);
@@ -492,7 +548,7 @@ __global__ __launch_bounds__(256, WR == 1 ? 1 : ND == 3 ? 3 : 2) void attention_
                 for (int i = 0; i < 8; i += 2) *(float2 *)(part + sl * 8 + i) = float2{v[i], v[i + 1]};
                 if (sl == 0) *(float2 *)(part + d32) = float2{top, total};
             } else {
-                const float inv = total == 0.0f ? 0.0f : 1.0f / total;
+                const float inv = total == 0.0f ? 1.0f : 1.0f / total;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) v[i] = pinned(v[i] * inv);
                 const int tok = (first + r) / p.group, hd = kvh * p.group + first + r - tok * p.group;
@@ -526,22 +582,32 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionParams p, 
     const size_t step = (size_t)BM * (d32 + 2);
     float top = -INFINITY, total = 0.0f, v[8] = {};
     auto add = [&](float m, float l, const float *x) {
-        if (m == -INFINITY && l == 0.0f) return;
-        const float to = fmaxf(top, m), keep = top == -INFINITY && total == 0.0f ? 0.0f : __builtin_amdgcn_exp2f((top - to) * c);
-        const float f = __builtin_amdgcn_exp2f((m - to) * c);
+        const float to = fmaxf(top, m), keep = top == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((top - to) * c);
+        const float f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m - to) * c);
         top = to;
         total = fmaf(total, keep, l * f);
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = fmaf(x[i], f, v[i] * keep);
     };
     if (sl < p.d8 && row < rows) {
-        for (int k = g; k < n; k += CG) {
-            const float *at = part + k * step;
-            const float2 w = *(const float2 *)(at + d32);
-            float x[8];
+        float x[8];
+        auto read = [&](int k) {
+            const float *at = part + k * step + sl * 8;
 #pragma unroll
-            for (int i = 0; i < 8; i += 2) *(float2 *)(x + i) = *(const float2 *)(at + sl * 8 + i);
+            for (int i = 0; i < 8; i += 2) *(float2 *)(x + i) = *(const float2 *)(at + i);
+        };
+        for (int k = g; k < n; k += CG) {
+            const float2 w = *(const float2 *)(part + k * step + d32);
+            read(k);
             add(w.x, w.y, x);
+        }
+        if (ended_odd(v)) {
+            float odd[8] = {};
+            for (int k = g; k < n; k += CG) {
+                read(k);
+                add_odd(x, odd);
+            }
+            take_odd(odd, v);
         }
     }
     if constexpr (CG > 1) {
@@ -551,9 +617,14 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionParams p, 
         __syncthreads();
         if (g > 0) return;
         for (int k = 1; k < min(n, CG); ++k) add(ml[k][sl].x, ml[k][sl].y, found[k][sl]);
+        if (ended_odd(v)) {
+            float odd[8] = {};
+            for (int k = 0; k < min(n, CG); ++k) add_odd(found[k][sl], odd);
+            take_odd(odd, v);
+        }
     }
     if (row >= rows || sl >= p.d8) return;
-    const float inv = total == 0.0f ? 0.0f : 1.0f / total;
+    const float inv = total == 0.0f ? 1.0f : 1.0f / total;
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = pinned(v[i] * inv);
     const int tok = row / p.group, hd = kvh * p.group + row - tok * p.group;

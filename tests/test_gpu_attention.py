@@ -247,3 +247,52 @@ def test_packed_to_their_own_bounds(bounds, k_bounds, nq, nk, causal, dtype):
     b, a = graph(*t, dtype, 4, 2, 64, bounds, k_bounds, causal=causal)
     (y,), _ = run(b, [a], dtype)
     tight(*t, dtype, 4, 2, 64, y, bounds, k_bounds, causal)
+
+
+ODD = [
+    # queries, keys, heads, kv, dim, causal, bounds: tiles that waves share, keys of each wave, both split over workgroups
+    (130, 300, 4, 2, 64, False, None), (130, 300, 2, 1, 96, True, None), (3, 300, 4, 2, 64, False, None), (1, 5000, 4, 1, 128, True, None),
+    (40, 2500, 2, 2, 32, False, None), (300, 300, 8, 8, 80, False, [0, 100, 101, 290]), (3000, 3000, 1, 1, 40, True, [0, 2900, 2990]),
+    (1100, 900, 16, 1, 8, True, None),
+]
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("nq,nk,heads,kv,dim,causal,bounds", ODD)
+def test_values_that_are_infinite_or_nan_and_seen(nq, nk, heads, kv, dim, causal, bounds, dtype):
+    # of keys whose weight is nothing beside later and earlier ones', and of ordinary ones: a result's channel is what
+    # its keys have there, wherever the keys are among tiles, waves and workgroups
+    from block_util import run
+    rng = np.random.default_rng([nq, nk, dim])
+    q, k, v = tensors(rng, (1, 1, nq), (1, 1, nk), heads, kv, dim, dtype)
+    q[..., ::dim] = 40
+    far = rng.random(nk) < 0.5                         # weights of exp(-200) and less
+    far[[0, nk // 2, nk - 1]] = True, False, False
+    k[..., ::dim] = np.where(far, 0, 5 * dim ** 0.5)[:, None]
+    rows = sorted(set(rng.choice(nk, 12)) | {0, nk - 1})
+    for i, j in enumerate(rows):
+        v[0, 0, j, rng.integers(kv * dim)] = (np.inf, -np.inf, np.nan)[i % 3]
+    v[0, 0, rows[1], 1], v[0, 0, rows[-2], 1] = np.inf, -np.inf
+    odd = np.where(np.isfinite(v), 0, v)
+    fine = np.where(np.isfinite(v), v, 0)
+    ref, size = oracle.attention(q, k, fine, heads, kv, dim, causal, 0.0, bounds, weight_of=np.abs)
+    ref = ref.reshape(nq, heads, dim)
+    seen = np.zeros(ref.shape)
+    of = odd.reshape(nk, kv, dim)
+    with np.errstate(invalid="ignore"):
+        for q0, q1, k0, k1 in oracle.attention_spans(nq, nk, 1, bounds):
+            total = np.concatenate([np.zeros((1, kv, dim)), np.cumsum(of[k0:k1], 0)])
+            for i in range(q0, q1):
+                end = min(max(i - q0 + 1 + (k1 - k0) - (q1 - q0), 0), k1 - k0) if causal else k1 - k0
+                seen[i] = np.repeat(total[end], heads // kv, 0)
+        ref = np.where(seen != 0, seen, ref).reshape(1, 1, nq, heads * dim)
+    assert np.isposinf(ref).any() and np.isneginf(ref).any() and np.isnan(ref).any() and np.isfinite(ref).any()
+    b, a = graph(q, k, v, dtype, heads, kv, dim, bounds, causal=causal)
+    log(f"[case] attention, infinities that are seen, {nq} on {nk}, {heads}/{kv} x {dim} causal {causal} {bounds} type {dtype}")
+    (y,), _ = run(b, [a], dtype, {a: dtype})
+    from block_util import HALF, within
+    r = (dim + 4) * 2.0 ** -24 * dim ** -0.5 * np.sqrt(np.square(q.reshape(-1, dim)).sum(1)).max() * np.sqrt(np.square(k.reshape(-1, dim)).sum(1)).max()
+    bound = (HALF[dtype] + 2 * r + 2.0 ** -18) * size + HALF[dtype] * np.where(np.isfinite(ref), np.abs(ref), 0) + 2.0 ** -32 * np.abs(fine).sum()
+    within(y, ref, bound)
+    (f,), _ = run(b, [a], dtype, materialize_all=True, fuse=False)     # sliced operands: the same bits
+    np.testing.assert_array_equal(f, y)
