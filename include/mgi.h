@@ -312,8 +312,11 @@ mgi_status mgi_graph_add_rms_norm(mgi_graph *g, int in, const float *weight, flo
  * max |x| <= 448 * 2^e over the block's finite values; values are rounded to
  * the nearest code, ties to even.  Infinities and NaN become NaN.  An 8-bit
  * tensor feeds mgi_graph_add_pointwise_fp8 or is a graph output, which holds
- * the values that it stands for (elsewhere MGI_ERR_UNSUPPORTED).  At most 2^14
- * channels (MGI_ERR_UNSUPPORTED). */
+ * the values that it stands for, rounded to the array's type (elsewhere
+ * MGI_ERR_UNSUPPORTED).  The codes next to a type's largest value stand for the
+ * power of two past it (fp16 values from 63488 on for 65536, bf16 ones from
+ * 1.9375 * 2^127 on for 2^128), an infinity in an array of that type.  At most
+ * 2^14 channels (MGI_ERR_UNSUPPORTED). */
 mgi_status mgi_graph_add_quantize(mgi_graph *g, int in, int *out);
 
 /* Pointwise (1x1) layer in 8-bit floating point, of an 8-bit tensor (other

@@ -311,3 +311,27 @@ def test_a_sum_that_only_its_norm_reads(dtype):
                 first = first or got[:2]
                 for a, c in zip(got, first):
                     np.testing.assert_array_equal(a, c)
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+def test_values_next_to_the_largest_in_8_bits(dtype):
+    # stand for the power of two past the type's range: an infinity in a 16-bit array, in fp32 that of fp16 is there
+    from block_util import TORCH, builder, given, run, stored
+    import torch
+    top = (2.0 ** 15, 2.0 ** 127)[dtype]
+    x = np.zeros((1, 1, 6, 130))
+    x[0, 0, :, 7] = top * np.array([1.75, 1.875, 1.921875, 1.9375, 1.9921875, -1.9921875])
+    x[..., 128:] = 3
+    x = stored(x, dtype)
+    assert np.isfinite(x).all()
+    ref = oracle.quantize(x)
+    assert ref[0, 0, 2, 7] == 1.875 * top and ref[0, 0, 3, 7] == 2 * top and ref[0, 0, 5, 7] == -2 * top
+    b = builder()
+    t = b.quantize(given(b, x, dtype))
+    log(f"[case] quantize next to the largest, type {dtype}")
+    (wide,), _ = run(b, [t], dtype)
+    (narrow,), _ = run(b, [t], dtype, {t: dtype})
+    with np.errstate(over="ignore"):
+        np.testing.assert_array_equal(wide, ref.astype(np.float32).astype(np.float64))
+    np.testing.assert_array_equal(narrow, torch.from_numpy(ref).to(TORCH[dtype]).double().numpy())
+    assert np.isinf(narrow[0, 0, 3:, 7]).all() and np.isfinite(narrow[0, 0, :3]).all()
