@@ -339,8 +339,9 @@ mgi_status mgi_graph_add_pointwise_fp8(mgi_graph *g, int in, int cout, const uns
  *     t = freqs[i] * position along axis axes[i];
  * the other channels of the heads are copied.  head_dim and from are multiples
  * of 8 (MGI_ERR_UNSUPPORTED).  axes, freqs: `pairs` values each, freqs finite,
- * in radians per position (angles keep their fraction of a turn for any 32-bit
- * position).  positions: an index input (n, h, w, axes) with each pixel's
+ * in radians per position (of frequencies up to 512 angles keep their fraction of
+ * a turn, to 2^-25 of one, for any 32-bit position; each doubling beyond costs a
+ * bit of it).  positions: an index input (n, h, w, axes) with each pixel's
  * position along every axis (any axis count up to 8), or -1: the axes are 0 the
  * image's number in the batch, 1 the pixel's row, 2 its column.
  * Output (n, h, w, heads * head_dim). */

@@ -100,3 +100,23 @@ def test_one_token_at_each_position_is_the_row():
     y = turned(x, pos)
     for i in range(6):
         np.testing.assert_array_equal(turned(x[:, :, i:i + 1], pos[:, :, i:i + 1]), y[:, :, i:i + 1])
+
+
+def test_high_frequencies_at_far_positions():
+    # the angles' fractions of a turn by 60 digits; within 2^-25 of a turn, the sine and its products as above
+    from decimal import Decimal, getcontext
+    from block_util import HALF, builder, given, run, stored, within
+    getcontext().prec = 60
+    turn = 2 * Decimal("3.14159265358979323846264338327950288419716939937510582097494")
+    freqs = [0.5, 7.3, 511.9, -123.456, 1.0, 2.0 ** -40, 300.0000001, -0.75]
+    pos = np.array([0, 1, -1, 12345, 2 ** 31 - 1, -2 ** 31, 2 ** 30 + 7, -1999999999], np.int64)
+    x = stored(np.random.default_rng(3).standard_normal((1, 1, len(pos), 16)), 0)
+    b = builder()
+    t = b.rotary(given(b, x, 0), 1, 16, [0] * 8, freqs, positions=b.index_input(pos.reshape(1, 1, -1, 1)))
+    log("[case] rotary, high frequencies at far positions")
+    (y,), _ = run(b, [t], 0, {t: 0})
+    angle = np.array([[float(Decimal(int(p)) * Decimal(f) % turn) for f in freqs] for p in pos])
+    lo, hi = x[0, 0, :, :8], x[0, 0, :, 8:]
+    ref = np.concatenate([lo * np.cos(angle) - hi * np.sin(angle), lo * np.sin(angle) + hi * np.cos(angle)], 1)
+    size = np.tile(np.abs(lo) + np.abs(hi), (1, 2))
+    within(y[0, 0], ref, HALF[0] * np.abs(ref) + 2.0 ** -25 + (2.0 ** -18 + 2 * np.pi * 2.0 ** -25) * size)
