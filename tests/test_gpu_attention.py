@@ -296,3 +296,24 @@ def test_values_that_are_infinite_or_nan_and_seen(nq, nk, heads, kv, dim, causal
     within(y, ref, bound)
     (f,), _ = run(b, [a], dtype, materialize_all=True, fuse=False)     # sliced operands: the same bits
     np.testing.assert_array_equal(f, y)
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("nq,nk,heads,kv,dim,causal,bounds", ODD)
+@pytest.mark.parametrize("left", [0.3, 0.01, 0.0])
+def test_keys_whose_scores_are_minus_infinity(left, nq, nk, heads, kv, dim, causal, bounds, dtype):
+    # weigh nothing, in whole tiles, waves and workgroups too; a row with no others gives zeros, and NaN in q or in a
+    # key that is seen makes the row NaN
+    from block_util import run
+    rng = np.random.default_rng([nq, nk, dim, 1])
+    q, k, v = tensors(rng, (1, 1, nq), (1, 1, nk), heads, kv, dim, dtype)
+    q[..., ::dim] = 1
+    k[0, 0, rng.random(nk) >= left, ::dim] = -np.inf
+    if nq > 20:
+        q[0, 0, nq // 2, 3] = np.nan
+    ref, size = oracle.attention(q, k, v, heads, kv, dim, causal, 0.0, bounds, weight_of=np.abs)
+    b, a = graph(q, k, v, dtype, heads, kv, dim, bounds, causal=causal)
+    log(f"[case] attention, scores of -inf but for {left}, {nq} on {nk}, {heads}/{kv} x {dim} causal {causal} {bounds} type {dtype}")
+    (y,), _ = run(b, [a], dtype, {a: dtype})
+    check(q, k, v, dtype, heads, kv, dim, y, bounds, causal=causal)
+    assert left or (y[np.isfinite(y)] == 0).all()
