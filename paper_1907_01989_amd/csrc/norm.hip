@@ -5,15 +5,16 @@
 //
 // The squares are summed in 64 bits, which no 16-bit value overflows and which
 // leaves the root's own and the two products with it and the weight as the only fp32
-// roundings (the conversions hide behind the loads: 16384 x 2048 takes the same time).
+// roundings; for codes what the products round off is kept, and one is left (both
+// hide behind the loads: 16384 x 2048 takes 53.1 us with and 52.7 without).
 //
 // One pass: a pixel's channels stay in registers (as the 16-bit values they
 // are) between the sum of squares and the output, so that each operand is read
 // once.  Scaling by a power of two is exact, so a code differs from the
-// definition's only where the fp32 norm rounds across a border between codes.
+// definition's only where the one rounding to fp32 crosses a border between codes.
 //
 // Bound by memory: 16384 x 2048 bf16 rows, two operands in, their sum and the values of
-// the 8-bit norm out, 268 MB in 52.7 us, 5.1 TB/s, what a copy of 1 GiB reaches.  A few rows
+// the 8-bit norm out, 268 MB in 53.1 us, 5.0 TB/s, what a copy of 1 GiB reaches.  A few rows
 // are bound by the host's call (1 x 4096: the kernel 2.9 us).
 #include "tokens.h"
 
@@ -21,6 +22,15 @@ namespace mgi {
 namespace kern {
 
 namespace {
+
+// x (scale + rest) w, rounded once: with what the two products leave behind, so that
+// a code of 8 bits is the neighbour's only where that one rounding crosses a border.
+// (Not finite where a product is not, which the codes do not tell apart.)
+__device__ __forceinline__ float scaled(float x, float scale, float rest, float w) {
+    const float p = pinned(x * scale), q = pinned(p * w);
+    const float behind = fmaf(x, rest, fmaf(x, scale, -p));
+    return pinned(q + fmaf(behind, w, fmaf(p, w, -q)));
+}
 
 // P pixels to a wave, 64 / P slices at a time.  P = 8: a wave's lanes cover 8
 // pixels x 8 slices, 128 bytes of either layout, twice to a block of 128
@@ -59,7 +69,7 @@ __global__ __launch_bounds__(1024) void norm_kernel(NormParams p) {
                 for (int c = 0; c < 8; ++c) squares = fma((double)E::get(h[r][j], c), (double)E::get(h[r][j], c), squares);
             }
         }
-    float scale = 1.0f;
+    float scale = 1.0f, rest = 0.0f;
     int power = 0;
     if constexpr (NORM) {
 #pragma unroll
@@ -75,6 +85,7 @@ __global__ __launch_bounds__(1024) void norm_kernel(NormParams p) {
         // normal fp32 value
         const double factor = 1.0 / sqrt(squares * p.inv_c + p.eps);
         scale = (float)__builtin_amdgcn_frexp_mant(factor);
+        if constexpr (TO8) rest = (float)(__builtin_amdgcn_frexp_mant(factor) - scale);
         power = __builtin_amdgcn_frexp_exp(factor);
     }
 #pragma unroll
@@ -87,7 +98,11 @@ __global__ __launch_bounds__(1024) void norm_kernel(NormParams p) {
                 const f4 *wp = (const f4 *)p.w + 2 * min(s, p.KB * 16 - 1);
                 const f4 lo = wp[0], hi = wp[1];
 #pragma unroll
-                for (int c = 0; c < 8; ++c) y[j][c] = pinned(ldexpf(E::get(h[r][j], c), power) * scale * (c < 4 ? lo[c & 3] : hi[c & 3]));
+                for (int c = 0; c < 8; ++c) {
+                    const float x = ldexpf(E::get(h[r][j], c), power), w = c < 4 ? lo[c & 3] : hi[c & 3];
+                    if constexpr (TO8) y[j][c] = scaled(x, scale, rest, w);
+                    else y[j][c] = pinned(x * scale * w);
+                }
             } else {
 #pragma unroll
                 for (int c = 0; c < 8; ++c) y[j][c] = E::get(h[r][j], c);

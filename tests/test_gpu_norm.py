@@ -335,3 +335,43 @@ def test_values_next_to_the_largest_in_8_bits(dtype):
         np.testing.assert_array_equal(wide, ref.astype(np.float32).astype(np.float64))
     np.testing.assert_array_equal(narrow, torch.from_numpy(ref).to(TORCH[dtype]).double().numpy())
     assert np.isinf(narrow[0, 0, 3:, 7]).all() and np.isfinite(narrow[0, 0, :3]).all()
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("n,h,w,c", CASES + [(1, 1, 2500, 264)])
+def test_codes_of_a_norm_are_the_exact_norms(n, h, w, c, dtype):
+    # (rounded to fp32 once and then to 8 bits: another code only within half a step of 2^-23 of a border between two)
+    from block_util import builder, given, run, stored
+    x = stored(case(n, h, w, c, 13), dtype)
+    b = builder(c)
+    t = b.rms_norm(given(b, x, dtype), eps=1e-5, to8=True)
+    ref = oracle.rms_norm(x, b.ops[t]["w"], b.ops[t]["eps"])
+    log(f"[case] codes of a norm {n}x{h}x{w}x{c} type {dtype}")
+    (y,), _ = run(b, [t], dtype)
+    near = 2.0 ** -24
+    same = [oracle.quantize(ref * a, oracle.block_exponents(ref * e)) for a in (1 - near, 1 + near) for e in (1 - near, 1 + near)]
+    lo, hi = np.minimum.reduce(same), np.maximum.reduce(same)
+    assert ((y >= lo) & (y <= hi)).all(), int((~((y >= lo) & (y <= hi))).sum())
+    assert (lo != hi).mean() < 1e-4 or y.size < 10000
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("c", [640, 16384])
+def test_codes_of_a_norm_next_to_borders(c, dtype):
+    # weights that bring every channel within a step of fp32 of the middle between two codes: the codes are those of
+    # the exact norm rounded to fp32 (two products would cross the middle for a third of them)
+    from block_util import builder, given, run, stored
+    rng = np.random.default_rng(c)
+    x = stored(case(1, 1, 1, c, 14) + 0.1, dtype)
+    x[x == 0] = 1
+    f = 1 / np.sqrt((x * x).mean() + np.float64(np.float32(1e-5)))
+    middle = (8.5 + rng.integers(0, 8, c)) / 8 * 2.0 ** rng.integers(-3, 4, c)
+    middle[::128] = 300                                             # (each block's exponent is 0)
+    w = (middle / (x.reshape(-1) * f)).astype(np.float32)
+    ref = (x * f * w.astype(np.float64)).astype(np.float32).astype(np.float64)
+    b = builder(c)
+    t = b.rms_norm(given(b, x, dtype), eps=1e-5, to8=True)
+    b.ops[t]["w"] = w
+    log(f"[case] codes of a norm next to borders, {c} channels, type {dtype}")
+    (y,), _ = run(b, [t], dtype)
+    np.testing.assert_array_equal(y, oracle.quantize(ref))
