@@ -367,7 +367,8 @@ mgi_status mgi_graph_add_rotary(mgi_graph *g, int in, const mgi_rotary_desc *d, 
  * the same (or, with k_bounds, an index input of as many values, those of its)
  * pixels of k and v.  Values are read up to the pixel count and not below their
  * predecessors (or 0): what runs back or past the end is an empty sequence's.  At
- * most 2^16 sequences (MGI_ERR_UNSUPPORTED).
+ * most 2^16 sequences (MGI_ERR_UNSUPPORTED); the time to find them grows with
+ * their square, and counts from some thousands of short ones on.
  * causal = 1: of a sequence's nk keys query i of nq sees 0 .. i + nk - nq.
  * Queries of no sequence, or that see no key, give zeros.  Keys and values
  * that a query does not see have no part in its result, also if infinite or

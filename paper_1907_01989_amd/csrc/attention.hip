@@ -17,14 +17,14 @@
 // keys, bf16: 503 to 548 us a call on different cards, 1.0 to 1.09 PFLOP/s, where a
 // library's product of 8192 x 8192 x 8192 reaches 1.21.  A wave's step has 1024 cycles of matrix instructions and about
 // as many of maxima, exponentials and sums, of which two waves on a SIMD hide little of
-// each other's (matrix instructions 49% of the cycles, vector ones as many).  Taking half
+// each other's (matrix instructions 58% of a compute unit's busy cycles, vector ones 57%).  Taking half
 // of the LDS reads of V out, or the exponentials, changed the time by 7% at most;
 // scores of the next tile computed between the weights of this one took 663 us against
 // 625 on the same card, a wave's priority made no difference.  Packed short sequences
-// (5003 tokens in 13 of them, 16 heads of 80: 42 us): 3500 cycles for the steps of three
-// waves on a SIMD, and the compute units that hold the longest sequence's tiles end
-// last.  One query on 32768 keys: bytes in flight, 134 MB in 29 us, 4.6 TB/s with the
-// start.
+// (5003 tokens in 13 of them, 16 heads of 80: 42 us): vector instructions 58%, matrix ones
+// 34% of the busy cycles, of three waves on a SIMD, and the compute units that hold the
+// longest sequence's tiles end last.  One query on 32768 keys: bytes in flight, 134 MB in
+// 29 us, 4.6 TB/s with the start.
 #include <algorithm>
 #include <type_traits>
 
@@ -90,7 +90,9 @@ __device__ __forceinline__ int from_left(int v, int first) { return __builtin_am
 
 // Finds tile `t` among the tiles of all sequences.  Bounds are read up to the
 // token count and not below their predecessors.  Two more sequences without
-// keys take the queries before the first bound and behind the last.
+// keys take the queries before the first bound and behind the last.  Every workgroup
+// goes through the bounds before its own, 64 at a time, which thousands of short
+// sequences pay for (16384 of 16 tokens, 8 heads of 64: 22.2 ms, as images 1.2).
 template <int BM>
 __device__ __forceinline__ Tile find_tile(const AttentionParams &p, int t) {
     Tile r;
@@ -561,7 +563,7 @@ __global__ __launch_bounds__(256, WR == 1 ? 1 : ND == 3 ? 3 : 2) void attention_
 // Joins the chunks of the rows that have several, in a launch of its own (by the
 // workgroup that is done last, as other kernels here do: its stores past the L2 and
 // its acquire take longer than the launch, 13 packed sequences 62 us against 41, one
-// query on 32768 keys the same 37).  A thread has 8 channels of every
+// query on 32768 keys 37 either way, before this kernel took 4.5 us there).  A thread has 8 channels of every
 // CG-th chunk of a row, then what CG threads found is joined in order.
 template <typename E, int BM, int CG>
 __global__ __launch_bounds__(256) void attention_join_kernel(AttentionParams p, AttentionGeom geo, int d32) {

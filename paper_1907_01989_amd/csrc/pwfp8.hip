@@ -140,8 +140,8 @@ __device__ __forceinline__ void store_pair(const PwFp8Params &p, f4 a, f4 b, int
 // and 16 * FM pixels; its eight waves take the blocks of inputs in turn, four at a
 // time with all loads in flight, and their sums are added in the order of the waves.
 // RAW: the pixels are 16-bit and are brought into 8 bits here, as the quantize
-// kernel does, which saves its launch (1 x 4096 x 4096: 6.5 us a call, of which the
-// host's part takes 5.2 to 5.5).
+// kernel does, which saves its launch (1 x 4096 x 4096: 6.7 us a call, 7.6 from the
+// kernel's start to its end; the host's part takes 5.2 to 5.5).
 template <typename E, int FM, bool RAW>
 __global__ __launch_bounds__(512) void pwfp8_few_kernel(PwFp8Params p) {
     __shared__ f4 red[8][FM][64];
