@@ -317,3 +317,29 @@ def test_keys_whose_scores_are_minus_infinity(left, nq, nk, heads, kv, dim, caus
     (y,), _ = run(b, [a], dtype, {a: dtype})
     check(q, k, v, dtype, heads, kv, dim, y, bounds, causal=causal)
     assert left or (y[np.isfinite(y)] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("q,k", [((2, 1, 150), (2, 1, 210)), ((2, 1, 2), (2, 1, 600)), ((1, 1, 1), (1, 1, 3000))])
+def test_operands_in_mixed_layouts(q, k, dtype):
+    # graph inputs read in place beside sliced tensors, views of a concatenation among them: the same bits
+    from block_util import builder, given, run
+    t = tensors(np.random.default_rng(q[2]), q, k, 6, 2, 72, dtype)
+    first = None
+    for sliced in range(8):
+        for joined in (False, True):
+            b = builder()
+            ids = []
+            for i, x in enumerate(t):
+                x = given(b, x, dtype)
+                if sliced >> i & 1:
+                    x = b.add(x, given(b, np.zeros_like(t[i]), dtype))
+                ids.append(x)
+            a = b.attention(*ids, 6, 2, 72)
+            outs = [a]
+            if joined and sliced & 6 == 6:
+                outs.append(b.conv(b.concat(ids[1:]), 8))
+            log(f"[case] attention {q} on {k}, sliced {sliced:03b} joined {joined} type {dtype}")
+            y = run(b, outs, dtype, {a: dtype})[0][0]
+            first = y if first is None else first
+            np.testing.assert_array_equal(y, first)
